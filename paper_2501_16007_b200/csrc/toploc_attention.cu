@@ -5,71 +5,15 @@
 // One pass over the keys with a running maximum m and sum l: when a tile raises m, what has been summed
 // so far shrinks by exp(m_old - m_new).  The query heads of a key head are rows of one matrix, (token,
 // head in group) row by row, so that every key and value is read once for all of them.
-#include "model_common.cuh"
+#include "attention_common.cuh"
 
 namespace {
 
 using namespace toploc_model;
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kRows = 32;   // rows of a block
 constexpr int kKeys = 32;   // keys of a tile, one per lane
 constexpr int kWarpRows = kRows / 4;
-constexpr int kSms = 148;   // of a B200: sizes the workspace and the split, whatever device answers
-
-struct AttentionParams {
-  const void* q;
-  const void* k;
-  const void* v;
-  void* out;
-  float* lse;
-  uint8_t* status;
-  float* part_out;  // [splits][total_tokens * q_heads][head_dim]
-  float* part_lse;  // [splits][total_tokens * q_heads], base 2
-  const int32_t* table;
-  const int32_t* offsets;
-  const int32_t* kv_lens;  // NULL: a prompt attends over its own rows
-  long long total_tokens;
-  long long q_token, q_head, out_token, out_head;
-  long long k_page, k_token, k_head, v_page, v_token, v_head, table_stride;
-  float scale_log2;
-  int head_dim, q_heads, kv_heads, group, num_seqs, max_new;
-  int page_size, num_pages, max_pages;
-  int row_tiles, splits;
-};
-
-// A sequence's rows and keys, held to what the call promised.
-struct SeqRange {
-  int first, rows, keys;
-  bool bad;
-};
-
-__device__ __forceinline__ SeqRange sequence(const AttentionParams& p, int i) {
-  SeqRange s;
-  const int a = p.offsets[i], b = p.offsets[i + 1];
-  s.first = max(a, 0);
-  long long rows = min((long long)b, p.total_tokens) - s.first;
-  s.bad = a < 0 || b < a || b > p.total_tokens || rows > p.max_new;
-  rows = max(0ll, min(rows, (long long)p.max_new));
-  s.rows = (int)rows;
-  if (p.kv_lens == nullptr) {
-    s.keys = s.rows;
-  } else {
-    const int kv = p.kv_lens[i];
-    const long long most = (long long)p.max_pages * p.page_size;
-    s.bad = s.bad || kv < 0 || kv > most;
-    s.keys = (int)max(0ll, min((long long)kv, most));
-  }
-  return s;
-}
-
-// The keys of part `split` of a sequence: whole tiles of 128.
-__device__ __forceinline__ void split_range(int keys, int splits, int split, int* begin, int* end) {
-  const int unit = ((keys + splits - 1) / splits + 127) / 128 * 128;
-  *begin = (int)min((long long)unit * split, (long long)keys);
-  *end = min(*begin + unit, keys);
-}
 
 // ---- the kernel on the fp32 units: every type, layout and head size ------------------------------
 //
@@ -248,14 +192,15 @@ __global__ void __launch_bounds__(128) toploc_attention_join_kernel(const Attent
   if (p.lse && lane == 0) p.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
-// Parts the keys are split into: enough blocks to fill the GPU twice over, at least 256 keys a part.
-int splits_of(const toploc_attention_layout* lay, const toploc_kv_layout* kv) {
+// Parts the keys of a paged cache are split into, by the bounds the host knows (`rows`: of a block).
+int splits_of(const toploc_attention_layout* lay, const toploc_kv_layout* kv, int rows) {
   if (kv->page_size <= 0) return 1;
-  const long long rows = (long long)lay->max_new_tokens * (lay->q_heads / lay->kv_heads);
-  const long long blocks = (rows + kRows - 1) / kRows * lay->kv_heads * lay->num_seqs;
-  if (blocks == 0) return 1;
+  const long long packed = (long long)lay->max_new_tokens * (lay->q_heads / lay->kv_heads);
+  const long long items = (packed + rows - 1) / rows * lay->kv_heads * lay->num_seqs;
+  if (items == 0) return 1;
   const long long most = (long long)kv->max_pages * kv->page_size;
-  return (int)max(1ll, min(min((2ll * kSms + blocks - 1) / blocks, most / 256), 64ll));
+  const long long wanted = items <= kSms / 2 ? kSms / items : 4ll * kSms / items;
+  return (int)max(1ll, min(min(wanted, most / 512), 64ll));
 }
 
 int check_layout(const toploc_attention_layout* lay, const toploc_kv_layout* kv) {
@@ -290,9 +235,11 @@ int launch_fp32(const AttentionParams& p, cudaStream_t stream) {
 }
 
 template <typename T>
-int launch_all(AttentionParams& p, cudaStream_t stream) {
+int launch_all(AttentionParams& p, const toploc_attention_layout* lay, const toploc_kv_layout* kv, bool tensor_cores,
+               cudaStream_t stream) {
   p.row_tiles = (int)(((long long)p.max_new * p.group + kRows - 1) / kRows);
-  int rc = p.head_dim <= 64 ? launch_fp32<T, 2>(p, stream)
+  int rc = tensor_cores ? launch_tensor_cores(p, lay, kv, stream)
+           : p.head_dim <= 64 ? launch_fp32<T, 2>(p, stream)
            : p.head_dim <= 128 ? launch_fp32<T, 4>(p, stream) : launch_fp32<T, 8>(p, stream);
   if (rc != TOPLOC_OK || p.splits == 1) return rc;
   const long long rows = p.total_tokens * p.q_heads;
@@ -322,7 +269,8 @@ int attention(const void* d_q, const void* d_k, const void* d_v, const toploc_at
   p.group = lay->q_heads / lay->kv_heads;
   p.num_seqs = lay->num_seqs; p.max_new = lay->max_new_tokens;
   p.page_size = kv->page_size; p.num_pages = kv->num_pages; p.max_pages = kv->max_pages;
-  p.splits = splits_of(lay, kv);
+  const bool tensor_cores = tensor_cores_take(lay, kv, d_q, d_k, d_v, d_out);
+  p.splits = splits_of(lay, kv, tensor_cores ? tensor_core_rows(lay) : kRows);
   if (p.splits > 1) {
     const size_t need = toploc_attention_workspace_bytes(lay, kv);
     if (!workspace || workspace_bytes < need) return TOPLOC_ERR_WORKSPACE;
@@ -331,14 +279,16 @@ int attention(const void* d_q, const void* d_k, const void* d_v, const toploc_at
     p.part_lse = p.part_out + (long long)p.splits * p.total_tokens * p.q_heads * p.head_dim;
   }
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  return lay->dtype == TOPLOC_DTYPE_BF16 ? launch_all<__nv_bfloat16>(p, stream) : launch_all<float>(p, stream);
+  return lay->dtype == TOPLOC_DTYPE_BF16 ? launch_all<__nv_bfloat16>(p, lay, kv, tensor_cores, stream)
+                                         : launch_all<float>(p, lay, kv, tensor_cores, stream);
 }
 
 }  // namespace
 
 extern "C" size_t toploc_attention_workspace_bytes(const toploc_attention_layout* lay, const toploc_kv_layout* kv) {
   if (check_layout(lay, kv) != TOPLOC_OK) return 0;
-  const int splits = splits_of(lay, kv);
+  // (which kernel takes the call also depends on the pointers: room for either)
+  const int splits = max(splits_of(lay, kv, kRows), splits_of(lay, kv, tensor_core_rows(lay)));
   return splits <= 1 ? 0 : (size_t)splits * lay->total_tokens * lay->q_heads * (lay->head_dim + 1) * 4;
 }
 

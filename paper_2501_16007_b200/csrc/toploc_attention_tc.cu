@@ -1,0 +1,790 @@
+// Attention on the tensor cores (bf16, head_dim 64 or 128).
+//
+//   S = Q K^T (128 rows x 128 keys, fp32 in tensor memory),  P = 2^(scale S - m),  O += P V
+//
+// The rows of a tile are (token, head of the group) pairs of one key head, so a tile of keys is read once
+// for all of them, a chunk of 32 tokens with four heads a group fills a tile, and a single token still
+// has its heads side by side.
+//
+// A block has ten warps: two groups of four that do the softmax, a thread per row (no exchange between
+// threads: the running maximum and sum of a row live in one), a warp that feeds keys and values through a
+// ring of tiles by tensor copies, and one that issues the products.  While one group works on its scores the
+// tensor cores run the other group's products.  The groups hold
+//   two row tiles against the same keys      (kTwoTiles: more than 128 rows), or
+//   one row tile against every other key tile (few rows, the single tokens among them: bound by reading
+//                                              the keys, so both groups serve the stream and join at the end).
+// Blocks are persistent: one an SM, walking over (sequence, row tile, key head, part of the keys); the feeding
+// warp runs ahead into the next item while the last one is finished.
+//
+// The output is not rescaled whenever the maximum grows but only where it grew by more than 2^8: P then stays
+// below 2^8, and O, the sum and P share the same reference, so the quotient is the same.
+#include "attention_common.cuh"
+#include "sm100.cuh"
+
+namespace {
+
+using namespace toploc_model;
+using namespace sm100;
+
+constexpr int kTcThreads = 320;
+constexpr int kItems = 4;                  // items announced ahead
+constexpr float kLazyLog2 = 8.0f;
+constexpr int kBlockBytes = 128 * 128;     // 128 rows of 64 elements
+
+// One piece of work: a tile of rows of one sequence and key head against a range of its keys.
+struct Item {
+  int seq;     // -1: no more work
+  int head;    // key head
+  int split;
+  int first;   // row of the packed tensors its sequence starts at
+  int behind;  // keys in front of the sequence's first new token (may be negative)
+  int row0;    // first packed row (token * group + head in group) of the tile
+  int rows;    // packed rows of the sequence
+  int kbegin;  // keys kbegin .. kend - 1, kbegin a multiple of the tile
+  int kend;
+  int n0, n1;  // tiles of the two groups (two row tiles), or n0 tiles in all
+  int pad;
+};
+
+template <int D, bool kTwoTiles>
+struct Shared {
+  static constexpr int kHalves = D / 64;
+  static constexpr int kTileBytes = kHalves * kBlockBytes;
+  static constexpr int kQTiles = kTwoTiles ? 2 : 1;
+  static constexpr int kStages = D == 128 ? 5 : 8;
+  struct Head {
+    uint64_t full[kStages], empty[kStages];
+    uint64_t s_full[2], p_full[2], o_full[2];
+    uint64_t q_full, q_empty, drain;
+    uint64_t join;  // both groups (one row tile): their sums are exchanged, their outputs read
+    uint64_t item_full[kItems], item_empty[kItems];
+    Item items[kItems];
+    uint32_t tmem;
+    int gave_up;
+    int bad_values[2];  // number of the item (by parity) in whose hidden keys' tiles a value was not finite
+  };
+  static constexpr int kHeadBytes = 1024;
+  static_assert(sizeof(Head) <= kHeadBytes, "head");
+  static constexpr int kExchangeBytes = kTwoTiles ? 0 : 2 * 128 * 2 * 4;
+  static constexpr int kBytes = 1024 + kHeadBytes + (kQTiles + kStages) * kTileBytes + kExchangeBytes;
+  static_assert(kBytes <= 232448, "shared memory of a block");
+};
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Two fp32 products and sums in one instruction.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p));
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+__device__ __forceinline__ uint32_t ring_stage(uint32_t n, int stages) { return n % (uint32_t)stages; }
+__device__ __forceinline__ uint32_t ring_parity(uint32_t n, int stages) { return (n / (uint32_t)stages) & 1u; }
+
+struct TcParams {
+  AttentionParams p;
+  int tile_rows;  // packed rows of a row tile: 128 rounded down to whole tokens
+  int box_rows;   // rows of a key copy
+  int q_bytes;    // bytes of a query tile's copy
+};
+
+// A wait of a whole warp: all lanes or none go on.
+__device__ __forceinline__ bool warp_wait(const uint64_t& bar, uint32_t parity, volatile int* gave_up) {
+  return __all_sync(0xFFFFFFFFu, barrier_wait(shared_address(&bar), parity, gave_up));
+}
+
+// Tiles of the ring an item takes, and the place of value tile j among them.
+template <bool kTwoTiles>
+__device__ __forceinline__ int item_tiles(const Item& im) {
+  return kTwoTiles ? max(im.n0, im.n1) : im.n0;
+}
+template <bool kTwoTiles>
+__device__ __forceinline__ int value_place(int j, int n) {
+  return kTwoTiles ? 2 * j + 1 : min(n, j + 2) + j;  // K0 V0 K1 V1 .. or K0 K1 V0 K2 V1 ..
+}
+
+template <int D, bool kTwoTiles>
+__global__ void __launch_bounds__(kTcThreads, 1)
+toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMap map_q,
+                           const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  using S = Shared<D, kTwoTiles>;
+  constexpr int kStages = S::kStages, kHalves = S::kHalves;
+  extern __shared__ unsigned char dynamic[];
+  const AttentionParams& p = tp.p;
+  unsigned char* base = dynamic + ((1024 - (shared_address(dynamic) & 1023)) & 1023);
+  typename S::Head& sh = *reinterpret_cast<typename S::Head*>(base);
+  unsigned char* q_tiles = base + S::kHeadBytes;
+  unsigned char* ring = q_tiles + S::kQTiles * S::kTileBytes;
+  float2* exchange = reinterpret_cast<float2*>(ring + kStages * S::kTileBytes);  // (maximum, sum) of [group][row]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* gave_up = &sh.gave_up;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      barrier_init(shared_address(&sh.full[i]), 1);
+      barrier_init(shared_address(&sh.empty[i]), 1);
+    }
+    for (int w = 0; w < 2; ++w) {
+      barrier_init(shared_address(&sh.s_full[w]), 1);
+      barrier_init(shared_address(&sh.p_full[w]), 4);
+      barrier_init(shared_address(&sh.o_full[w]), 1);
+      sh.bad_values[w] = -1;
+    }
+    barrier_init(shared_address(&sh.q_full), 1);
+    barrier_init(shared_address(&sh.q_empty), 1);
+    barrier_init(shared_address(&sh.drain), 1);
+    barrier_init(shared_address(&sh.join), 8);
+    for (int i = 0; i < kItems; ++i) {
+      barrier_init(shared_address(&sh.item_full[i]), 1);
+      barrier_init(shared_address(&sh.item_empty[i]), 9);
+    }
+    sh.gave_up = 0;
+    barrier_init_fence();
+  }
+  if (warp == 9) tmem_alloc(shared_address(&sh.tmem), 512);
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tmem = sh.tmem;
+  constexpr uint32_t kOut = 256;  // scores of group w at 128 w, outputs at 256 + D w
+
+  if (warp == 8) {
+    // ---- feeding: finds the items, copies queries, keys and values ----
+    if (lane == 0) {
+      prefetch_map(&map_q);
+      prefetch_map(&map_k);
+      prefetch_map(&map_v);
+    }
+    const bool paged = p.kv_lens != nullptr;
+    const int rows_item = S::kQTiles * tp.tile_rows;
+    long long item = blockIdx.x, before = 0;  // before: items of the sequences in front of the batch of 32
+    int batch = -32;
+    SeqRange mine = {};
+    long long incl = 0, batch_items = 0;
+    uint32_t fed = 0, q_uses = 0;
+    for (uint32_t number = 0;; ++number) {
+      // the item's sequence: lanes hold 32 sequences and the prefix sum of their items
+      bool more = true;
+      while (batch < 0 || item >= before + batch_items) {
+        before += batch_items;
+        batch = batch < 0 ? 0 : batch + 32;
+        if (batch >= p.num_seqs) {
+          more = false;
+          break;
+        }
+        mine = SeqRange{0, 0, 0, false};
+        if (batch + lane < p.num_seqs) mine = sequence(p, batch + lane);
+        if (mine.bad && p.status && blockIdx.x == 0) p.status[batch + lane] = TOPLOC_SEQ_BAD_LENGTH;
+        const long long tiles = ((long long)mine.rows * p.group + rows_item - 1) / rows_item;
+        incl = tiles * p.kv_heads * p.splits;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+          const long long up = __shfl_up_sync(0xFFFFFFFFu, incl, off);
+          if (lane >= off) incl += up;
+        }
+        batch_items = __shfl_sync(0xFFFFFFFFu, incl, 31);
+      }
+      const uint32_t slot = number % kItems;
+      if (!warp_wait(sh.item_empty[slot], ((number / kItems) & 1) ^ 1, gave_up)) break;
+      Item im = {};
+      im.seq = -1;
+      if (more) {
+        const unsigned ahead = __ballot_sync(0xFFFFFFFFu, item < before + incl);
+        const int src = __ffs(ahead) - 1;
+        const SeqRange s = {__shfl_sync(0xFFFFFFFFu, mine.first, src), __shfl_sync(0xFFFFFFFFu, mine.rows, src),
+                            __shfl_sync(0xFFFFFFFFu, mine.keys, src), false};
+        const long long upto = src == 0 ? 0 : __shfl_sync(0xFFFFFFFFu, incl, src - 1);
+        const long long rest = item - before - upto, per_tile = (long long)p.kv_heads * p.splits;
+        im.seq = batch + src;
+        im.split = (int)(rest % p.splits);
+        im.head = (int)(rest / p.splits % p.kv_heads);
+        im.first = s.first;
+        im.rows = s.rows * p.group;
+        const int tiles = (im.rows + rows_item - 1) / rows_item;
+        im.row0 = (tiles - 1 - (int)(rest / per_tile)) * rows_item;  // the longest first
+        im.behind = s.keys - s.rows;
+        int kend;
+        split_range(s.keys, p.splits, im.split, &im.kbegin, &kend);
+        const auto tiles_upto = [&](int last_row) {  // tiles up to the newest key that packed row `last_row` sees
+          const int seen = min(kend, im.behind + last_row / p.group + 1);
+          return seen > im.kbegin ? (seen - im.kbegin + kKeyTile - 1) / kKeyTile : 0;
+        };
+        const int last_row = min(im.rows, im.row0 + rows_item) - 1;
+        im.kend = min(kend, im.behind + last_row / p.group + 1);
+        if (kTwoTiles) {
+          const int last0 = min(im.rows, im.row0 + tp.tile_rows) - 1;
+          im.n0 = tiles_upto(last0);
+          im.n1 = last_row > last0 ? tiles_upto(last_row) : 0;
+        } else {
+          im.n0 = tiles_upto(last_row);
+        }
+      }
+      if (lane == 0) {
+        sh.items[slot] = im;
+        barrier_arrive(shared_address(&sh.item_full[slot]));
+      }
+      __syncwarp();
+      if (!more) break;
+      const int n = item_tiles<kTwoTiles>(im);
+      item += gridDim.x;
+      if (n == 0) continue;
+
+
+      // queries: each tile in blocks of 64 channels
+      if (!warp_wait(sh.q_empty, (q_uses & 1) ^ 1, gave_up)) break;
+      ++q_uses;
+      const bool second = kTwoTiles && im.row0 + tp.tile_rows < im.rows;
+      const uint32_t q_bar = shared_address(&sh.q_full);
+      if (lane == 0) barrier_arrive_expect(q_bar, (second ? 2 : 1) * tp.q_bytes);
+      __syncwarp();
+      if (lane < kHalves * (second ? 2 : 1)) {
+        const int w = lane / kHalves, h = lane % kHalves;
+        copy_3d(shared_address(q_tiles + w * S::kTileBytes + h * kBlockBytes), &map_q, q_bar, h * 64, im.head * p.group,
+                im.first + (im.row0 + w * tp.tile_rows) / p.group);
+      }
+
+      // keys and values
+      const int my_page = lane / kHalves, my_half = lane % kHalves;
+      const auto page_of = [&](int j) {  // this lane's page of key tile j
+        if (!paged || j >= n) return 0;
+        const int key0 = im.kbegin + j * kKeyTile, col = key0 / p.page_size + my_page;
+        if (my_page * tp.box_rows >= kKeyTile || key0 + my_page * tp.box_rows >= im.kend) return 0;
+        int page = p.table[im.seq * p.table_stride + col];
+        if (page < 0 || page >= p.num_pages) {
+          if (p.status) p.status[im.seq] = TOPLOC_SEQ_BAD_PAGE;
+          page = p.num_pages;  // past the end: the copy fills zeros
+        }
+        return page;
+      };
+      const auto feed = [&](const CUtensorMap* map, int j, int page) {
+        const uint32_t stage = ring_stage(fed, kStages), bar = shared_address(&sh.full[stage]);
+        if (!warp_wait(sh.empty[stage], ring_parity(fed, kStages) ^ 1, gave_up)) return false;
+        ++fed;
+        const int key0 = im.kbegin + j * kKeyTile, left = min(kKeyTile, im.kend - key0);
+        const int copies = paged ? (left + tp.box_rows - 1) / tp.box_rows : 1;
+        if (lane == 0) barrier_arrive_expect(bar, copies * kHalves * tp.box_rows * 128);
+        __syncwarp();
+        if (lane < copies * kHalves) {
+          const uint32_t dst = shared_address(ring + stage * S::kTileBytes + my_half * kBlockBytes) +
+                               my_page * tp.box_rows * 128;
+          if (paged)
+            copy_4d(dst, map, bar, my_half * 64, key0 % p.page_size, im.head, page);
+          else
+            copy_4d(dst, map, bar, my_half * 64, im.first + key0, im.head, 0);
+        }
+        return true;
+      };
+      bool fine = true;
+      int page = page_of(0), next = page_of(1);  // looked up ahead of their use
+      if (kTwoTiles) {
+        for (int j = 0; fine && j < n; ++j) {
+          fine = feed(&map_k, j, page) && feed(&map_v, j, page);
+          page = next;
+          next = page_of(j + 2);
+        }
+      } else {
+        fine = feed(&map_k, 0, page);
+        for (int j = 0; fine && j < n; ++j) {
+          const int after = page_of(j + 2);
+          if (j + 1 < n) fine = feed(&map_k, j + 1, next);
+          fine = fine && feed(&map_v, j, page);
+          page = next;
+          next = after;
+        }
+      }
+      if (!fine) break;
+    }
+    if (*gave_up) {  // copies in flight have to land before the block ends
+      if (q_uses > 0) barrier_drain(shared_address(&sh.q_full), (q_uses - 1) & 1);
+      for (uint32_t i = fed > kStages ? fed - kStages : 0; i < fed; ++i)
+        barrier_drain(shared_address(&sh.full[ring_stage(i, kStages)]), ring_parity(i, kStages));
+    }
+  } else if (warp == 9) {
+    // ---- products: one thread issues them all ----
+    if (lane == 0) {
+      constexpr uint32_t kScores = bf16_product(128, false), kValues = bf16_product(D, true);
+      const uint32_t q_at = shared_address(q_tiles), ring_at = shared_address(ring);
+      uint32_t used = 0, q_uses = 0, p_uses[2] = {0, 0};
+      const auto full = [&](uint32_t n) {
+        const bool ok = barrier_wait(shared_address(&sh.full[ring_stage(n, kStages)]), ring_parity(n, kStages), gave_up);
+        tmem_fence_after();
+        return ok;
+      };
+      const auto release = [&](uint32_t n) { mma_commit(shared_address(&sh.empty[ring_stage(n, kStages)])); };
+      const auto scores = [&](int w, uint32_t n) {  // scores of group w against the key tile at place n
+        const uint32_t a = q_at + (kTwoTiles ? w : 0) * S::kTileBytes, b = ring_at + ring_stage(n, kStages) * S::kTileBytes;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t at = (k / 4) * kBlockBytes + (k % 4) * 32;
+          mma_shared(tmem + 128 * w, swizzled_operand(a + at, 16), swizzled_operand(b + at, 16), kScores, k > 0);
+        }
+        mma_commit(shared_address(&sh.s_full[w]));
+      };
+      const auto values = [&](int w, uint32_t n, bool add) {
+        const uint32_t b = ring_at + ring_stage(n, kStages) * S::kTileBytes;
+#pragma unroll
+        for (int k = 0; k < kKeyTile / 16; ++k)
+          mma_tmem(tmem + kOut + D * w, tmem + 128 * w + 8 * k, swizzled_operand(b + k * 2048, kBlockBytes), kValues,
+                   add || k > 0);
+        mma_commit(shared_address(&sh.o_full[w]));
+      };
+      const auto weights = [&](int w) {  // the group's weights are in tensor memory
+        const bool ok = barrier_wait(shared_address(&sh.p_full[w]), p_uses[w]++ & 1, gave_up);
+        tmem_fence_after();
+        return ok;
+      };
+      for (uint32_t number = 0;; ++number) {
+        const uint32_t slot = number % kItems;
+        if (!barrier_wait(shared_address(&sh.item_full[slot]), (number / kItems) & 1, gave_up)) break;
+        const int seq = sh.items[slot].seq, n0 = sh.items[slot].n0, n1 = sh.items[slot].n1;
+        barrier_arrive(shared_address(&sh.item_empty[slot]));
+        if (seq < 0) break;
+        const int n = kTwoTiles ? max(n0, n1) : n0;
+        if (n == 0) continue;
+        bool ok = barrier_wait(shared_address(&sh.q_full), q_uses++ & 1, gave_up);
+        tmem_fence_after();
+        if (kTwoTiles) {
+          ok = ok && full(used);
+          if (!ok) break;
+          if (n0 > 0) scores(0, used);
+          if (n1 > 0) scores(1, used);
+          release(used);
+          if (n == 1) mma_commit(shared_address(&sh.q_empty));
+          for (int j = 0; ok && j < n; ++j) {
+            const uint32_t v_at = used + 2 * j + 1, k_at = v_at + 1;
+            ok = full(v_at);
+            bool key_there = false;
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              const int nw = w ? n1 : n0;
+              if (!ok || j >= nw) continue;
+              ok = weights(w);
+              if (!ok) break;
+              values(w, v_at, j > 0);
+              if (j + 1 < nw) {
+                if (!key_there) ok = full(k_at);
+                if (!ok) break;
+                key_there = true;
+                scores(w, k_at);
+              }
+            }
+            if (!ok) break;
+            release(v_at);
+            if (j + 1 < n) {
+              release(k_at);
+              if (j + 2 == n) mma_commit(shared_address(&sh.q_empty));
+            }
+          }
+        } else {
+          uint32_t at = used;
+          for (int w = 0; ok && w < min(n, 2); ++w, ++at) {
+            ok = full(at);
+            if (!ok) break;
+            scores(w, at);
+            release(at);
+          }
+          if (n <= 2 && ok) mma_commit(shared_address(&sh.q_empty));
+          for (int j = 0; ok && j < n; ++j) {
+            const int w = j & 1;
+            ok = full(at) && weights(w);
+            if (!ok) break;
+            values(w, at, j >= 2);
+            release(at++);
+            if (j + 2 < n) {
+              ok = full(at);
+              if (!ok) break;
+              scores(w, at);
+              release(at++);
+              if (j + 3 == n) mma_commit(shared_address(&sh.q_empty));
+            }
+          }
+        }
+        if (!ok) break;
+        used += 2 * n;
+      }
+      if (*gave_up) {  // products in flight have to end before tensor memory is freed
+        mma_commit(shared_address(&sh.drain));
+        barrier_drain(shared_address(&sh.drain), 0);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---- softmax: a thread per row ----
+    const int w = warp >> 2, r = threadIdx.x & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 rows of tensor memory
+    const uint32_t s_at = tmem + lanes + 128 * w;
+    uint32_t used = 0, s_uses = 0, pv[2] = {0, 0};
+    const float scale = p.scale_log2;
+    uint32_t joins = 0;
+    const auto join = [&] {  // both groups are here
+      __syncwarp();
+      if (lane == 0) barrier_arrive(shared_address(&sh.join));
+      return warp_wait(sh.join, joins++ & 1, gave_up);
+    };
+    for (uint32_t number = 0;; ++number) {
+      const uint32_t slot = number % kItems;
+      if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
+      const Item im = sh.items[slot];
+      __syncwarp();
+      if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
+      if (im.seq < 0) break;
+      const int n = item_tiles<kTwoTiles>(im);
+      const int row = im.row0 + (kTwoTiles ? w * tp.tile_rows : 0) + r;      // packed row
+      const bool valid = r < tp.tile_rows && row < im.rows;
+      const int token = row / p.group;
+      const int newest = valid ? im.behind + token : -1;                     // the newest key the row sees
+      // keys up to `common` are seen by every row of the group's tile
+      const int common = im.behind + (im.row0 + (kTwoTiles ? w * tp.tile_rows : 0)) / p.group;
+      const int hidden_from = max(im.behind + im.row0 / p.group + 1, 0);     // first key hidden from a row of the item
+      const bool live = __any_sync(0xFFFFFFFFu, valid);                      // else nobody reads the warp's rows
+      const int tiles = kTwoTiles ? (w ? im.n1 : im.n0) : (n + 1 - w) / 2;
+      float m = -INFINITY, l = 0.f;
+      bool ok = true;
+      for (int i = 0; i < tiles; ++i) {
+        const int j = kTwoTiles ? i : 2 * i + w;
+        const int key0 = im.kbegin + j * kKeyTile;
+        const bool masked = key0 + kKeyTile - 1 > common;
+        ok = warp_wait(sh.s_full[w], s_uses++ & 1, gave_up);
+        if (!ok) break;
+        if (live) {
+          tmem_fence_after();
+          uint32_t s[4][32];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_load(s[c], s_at + 32 * c);
+          tmem_wait_load();
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ready(s[c]);
+          if (masked) {
+            const int last = newest - key0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (32 * c + e > last) s[c][e] = 0xFF800000u;  // -inf, whatever was there
+          }
+          float top[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            top[c] = __uint_as_float(s[c][0]);
+#pragma unroll
+            for (int e = 1; e < 32; ++e) top[c] = fmaxf(top[c], __uint_as_float(s[c][e]));
+          }
+          const float peak = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+          // (peak - m) * scale > the limit, also where m is -inf; not where both are
+          const bool grow = valid && peak > m && !((peak - m) * scale <= kLazyLog2);
+          if (__any_sync(0xFFFFFFFFu, grow)) {
+            const float shrink = grow ? exp2_approx((m - peak) * scale) : 1.f;
+            if (grow) m = peak;
+            l *= shrink;
+            if (i > 0) {  // what the group has summed so far, once its last product is done
+              ok = warp_wait(sh.o_full[w], (pv[w] - 1) & 1, gave_up);
+              if (!ok) break;
+              tmem_fence_after();
+              const uint64_t both = pair(shrink, shrink);
+#pragma unroll 1
+              for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                tmem_load(o, tmem + lanes + kOut + D * w + 32 * c);
+                tmem_wait_load();
+                tmem_ready(o);
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                  float a, b;
+                  unpair(fma_pair(pair(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), both, 0ull), a, b);
+                  o[e] = __float_as_uint(a);
+                  o[e + 1] = __float_as_uint(b);
+                }
+                tmem_store(tmem + lanes + kOut + D * w + 32 * c, o);
+              }
+            }
+          }
+          const float ref = m == -INFINITY ? 0.f : m * scale;
+          const uint64_t scales = pair(scale, scale), refs = pair(-ref, -ref);
+          uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t packed[16];
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              float a, b;
+              unpair(fma_pair(pair(__uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1])), scales, refs), a, b);
+              a = exp2_approx(a);
+              b = exp2_approx(b);
+              sum[(e >> 1) & 1] = add_pair(sum[(e >> 1) & 1], pair(a, b));
+              packed[e >> 1] = pack_bf16(a, b);
+            }
+            tmem_store(s_at + 16 * c, packed);
+          }
+          float a, b;
+          unpair(add_pair(sum[0], sum[1]), a, b);
+          l += a + b;
+        }
+        if (masked) {
+          // Values of hidden keys meet weights of zero, and 0 * NaN is NaN: rows past the item's keys (never
+          // loaded, or another sequence's) become zero; a value in front of them that is not finite too, and
+          // the rows that do see it get it back at the end.
+          const uint32_t place = used + value_place<kTwoTiles>(j, n), stage = ring_stage(place, kStages);
+          ok = warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up);
+          if (!ok) break;
+          const int from = max(hidden_from - key0, 0);
+          unsigned char* tile = ring + stage * S::kTileBytes;
+          for (int e = r; e < (kKeyTile - from) * 8; e += 128) {
+            const int j_row = from + (e >> 3);
+            const bool past = key0 + j_row >= im.kend;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+              uint4* at = reinterpret_cast<uint4*>(tile + h * kBlockBytes + j_row * 128 + (e & 7) * 16);
+              uint4 v = make_uint4(0, 0, 0, 0);
+              bool write = past;
+              if (!past) {
+                v = *at;
+                uint32_t* x = &v.x;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                  if ((x[q] & 0x7F80u) == 0x7F80u) x[q] &= 0xFFFF0000u, write = true;
+                  if ((x[q] & 0x7F800000u) == 0x7F800000u) x[q] &= 0xFFFFu, write = true;
+                }
+                if (write) {
+                  *(volatile int*)&sh.bad_values[number & 1] = (int)number;
+                  __threadfence_block();
+                }
+              }
+              if (write) *at = v;
+            }
+          }
+          fence_async_shared();
+        }
+        if (live) tmem_wait_store();
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) barrier_arrive(shared_address(&sh.p_full[w]));
+        ++pv[w];
+      }
+      if (!ok) break;
+      used += 2 * n;
+
+      // ---- the rows' results ----
+      if (!kTwoTiles) pv[w ^ 1] += (n + 1 - (w ^ 1)) / 2;
+      float weight[2] = {1.f, 0.f}, total = l, top = m;  // of this group's outputs and of the other's
+      if (!kTwoTiles) {
+        exchange[w * 128 + r] = make_float2(m, l);
+        ok = join();
+        if (!ok) break;
+        const float2 a = exchange[r], b = exchange[128 + r];
+        top = fmaxf(a.x, b.x);
+        const float ref = top == -INFINITY ? 0.f : top;
+        weight[0] = a.x == -INFINITY ? 0.f : exp2_approx((a.x - ref) * scale);
+        weight[1] = b.x == -INFINITY ? 0.f : exp2_approx((b.x - ref) * scale);
+        if (a.x == INFINITY || b.x == INFINITY) weight[0] = weight[1] = NAN;
+        total = a.y * weight[0] + b.y * weight[1];
+        // a NaN score leaves no trace in a maximum
+        if (a.y != a.y || b.y != b.y) total = NAN;
+      }
+      const bool any_keys = total != 0.f;
+      const float inv = any_keys ? 1.f / total : 0.f;
+      const int head = im.head * p.group + row - token * p.group;
+      const long long at = (long long)(im.first + token) * p.q_heads + head;
+      const bool two_sided = !kTwoTiles && n > 1;
+      // two row tiles: a group writes its rows; one: each group writes half of the channels
+      constexpr int kWidth = kTwoTiles ? D : D / 2;
+      const int c0 = kTwoTiles ? 0 : w * kWidth;
+      if (tiles > 0 && kTwoTiles) ok = warp_wait(sh.o_full[w], (pv[w] - 1) & 1, gave_up);
+      if (!kTwoTiles && n > 0) {
+        ok = warp_wait(sh.o_full[0], (pv[0] - 1) & 1, gave_up);
+        if (n > 1) ok = ok && warp_wait(sh.o_full[1], (pv[1] - 1) & 1, gave_up);
+      }
+      if (!ok) break;
+      tmem_fence_after();
+      const bool repair = *(volatile int*)&sh.bad_values[number & 1] == (int)number;
+#pragma unroll 1
+      for (int c = c0; c < c0 + kWidth; c += 32) {
+        float o[32];
+        if (live && (kTwoTiles ? tiles : n) > 0) {
+          uint32_t x[32];
+          tmem_load(x, tmem + lanes + kOut + (kTwoTiles ? D * w : 0) + c);
+          tmem_wait_load();
+          tmem_ready(x);
+          const float w0 = kTwoTiles ? 1.f : weight[0];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = kTwoTiles ? __uint_as_float(x[e]) : w0 == 0.f ? 0.f : __uint_as_float(x[e]) * w0;
+          if (two_sided) {
+            tmem_load(x, tmem + lanes + kOut + D + c);
+            tmem_wait_load();
+            tmem_ready(x);
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (weight[1] != 0.f) o[e] = fmaf(__uint_as_float(x[e]), weight[1], o[e]);
+          }
+        }
+        if (!valid) continue;
+        if (!any_keys) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+        }
+        if (repair) {  // values that were taken out of tiles with hidden keys: back to the rows that see them
+          const int begin = max(im.kbegin, hidden_from);
+          for (int key = begin; key <= min(newest, im.kend - 1); ++key) {
+            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + (long long)im.head * p.v_head + c;
+            if (p.kv_lens) {
+              const int col = key / p.page_size, page = p.table[im.seq * p.table_stride + col];
+              if (page < 0 || page >= p.num_pages) continue;
+              v += page * p.v_page + (long long)(key - col * p.page_size) * p.v_token;
+            } else {
+              v += (long long)(im.first + key) * p.v_token;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float f = __bfloat162float(v[e]);
+              if (!(fabsf(f) < INFINITY)) o[e] += f;
+            }
+          }
+        }
+        if (p.splits == 1) {
+          uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + (im.first + token) * p.out_token +
+                                                head * p.out_head + c);
+#pragma unroll
+          for (int e = 0; e < 32; e += 8)
+            out[e / 8] = make_uint4(pack_bf16(o[e] * inv, o[e + 1] * inv), pack_bf16(o[e + 2] * inv, o[e + 3] * inv),
+                                    pack_bf16(o[e + 4] * inv, o[e + 5] * inv), pack_bf16(o[e + 6] * inv, o[e + 7] * inv));
+        } else {
+          float4* out = reinterpret_cast<float4*>(p.part_out + (im.split * p.total_tokens * p.q_heads + at) * D + c);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            out[e / 4] = make_float4(o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv);
+        }
+      }
+      if (valid && (kTwoTiles || w == 0)) {
+        const float lse2 = any_keys ? (top == -INFINITY ? 0.f : top) * scale + log2f(total) : -INFINITY;
+        if (p.splits > 1)
+          p.part_lse[im.split * p.total_tokens * p.q_heads + at] = lse2;
+        else if (p.lse)
+          p.lse[at] = lse2 * kLn2;
+      }
+      if (!kTwoTiles) {  // both have read: the next item may overwrite
+        tmem_fence_before();
+        if (!join()) break;
+      }
+    }
+  }
+  __syncthreads();
+  if (sh.gave_up && p.status && blockIdx.x < (unsigned)p.num_seqs && threadIdx.x == 0) {
+    for (int i = blockIdx.x; i < p.num_seqs; i += gridDim.x) p.status[i] = TOPLOC_SEQ_WAIT_EXPIRED;
+  }
+  if (warp == 9) tmem_free(tmem, 512);
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+  static const EncodeTiled fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiled>(p);
+  }();
+  return fn;
+}
+
+// A bf16 tensor [.., extent[1], extent[0]] copied in boxes of 64 contiguous elements with the 128-byte swizzle.
+// strides: elements, of dimensions 1 and up (of no meaning where the extent is 1).
+bool make_map(CUtensorMap* map, const void* at, int rank, const int64_t* extent, const int64_t* stride, const int* box) {
+  cuuint64_t sizes[4], steps[3];
+  cuuint32_t boxes[4], ones[4] = {1, 1, 1, 1};
+  for (int i = 0; i < rank; ++i) {
+    sizes[i] = (cuuint64_t)extent[i];
+    boxes[i] = (cuuint32_t)box[i];
+    if (i > 0) steps[i - 1] = extent[i] == 1 ? 16 : (cuuint64_t)stride[i - 1] * 2;
+  }
+  return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(at), sizes, steps, boxes,
+                        ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool kTwoTiles>
+int launch(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int blocks,
+           cudaStream_t stream) {
+  constexpr int kBytes = Shared<D, kTwoTiles>::kBytes;
+  if (cudaFuncSetAttribute(toploc_attention_tc_kernel<D, kTwoTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           kBytes) != cudaSuccess)
+    return TOPLOC_ERR_CUDA;
+  toploc_attention_tc_kernel<D, kTwoTiles><<<blocks, kTcThreads, kBytes, stream>>>(tp, q, k, v);
+  return launched();
+}
+
+}  // namespace
+
+namespace toploc_model {
+
+bool tensor_cores_take(const toploc_attention_layout* lay, const toploc_kv_layout* kv, const void* q, const void* k,
+                       const void* v, const void* out) {
+  if (lay->dtype != TOPLOC_DTYPE_BF16 || (lay->head_dim != 64 && lay->head_dim != 128)) return false;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16)) return false;
+  const int page = kv->page_size;
+  if (page > 0 && (page % 8 != 0 || (kKeyTile % page != 0 && page % kKeyTile != 0) || kv->num_pages == 0)) return false;
+  // steps of a tensor copy are positive multiples of 16 bytes below 2^40
+  const auto step = [](int64_t stride, int64_t extent) {
+    return extent <= 1 || (stride > 0 && stride % 8 == 0 && stride < ((int64_t)1 << 39));
+  };
+  return step(lay->q_token_stride, lay->total_tokens) && step(lay->q_head_stride, lay->q_heads) &&
+         step(lay->out_token_stride, lay->total_tokens) && step(lay->out_head_stride, lay->q_heads) &&
+         step(kv->k_token_stride, page > 0 ? page : lay->total_tokens) && step(kv->k_head_stride, lay->kv_heads) &&
+         step(kv->v_token_stride, page > 0 ? page : lay->total_tokens) && step(kv->v_head_stride, lay->kv_heads) &&
+         (page == 0 || (step(kv->k_page_stride, kv->num_pages) && step(kv->v_page_stride, kv->num_pages)));
+}
+
+int launch_tensor_cores(const AttentionParams& p, const toploc_attention_layout* lay, const toploc_kv_layout* kv,
+                        cudaStream_t stream) {
+  if (encode_tiled() == nullptr) return TOPLOC_ERR_CUDA;
+  const int page = kv->page_size, rows = tensor_core_rows(lay);
+  const bool two = rows > 128 / p.group * p.group;
+  const int tokens = min(128 / p.group, p.max_new);  // of a query copy
+  TcParams tp;
+  tp.p = p;
+  tp.tile_rows = 128 / p.group * p.group;
+  tp.box_rows = page > 0 ? min(page, kKeyTile) : kKeyTile;
+  tp.q_bytes = p.head_dim * 2 * p.group * tokens;
+  CUtensorMap q, k, v;
+  const int64_t q_extent[3] = {p.head_dim, p.q_heads, p.total_tokens}, q_stride[2] = {p.q_head, p.q_token};
+  const int q_box[3] = {64, p.group, tokens};
+  const int64_t kv_extent[4] = {p.head_dim, page > 0 ? page : p.total_tokens, p.kv_heads, page > 0 ? p.num_pages : 1};
+  const int64_t k_stride[3] = {p.k_token, p.k_head, p.k_page}, v_stride[3] = {p.v_token, p.v_head, p.v_page};
+  const int kv_box[4] = {64, tp.box_rows, 1, 1};
+  if (!make_map(&q, p.q, 3, q_extent, q_stride, q_box) || !make_map(&k, p.k, 4, kv_extent, k_stride, kv_box) ||
+      !make_map(&v, p.v, 4, kv_extent, v_stride, kv_box))
+    return TOPLOC_ERR_CUDA;
+  int sms = 0;
+  if (const int rc = check_device(&sms)) return rc;
+  const int rows_item = two ? 2 * tp.tile_rows : tp.tile_rows;
+  const long long items = (long long)p.num_seqs * p.kv_heads * p.splits *
+                          (((long long)p.max_new * p.group + rows_item - 1) / rows_item);
+  const int blocks = (int)min(items, (long long)sms);
+  if (p.head_dim == 128)
+    return two ? launch<128, true>(tp, q, k, v, blocks, stream) : launch<128, false>(tp, q, k, v, blocks, stream);
+  return two ? launch<64, true>(tp, q, k, v, blocks, stream) : launch<64, false>(tp, q, k, v, blocks, stream);
+}
+
+}  // namespace toploc_model
