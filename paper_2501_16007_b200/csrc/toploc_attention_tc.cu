@@ -26,8 +26,11 @@ namespace {
 using namespace toploc_model;
 using namespace sm100;
 
-constexpr int kTcThreads = 320;
+constexpr int kTcThreads = 384;            // two groups of softmax, and one whose first two warps feed and issue
 constexpr int kItems = 4;                  // items announced ahead
+// Registers move from the third group of warps to the softmax, whose threads hold a row of 128 scores.  The block is
+// launched with 168 a thread (65536 / 384, in steps of 8); 2 * 216 + 72 = 3 * 168.
+constexpr int kSoftmaxRegisters = 216, kOtherRegisters = 72;
 constexpr float kLazyLog2 = 8.0f;
 constexpr int kBlockBytes = 128 * 128;     // 128 rows of 64 elements
 
@@ -167,6 +170,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
   constexpr uint32_t kOut = 256;  // scores of group w at 128 w, outputs at 256 + D w
 
   if (warp == 8) {
+    lower_registers<kOtherRegisters>();
     // ---- feeding: finds the items, copies queries, keys and values ----
     if (lane == 0) {
       prefetch_map(&map_q);
@@ -318,6 +322,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
         barrier_drain(shared_address(&sh.full[ring_stage(i, kStages)]), ring_parity(i, kStages));
     }
   } else if (warp == 9) {
+    lower_registers<kOtherRegisters>();
     // ---- products: one thread issues them all ----
     if (lane == 0) {
       constexpr uint32_t kScores = bf16_product(128, false), kValues = bf16_product(D, true);
@@ -426,7 +431,10 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       }
     }
     __syncwarp();
+  } else if (warp > 9) {
+    lower_registers<kOtherRegisters>();
   } else {
+    raise_registers<kSoftmaxRegisters>();
     // ---- softmax: a thread per row ----
     const int w = warp >> 2, r = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 rows of tensor memory
