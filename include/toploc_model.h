@@ -155,8 +155,9 @@ typedef struct {
  *                largest possible; BAD_PAGE; WAIT_EXPIRED), else left as it is;
  *                nothing outside the cache is read in any case
  * d_workspace    DEVICE toploc_attention_workspace_bytes, 16-byte aligned:
- *                partial results where few rows meet a long cache and the keys
- *                are split over blocks (always joined in the same order)
+ *                partial results of rows whose keys are split over blocks
+ *                (always joined in the same order); contents are undefined
+ *                afterwards, and calls that can overlap need one each
  * Asynchronous, deterministic.
  *
  * Variants, by a rule on types and layout: bf16 with head_dim 64 or 128, rows
@@ -176,11 +177,11 @@ int toploc_attention_paged(const void* d_q, const void* d_k_cache, const void* d
  * i is rows seq_offsets[i] .. seq_offsets[i + 1] - 1 of q, k and v, and a row
  * sees its own sequence's rows up to itself.  Everything else as above, with
  * d_k, d_v DEVICE [total_tokens, kv_heads, head_dim] (views of one tensor are
- * fine: strides).  Needs no workspace.
+ * fine: strides), and kv with page_size 0.
  */
 int toploc_attention_prompt(const void* d_q, const void* d_k, const void* d_v, const toploc_attention_layout* lay,
                             const toploc_kv_layout* kv, const int32_t* d_seq_offsets, void* d_out, float* d_lse_opt,
-                            uint8_t* d_status_opt, void* cuda_stream);
+                            uint8_t* d_status_opt, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* ---- norm ------------------------------------------------------------- */
 

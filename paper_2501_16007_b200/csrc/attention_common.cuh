@@ -8,7 +8,7 @@ namespace toploc_model {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kSms = 148;      // of a B200: sizes the workspace and the split, whatever device answers
-constexpr int kKeyTile = 128;  // keys of a tile of the tensor-core kernel; parts are whole tiles
+constexpr int kKeyTile = 128;  // keys of a tile of the tensor-core kernel
 
 struct AttentionParams {
   const void* q;
@@ -17,8 +17,8 @@ struct AttentionParams {
   void* out;
   float* lse;
   uint8_t* status;
-  float* part_out;  // [splits][total_tokens * q_heads][head_dim]
-  float* part_lse;  // [splits][total_tokens * q_heads], base 2
+  float* part_out;  // results over a part of the keys, and their lse (base 2)
+  float* part_lse;
   const int32_t* table;
   const int32_t* offsets;
   const int32_t* kv_lens;  // NULL: a prompt attends over its own rows
@@ -56,24 +56,13 @@ __device__ __forceinline__ SeqRange sequence(const AttentionParams& p, int i) {
   return s;
 }
 
-// The keys of part `split` of a sequence: whole tiles of 128.
-__device__ __forceinline__ void split_range(int keys, int splits, int split, int* begin, int* end) {
-  const int unit = ((keys + splits - 1) / splits + kKeyTile - 1) / kKeyTile * kKeyTile;
-  *begin = (int)min((long long)unit * split, (long long)keys);
-  *end = min(*begin + unit, keys);
-}
-
 // ---- the tensor-core kernel (toploc_attention_tc.cu) --------------------------------------------
 
 // Whether the tensor-core kernel takes these types, pointers and strides.
 bool tensor_cores_take(const toploc_attention_layout* lay, const toploc_kv_layout* kv, const void* q, const void* k,
                        const void* v, const void* out);
-// Rows of an item: every head of a key head, one tile of 128 rows (whole tokens) or two.
-inline int tensor_core_rows(const toploc_attention_layout* lay) {
-  const int group = lay->q_heads / lay->kv_heads, rows = 128 / group * group;
-  return (long long)lay->max_new_tokens * group <= rows ? rows : 2 * rows;
-}
-int launch_tensor_cores(const AttentionParams& p, const toploc_attention_layout* lay, const toploc_kv_layout* kv,
+size_t tensor_core_workspace_bytes(const toploc_attention_layout* lay);
+int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, const toploc_kv_layout* kv, void* workspace,
                         cudaStream_t stream);
 
 }  // namespace toploc_model

@@ -15,6 +15,13 @@ constexpr int kRows = 32;   // rows of a block
 constexpr int kKeys = 32;   // keys of a tile, one per lane
 constexpr int kWarpRows = kRows / 4;
 
+// The keys of part `split` of a sequence: a multiple of 128 keys each.
+__device__ __forceinline__ void split_range(int keys, int splits, int split, int* begin, int* end) {
+  const int unit = ((keys + splits - 1) / splits + 128 - 1) / 128 * 128;
+  *begin = (int)min((long long)unit * split, (long long)keys);
+  *end = min(*begin + unit, keys);
+}
+
 // ---- the kernel on the fp32 units: every type, layout and head size ------------------------------
 //
 // A block of four warps takes 32 rows of one key head against tiles of 32 keys in shared memory (fp32).
@@ -192,15 +199,14 @@ __global__ void __launch_bounds__(128) toploc_attention_join_kernel(const Attent
   if (p.lse && lane == 0) p.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
-// Parts the keys of a paged cache are split into, by the bounds the host knows (`rows`: of a block).
-int splits_of(const toploc_attention_layout* lay, const toploc_kv_layout* kv, int rows) {
+// Parts the keys of a paged cache are split into (fp32 units), by the bounds the host knows.
+int splits_of(const toploc_attention_layout* lay, const toploc_kv_layout* kv) {
   if (kv->page_size <= 0) return 1;
   const long long packed = (long long)lay->max_new_tokens * (lay->q_heads / lay->kv_heads);
-  const long long items = (packed + rows - 1) / rows * lay->kv_heads * lay->num_seqs;
+  const long long items = (packed + kRows - 1) / kRows * lay->kv_heads * lay->num_seqs;
   if (items == 0) return 1;
   const long long most = (long long)kv->max_pages * kv->page_size;
-  const long long wanted = items <= kSms / 2 ? kSms / items : 4ll * kSms / items;
-  return (int)max(1ll, min(min(wanted, most / 512), 64ll));
+  return (int)max(1ll, min(min((4ll * kSms + items - 1) / items, most / 256), 64ll));
 }
 
 int check_layout(const toploc_attention_layout* lay, const toploc_kv_layout* kv) {
@@ -222,6 +228,17 @@ int check_layout(const toploc_attention_layout* lay, const toploc_kv_layout* kv)
   return TOPLOC_OK;
 }
 
+bool tensor_core_types(const toploc_attention_layout* lay) {
+  return lay->dtype == TOPLOC_DTYPE_BF16 && (lay->head_dim == 64 || lay->head_dim == 128);
+}
+
+size_t workspace_bytes_of(const toploc_attention_layout* lay, const toploc_kv_layout* kv, bool tensor_cores) {
+  if (lay->num_seqs == 0 || lay->total_tokens == 0 || lay->max_new_tokens == 0) return 0;
+  if (tensor_cores) return tensor_core_workspace_bytes(lay);
+  const int splits = splits_of(lay, kv);
+  return splits <= 1 ? 0 : (size_t)splits * lay->total_tokens * lay->q_heads * (lay->head_dim + 1) * 4;
+}
+
 template <typename T, int CHUNKS>
 int launch_fp32(const AttentionParams& p, cudaStream_t stream) {
   const int bytes = (kRows + 2 * kKeys) * (p.head_dim + 4) * 4;
@@ -235,11 +252,9 @@ int launch_fp32(const AttentionParams& p, cudaStream_t stream) {
 }
 
 template <typename T>
-int launch_all(AttentionParams& p, const toploc_attention_layout* lay, const toploc_kv_layout* kv, bool tensor_cores,
-               cudaStream_t stream) {
+int launch_all(AttentionParams& p, cudaStream_t stream) {
   p.row_tiles = (int)(((long long)p.max_new * p.group + kRows - 1) / kRows);
-  int rc = tensor_cores ? launch_tensor_cores(p, lay, kv, stream)
-           : p.head_dim <= 64 ? launch_fp32<T, 2>(p, stream)
+  const int rc = p.head_dim <= 64 ? launch_fp32<T, 2>(p, stream)
            : p.head_dim <= 128 ? launch_fp32<T, 4>(p, stream) : launch_fp32<T, 8>(p, stream);
   if (rc != TOPLOC_OK || p.splits == 1) return rc;
   const long long rows = p.total_tokens * p.q_heads;
@@ -270,17 +285,17 @@ int attention(const void* d_q, const void* d_k, const void* d_v, const toploc_at
   p.num_seqs = lay->num_seqs; p.max_new = lay->max_new_tokens;
   p.page_size = kv->page_size; p.num_pages = kv->num_pages; p.max_pages = kv->max_pages;
   const bool tensor_cores = tensor_cores_take(lay, kv, d_q, d_k, d_v, d_out);
-  p.splits = splits_of(lay, kv, tensor_cores ? tensor_core_rows(lay) : kRows);
+  const size_t need = workspace_bytes_of(lay, kv, tensor_cores);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return TOPLOC_ERR_WORKSPACE;
+  if (need > 0 && !aligned(workspace, 16)) return TOPLOC_ERR_INVALID_ARGUMENT;
+  const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  if (tensor_cores) return launch_tensor_cores(p, lay, kv, workspace, stream);
+  p.splits = splits_of(lay, kv);
   if (p.splits > 1) {
-    const size_t need = toploc_attention_workspace_bytes(lay, kv);
-    if (!workspace || workspace_bytes < need) return TOPLOC_ERR_WORKSPACE;
-    if (!aligned(workspace, 16)) return TOPLOC_ERR_INVALID_ARGUMENT;
     p.part_out = static_cast<float*>(workspace);
     p.part_lse = p.part_out + (long long)p.splits * p.total_tokens * p.q_heads * p.head_dim;
   }
-  const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  return lay->dtype == TOPLOC_DTYPE_BF16 ? launch_all<__nv_bfloat16>(p, lay, kv, tensor_cores, stream)
-                                         : launch_all<float>(p, lay, kv, tensor_cores, stream);
+  return lay->dtype == TOPLOC_DTYPE_BF16 ? launch_all<__nv_bfloat16>(p, stream) : launch_all<float>(p, stream);
 }
 
 }  // namespace
@@ -288,8 +303,7 @@ int attention(const void* d_q, const void* d_k, const void* d_v, const toploc_at
 extern "C" size_t toploc_attention_workspace_bytes(const toploc_attention_layout* lay, const toploc_kv_layout* kv) {
   if (check_layout(lay, kv) != TOPLOC_OK) return 0;
   // (which kernel takes the call also depends on the pointers: room for either)
-  const int splits = max(splits_of(lay, kv, kRows), splits_of(lay, kv, tensor_core_rows(lay)));
-  return splits <= 1 ? 0 : (size_t)splits * lay->total_tokens * lay->q_heads * (lay->head_dim + 1) * 4;
+  return max(workspace_bytes_of(lay, kv, false), tensor_core_types(lay) ? workspace_bytes_of(lay, kv, true) : 0);
 }
 
 extern "C" int toploc_attention_paged(const void* d_q, const void* d_k_cache, const void* d_v_cache,
@@ -309,11 +323,12 @@ extern "C" int toploc_attention_paged(const void* d_q, const void* d_k_cache, co
 extern "C" int toploc_attention_prompt(const void* d_q, const void* d_k, const void* d_v,
                                        const toploc_attention_layout* lay, const toploc_kv_layout* kv,
                                        const int32_t* d_seq_offsets, void* d_out, float* d_lse_opt,
-                                       uint8_t* d_status_opt, void* cuda_stream) {
+                                       uint8_t* d_status_opt, void* d_workspace, size_t workspace_bytes,
+                                       void* cuda_stream) {
   if (const int rc = check_layout(lay, kv)) return rc;
   if (kv->page_size != 0) return TOPLOC_ERR_INVALID_ARGUMENT;
   if (lay->num_seqs == 0 || lay->max_new_tokens == 0 || lay->total_tokens == 0) return TOPLOC_OK;
   if (!d_q || !d_k || !d_v || !d_seq_offsets || !d_out) return TOPLOC_ERR_INVALID_ARGUMENT;
-  return attention(d_q, d_k, d_v, lay, kv, nullptr, d_seq_offsets, nullptr, d_out, d_lse_opt, d_status_opt, nullptr, 0,
-                   cuda_stream);
+  return attention(d_q, d_k, d_v, lay, kv, nullptr, d_seq_offsets, nullptr, d_out, d_lse_opt, d_status_opt, d_workspace,
+                   workspace_bytes, cuda_stream);
 }

@@ -6,15 +6,20 @@
 // for all of them, a chunk of 32 tokens with four heads a group fills a tile, and a single token still
 // has its heads side by side.
 //
-// A block has ten warps: two groups of four that do the softmax, a thread per row (no exchange between
-// threads: the running maximum and sum of a row live in one), a warp that feeds keys and values through a
-// ring of tiles by tensor copies, and one that issues the products.  While one group works on its scores the
-// tensor cores run the other group's products.  The groups hold
-//   two row tiles against the same keys      (kTwoTiles: more than 128 rows), or
-//   one row tile against every other key tile (few rows, the single tokens among them: bound by reading
-//                                              the keys, so both groups serve the stream and join at the end).
-// Blocks are persistent: one an SM, walking over (sequence, row tile, key head, part of the keys); the feeding
-// warp runs ahead into the next item while the last one is finished.
+// A block has two groups of four warps that do the softmax, a thread per row (no exchange between threads: the
+// running maximum and sum of a row live in one), a warp that feeds keys and values through a ring of tiles by tensor
+// copies, and one that issues the products.  While one group works on its scores the tensor cores run the other
+// group's products.  The groups hold, item by item,
+//   two row tiles against the same keys      (more than 128 rows), or
+//   one row tile against every other key tile (few rows, single tokens among them: bound by reading the keys, so both
+//                                              groups serve the stream and join at the end).
+//
+// The work is cut evenly, not by items: the keys that all row tiles see, one after the other, are one long line, and
+// each of the persistent blocks (one an SM) takes an equal stretch of it.  A tile whose keys lie in several stretches
+// leaves partial results (normalised outputs and lse) that a second kernel joins, always in the same order.  So a
+// single long sequence and a batch of ragged ones both keep every SM busy to the end, whatever the lengths on the
+// device are; there is no bound on them to tune by.  The feeding warp runs ahead into the next item while the last one
+// is finished.
 //
 // The output is not rescaled whenever the maximum grows but only where it grew by more than 2^8: P then stays
 // below 2^8, and O, the sum and P share the same reference, so the quotient is the same.
@@ -34,27 +39,32 @@ constexpr int kSoftmaxRegisters = 216, kOtherRegisters = 72;
 constexpr float kLazyLog2 = 8.0f;
 constexpr int kBlockBytes = 128 * 128;     // 128 rows of 64 elements
 
-// One piece of work: a tile of rows of one sequence and key head against a range of its keys.
+// One piece of work: two tiles of rows (or the one that is left) of a sequence and key head against a range of keys.
 struct Item {
   int seq;     // -1: no more work
   int head;    // key head
-  int split;
+  int slot;    // where the result goes: -1 the output, 0 a part whose row tile began in an earlier block, 1 in this one
   int first;   // row of the packed tensors its sequence starts at
   int behind;  // keys in front of the sequence's first new token (may be negative)
-  int row0;    // first packed row (token * group + head in group) of the tile
+  int row0;    // first packed row (token * group + head in group)
   int rows;    // packed rows of the sequence
   int kbegin;  // keys kbegin .. kend - 1, kbegin a multiple of the tile
   int kend;
-  int n0, n1;  // tiles of the two groups (two row tiles), or n0 tiles in all
-  int pad;
+  int two;     // two row tiles
+  int n0, n1;  // key tiles of the two groups, or n0 in all
 };
 
-template <int D, bool kTwoTiles>
+// The parts a block leaves, for the join.
+struct Part {
+  int seq, head, row0, first, rows;  // seq -1: none
+  int last;                          // slot 0: the row tile's keys end here
+};
+
+template <int D>
 struct Shared {
   static constexpr int kHalves = D / 64;
   static constexpr int kTileBytes = kHalves * kBlockBytes;
-  static constexpr int kQTiles = kTwoTiles ? 2 : 1;
-  static constexpr int kStages = D == 128 ? 5 : 8;
+  static constexpr int kStages = D == 128 ? 5 : 10;
   struct Head {
     uint64_t full[kStages], empty[kStages];
     uint64_t s_full[2], p_full[2], o_full[2];
@@ -66,10 +76,9 @@ struct Shared {
     int gave_up;
     int bad_values[2];  // number of the item (by parity) in whose hidden keys' tiles a value was not finite
   };
-  static constexpr int kHeadBytes = 1024;
+  static constexpr int kHeadBytes = 1024, kExchangeBytes = 2 * 128 * 8;
   static_assert(sizeof(Head) <= kHeadBytes, "head");
-  static constexpr int kExchangeBytes = kTwoTiles ? 0 : 2 * 128 * 2 * 4;
-  static constexpr int kBytes = 1024 + kHeadBytes + (kQTiles + kStages) * kTileBytes + kExchangeBytes;
+  static constexpr int kBytes = kHeadBytes + kExchangeBytes + (2 + kStages) * kTileBytes;
   static_assert(kBytes <= 232448, "shared memory of a block");
 };
 
@@ -107,6 +116,7 @@ struct TcParams {
   int tile_rows;  // packed rows of a row tile: 128 rounded down to whole tokens
   int box_rows;   // rows of a key copy
   int q_bytes;    // bytes of a query tile's copy
+  Part* parts;    // [blocks][2]
 };
 
 // A wait of a whole warp: all lanes or none go on.
@@ -115,31 +125,113 @@ __device__ __forceinline__ bool warp_wait(const uint64_t& bar, uint32_t parity, 
 }
 
 // Tiles of the ring an item takes, and the place of value tile j among them.
-template <bool kTwoTiles>
-__device__ __forceinline__ int item_tiles(const Item& im) {
-  return kTwoTiles ? max(im.n0, im.n1) : im.n0;
-}
-template <bool kTwoTiles>
-__device__ __forceinline__ int value_place(int j, int n) {
-  return kTwoTiles ? 2 * j + 1 : min(n, j + 2) + j;  // K0 V0 K1 V1 .. or K0 K1 V0 K2 V1 ..
+__device__ __forceinline__ int item_tiles(const Item& im) { return im.two ? max(im.n0, im.n1) : im.n0; }
+__device__ __forceinline__ int value_place(bool two, int j, int n) {
+  return two ? 2 * j + 1 : min(n, j + 2) + j;  // K0 V0 K1 V1 .. or K0 K1 V0 K2 V1 ..
 }
 
-template <int D, bool kTwoTiles>
+// ---- the line of work ----------------------------------------------------------------------------
+//
+// A sequence of T rows and c keys in front of them has L levels of rows_item rows per key head; a level stands for
+// kLevelCost (what an item costs beside its keys, in keys) + c + the tokens up to its end.  Sequences follow one
+// another, in them key heads, in them levels.
+
+constexpr long long kLevelCost = 192;
+constexpr long long kLeastShare = 6 * kKeyTile;  // less is not worth a block of its own
+
+struct Line {
+  long long front;  // kLevelCost + keys in front
+  int rows_item, tokens_item, tokens, levels;
+  __device__ Line(const TcParams& tp, const SeqRange& s)
+      : front(kLevelCost + max(s.keys - s.rows, 0)), rows_item(2 * tp.tile_rows), tokens_item(rows_item / tp.p.group),
+        tokens(s.rows), levels((s.rows + tokens_item - 1) / tokens_item) {}
+  __device__ long long upto(int level) const {  // of levels 0 .. level - 1
+    const long long whole = level * front + (long long)tokens_item * level * (level + 1) / 2;
+    return level < levels ? whole : whole - ((long long)levels * tokens_item - tokens);
+  }
+};
+
+// A place on the line: a key tile of a level.
+struct Place {
+  int seq, head, level, tile;
+};
+
+__device__ __forceinline__ bool before(const Place& a, const Place& b) {
+  if (a.seq != b.seq) return a.seq < b.seq;
+  if (a.head != b.head) return a.head < b.head;
+  if (a.level != b.level) return a.level < b.level;
+  return a.tile < b.tile;
+}
+
+// Key tiles that a level's rows see in all.
+__device__ __forceinline__ int tiles_seen(const SeqRange& s, int tokens_upto) {
+  const int seen = min(s.keys, s.keys - s.rows + tokens_upto);
+  return seen > 0 ? (seen + kKeyTile - 1) / kKeyTile : 0;
+}
+
+constexpr int kRuns = kTcThreads;
+
+// Where position `at` of the line falls; a cut in front of a level's second tile or behind its last but one moves to the
+// level's ends.
+__device__ __forceinline__ Place find_place(const TcParams& tp, const long long* run_cost, int per, long long at) {
+  const AttentionParams& p = tp.p;
+  if (at >= run_cost[kRuns]) return Place{p.num_seqs, 0, 0, 0};
+  int lo = 0, hi = kRuns;  // run_cost[lo] <= at < run_cost[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (run_cost[mid] <= at) lo = mid; else hi = mid;
+  }
+  at -= run_cost[lo];
+  for (int i = lo * per; i < p.num_seqs; ++i) {
+    const SeqRange s = sequence(p, i);
+    const Line line(tp, s);
+    const long long one = line.upto(line.levels), all = one * p.kv_heads;
+    if (at >= all) {
+      at -= all;
+      continue;
+    }
+    Place place = {i, (int)(at / one), 0, 0};
+    at -= place.head * one;
+    int a = 0, b = line.levels;  // upto(a) <= at < upto(b)
+    while (b - a > 1) {
+      const int mid = (a + b) >> 1;
+      if (line.upto(mid) <= at) a = mid; else b = mid;
+    }
+    place.level = a;
+    at -= line.upto(a);
+    const int n = tiles_seen(s, min((a + 1) * line.tokens_item, line.tokens));
+    const long long tile = (at - kLevelCost + kKeyTile / 2) / kKeyTile;
+    if (at <= kLevelCost || tile <= 1) return place;
+    if (tile >= n - 1) {
+      if (++place.level == line.levels) {
+        place.level = 0;
+        if (++place.head == p.kv_heads) return Place{i + 1, 0, 0, 0};
+      }
+      return place;
+    }
+    place.tile = (int)tile;
+    return place;
+  }
+  return Place{p.num_seqs, 0, 0, 0};
+}
+
+template <int D>
 __global__ void __launch_bounds__(kTcThreads, 1)
 toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMap map_q,
                            const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
-  using S = Shared<D, kTwoTiles>;
+  using S = Shared<D>;
   constexpr int kStages = S::kStages, kHalves = S::kHalves;
-  extern __shared__ unsigned char dynamic[];
+  extern __shared__ __align__(1024) unsigned char base[];
   const AttentionParams& p = tp.p;
-  unsigned char* base = dynamic + ((1024 - (shared_address(dynamic) & 1023)) & 1023);
   typename S::Head& sh = *reinterpret_cast<typename S::Head*>(base);
-  unsigned char* q_tiles = base + S::kHeadBytes;
-  unsigned char* ring = q_tiles + S::kQTiles * S::kTileBytes;
-  float2* exchange = reinterpret_cast<float2*>(ring + kStages * S::kTileBytes);  // (maximum, sum) of [group][row]
+  float2* exchange = reinterpret_cast<float2*>(base + S::kHeadBytes);  // (maximum, sum) of [group][row]
+  unsigned char* q_tiles = base + S::kHeadBytes + S::kExchangeBytes;
+  unsigned char* ring = q_tiles + 2 * S::kTileBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* gave_up = &sh.gave_up;
 
+  // tell the join kernel that it may be scheduled (it waits for this grid to end)
+  asm volatile("griddepcontrol.launch_dependents;");
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       barrier_init(shared_address(&sh.full[i]), 1);
@@ -163,6 +255,32 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
     barrier_init_fence();
   }
   if (warp == 9) tmem_alloc(shared_address(&sh.tmem), 512);
+  // the line: a run of sequences per thread, and the work in front of every run (kept where the ring comes later)
+  long long* run_cost = reinterpret_cast<long long*>(ring);
+  long long* warp_cost = run_cost + kRuns + 1;
+  const int per = (p.num_seqs + kRuns - 1) / kRuns;
+  {
+    long long cost = 0;
+    for (int i = threadIdx.x * per; i < min(((int)threadIdx.x + 1) * per, p.num_seqs); ++i) {
+      const SeqRange s = sequence(p, i);
+      if (s.bad && p.status && blockIdx.x == 0) p.status[i] = TOPLOC_SEQ_BAD_LENGTH;
+      const Line line(tp, s);
+      cost += line.upto(line.levels) * p.kv_heads;
+    }
+    long long incl = cost;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const long long up = __shfl_up_sync(0xFFFFFFFFu, incl, off);
+      if (lane >= off) incl += up;
+    }
+    if (lane == 31) warp_cost[warp] = incl;
+    __syncthreads();
+    long long in_front = incl - cost;
+    for (int w = 0; w < warp; ++w) in_front += warp_cost[w];
+    run_cost[threadIdx.x] = in_front;
+    if (threadIdx.x == kRuns - 1) run_cost[kRuns] = in_front + cost;
+    fence_async_shared();  // tensor copies write there next
+  }
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
@@ -178,67 +296,61 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       prefetch_map(&map_v);
     }
     const bool paged = p.kv_lens != nullptr;
-    const int rows_item = S::kQTiles * tp.tile_rows;
-    long long item = blockIdx.x, before = 0;  // before: items of the sequences in front of the batch of 32
-    int batch = -32;
-    SeqRange mine = {};
-    long long incl = 0, batch_items = 0;
+    const int rows_item = 2 * tp.tile_rows, tokens_item = rows_item / p.group;
+    const long long all = run_cost[kRuns];
+    const long long share = max((all + gridDim.x - 1) / gridDim.x, kLeastShare);
+    Place at = find_place(tp, run_cost, per, share * blockIdx.x);
+    const Place end = find_place(tp, run_cost, per, share * (blockIdx.x + 1));
+    __syncwarp();  // run_cost has been read: the ring's place is free
+    SeqRange s = {0, 0, 0, false};
+    int s_of = -1;
     uint32_t fed = 0, q_uses = 0;
+    if (lane < 2 && tp.parts) tp.parts[2 * blockIdx.x + lane].seq = -1;
+    __syncwarp();
     for (uint32_t number = 0;; ++number) {
-      // the item's sequence: lanes hold 32 sequences and the prefix sum of their items
-      bool more = true;
-      while (batch < 0 || item >= before + batch_items) {
-        before += batch_items;
-        batch = batch < 0 ? 0 : batch + 32;
-        if (batch >= p.num_seqs) {
-          more = false;
-          break;
+      while (before(at, end)) {  // the sequence of the next item, past those without rows
+        if (s_of != at.seq) {
+          s = sequence(p, at.seq);
+          s_of = at.seq;
         }
-        mine = SeqRange{0, 0, 0, false};
-        if (batch + lane < p.num_seqs) mine = sequence(p, batch + lane);
-        if (mine.bad && p.status && blockIdx.x == 0) p.status[batch + lane] = TOPLOC_SEQ_BAD_LENGTH;
-        const long long tiles = ((long long)mine.rows * p.group + rows_item - 1) / rows_item;
-        incl = tiles * p.kv_heads * p.splits;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-          const long long up = __shfl_up_sync(0xFFFFFFFFu, incl, off);
-          if (lane >= off) incl += up;
-        }
-        batch_items = __shfl_sync(0xFFFFFFFFu, incl, 31);
+        if (s.rows > 0) break;
+        at = Place{at.seq + 1, 0, 0, 0};
       }
+      const bool more = before(at, end);
       const uint32_t slot = number % kItems;
       if (!warp_wait(sh.item_empty[slot], ((number / kItems) & 1) ^ 1, gave_up)) break;
       Item im = {};
       im.seq = -1;
       if (more) {
-        const unsigned ahead = __ballot_sync(0xFFFFFFFFu, item < before + incl);
-        const int src = __ffs(ahead) - 1;
-        const SeqRange s = {__shfl_sync(0xFFFFFFFFu, mine.first, src), __shfl_sync(0xFFFFFFFFu, mine.rows, src),
-                            __shfl_sync(0xFFFFFFFFu, mine.keys, src), false};
-        const long long upto = src == 0 ? 0 : __shfl_sync(0xFFFFFFFFu, incl, src - 1);
-        const long long rest = item - before - upto, per_tile = (long long)p.kv_heads * p.splits;
-        im.seq = batch + src;
-        im.split = (int)(rest % p.splits);
-        im.head = (int)(rest / p.splits % p.kv_heads);
+        im.seq = at.seq;
+        im.head = at.head;
         im.first = s.first;
-        im.rows = s.rows * p.group;
-        const int tiles = (im.rows + rows_item - 1) / rows_item;
-        im.row0 = (tiles - 1 - (int)(rest / per_tile)) * rows_item;  // the longest first
         im.behind = s.keys - s.rows;
-        int kend;
-        split_range(s.keys, p.splits, im.split, &im.kbegin, &kend);
-        const auto tiles_upto = [&](int last_row) {  // tiles up to the newest key that packed row `last_row` sees
-          const int seen = min(kend, im.behind + last_row / p.group + 1);
-          return seen > im.kbegin ? (seen - im.kbegin + kKeyTile - 1) / kKeyTile : 0;
-        };
-        const int last_row = min(im.rows, im.row0 + rows_item) - 1;
-        im.kend = min(kend, im.behind + last_row / p.group + 1);
-        if (kTwoTiles) {
-          const int last0 = min(im.rows, im.row0 + tp.tile_rows) - 1;
-          im.n0 = tiles_upto(last0);
-          im.n1 = last_row > last0 ? tiles_upto(last_row) : 0;
+        im.row0 = at.level * rows_item;
+        im.rows = s.rows * p.group;
+        const int tokens = min((at.level + 1) * tokens_item, s.rows);
+        const int all_tiles = tiles_seen(s, tokens);
+        const bool ends_here = end.seq == at.seq && end.head == at.head && end.level == at.level;
+        const int tile_end = ends_here ? end.tile : all_tiles;
+        im.kbegin = at.tile * kKeyTile;
+        im.kend = min(min(s.keys, im.behind + tokens), tile_end * kKeyTile);
+        im.two = im.row0 + tp.tile_rows < im.rows;
+        if (im.two) {
+          const int first = tiles_seen(s, at.level * tokens_item + tokens_item / 2);
+          im.n0 = max(min(first, tile_end) - at.tile, 0);
+          im.n1 = max(tile_end - at.tile, 0);
         } else {
-          im.n0 = tiles_upto(last_row);
+          im.n0 = max(tile_end - at.tile, 0);
+        }
+        im.slot = at.tile > 0 ? 0 : ends_here ? 1 : -1;
+        if (im.slot >= 0 && lane == 0)
+          tp.parts[2 * blockIdx.x + im.slot] = Part{im.seq, im.head, im.row0, im.first, im.rows, ends_here ? 0 : 1};
+        at.tile = 0;  // the next item
+        if (ends_here) {
+          at = end;
+        } else if (rows_item * (++at.level) >= im.rows) {
+          at.level = 0;
+          if (++at.head == p.kv_heads) at = Place{at.seq + 1, 0, 0, 0};
         }
       }
       if (lane == 0) {
@@ -247,15 +359,14 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       }
       __syncwarp();
       if (!more) break;
-      const int n = item_tiles<kTwoTiles>(im);
-      item += gridDim.x;
+      const int n = item_tiles(im);
       if (n == 0) continue;
 
 
       // queries: each tile in blocks of 64 channels
       if (!warp_wait(sh.q_empty, (q_uses & 1) ^ 1, gave_up)) break;
       ++q_uses;
-      const bool second = kTwoTiles && im.row0 + tp.tile_rows < im.rows;
+      const bool second = im.two;
       const uint32_t q_bar = shared_address(&sh.q_full);
       if (lane == 0) barrier_arrive_expect(q_bar, (second ? 2 : 1) * tp.q_bytes);
       __syncwarp();
@@ -298,7 +409,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       };
       bool fine = true;
       int page = page_of(0), next = page_of(1);  // looked up ahead of their use
-      if (kTwoTiles) {
+      if (im.two) {
         for (int j = 0; fine && j < n; ++j) {
           fine = feed(&map_k, j, page) && feed(&map_v, j, page);
           page = next;
@@ -334,8 +445,8 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
         return ok;
       };
       const auto release = [&](uint32_t n) { mma_commit(shared_address(&sh.empty[ring_stage(n, kStages)])); };
-      const auto scores = [&](int w, uint32_t n) {  // scores of group w against the key tile at place n
-        const uint32_t a = q_at + (kTwoTiles ? w : 0) * S::kTileBytes, b = ring_at + ring_stage(n, kStages) * S::kTileBytes;
+      const auto scores = [&](int w, uint32_t n, bool two) {  // scores of group w against the key tile at place n
+        const uint32_t a = q_at + (two ? w : 0) * S::kTileBytes, b = ring_at + ring_stage(n, kStages) * S::kTileBytes;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const uint32_t at = (k / 4) * kBlockBytes + (k % 4) * 32;
@@ -360,17 +471,18 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
         const uint32_t slot = number % kItems;
         if (!barrier_wait(shared_address(&sh.item_full[slot]), (number / kItems) & 1, gave_up)) break;
         const int seq = sh.items[slot].seq, n0 = sh.items[slot].n0, n1 = sh.items[slot].n1;
+        const bool two = sh.items[slot].two;
         barrier_arrive(shared_address(&sh.item_empty[slot]));
         if (seq < 0) break;
-        const int n = kTwoTiles ? max(n0, n1) : n0;
+        const int n = two ? max(n0, n1) : n0;
         if (n == 0) continue;
         bool ok = barrier_wait(shared_address(&sh.q_full), q_uses++ & 1, gave_up);
         tmem_fence_after();
-        if (kTwoTiles) {
+        if (two) {
           ok = ok && full(used);
           if (!ok) break;
-          if (n0 > 0) scores(0, used);
-          if (n1 > 0) scores(1, used);
+          if (n0 > 0) scores(0, used, true);
+          if (n1 > 0) scores(1, used, true);
           release(used);
           if (n == 1) mma_commit(shared_address(&sh.q_empty));
           for (int j = 0; ok && j < n; ++j) {
@@ -388,7 +500,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
                 if (!key_there) ok = full(k_at);
                 if (!ok) break;
                 key_there = true;
-                scores(w, k_at);
+                scores(w, k_at, true);
               }
             }
             if (!ok) break;
@@ -403,7 +515,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
           for (int w = 0; ok && w < min(n, 2); ++w, ++at) {
             ok = full(at);
             if (!ok) break;
-            scores(w, at);
+            scores(w, at, false);
             release(at);
           }
           if (n <= 2 && ok) mma_commit(shared_address(&sh.q_empty));
@@ -416,7 +528,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
             if (j + 2 < n) {
               ok = full(at);
               if (!ok) break;
-              scores(w, at);
+              scores(w, at, false);
               release(at++);
               if (j + 3 == n) mma_commit(shared_address(&sh.q_empty));
             }
@@ -454,20 +566,21 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       __syncwarp();
       if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
       if (im.seq < 0) break;
-      const int n = item_tiles<kTwoTiles>(im);
-      const int row = im.row0 + (kTwoTiles ? w * tp.tile_rows : 0) + r;      // packed row
+      const int n = item_tiles(im);
+      const bool two = im.two;
+      const int row = im.row0 + (two ? w * tp.tile_rows : 0) + r;            // packed row
       const bool valid = r < tp.tile_rows && row < im.rows;
       const int token = row / p.group;
       const int newest = valid ? im.behind + token : -1;                     // the newest key the row sees
       // keys up to `common` are seen by every row of the group's tile
-      const int common = im.behind + (im.row0 + (kTwoTiles ? w * tp.tile_rows : 0)) / p.group;
+      const int common = im.behind + (im.row0 + (two ? w * tp.tile_rows : 0)) / p.group;
       const int hidden_from = max(im.behind + im.row0 / p.group + 1, 0);     // first key hidden from a row of the item
       const bool live = __any_sync(0xFFFFFFFFu, valid);                      // else nobody reads the warp's rows
-      const int tiles = kTwoTiles ? (w ? im.n1 : im.n0) : (n + 1 - w) / 2;
+      const int tiles = two ? (w ? im.n1 : im.n0) : (n + 1 - w) / 2;
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       for (int i = 0; i < tiles; ++i) {
-        const int j = kTwoTiles ? i : 2 * i + w;
+        const int j = two ? i : 2 * i + w;
         const int key0 = im.kbegin + j * kKeyTile;
         const bool masked = key0 + kKeyTile - 1 > common;
         ok = warp_wait(sh.s_full[w], s_uses++ & 1, gave_up);
@@ -549,7 +662,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
           // Values of hidden keys meet weights of zero, and 0 * NaN is NaN: rows past the item's keys (never
           // loaded, or another sequence's) become zero; a value in front of them that is not finite too, and
           // the rows that do see it get it back at the end.
-          const uint32_t place = used + value_place<kTwoTiles>(j, n), stage = ring_stage(place, kStages);
+          const uint32_t place = used + value_place(two, j, n), stage = ring_stage(place, kStages);
           ok = warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up);
           if (!ok) break;
           const int from = max(hidden_from - key0, 0);
@@ -590,9 +703,9 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       used += 2 * n;
 
       // ---- the rows' results ----
-      if (!kTwoTiles) pv[w ^ 1] += (n + 1 - (w ^ 1)) / 2;
-      float weight[2] = {1.f, 0.f}, total = l, top = m;  // of this group's outputs and of the other's
-      if (!kTwoTiles) {
+      pv[w ^ 1] += two ? (w ? im.n0 : im.n1) : (n + 1 - (w ^ 1)) / 2;  // the other group's products
+      float weight[2] = {1.f, 0.f}, total = l, top = m;  // one row tile: of the groups' outputs
+      if (!two) {
         exchange[w * 128 + r] = make_float2(m, l);
         ok = join();
         if (!ok) break;
@@ -601,40 +714,37 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
         const float ref = top == -INFINITY ? 0.f : top;
         weight[0] = a.x == -INFINITY ? 0.f : exp2_approx((a.x - ref) * scale);
         weight[1] = b.x == -INFINITY ? 0.f : exp2_approx((b.x - ref) * scale);
-        if (a.x == INFINITY || b.x == INFINITY) weight[0] = weight[1] = NAN;
+        if (top == INFINITY) weight[0] = weight[1] = NAN;
         total = a.y * weight[0] + b.y * weight[1];
-        // a NaN score leaves no trace in a maximum
-        if (a.y != a.y || b.y != b.y) total = NAN;
+        if (a.y != a.y || b.y != b.y) total = NAN;  // a NaN score leaves no trace in a maximum
       }
       const bool any_keys = total != 0.f;
       const float inv = any_keys ? 1.f / total : 0.f;
       const int head = im.head * p.group + row - token * p.group;
       const long long at = (long long)(im.first + token) * p.q_heads + head;
-      const bool two_sided = !kTwoTiles && n > 1;
+      // where the row's part of a split tile goes
+      const long long part = ((long long)blockIdx.x * 2 + im.slot) * (2 * tp.tile_rows) + (row - im.row0);
       // two row tiles: a group writes its rows; one: each group writes half of the channels
-      constexpr int kWidth = kTwoTiles ? D : D / 2;
-      const int c0 = kTwoTiles ? 0 : w * kWidth;
-      if (tiles > 0 && kTwoTiles) ok = warp_wait(sh.o_full[w], (pv[w] - 1) & 1, gave_up);
-      if (!kTwoTiles && n > 0) {
-        ok = warp_wait(sh.o_full[0], (pv[0] - 1) & 1, gave_up);
-        if (n > 1) ok = ok && warp_wait(sh.o_full[1], (pv[1] - 1) & 1, gave_up);
-      }
+      const int width = two ? D : D / 2, c0 = two ? 0 : w * width;
+      const bool mine = (two ? tiles : n) > 0, others = !two && n > 1;
+      const uint32_t o_at = tmem + lanes + kOut + (two ? D * w : 0);
+      if (two ? mine && w == 0 : mine) ok = warp_wait(sh.o_full[0], (pv[0] - 1) & 1, gave_up);
+      if (two ? mine && w == 1 : others) ok = ok && warp_wait(sh.o_full[1], (pv[1] - 1) & 1, gave_up);
       if (!ok) break;
       tmem_fence_after();
       const bool repair = *(volatile int*)&sh.bad_values[number & 1] == (int)number;
 #pragma unroll 1
-      for (int c = c0; c < c0 + kWidth; c += 32) {
+      for (int c = c0; c < c0 + width; c += 32) {
         float o[32];
-        if (live && (kTwoTiles ? tiles : n) > 0) {
+        if (live && mine) {
           uint32_t x[32];
-          tmem_load(x, tmem + lanes + kOut + (kTwoTiles ? D * w : 0) + c);
+          tmem_load(x, o_at + c);
           tmem_wait_load();
           tmem_ready(x);
-          const float w0 = kTwoTiles ? 1.f : weight[0];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = kTwoTiles ? __uint_as_float(x[e]) : w0 == 0.f ? 0.f : __uint_as_float(x[e]) * w0;
-          if (two_sided) {
-            tmem_load(x, tmem + lanes + kOut + D + c);
+          for (int e = 0; e < 32; ++e) o[e] = weight[0] == 0.f ? 0.f : __uint_as_float(x[e]) * weight[0];
+          if (others) {
+            tmem_load(x, o_at + D + c);
             tmem_wait_load();
             tmem_ready(x);
 #pragma unroll
@@ -665,7 +775,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
             }
           }
         }
-        if (p.splits == 1) {
+        if (im.slot < 0) {
           uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + (im.first + token) * p.out_token +
                                                 head * p.out_head + c);
 #pragma unroll
@@ -673,20 +783,20 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
             out[e / 8] = make_uint4(pack_bf16(o[e] * inv, o[e + 1] * inv), pack_bf16(o[e + 2] * inv, o[e + 3] * inv),
                                     pack_bf16(o[e + 4] * inv, o[e + 5] * inv), pack_bf16(o[e + 6] * inv, o[e + 7] * inv));
         } else {
-          float4* out = reinterpret_cast<float4*>(p.part_out + (im.split * p.total_tokens * p.q_heads + at) * D + c);
+          float4* out = reinterpret_cast<float4*>(p.part_out + part * D + c);
 #pragma unroll
           for (int e = 0; e < 32; e += 4)
             out[e / 4] = make_float4(o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv);
         }
       }
-      if (valid && (kTwoTiles || w == 0)) {
+      if (valid && (two || w == 0)) {
         const float lse2 = any_keys ? (top == -INFINITY ? 0.f : top) * scale + log2f(total) : -INFINITY;
-        if (p.splits > 1)
-          p.part_lse[im.split * p.total_tokens * p.q_heads + at] = lse2;
+        if (im.slot >= 0)
+          p.part_lse[part] = lse2;
         else if (p.lse)
           p.lse[at] = lse2 * kLn2;
       }
-      if (!kTwoTiles) {  // both have read: the next item may overwrite
+      if (!two) {  // both have read: the next item may overwrite
         tmem_fence_before();
         if (!join()) break;
       }
@@ -697,6 +807,54 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
     for (int i = blockIdx.x; i < p.num_seqs; i += gridDim.x) p.status[i] = TOPLOC_SEQ_WAIT_EXPIRED;
   }
   if (warp == 9) tmem_free(tmem, 512);
+}
+
+// ---- joining the parts ---------------------------------------------------------------------------
+//
+// Block (b, y) looks after the row tile that block b of the first kernel began and did not finish: its parts are that
+// block's slot 1 and slot 0 of the next ones up to the one that finished it.  Part i has out_i = sum p v / sum p and
+// lse_i over its keys; the whole is sum_i w_i out_i / sum_i w_i, w_i = 2^(lse_i - max).  A warp per row, parts in order.
+constexpr int kJoinRows = 16;  // rows of a block
+
+template <int D>
+__global__ void __launch_bounds__(128) toploc_attention_tc_join_kernel(const TcParams tp) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const AttentionParams& p = tp.p;
+  const int b = blockIdx.x, lane = threadIdx.x & 31, rows_item = 2 * tp.tile_rows;
+  const Part part = tp.parts[2 * b + 1];
+  if (part.seq < 0) return;
+  int end = b + 1;  // the last block with a part
+  while (end < (int)gridDim.x - 1 && tp.parts[2 * end].seq >= 0 && !tp.parts[2 * end].last) ++end;
+  const int begin_row = blockIdx.y * kJoinRows + (threadIdx.x >> 5);
+  for (int r = begin_row; r < (int)(blockIdx.y + 1) * kJoinRows; r += 4) {
+    const int row = part.row0 + r;
+    if (r >= rows_item || row >= part.rows) break;
+    const auto place = [&](int i) { return (long long)(i == b ? 2 * b + 1 : 2 * i) * rows_item + r; };
+    float top = -INFINITY;
+    for (int i = b + lane; i <= end; i += 32) top = fmaxf(top, p.part_lse[place(i)]);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, off));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, o[D / 32];
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
+    for (int i = b; i <= end; ++i) {
+      const float w = exp2f(p.part_lse[place(i)] - ref);
+      sum += w;
+      if (w == 0.f) continue;
+      const float* from = p.part_out + place(i) * D + lane * (D / 32);
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) o[e] = fmaf(w, from[e], o[e]);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int token = row / p.group, head = part.head * p.group + row - token * p.group;
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + (part.first + token) * p.out_token + head * p.out_head +
+                         lane * (D / 32);
+#pragma unroll
+    for (int e = 0; e < D / 32; e += 2) *reinterpret_cast<uint32_t*>(out + e) = pack_bf16(o[e] * inv, o[e + 1] * inv);
+    if (p.lse && lane == 0)
+      p.lse[(long long)(part.first + token) * p.q_heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+  }
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -732,15 +890,26 @@ bool make_map(CUtensorMap* map, const void* at, int rank, const int64_t* extent,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool kTwoTiles>
+template <int D>
 int launch(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int blocks,
            cudaStream_t stream) {
-  constexpr int kBytes = Shared<D, kTwoTiles>::kBytes;
-  if (cudaFuncSetAttribute(toploc_attention_tc_kernel<D, kTwoTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           kBytes) != cudaSuccess)
+  constexpr int kBytes = Shared<D>::kBytes;
+  if (cudaFuncSetAttribute(toploc_attention_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) !=
+      cudaSuccess)
     return TOPLOC_ERR_CUDA;
-  toploc_attention_tc_kernel<D, kTwoTiles><<<blocks, kTcThreads, kBytes, stream>>>(tp, q, k, v);
-  return launched();
+  toploc_attention_tc_kernel<D><<<blocks, kTcThreads, kBytes, stream>>>(tp, q, k, v);
+  if (const int rc = launched()) return rc;
+  if (blocks == 1) return TOPLOC_OK;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = dim3((unsigned)blocks, (unsigned)((2 * tp.tile_rows + kJoinRows - 1) / kJoinRows));
+  config.blockDim = dim3(128);
+  config.stream = stream;
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  config.attrs = &early;
+  config.numAttrs = 1;
+  return cudaLaunchKernelEx(&config, toploc_attention_tc_join_kernel<D>, tp) == cudaSuccess ? TOPLOC_OK : TOPLOC_ERR_CUDA;
 }
 
 }  // namespace
@@ -764,17 +933,29 @@ bool tensor_cores_take(const toploc_attention_layout* lay, const toploc_kv_layou
          (page == 0 || (step(kv->k_page_stride, kv->num_pages) && step(kv->v_page_stride, kv->num_pages)));
 }
 
-int launch_tensor_cores(const AttentionParams& p, const toploc_attention_layout* lay, const toploc_kv_layout* kv,
+// Parts (outputs, lse, who they belong to) of two row tiles a block.
+size_t tensor_core_workspace_bytes(const toploc_attention_layout* lay) {
+  const int group = lay->q_heads / lay->kv_heads;
+  return (size_t)2 * kSms * (2 * (128 / group * group) * (size_t)(lay->head_dim + 1) * 4 + sizeof(Part));
+}
+
+int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, const toploc_kv_layout* kv, void* workspace,
                         cudaStream_t stream) {
   if (encode_tiled() == nullptr) return TOPLOC_ERR_CUDA;
-  const int page = kv->page_size, rows = tensor_core_rows(lay);
-  const bool two = rows > 128 / p.group * p.group;
+  const int page = kv->page_size;
   const int tokens = min(128 / p.group, p.max_new);  // of a query copy
+  int sms = 0;
+  if (const int rc = check_device(&sms)) return rc;
+  const int blocks = min(sms, kSms);
   TcParams tp;
-  tp.p = p;
   tp.tile_rows = 128 / p.group * p.group;
   tp.box_rows = page > 0 ? min(page, kKeyTile) : kKeyTile;
   tp.q_bytes = p.head_dim * 2 * p.group * tokens;
+  const long long part_rows = (long long)2 * blocks * 2 * tp.tile_rows;
+  p.part_out = static_cast<float*>(workspace);
+  p.part_lse = p.part_out + part_rows * p.head_dim;
+  tp.parts = reinterpret_cast<Part*>(p.part_lse + part_rows);
+  tp.p = p;
   CUtensorMap q, k, v;
   const int64_t q_extent[3] = {p.head_dim, p.q_heads, p.total_tokens}, q_stride[2] = {p.q_head, p.q_token};
   const int q_box[3] = {64, p.group, tokens};
@@ -784,15 +965,7 @@ int launch_tensor_cores(const AttentionParams& p, const toploc_attention_layout*
   if (!make_map(&q, p.q, 3, q_extent, q_stride, q_box) || !make_map(&k, p.k, 4, kv_extent, k_stride, kv_box) ||
       !make_map(&v, p.v, 4, kv_extent, v_stride, kv_box))
     return TOPLOC_ERR_CUDA;
-  int sms = 0;
-  if (const int rc = check_device(&sms)) return rc;
-  const int rows_item = two ? 2 * tp.tile_rows : tp.tile_rows;
-  const long long items = (long long)p.num_seqs * p.kv_heads * p.splits *
-                          (((long long)p.max_new * p.group + rows_item - 1) / rows_item);
-  const int blocks = (int)min(items, (long long)sms);
-  if (p.head_dim == 128)
-    return two ? launch<128, true>(tp, q, k, v, blocks, stream) : launch<128, false>(tp, q, k, v, blocks, stream);
-  return two ? launch<64, true>(tp, q, k, v, blocks, stream) : launch<64, false>(tp, q, k, v, blocks, stream);
+  return p.head_dim == 128 ? launch<128>(tp, q, k, v, blocks, stream) : launch<64>(tp, q, k, v, blocks, stream);
 }
 
 }  // namespace toploc_model

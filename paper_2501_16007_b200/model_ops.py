@@ -74,7 +74,8 @@ def _library():
         lib.toploc_attention_paged.argtypes = [_vp, _vp, _vp, att_p, kv_p, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                                ctypes.c_size_t, _vp]
         lib.toploc_attention_prompt.restype = ctypes.c_int
-        lib.toploc_attention_prompt.argtypes = [_vp, _vp, _vp, att_p, kv_p, _vp, _vp, _vp, _vp, _vp]
+        lib.toploc_attention_prompt.argtypes = [_vp, _vp, _vp, att_p, kv_p, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t,
+                                                _vp]
         lib.toploc_rmsnorm_residual.restype = ctypes.c_int
         lib.toploc_rmsnorm_residual.argtypes = [_vp, _vp, _vp, ctypes.c_float, ctypes.POINTER(ToplocNormLayout), _vp,
                                                 _vp, _vp, _vp]
@@ -185,6 +186,15 @@ def _attention_layout(q, kv_heads, num_seqs, max_new_tokens, scale, out, lse):
                                  out.stride(1))
 
 
+def _attention_workspace(lib, lay_p, kv_p, workspace, dev):
+    if workspace is None:
+        need = lib.toploc_attention_workspace_bytes(lay_p, kv_p)
+        if need == 0:
+            return None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
 def toploc_attention_workspace_bytes(q, k_cache, v_cache, block_table, max_new_tokens):
     """Bytes of workspace toploc_attention_paged needs for these tensors (0: none)."""
     lay = _attention_layout(q, k_cache.shape[2], block_table.shape[0], max_new_tokens, None, q, None)
@@ -216,18 +226,15 @@ def toploc_attention_paged(q, k_cache, v_cache, block_table, seq_offsets, kv_len
     _need(k_cache.dtype == q.dtype and k_cache.shape[3] == q.shape[2], "the caches must have q's type and head_dim")
     lib = _library()
     lay_p, kv_p = ctypes.byref(lay), ctypes.byref(kv)
-    if workspace is None:
-        need = lib.toploc_attention_workspace_bytes(lay_p, kv_p)
-        if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    workspace, size = _attention_workspace(lib, lay_p, kv_p, workspace, dev)
     _call(lib.toploc_attention_paged, "toploc_attention_paged", dev, stream, _ptr(q), _ptr(k_cache), _ptr(v_cache),
           lay_p, kv_p, _ptr(block_table), _ptr(seq_offsets), _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(status),
-          _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+          _ptr(workspace), size)
     return out, lse
 
 
 def toploc_attention_prompt(q, k, v, seq_offsets, max_tokens, scale=None, out=None, lse=None, want_lse=False,
-                            status=None, stream=None):
+                            status=None, workspace=None, stream=None):
     """Causal attention over packed prompts: q [tokens, q_heads, head_dim], k and v [tokens, kv_heads, head_dim]
     (views of one tensor are fine), seq_offsets int32 [n + 1], max_tokens bounds a sequence's length.  Returns
     (out, lse or None)."""
@@ -235,7 +242,7 @@ def toploc_attention_prompt(q, k, v, seq_offsets, max_tokens, scale=None, out=No
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None and want_lse:
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    dev = _device("toploc_attention_prompt", q, k, v, seq_offsets, out, lse, status)
+    dev = _device("toploc_attention_prompt", q, k, v, seq_offsets, out, lse, status, workspace)
     n = seq_offsets.shape[0] - 1
     _need(n >= 0, "seq_offsets must have num_seqs + 1 entries")
     _vector(seq_offsets, torch.int32, n + 1, "seq_offsets")
@@ -246,8 +253,11 @@ def toploc_attention_prompt(q, k, v, seq_offsets, max_tokens, scale=None, out=No
           "k and v must be [tokens, kv_heads, head_dim] of q's type, the last dimension contiguous")
     lay = _attention_layout(q, k.shape[1], n, max_tokens, scale, out, lse)
     kv = ToplocKvLayout(0, 0, 0, 0, 0, 0, k.stride(0), k.stride(1), 0, v.stride(0), v.stride(1))
-    _call(_library().toploc_attention_prompt, "toploc_attention_prompt", dev, stream, _ptr(q), _ptr(k), _ptr(v),
-          ctypes.byref(lay), ctypes.byref(kv), _ptr(seq_offsets), _ptr(out), _ptr(lse), _ptr(status))
+    lib = _library()
+    lay_p, kv_p = ctypes.byref(lay), ctypes.byref(kv)
+    workspace, size = _attention_workspace(lib, lay_p, kv_p, workspace, dev)
+    _call(lib.toploc_attention_prompt, "toploc_attention_prompt", dev, stream, _ptr(q), _ptr(k), _ptr(v), lay_p, kv_p,
+          _ptr(seq_offsets), _ptr(out), _ptr(lse), _ptr(status), _ptr(workspace), size)
     return out, lse
 
 

@@ -112,7 +112,7 @@ def test_attention_layout_refusals(lib, lay, code):
     assert paged(lib, bad) == code
     flat = kv_layout(page_size=0)
     assert lib.toploc_attention_prompt(OK, OK, OK, ctypes.byref(bad), ctypes.byref(flat), OK, OK, None, None,
-                                       None) == code
+                                       None, 0, None) == code
     assert lib.toploc_attention_workspace_bytes(ctypes.byref(bad), ctypes.byref(kv_layout())) == 0
 
 
@@ -129,20 +129,22 @@ def test_attention_argument_refusals(lib):
         assert paged(lib, attention_layout(**empty)) == 0                       # nothing to do, nothing touched
     flat, lay = kv_layout(page_size=0), attention_layout()
     for i in (0, 1, 2, 5, 6):
-        args = [OK, OK, OK, ctypes.byref(lay), ctypes.byref(flat), OK, OK, None, None, None]
+        args = [OK, OK, OK, ctypes.byref(lay), ctypes.byref(flat), OK, OK, None, None, None, 0, None]
         args[i] = None
         assert lib.toploc_attention_prompt(*args) == INVALID, i
     assert lib.toploc_attention_prompt(OK, OK, OK, ctypes.byref(lay), ctypes.byref(kv_layout()), OK, OK, None, None,
-                                       None) == INVALID
+                                       None, 0, None) == INVALID
 
 
-def test_workspace_only_where_the_keys_are_split(lib):
+def test_workspace(lib):
     def need(lay, kv):
         return lib.toploc_attention_workspace_bytes(ctypes.byref(lay), ctypes.byref(kv))
-    long = kv_layout(max_pages=8192, table_stride=8192)
-    assert need(attention_layout(num_seqs=1, total_tokens=1, max_new_tokens=1), long) >= 2 * 8 * 129 * 4
-    assert need(attention_layout(num_seqs=4096, total_tokens=4096, max_new_tokens=1), long) == 0
-    assert need(attention_layout(num_seqs=1, total_tokens=1, max_new_tokens=1), kv_layout()) == 0
+    long, one = kv_layout(max_pages=8192, table_stride=8192), dict(num_seqs=1, total_tokens=1, max_new_tokens=1)
+    assert need(attention_layout(**one), long) >= 148 * 2 * 256 * 129 * 4       # parts of two row tiles a block
+    assert need(attention_layout(dtype=1, **one), long) >= 2 * 8 * 129 * 4      # fp32: the keys in parts
+    assert need(attention_layout(dtype=1, **one), kv_layout()) == 0
+    assert need(attention_layout(dtype=1, num_seqs=4096, total_tokens=4096, max_new_tokens=1), long) == 0
+    assert need(attention_layout(num_seqs=0), long) == 0
 
 
 def norm(lib, lay=None, eps=1e-5, **kw):
