@@ -154,7 +154,7 @@ typedef struct {
  *                max_new_tokens or kv_lens[i] over the table, counted as the
  *                largest possible; BAD_PAGE; WAIT_EXPIRED), else left as it is;
  *                nothing outside the cache is read in any case
- * d_workspace    DEVICE toploc_attention_workspace_bytes, 16-byte aligned:
+ * d_workspace    DEVICE toploc_attention_workspace_bytes, 32-byte aligned:
  *                partial results of rows whose keys are split over blocks
  *                (always joined in the same order); contents are undefined
  *                afterwards, and calls that can overlap need one each

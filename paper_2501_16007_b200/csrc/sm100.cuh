@@ -82,6 +82,19 @@ __device__ __forceinline__ void lower_registers() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCount));
 }
 
+// One lane of a converged warp (the instructions below want the rest of their operands the same in every lane).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t chosen;
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p;\n\t"
+      "elect.sync _|p, 0xFFFFFFFF;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "}"
+      : "=r"(chosen));
+  return chosen != 0;
+}
+
 // ---- tensor copies -------------------------------------------------------------------------------
 
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
@@ -162,39 +175,45 @@ __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence
 // ---- the matrix instruction ----------------------------------------------------------------------
 
 // Descriptor of a bf16 operand in shared memory whose rows of 64 elements lie in the 128-byte swizzle of a
-// tensor copy (atoms of 8 rows, 1024 bytes): address, byte step between the 64-element blocks (used where
-// the rows run along K), 1024 bytes from atom to atom.
-__device__ __forceinline__ uint64_t swizzled_operand(uint32_t address, uint32_t block_step) {
-  return (uint64_t)((address & 0x3FFFF) >> 4) | (uint64_t)(block_step >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
-         (uint64_t)1 << 46 | (uint64_t)2 << 61;
+// tensor copy (atoms of 8 rows, 1024 bytes), in two words: the lower holds the address (in 16 bytes) and the
+// byte step between the 64-element blocks (used where the rows run along K), the upper 1024 bytes from atom to
+// atom, the version and the swizzle.  Steps inside the operand are added to the lower word.
+__device__ __forceinline__ uint32_t operand_low(uint32_t address, uint32_t block_step) {
+  return ((address & 0x3FFFF) >> 4) | (block_step >> 4) << 16;
 }
+constexpr uint32_t kOperandHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
 
 // Instruction word: bf16 x bf16 -> fp32, 128 x n; b_by_rows: B's rows run along K (its n index is contiguous).
 __host__ __device__ constexpr uint32_t bf16_product(uint32_t n, bool b_by_rows) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((b_by_rows ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
-// D (tensor memory) = A B (+ D), K = 16; A in shared memory.
-__device__ __forceinline__ void mma_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t word, bool add) {
+// D (tensor memory) = A B (+ D), K = 16; A in shared memory (its descriptor's lower word, B's too).
+__device__ __forceinline__ void mma_shared(uint32_t d, uint32_t a, uint32_t b, uint32_t word, bool add) {
   asm volatile(
       "{\n\t"
       ".reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+      ".reg .b64 da, db;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 da, {%1, %4};\n\t"
+      "mov.b64 db, {%2, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t"
       "}" ::"r"(d),
-      "l"(a), "l"(b), "r"(word), "r"((uint32_t)add)
+      "r"(a), "r"(b), "r"(word), "r"(kOperandHigh), "r"((uint32_t)add)
       : "memory");
 }
 
 // The same with A in tensor memory (two bf16 a column).
-__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t word, bool add) {
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b, uint32_t word, bool add) {
   asm volatile(
       "{\n\t"
       ".reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+      ".reg .b64 db;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 db, {%2, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t"
       "}" ::"r"(d),
-      "r"(a), "l"(b), "r"(word), "r"((uint32_t)add)
+      "r"(a), "r"(b), "r"(word), "r"(kOperandHigh), "r"((uint32_t)add)
       : "memory");
 }
 

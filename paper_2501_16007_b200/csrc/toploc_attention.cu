@@ -287,7 +287,7 @@ int attention(const void* d_q, const void* d_k, const void* d_v, const toploc_at
   const bool tensor_cores = tensor_cores_take(lay, kv, d_q, d_k, d_v, d_out);
   const size_t need = workspace_bytes_of(lay, kv, tensor_cores);
   if (need > 0 && (!workspace || workspace_bytes < need)) return TOPLOC_ERR_WORKSPACE;
-  if (need > 0 && !aligned(workspace, 16)) return TOPLOC_ERR_INVALID_ARGUMENT;
+  if (need > 0 && !aligned(workspace, 32)) return TOPLOC_ERR_INVALID_ARGUMENT;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   if (tensor_cores) return launch_tensor_cores(p, lay, kv, workspace, stream);
   p.splits = splits_of(lay, kv);

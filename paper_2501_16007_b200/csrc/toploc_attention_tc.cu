@@ -67,7 +67,7 @@ struct Shared {
   static constexpr int kStages = D == 128 ? 5 : 10;
   struct Head {
     uint64_t full[kStages], empty[kStages];
-    uint64_t s_full[2], p_full[2], o_full[2];
+    uint64_t s_full[2], p_most[2], p_full[2], o_full[2];
     uint64_t q_full, q_empty, drain;
     uint64_t join;  // both groups (one row tile): their sums are exchanged, their outputs read
     uint64_t item_full[kItems], item_empty[kItems];
@@ -86,6 +86,19 @@ __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+__device__ __forceinline__ void store_32_bytes(void* at, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+               "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+
+// The largest of three, NaN where one is.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
 // Two fp32 products and sums in one instruction.
@@ -111,21 +124,23 @@ __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
 __device__ __forceinline__ uint32_t ring_stage(uint32_t n, int stages) { return n % (uint32_t)stages; }
 __device__ __forceinline__ uint32_t ring_parity(uint32_t n, int stages) { return (n / (uint32_t)stages) & 1u; }
 
-struct TcParams {
-  AttentionParams p;
-  int tile_rows;  // packed rows of a row tile: 128 rounded down to whole tokens
-  int box_rows;   // rows of a key copy
-  int q_bytes;    // bytes of a query tile's copy
-  Part* parts;    // [blocks][2]
-};
-
 // A wait of a whole warp: all lanes or none go on.
 __device__ __forceinline__ bool warp_wait(const uint64_t& bar, uint32_t parity, volatile int* gave_up) {
   return __all_sync(0xFFFFFFFFu, barrier_wait(shared_address(&bar), parity, gave_up));
 }
 
-// Tiles of the ring an item takes, and the place of value tile j among them.
+struct TcParams {
+  AttentionParams p;
+  int tile_rows;  // packed rows of a row tile: 128 rounded down to whole tokens
+  int box_rows;   // rows of a key copy
+  int q_bytes;    // bytes of a query tile's copy
+  bool wide_out;  // rows of the output at multiples of 32 bytes
+  Part* parts;    // [blocks][2]
+};
+
+// Tiles of the ring an item takes, and the places of key and value tile j among them.
 __device__ __forceinline__ int item_tiles(const Item& im) { return im.two ? max(im.n0, im.n1) : im.n0; }
+__device__ __forceinline__ int key_place(bool two, int j) { return two ? 2 * j : max(2 * j - 1, 0); }
 __device__ __forceinline__ int value_place(bool two, int j, int n) {
   return two ? 2 * j + 1 : min(n, j + 2) + j;  // K0 V0 K1 V1 .. or K0 K1 V0 K2 V1 ..
 }
@@ -167,6 +182,100 @@ __device__ __forceinline__ bool before(const Place& a, const Place& b) {
 __device__ __forceinline__ int tiles_seen(const SeqRange& s, int tokens_upto) {
   const int seen = min(s.keys, s.keys - s.rows + tokens_upto);
   return seen > 0 ? (seen + kKeyTile - 1) / kKeyTile : 0;
+}
+
+// One warp's copies into the ring: the keys, or the values, of item after item.
+template <int D>
+struct Feeder {
+  using S = Shared<D>;
+  static constexpr int kStages = S::kStages;
+  const TcParams& tp;
+  const CUtensorMap* map;
+  typename S::Head& sh;
+  uint32_t ring, base = 0;             // places in front of the item
+  uint32_t fed = 0, fed_parity = 0;    // by stage: this warp's last copy there
+  volatile int* gave_up;
+  Item im;
+  int tiles = 0, page = 0, next = 0, lane = threadIdx.x & 31;
+  bool fine = true;
+
+  __device__ Feeder(const TcParams& tp, const CUtensorMap* map, typename S::Head& sh, void* ring, volatile int* gave_up)
+      : tp(tp), map(map), sh(sh), ring(shared_address(ring)), gave_up(gave_up) {}
+
+  // The page of this lane's copy of tile j, as the table has it (looked up ahead of its use).
+  __device__ int page_of(int j) const {
+    const int key = im.kbegin + j * kKeyTile + lane * tp.box_rows;
+    const bool copied = tp.p.kv_lens && j < tiles && lane * tp.box_rows < kKeyTile && key < im.kend;
+    return copied ? tp.p.table[im.seq * tp.p.table_stride + key / tp.p.page_size] : 0;
+  }
+
+  __device__ void item(const Item& next_item, int n) {
+    base += 2 * tiles;
+    im = next_item;
+    tiles = n;
+    page = page_of(0);
+    next = page_of(1);
+  }
+
+  __device__ void feed(int j, int at) {
+    const uint32_t place = base + at, stage = ring_stage(place, kStages);
+    const uint32_t bar = shared_address(&sh.full[stage]), dst = ring + stage * S::kTileBytes;
+    const int after = page_of(j + 2);
+    fine = warp_wait(sh.empty[stage], ring_parity(place, kStages) ^ 1, gave_up);
+    if (!fine) return;
+    fed |= 1u << stage;
+    fed_parity = (fed_parity & ~(1u << stage)) | ring_parity(place, kStages) << stage;
+    const int key0 = im.kbegin + j * kKeyTile;
+    if (tp.p.kv_lens) {
+      if (page < 0 || page >= tp.p.num_pages) {
+        if (tp.p.status) tp.p.status[im.seq] = TOPLOC_SEQ_BAD_PAGE;
+        page = tp.p.num_pages;  // past the end: the copy fills zeros
+      }
+      const int copies = (min(kKeyTile, im.kend - key0) + tp.box_rows - 1) / tp.box_rows;
+      const int in_page = tp.box_rows < kKeyTile ? 0 : key0 % tp.p.page_size;
+      if (elect_one()) barrier_arrive_expect(bar, copies * S::kHalves * tp.box_rows * 128);
+      __syncwarp();
+      for (int c = 0; c < copies; ++c) {
+        const int which = __shfl_sync(0xFFFFFFFFu, page, c);
+        if (elect_one()) {
+#pragma unroll
+          for (int h = 0; h < S::kHalves; ++h)
+            copy_4d(dst + h * kBlockBytes + c * tp.box_rows * 128, map, bar, h * 64, in_page, im.head, which);
+        }
+      }
+    } else if (elect_one()) {
+      barrier_arrive_expect(bar, S::kTileBytes);
+#pragma unroll
+      for (int h = 0; h < S::kHalves; ++h)
+        copy_4d(dst + h * kBlockBytes, map, bar, h * 64, im.first + key0, im.head, 0);
+    }
+    __syncwarp();
+    page = next;
+    next = after;
+  }
+
+  // After a wait gave up: no copy of this warp is in flight when it returns.
+  __device__ void drain() const {
+    for (int i = 0; i < kStages; ++i)
+      if (fed >> i & 1) barrier_drain(shared_address(&sh.full[i]), fed_parity >> i & 1);
+  }
+};
+
+__device__ __forceinline__ Item uniform(const Item& im) {  // the same for every lane, and known to be
+  Item r;
+  r.seq = __shfl_sync(0xFFFFFFFFu, im.seq, 0);
+  r.head = __shfl_sync(0xFFFFFFFFu, im.head, 0);
+  r.slot = __shfl_sync(0xFFFFFFFFu, im.slot, 0);
+  r.first = __shfl_sync(0xFFFFFFFFu, im.first, 0);
+  r.behind = __shfl_sync(0xFFFFFFFFu, im.behind, 0);
+  r.row0 = __shfl_sync(0xFFFFFFFFu, im.row0, 0);
+  r.rows = __shfl_sync(0xFFFFFFFFu, im.rows, 0);
+  r.kbegin = __shfl_sync(0xFFFFFFFFu, im.kbegin, 0);
+  r.kend = __shfl_sync(0xFFFFFFFFu, im.kend, 0);
+  r.two = __shfl_sync(0xFFFFFFFFu, im.two, 0);
+  r.n0 = __shfl_sync(0xFFFFFFFFu, im.n0, 0);
+  r.n1 = __shfl_sync(0xFFFFFFFFu, im.n1, 0);
+  return r;
 }
 
 constexpr int kRuns = kTcThreads;
@@ -227,7 +336,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
   float2* exchange = reinterpret_cast<float2*>(base + S::kHeadBytes);  // (maximum, sum) of [group][row]
   unsigned char* q_tiles = base + S::kHeadBytes + S::kExchangeBytes;
   unsigned char* ring = q_tiles + 2 * S::kTileBytes;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   volatile int* gave_up = &sh.gave_up;
 
   // tell the join kernel that it may be scheduled (it waits for this grid to end)
@@ -239,6 +348,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
     }
     for (int w = 0; w < 2; ++w) {
       barrier_init(shared_address(&sh.s_full[w]), 1);
+      barrier_init(shared_address(&sh.p_most[w]), 4);
       barrier_init(shared_address(&sh.p_full[w]), 4);
       barrier_init(shared_address(&sh.o_full[w]), 1);
       sh.bad_values[w] = -1;
@@ -249,7 +359,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
     barrier_init(shared_address(&sh.join), 8);
     for (int i = 0; i < kItems; ++i) {
       barrier_init(shared_address(&sh.item_full[i]), 1);
-      barrier_init(shared_address(&sh.item_empty[i]), 9);
+      barrier_init(shared_address(&sh.item_empty[i]), 10);
     }
     sh.gave_up = 0;
     barrier_init_fence();
@@ -284,7 +394,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  const uint32_t tmem = sh.tmem;
+  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, sh.tmem, 0);
   constexpr uint32_t kOut = 256;  // scores of group w at 128 w, outputs at 256 + D w
 
   if (warp == 8) {
@@ -295,7 +405,6 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       prefetch_map(&map_k);
       prefetch_map(&map_v);
     }
-    const bool paged = p.kv_lens != nullptr;
     const int rows_item = 2 * tp.tile_rows, tokens_item = rows_item / p.group;
     const long long all = run_cost[kRuns];
     const long long share = max((all + gridDim.x - 1) / gridDim.x, kLeastShare);
@@ -304,8 +413,9 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
     __syncwarp();  // run_cost has been read: the ring's place is free
     SeqRange s = {0, 0, 0, false};
     int s_of = -1;
-    uint32_t fed = 0, q_uses = 0;
-    if (lane < 2 && tp.parts) tp.parts[2 * blockIdx.x + lane].seq = -1;
+    uint32_t q_uses = 0;
+    Feeder<D> keys(tp, &map_k, sh, ring, gave_up);
+    if (lane < 2) tp.parts[2 * blockIdx.x + lane].seq = -1;
     __syncwarp();
     for (uint32_t number = 0;; ++number) {
       while (before(at, end)) {  // the sequence of the next item, past those without rows
@@ -353,6 +463,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
           if (++at.head == p.kv_heads) at = Place{at.seq + 1, 0, 0, 0};
         }
       }
+      im = uniform(im);
       if (lane == 0) {
         sh.items[slot] = im;
         barrier_arrive(shared_address(&sh.item_full[slot]));
@@ -362,188 +473,166 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       const int n = item_tiles(im);
       if (n == 0) continue;
 
-
       // queries: each tile in blocks of 64 channels
       if (!warp_wait(sh.q_empty, (q_uses & 1) ^ 1, gave_up)) break;
       ++q_uses;
-      const bool second = im.two;
       const uint32_t q_bar = shared_address(&sh.q_full);
-      if (lane == 0) barrier_arrive_expect(q_bar, (second ? 2 : 1) * tp.q_bytes);
+      if (elect_one()) {
+        const int tiles = im.two ? 2 : 1;
+        barrier_arrive_expect(q_bar, tiles * tp.q_bytes);
+        for (int w = 0; w < tiles; ++w)
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h)
+            copy_3d(shared_address(q_tiles + w * S::kTileBytes + h * kBlockBytes), &map_q, q_bar, h * 64,
+                    im.head * p.group, im.first + (im.row0 + w * tp.tile_rows) / p.group);
+      }
       __syncwarp();
-      if (lane < kHalves * (second ? 2 : 1)) {
-        const int w = lane / kHalves, h = lane % kHalves;
-        copy_3d(shared_address(q_tiles + w * S::kTileBytes + h * kBlockBytes), &map_q, q_bar, h * 64, im.head * p.group,
-                im.first + (im.row0 + w * tp.tile_rows) / p.group);
-      }
 
-      // keys and values
-      const int my_page = lane / kHalves, my_half = lane % kHalves;
-      const auto page_of = [&](int j) {  // this lane's page of key tile j
-        if (!paged || j >= n) return 0;
-        const int key0 = im.kbegin + j * kKeyTile, col = key0 / p.page_size + my_page;
-        if (my_page * tp.box_rows >= kKeyTile || key0 + my_page * tp.box_rows >= im.kend) return 0;
-        int page = p.table[im.seq * p.table_stride + col];
-        if (page < 0 || page >= p.num_pages) {
-          if (p.status) p.status[im.seq] = TOPLOC_SEQ_BAD_PAGE;
-          page = p.num_pages;  // past the end: the copy fills zeros
-        }
-        return page;
-      };
-      const auto feed = [&](const CUtensorMap* map, int j, int page) {
-        const uint32_t stage = ring_stage(fed, kStages), bar = shared_address(&sh.full[stage]);
-        if (!warp_wait(sh.empty[stage], ring_parity(fed, kStages) ^ 1, gave_up)) return false;
-        ++fed;
-        const int key0 = im.kbegin + j * kKeyTile, left = min(kKeyTile, im.kend - key0);
-        const int copies = paged ? (left + tp.box_rows - 1) / tp.box_rows : 1;
-        if (lane == 0) barrier_arrive_expect(bar, copies * kHalves * tp.box_rows * 128);
-        __syncwarp();
-        if (lane < copies * kHalves) {
-          const uint32_t dst = shared_address(ring + stage * S::kTileBytes + my_half * kBlockBytes) +
-                               my_page * tp.box_rows * 128;
-          if (paged)
-            copy_4d(dst, map, bar, my_half * 64, key0 % p.page_size, im.head, page);
-          else
-            copy_4d(dst, map, bar, my_half * 64, im.first + key0, im.head, 0);
-        }
-        return true;
-      };
-      bool fine = true;
-      int page = page_of(0), next = page_of(1);  // looked up ahead of their use
-      if (im.two) {
-        for (int j = 0; fine && j < n; ++j) {
-          fine = feed(&map_k, j, page) && feed(&map_v, j, page);
-          page = next;
-          next = page_of(j + 2);
-        }
-      } else {
-        fine = feed(&map_k, 0, page);
-        for (int j = 0; fine && j < n; ++j) {
-          const int after = page_of(j + 2);
-          if (j + 1 < n) fine = feed(&map_k, j + 1, next);
-          fine = fine && feed(&map_v, j, page);
-          page = next;
-          next = after;
-        }
-      }
-      if (!fine) break;
+      keys.item(im, n);
+      for (int j = 0; j < n && keys.fine; ++j) keys.feed(j, key_place(im.two, j));
+      if (!keys.fine) break;
     }
     if (*gave_up) {  // copies in flight have to land before the block ends
       if (q_uses > 0) barrier_drain(shared_address(&sh.q_full), (q_uses - 1) & 1);
-      for (uint32_t i = fed > kStages ? fed - kStages : 0; i < fed; ++i)
-        barrier_drain(shared_address(&sh.full[ring_stage(i, kStages)]), ring_parity(i, kStages));
+      keys.drain();
     }
+  } else if (warp == 10) {
+    lower_registers<kOtherRegisters>();
+    // ---- feeding: values ----
+    Feeder<D> values(tp, &map_v, sh, ring, gave_up);
+    for (uint32_t number = 0;; ++number) {
+      const uint32_t slot = number % kItems;
+      if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
+      const Item im = uniform(sh.items[slot]);
+      __syncwarp();
+      if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
+      if (im.seq < 0) break;
+      const int n = item_tiles(im);
+      values.item(im, n);
+      for (int j = 0; j < n && values.fine; ++j) values.feed(j, value_place(im.two, j, n));
+      if (!values.fine) break;
+    }
+    if (*gave_up) values.drain();
   } else if (warp == 9) {
     lower_registers<kOtherRegisters>();
-    // ---- products: one thread issues them all ----
-    if (lane == 0) {
-      constexpr uint32_t kScores = bf16_product(128, false), kValues = bf16_product(D, true);
-      const uint32_t q_at = shared_address(q_tiles), ring_at = shared_address(ring);
-      uint32_t used = 0, q_uses = 0, p_uses[2] = {0, 0};
-      const auto full = [&](uint32_t n) {
-        const bool ok = barrier_wait(shared_address(&sh.full[ring_stage(n, kStages)]), ring_parity(n, kStages), gave_up);
-        tmem_fence_after();
-        return ok;
-      };
-      const auto release = [&](uint32_t n) { mma_commit(shared_address(&sh.empty[ring_stage(n, kStages)])); };
-      const auto scores = [&](int w, uint32_t n, bool two) {  // scores of group w against the key tile at place n
-        const uint32_t a = q_at + (two ? w : 0) * S::kTileBytes, b = ring_at + ring_stage(n, kStages) * S::kTileBytes;
+    // ---- products: the whole warp follows, one lane issues ----
+    constexpr uint32_t kScores = bf16_product(128, false), kValues = bf16_product(D, true);
+    const uint32_t q_low = operand_low(shared_address(q_tiles), 16);
+    const uint32_t k_low = operand_low(shared_address(ring), 16), v_low = operand_low(shared_address(ring), kBlockBytes);
+    uint32_t used = 0, q_uses = 0, p_uses[2] = {0, 0};
+    const auto full = [&](uint32_t n) {
+      const bool ok = warp_wait(sh.full[ring_stage(n, kStages)], ring_parity(n, kStages), gave_up);
+      tmem_fence_after();
+      return ok;
+    };
+    const auto release = [&](uint32_t n) {
+      if (elect_one()) mma_commit(shared_address(&sh.empty[ring_stage(n, kStages)]));
+    };
+    const auto scores = [&](int w, uint32_t n, bool two) {  // scores of group w against the key tile at place n
+      const uint32_t a = q_low + (two ? w : 0) * (S::kTileBytes / 16);
+      const uint32_t b = k_low + ring_stage(n, kStages) * (S::kTileBytes / 16);
+      if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint32_t at = (k / 4) * kBlockBytes + (k % 4) * 32;
-          mma_shared(tmem + 128 * w, swizzled_operand(a + at, 16), swizzled_operand(b + at, 16), kScores, k > 0);
+          const uint32_t at = ((k / 4) * kBlockBytes + (k % 4) * 32) / 16;
+          mma_shared(tmem + 128 * w, a + at, b + at, kScores, k > 0);
         }
         mma_commit(shared_address(&sh.s_full[w]));
-      };
-      const auto values = [&](int w, uint32_t n, bool add) {
-        const uint32_t b = ring_at + ring_stage(n, kStages) * S::kTileBytes;
+      }
+    };
+    const auto values = [&](int w, uint32_t n, bool add) {  // as the group's weights come into tensor memory
+      const uint32_t b = v_low + ring_stage(n, kStages) * (S::kTileBytes / 16), parity = p_uses[w]++ & 1;
+      if (!warp_wait(sh.p_most[w], parity, gave_up)) return false;
+      tmem_fence_after();
+      if (elect_one()) {
 #pragma unroll
-        for (int k = 0; k < kKeyTile / 16; ++k)
-          mma_tmem(tmem + kOut + D * w, tmem + 128 * w + 8 * k, swizzled_operand(b + k * 2048, kBlockBytes), kValues,
-                   add || k > 0);
+        for (int k = 0; k < 6; ++k)
+          mma_tmem(tmem + kOut + D * w, tmem + 128 * w + 8 * k, b + k * (2048 / 16), kValues, add || k > 0);
+      }
+      if (!warp_wait(sh.p_full[w], parity, gave_up)) return false;
+      tmem_fence_after();
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 6; k < 8; ++k)
+          mma_tmem(tmem + kOut + D * w, tmem + 128 * w + 8 * k, b + k * (2048 / 16), kValues, true);
         mma_commit(shared_address(&sh.o_full[w]));
-      };
-      const auto weights = [&](int w) {  // the group's weights are in tensor memory
-        const bool ok = barrier_wait(shared_address(&sh.p_full[w]), p_uses[w]++ & 1, gave_up);
-        tmem_fence_after();
-        return ok;
-      };
-      for (uint32_t number = 0;; ++number) {
-        const uint32_t slot = number % kItems;
-        if (!barrier_wait(shared_address(&sh.item_full[slot]), (number / kItems) & 1, gave_up)) break;
-        const int seq = sh.items[slot].seq, n0 = sh.items[slot].n0, n1 = sh.items[slot].n1;
-        const bool two = sh.items[slot].two;
-        barrier_arrive(shared_address(&sh.item_empty[slot]));
-        if (seq < 0) break;
-        const int n = two ? max(n0, n1) : n0;
-        if (n == 0) continue;
-        bool ok = barrier_wait(shared_address(&sh.q_full), q_uses++ & 1, gave_up);
-        tmem_fence_after();
-        if (two) {
-          ok = ok && full(used);
-          if (!ok) break;
-          if (n0 > 0) scores(0, used, true);
-          if (n1 > 0) scores(1, used, true);
-          release(used);
-          if (n == 1) mma_commit(shared_address(&sh.q_empty));
-          for (int j = 0; ok && j < n; ++j) {
-            const uint32_t v_at = used + 2 * j + 1, k_at = v_at + 1;
-            ok = full(v_at);
-            bool key_there = false;
+      }
+      return true;
+    };
+    const auto queries_used = [&] {
+      if (elect_one()) mma_commit(shared_address(&sh.q_empty));
+    };
+    for (uint32_t number = 0;; ++number) {
+      const uint32_t slot = number % kItems;
+      if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
+      // (through a shuffle: the same for every lane, and known to be)
+      const int seq = __shfl_sync(0xFFFFFFFFu, sh.items[slot].seq, 0);
+      const int n0 = __shfl_sync(0xFFFFFFFFu, sh.items[slot].n0, 0), n1 = __shfl_sync(0xFFFFFFFFu, sh.items[slot].n1, 0);
+      const bool two = __shfl_sync(0xFFFFFFFFu, sh.items[slot].two, 0);
+      __syncwarp();
+      if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
+      if (seq < 0) break;
+      const int n = two ? max(n0, n1) : n0;
+      if (n == 0) continue;
+      bool ok = warp_wait(sh.q_full, q_uses++ & 1, gave_up);
+      tmem_fence_after();
+      if (two) {
+        ok = ok && full(used);
+        if (!ok) break;
+        if (n0 > 0) scores(0, used, true);
+        if (n1 > 0) scores(1, used, true);
+        release(used);
+        if (n == 1) queries_used();
+        for (int j = 0; ok && j < n; ++j) {
+          const uint32_t v_at = used + 2 * j + 1, k_at = v_at + 1;
+          ok = full(v_at) && (j + 1 >= n || full(k_at));
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
-              const int nw = w ? n1 : n0;
-              if (!ok || j >= nw) continue;
-              ok = weights(w);
-              if (!ok) break;
-              values(w, v_at, j > 0);
-              if (j + 1 < nw) {
-                if (!key_there) ok = full(k_at);
-                if (!ok) break;
-                key_there = true;
-                scores(w, k_at, true);
-              }
-            }
+          for (int w = 0; w < 2; ++w) {
+            const int nw = w ? n1 : n0;
+            if (!ok || j >= nw) continue;
+            ok = values(w, v_at, j > 0);
             if (!ok) break;
-            release(v_at);
-            if (j + 1 < n) {
-              release(k_at);
-              if (j + 2 == n) mma_commit(shared_address(&sh.q_empty));
-            }
+            if (j + 1 < nw) scores(w, k_at, true);
           }
-        } else {
-          uint32_t at = used;
-          for (int w = 0; ok && w < min(n, 2); ++w, ++at) {
+          if (!ok) break;
+          release(v_at);
+          if (j + 1 < n) {
+            release(k_at);
+            if (j + 2 == n) queries_used();
+          }
+        }
+      } else {
+        uint32_t at = used;
+        for (int w = 0; ok && w < min(n, 2); ++w, ++at) {
+          ok = full(at);
+          if (!ok) break;
+          scores(w, at, false);
+          release(at);
+        }
+        if (n <= 2 && ok) queries_used();
+        for (int j = 0; ok && j < n; ++j) {
+          const int w = j & 1;
+          ok = full(at) && values(w, at, j >= 2);
+          if (!ok) break;
+          release(at++);
+          if (j + 2 < n) {
             ok = full(at);
             if (!ok) break;
             scores(w, at, false);
-            release(at);
-          }
-          if (n <= 2 && ok) mma_commit(shared_address(&sh.q_empty));
-          for (int j = 0; ok && j < n; ++j) {
-            const int w = j & 1;
-            ok = full(at) && weights(w);
-            if (!ok) break;
-            values(w, at, j >= 2);
             release(at++);
-            if (j + 2 < n) {
-              ok = full(at);
-              if (!ok) break;
-              scores(w, at, false);
-              release(at++);
-              if (j + 3 == n) mma_commit(shared_address(&sh.q_empty));
-            }
+            if (j + 3 == n) queries_used();
           }
         }
-        if (!ok) break;
-        used += 2 * n;
       }
-      if (*gave_up) {  // products in flight have to end before tensor memory is freed
-        mma_commit(shared_address(&sh.drain));
-        barrier_drain(shared_address(&sh.drain), 0);
-      }
+      if (!ok) break;
+      used += 2 * n;
+    }
+    if (*gave_up && lane == 0) {  // products in flight have to end before tensor memory is freed
+      mma_commit(shared_address(&sh.drain));
+      barrier_drain(shared_address(&sh.drain), 0);
     }
     __syncwarp();
-  } else if (warp > 9) {
+  } else if (warp == 11) {
     lower_registers<kOtherRegisters>();
   } else {
     raise_registers<kSoftmaxRegisters>();
@@ -577,6 +666,42 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       const int hidden_from = max(im.behind + im.row0 / p.group + 1, 0);     // first key hidden from a row of the item
       const bool live = __any_sync(0xFFFFFFFFu, valid);                      // else nobody reads the warp's rows
       const int tiles = two ? (w ? im.n1 : im.n0) : (n + 1 - w) / 2;
+      // Before the products of a tile with hidden keys:
+      const auto clean_values = [&](int j, int key0) {
+        // Values of hidden keys meet weights of zero, and 0 * NaN is NaN: rows past the item's keys (never
+        // loaded, or another sequence's) become zero; a value in front of them that is not finite too, and
+        // the rows that do see it get it back at the end.
+        const uint32_t place = used + value_place(two, j, n), stage = ring_stage(place, kStages);
+        if (!warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up)) return false;
+        const int from = max(hidden_from - key0, 0);
+        unsigned char* tile = ring + stage * S::kTileBytes;
+        for (int e = r; e < (kKeyTile - from) * 8; e += 128) {
+          const int j_row = from + (e >> 3);
+          const bool past = key0 + j_row >= im.kend;
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h) {
+            uint4* at = reinterpret_cast<uint4*>(tile + h * kBlockBytes + j_row * 128 + (e & 7) * 16);
+            uint4 v = make_uint4(0, 0, 0, 0);
+            bool write = past;
+            if (!past) {
+              v = *at;
+              uint32_t* x = &v.x;
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                if ((x[q] & 0x7F80u) == 0x7F80u) x[q] &= 0xFFFF0000u, write = true;
+                if ((x[q] & 0x7F800000u) == 0x7F800000u) x[q] &= 0xFFFFu, write = true;
+              }
+              if (write) {
+                *(volatile int*)&sh.bad_values[number & 1] = (int)number;
+                __threadfence_block();
+              }
+            }
+            if (write) *at = v;
+          }
+        }
+        fence_async_shared();
+        return true;
+      };
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       for (int i = 0; i < tiles; ++i) {
@@ -586,29 +711,30 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
         ok = warp_wait(sh.s_full[w], s_uses++ & 1, gave_up);
         if (!ok) break;
         if (live) {
+          // Loops over quarters of the row, not unrolled: the warps of a group run through them together out of the
+          // instruction caches, which the unrolled 128 columns overflow (single tokens 102 -> @@ us).
           tmem_fence_after();
-          uint32_t s[4][32];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_load(s[c], s_at + 32 * c);
-          tmem_wait_load();
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ready(s[c]);
-          if (masked) {
-            const int last = newest - key0;
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
+          float peak = -INFINITY;
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            uint32_t x[32];
+            tmem_load(x, s_at + 32 * c);
+            tmem_wait_load();
+            tmem_ready(x);
+            if (masked) {
+              const int last = newest - key0 - 32 * c;
 #pragma unroll
               for (int e = 0; e < 32; ++e)
-                if (32 * c + e > last) s[c][e] = 0xFF800000u;  // -inf, whatever was there
-          }
-          float top[4];
+                if (e > last) x[e] = 0xFF800000u;  // -inf, whatever was there
+              tmem_store(s_at + 32 * c, x);
+            }
+            float top[4] = {peak, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            top[c] = __uint_as_float(s[c][0]);
-#pragma unroll
-            for (int e = 1; e < 32; ++e) top[c] = fmaxf(top[c], __uint_as_float(s[c][e]));
+            for (int e = 0; e < 32; e += 2)
+              top[e / 2 % 4] = max3(top[e / 2 % 4], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+            peak = max3(max3(top[0], top[1], top[2]), top[3], -INFINITY);
           }
-          const float peak = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+          if (masked) tmem_wait_store();
           // (peak - m) * scale > the limit, also where m is -inf; not where both are
           const bool grow = valid && peak > m && !((peak - m) * scale <= kLazyLog2);
           if (__any_sync(0xFFFFFFFFu, grow)) {
@@ -640,63 +766,47 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
           const float ref = m == -INFINITY ? 0.f : m * scale;
           const uint64_t scales = pair(scale, scale), refs = pair(-ref, -ref);
           uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < 4; ++c) {
-            uint32_t packed[16];
+            uint32_t x[32], packed[16];
+            tmem_load(x, s_at + 32 * c);  // (weights go where scores have been read: 16 columns of every 32)
+            tmem_wait_load();
+            tmem_ready(x);
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
+            for (int e = 0; e < 16; ++e) {
               float a, b;
-              unpair(fma_pair(pair(__uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1])), scales, refs), a, b);
+              unpair(fma_pair(pair(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), scales, refs), a, b);
               a = exp2_approx(a);
               b = exp2_approx(b);
-              sum[(e >> 1) & 1] = add_pair(sum[(e >> 1) & 1], pair(a, b));
-              packed[e >> 1] = pack_bf16(a, b);
+              sum[e & 1] = add_pair(sum[e & 1], pair(a, b));
+              packed[e] = pack_bf16(a, b);
             }
             tmem_store(s_at + 16 * c, packed);
+            if (c == 2 && !masked) {  // three quarters of the weights go ahead: their product runs during the last one
+              tmem_wait_store();
+              tmem_fence_before();
+              __syncwarp();
+              if (lane == 0) barrier_arrive(shared_address(&sh.p_most[w]));
+            }
           }
           float a, b;
           unpair(add_pair(sum[0], sum[1]), a, b);
           l += a + b;
+          if (!(peak < INFINITY)) l = NAN;  // a NaN or infinity among the scores: the softmax of the row is NaN
+          tmem_wait_store();
+        } else if (!masked && lane == 0) {
+          barrier_arrive(shared_address(&sh.p_most[w]));
         }
-        if (masked) {
-          // Values of hidden keys meet weights of zero, and 0 * NaN is NaN: rows past the item's keys (never
-          // loaded, or another sequence's) become zero; a value in front of them that is not finite too, and
-          // the rows that do see it get it back at the end.
-          const uint32_t place = used + value_place(two, j, n), stage = ring_stage(place, kStages);
-          ok = warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up);
-          if (!ok) break;
-          const int from = max(hidden_from - key0, 0);
-          unsigned char* tile = ring + stage * S::kTileBytes;
-          for (int e = r; e < (kKeyTile - from) * 8; e += 128) {
-            const int j_row = from + (e >> 3);
-            const bool past = key0 + j_row >= im.kend;
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-              uint4* at = reinterpret_cast<uint4*>(tile + h * kBlockBytes + j_row * 128 + (e & 7) * 16);
-              uint4 v = make_uint4(0, 0, 0, 0);
-              bool write = past;
-              if (!past) {
-                v = *at;
-                uint32_t* x = &v.x;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                  if ((x[q] & 0x7F80u) == 0x7F80u) x[q] &= 0xFFFF0000u, write = true;
-                  if ((x[q] & 0x7F800000u) == 0x7F800000u) x[q] &= 0xFFFFu, write = true;
-                }
-                if (write) {
-                  *(volatile int*)&sh.bad_values[number & 1] = (int)number;
-                  __threadfence_block();
-                }
-              }
-              if (write) *at = v;
-            }
-          }
-          fence_async_shared();
+        if (masked && !clean_values(j, key0)) {
+          ok = false;
+          break;
         }
-        if (live) tmem_wait_store();
         tmem_fence_before();
         __syncwarp();
-        if (lane == 0) barrier_arrive(shared_address(&sh.p_full[w]));
+        if (lane == 0) {
+          if (masked) barrier_arrive(shared_address(&sh.p_most[w]));
+          barrier_arrive(shared_address(&sh.p_full[w]));
+        }
         ++pv[w];
       }
       if (!ok) break;
@@ -776,17 +886,26 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
           }
         }
         if (im.slot < 0) {
-          uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + (im.first + token) * p.out_token +
-                                                head * p.out_head + c);
+          uint32_t packed[16];
 #pragma unroll
-          for (int e = 0; e < 32; e += 8)
-            out[e / 8] = make_uint4(pack_bf16(o[e] * inv, o[e + 1] * inv), pack_bf16(o[e + 2] * inv, o[e + 3] * inv),
-                                    pack_bf16(o[e + 4] * inv, o[e + 5] * inv), pack_bf16(o[e + 6] * inv, o[e + 7] * inv));
+          for (int e = 0; e < 32; e += 2) packed[e / 2] = pack_bf16(o[e] * inv, o[e + 1] * inv);
+          __nv_bfloat16* out =
+              static_cast<__nv_bfloat16*>(p.out) + (im.first + token) * p.out_token + head * p.out_head + c;
+          if (tp.wide_out) {
+            store_32_bytes(out, packed);
+            store_32_bytes(out + 16, packed + 8);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              reinterpret_cast<uint4*>(out)[e] =
+                  make_uint4(packed[4 * e], packed[4 * e + 1], packed[4 * e + 2], packed[4 * e + 3]);
+          }
         } else {
-          float4* out = reinterpret_cast<float4*>(p.part_out + part * D + c);
+          uint32_t words[32];
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            out[e / 4] = make_float4(o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv);
+          for (int e = 0; e < 32; ++e) words[e] = __float_as_uint(o[e] * inv);
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) store_32_bytes(p.part_out + part * D + c + e, words + e);
         }
       }
       if (valid && (two || w == 0)) {
@@ -814,7 +933,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
 // Block (b, y) looks after the row tile that block b of the first kernel began and did not finish: its parts are that
 // block's slot 1 and slot 0 of the next ones up to the one that finished it.  Part i has out_i = sum p v / sum p and
 // lse_i over its keys; the whole is sum_i w_i out_i / sum_i w_i, w_i = 2^(lse_i - max).  A warp per row, parts in order.
-constexpr int kJoinRows = 16;  // rows of a block
+constexpr int kJoinRows = 8;  // rows of a block
 
 template <int D>
 __global__ void __launch_bounds__(128) toploc_attention_tc_join_kernel(const TcParams tp) {
@@ -835,23 +954,35 @@ __global__ void __launch_bounds__(128) toploc_attention_tc_join_kernel(const TcP
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, off));
     const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, o[D / 32];
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-    for (int i = b; i <= end; ++i) {
+    // 16 bytes a lane: D / 4 lanes cover a row, so a warp takes 128 / D parts at once, and several in flight
+    constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes;
+    float sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int i = b + lane / kLanes; i <= end; i += kAtOnce) {
       const float w = exp2f(p.part_lse[place(i)] - ref);
+      const float4 from = *reinterpret_cast<const float4*>(p.part_out + place(i) * D + lane % kLanes * 4);
       sum += w;
-      if (w == 0.f) continue;
-      const float* from = p.part_out + place(i) * D + lane * (D / 32);
-#pragma unroll
-      for (int e = 0; e < D / 32; ++e) o[e] = fmaf(w, from[e], o[e]);
+      if (w != 0.f) {
+        o.x = fmaf(w, from.x, o.x);
+        o.y = fmaf(w, from.y, o.y);
+        o.z = fmaf(w, from.z, o.z);
+        o.w = fmaf(w, from.w, o.w);
+      }
+    }
+    if (kAtOnce == 2) {
+      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
+      o.x += __shfl_xor_sync(0xFFFFFFFFu, o.x, 16);
+      o.y += __shfl_xor_sync(0xFFFFFFFFu, o.y, 16);
+      o.z += __shfl_xor_sync(0xFFFFFFFFu, o.z, 16);
+      o.w += __shfl_xor_sync(0xFFFFFFFFu, o.w, 16);
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int token = row / p.group, head = part.head * p.group + row - token * p.group;
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + (part.first + token) * p.out_token + head * p.out_head +
-                         lane * (D / 32);
-#pragma unroll
-    for (int e = 0; e < D / 32; e += 2) *reinterpret_cast<uint32_t*>(out + e) = pack_bf16(o[e] * inv, o[e + 1] * inv);
+    if (lane < kLanes) {
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + (part.first + token) * p.out_token + head * p.out_head;
+      reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    }
     if (p.lse && lane == 0)
       p.lse[(long long)(part.first + token) * p.q_heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
   }
@@ -951,6 +1082,7 @@ int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, 
   tp.tile_rows = 128 / p.group * p.group;
   tp.box_rows = page > 0 ? min(page, kKeyTile) : kKeyTile;
   tp.q_bytes = p.head_dim * 2 * p.group * tokens;
+  tp.wide_out = aligned(p.out, 32) && p.out_token % 16 == 0 && p.out_head % 16 == 0;
   const long long part_rows = (long long)2 * blocks * 2 * tp.tile_rows;
   p.part_out = static_cast<float*>(workspace);
   p.part_lse = p.part_out + part_rows * p.head_dim;
