@@ -18,8 +18,9 @@ struct NormParams {
   void* y;
   float* scales;
   long long rows, x_stride, residual_stride, residual_out_stride, y_stride;
-  float eps;
+  float eps, per_channel;  // 1 / hidden
   int hidden, group, groups;
+  int group_shift;         // group = 2^group_shift accesses (groups of neighbouring lanes)
 };
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -29,7 +30,11 @@ __device__ __forceinline__ float warp_sum(float v) {
 }
 
 // max that keeps a NaN: a row with one gets a NaN scale, as the formula has it
-__device__ __forceinline__ float max_nan(float a, float b) { return (a > b || a != a) ? a : b; }
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 
 __device__ __forceinline__ float warp_max_nan(float v) {
 #pragma unroll
@@ -37,12 +42,180 @@ __device__ __forceinline__ float warp_max_nan(float v) {
   return v;
 }
 
+__device__ __forceinline__ float reciprocal(float s) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+  return r;
+}
+
 __device__ __forceinline__ float scale_of(float amax) {
-  const float s = __fdiv_rn(amax, kE4m3Max);
+  const float s = amax * (1.0f / kE4m3Max);
   return s < kSmallestScale ? kSmallestScale : s;
 }
 
-// A block per row, the row's h in shared memory between the two passes.
+// Bound by memory: x and residual are read once, residual_out and y written once.  A block takes a row and keeps it in
+// registers between the two passes, 16 bytes an access where rows allow it.  What has to be in flight on an SM (50 KB and
+// more) comes from its many threads, not from many values a thread: 16 values a thread and 32 registers (2048 threads an
+// SM) take 620 us for 65536 x 8192 bf16 with e4m3 groups of 128 (6.1 TB/s), 32 values 715 us.  Rows that are no vectors:
+// 1024 threads of up to 8 values (4095 x 5001 fp32: 64 us, with 32 values 135).
+//
+// kVec elements an access, kPer accesses a thread, access v of a row to thread v % threads.
+enum Mode { kSame, kRowScale, kGroupScale };
+
+template <typename T, int kVec>
+__device__ __forceinline__ void load_values(const T* p, float* v) {
+  if constexpr (kVec == 1) {
+    v[0] = to_float(p[0]);
+  } else {
+    const uint4 q = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[2 * i] = bf16_low(w[i]), v[2 * i + 1] = bf16_high(w[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
+    }
+  }
+}
+
+template <typename T, int kVec>
+__device__ __forceinline__ void store_values(T* p, const float* v) {
+  if constexpr (kVec == 1) {
+    store_as(p, v[0]);
+  } else if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(p) =
+        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  } else {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+template <int kVec>
+__device__ __forceinline__ void store_e4m3(uint8_t* p, const float* v) {
+  if constexpr (kVec == 1) {
+    *p = __nv_cvt_float_to_fp8(v[0], __NV_SATFINITE, __NV_E4M3);
+  } else {
+    uint32_t w[kVec / 4];
+#pragma unroll
+    for (int i = 0; i < kVec / 4; ++i)
+      w[i] = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * i], v[4 * i + 1]), __NV_SATFINITE, __NV_E4M3) |
+             (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v[4 * i + 2], v[4 * i + 3]), __NV_SATFINITE, __NV_E4M3) << 16;
+    if constexpr (kVec == 4)
+      *reinterpret_cast<uint32_t*>(p) = w[0];
+    else
+      *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  }
+}
+
+template <typename T, int kVec, int kPer, Mode kMode>
+__global__ void __launch_bounds__(kVec > 1 || kPer > 8 ? 512 : 1024, kVec * kPer > 16 ? 1 : kVec > 1 ? 4 : kPer <= 5 ? 2 : 1)
+    toploc_rmsnorm_rows_kernel(const NormParams p) {
+  __shared__ float partial[32], partial_max[32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
+  const long long row = blockIdx.x;
+  const T* x = static_cast<const T*>(p.x) + row * p.x_stride;
+  const T* r = static_cast<const T*>(p.residual) + row * p.residual_stride;
+  T* ro = static_cast<T*>(p.residual_out) + row * p.residual_out_stride;
+  const T* w = static_cast<const T*>(p.weight);
+  float h[kPer][kVec];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int c = (tid + i * threads) * kVec;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) h[i][e] = 0.f;
+    if (c < p.hidden) load_values<T, kVec>(x + c, h[i]);
+  }
+  if (p.residual) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int c = (tid + i * threads) * kVec;
+      if (c < p.hidden) {
+        float v[kVec];
+        load_values<T, kVec>(r + c, v);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) h[i][e] += v[e];
+      }
+    }
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) ss = fmaf(h[i][e], h[i][e], ss);
+  ss = warp_sum(ss);
+  if (lane == 0) partial[warp] = ss;
+  if (p.residual_out) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int c = (tid + i * threads) * kVec;
+      if (c < p.hidden) store_values<T, kVec>(ro + c, h[i]);
+    }
+  }
+  __syncthreads();
+  float total = warp_sum(lane < warps ? partial[lane] : 0.f);
+  const float scale = rsqrtf(fmaf(total, p.per_channel, p.eps));
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int c = (tid + i * threads) * kVec;
+    if (c < p.hidden) {
+      float v[kVec];
+      load_values<T, kVec>(w + c, v);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) h[i][e] = h[i][e] * scale * v[e];
+    }
+  }
+  if constexpr (kMode == kSame) {
+    T* y = static_cast<T*>(p.y) + row * p.y_stride;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int c = (tid + i * threads) * kVec;
+      if (c < p.hidden) store_values<T, kVec>(y + c, h[i]);
+    }
+  } else {
+    uint8_t* y = static_cast<uint8_t*>(p.y) + row * p.y_stride;
+    float amax[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      amax[i] = 0.f;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) amax[i] = max_nan(fabsf(h[i][e]), amax[i]);
+    }
+    float row_scale = 0.f;
+    if constexpr (kMode == kRowScale) {
+      float top = amax[0];
+#pragma unroll
+      for (int i = 1; i < kPer; ++i) top = max_nan(amax[i], top);
+      top = warp_max_nan(top);
+      if (lane == 0) partial_max[warp] = top;
+      __syncthreads();
+      row_scale = scale_of(warp_max_nan(lane < warps ? partial_max[lane] : 0.f));
+      if (tid == 0) p.scales[row] = row_scale;
+    }
+    if constexpr (kMode == kGroupScale) {  // a group is the accesses of neighbouring lanes (2^n of them)
+      for (int off = 1 << p.group_shift >> 1; off > 0; off >>= 1) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) amax[i] = max_nan(amax[i], __shfl_xor_sync(0xFFFFFFFFu, amax[i], off));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int v = tid + i * threads, c = v * kVec;
+      float s = row_scale;
+      if constexpr (kMode == kGroupScale) {
+        s = scale_of(amax[i]);
+        if (c < p.hidden && (v & ((1 << p.group_shift) - 1)) == 0) p.scales[row * p.groups + (v >> p.group_shift)] = s;
+      }
+      // y / s as y * (1 / s): off by an fp32 rounding or two, which moves an e4m3 result only next to the middle of two
+      const float inv = reciprocal(s);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) h[i][e] *= inv;
+      if (c < p.hidden) store_e4m3<kVec>(y + c, h[i]);
+    }
+  }
+}
+
+// Any hidden size, layout and group: a block per row, the row's h in shared memory between the two passes.
 template <typename T, bool QUANT>
 __global__ void __launch_bounds__(256) toploc_rmsnorm_residual_kernel(const NormParams p) {
   extern __shared__ float h[];
@@ -67,7 +240,7 @@ __global__ void __launch_bounds__(256) toploc_rmsnorm_residual_kernel(const Norm
   float total = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) total += partial[i];
-  const float scale = rsqrtf(total / (float)p.hidden + p.eps);
+  const float scale = rsqrtf(fmaf(total, p.per_channel, p.eps));
   if constexpr (!QUANT) {
     T* y = static_cast<T*>(p.y) + row * p.y_stride;
     for (int c = tid; c < p.hidden; c += 256) store_as(y + c, h[c] * scale * to_float(w[c]));
@@ -81,21 +254,71 @@ __global__ void __launch_bounds__(256) toploc_rmsnorm_residual_kernel(const Norm
         h[c] = v;
         amax = max_nan(fabsf(v), amax);
       }
-      const float s = scale_of(warp_max_nan(amax));
-      for (int c = begin + lane; c < end; c += 32) y[c] = __nv_fp8_e4m3(__fdiv_rn(h[c], s));
+      const float s = scale_of(warp_max_nan(amax)), inv = reciprocal(s);
+      for (int c = begin + lane; c < end; c += 32) y[c] = __nv_fp8_e4m3(h[c] * inv);
       if (lane == 0) p.scales[row * p.groups + g] = s;
     }
   }
 }
 
 template <typename T, bool QUANT>
-int launch(const NormParams& p, cudaStream_t stream) {
+int launch_any(const NormParams& p, cudaStream_t stream) {
   const size_t bytes = (size_t)p.hidden * 4;
   if (bytes > 40 * 1024 && cudaFuncSetAttribute(toploc_rmsnorm_residual_kernel<T, QUANT>,
                                                 cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess)
     return TOPLOC_ERR_CUDA;
   toploc_rmsnorm_residual_kernel<T, QUANT><<<(unsigned)p.rows, 256, bytes, stream>>>(p);
   return launched();
+}
+
+template <typename T, int kVec, int kPer>
+int launch_rows(const NormParams& p, Mode mode, int threads, cudaStream_t stream) {
+  const unsigned rows = (unsigned)p.rows;
+  if (mode == kSame)
+    toploc_rmsnorm_rows_kernel<T, kVec, kPer, kSame><<<rows, threads, 0, stream>>>(p);
+  else if (mode == kRowScale)
+    toploc_rmsnorm_rows_kernel<T, kVec, kPer, kRowScale><<<rows, threads, 0, stream>>>(p);
+  else
+    toploc_rmsnorm_rows_kernel<T, kVec, kPer, kGroupScale><<<rows, threads, 0, stream>>>(p);
+  return launched();
+}
+
+// The row in registers where it fits 512 threads of 32 values (and a group's lanes are neighbours), else in shared
+// memory.
+template <typename T>
+int launch(NormParams& p, bool quant, bool vectors, cudaStream_t stream) {
+  constexpr int kWide = 16 / sizeof(T);
+  const int vec = vectors ? kWide : 1, accesses = (p.hidden + vec - 1) / vec;
+  const Mode mode = !quant ? kSame : p.groups == 1 ? kRowScale : kGroupScale;
+  const int lanes = p.group / vec;  // of a group
+  const bool fits = accesses <= 512 * (32 / vec) &&
+                    (mode != kGroupScale || (p.group % vec == 0 && lanes <= 32 && (lanes & (lanes - 1)) == 0));
+  if (!fits) return quant ? launch_any<T, true>(p, stream) : launch_any<T, false>(p, stream);
+  while (1 << p.group_shift < lanes && p.group_shift < 5) ++p.group_shift;
+  int per = 1;
+  if (vectors) {
+    while (per * 512 < accesses) per *= 2;
+  } else {
+    for (const int more : {2, 3, 5, 8, 32})
+      if (per * (per > 8 ? 512 : 1024) < accesses) per = more;
+  }
+  const int threads = ((accesses + per - 1) / per + 31) / 32 * 32;
+  if (vectors) {
+    switch (per) {
+      case 1: return launch_rows<T, kWide, 1>(p, mode, threads, stream);
+      case 2: return launch_rows<T, kWide, 2>(p, mode, threads, stream);
+      case 4: return launch_rows<T, kWide, 4>(p, mode, threads, stream);
+      default: return launch_rows<T, kWide, 32 / kWide>(p, mode, threads, stream);
+    }
+  }
+  switch (per) {
+    case 1: return launch_rows<T, 1, 1>(p, mode, threads, stream);
+    case 2: return launch_rows<T, 1, 2>(p, mode, threads, stream);
+    case 3: return launch_rows<T, 1, 3>(p, mode, threads, stream);
+    case 5: return launch_rows<T, 1, 5>(p, mode, threads, stream);
+    case 8: return launch_rows<T, 1, 8>(p, mode, threads, stream);
+    default: return launch_rows<T, 1, 32>(p, mode, threads, stream);
+  }
 }
 
 }  // namespace
@@ -119,11 +342,16 @@ extern "C" int toploc_rmsnorm_residual(const void* d_x, const void* d_residual_o
   if (!aligned(d_y, quant ? 1 : size) || (quant && !aligned(d_scales_opt, 4))) return TOPLOC_ERR_INVALID_ARGUMENT;
   if (const int rc = check_device()) return rc;
   NormParams p = {d_x, d_residual_opt, d_weight, d_residual_out_opt, d_y, d_scales_opt, lay->rows, lay->x_stride,
-                  lay->residual_stride, lay->residual_out_stride, lay->y_stride, eps, lay->hidden, lay->group, 0};
+                  lay->residual_stride, lay->residual_out_stride, lay->y_stride, eps, 1.0f / (float)lay->hidden, lay->hidden,
+                  lay->group, 0, 0};
   if (p.group == 0 || p.group > p.hidden) p.group = p.hidden;
   p.groups = (p.hidden + p.group - 1) / p.group;
+  const int64_t per = 16 / size;
+  bool vectors = p.hidden % per == 0 && p.x_stride % per == 0 && aligned(d_x, 16) && aligned(d_weight, 16) &&
+                 p.y_stride % per == 0 && aligned(d_y, quant ? per : 16);
+  if (d_residual_opt) vectors = vectors && p.residual_stride % per == 0 && aligned(d_residual_opt, 16);
+  if (d_residual_out_opt) vectors = vectors && p.residual_out_stride % per == 0 && aligned(d_residual_out_opt, 16);
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  if (lay->dtype == TOPLOC_DTYPE_BF16)
-    return quant ? launch<__nv_bfloat16, true>(p, stream) : launch<__nv_bfloat16, false>(p, stream);
-  return quant ? launch<float, true>(p, stream) : launch<float, false>(p, stream);
+  return lay->dtype == TOPLOC_DTYPE_BF16 ? launch<__nv_bfloat16>(p, quant, vectors, stream)
+                                         : launch<float>(p, quant, vectors, stream);
 }

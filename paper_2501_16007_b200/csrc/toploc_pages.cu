@@ -30,6 +30,7 @@ struct PlanParams {
   uint8_t* status;
   long long table_stride, max_tokens;
   int num_seqs, num_free, page_size, max_pages;
+  bool wide;  // slots and positions at 16-byte aligned places
 };
 
 // One sequence as the plan sees it, given the tokens and the pages in front of it.
@@ -41,6 +42,11 @@ struct PlannedSeq {
   int pages_before, pages_needed;
   int status;
 };
+
+// (32-bit: a 64-bit division takes several times as long, and the plan does a dozen one after the other)
+__device__ __forceinline__ int pages_for(int tokens, int page_size) {
+  return (int)(((unsigned)tokens + (unsigned)page_size - 1u) / (unsigned)page_size);
+}
 
 // The lengths alone: tokens, pages asked for, and the conditions that do not depend on the pool.
 __device__ __forceinline__ PlannedSeq look_at(const PlanParams& p, int i, long long first_token) {
@@ -59,12 +65,12 @@ __device__ __forceinline__ PlannedSeq look_at(const PlanParams& p, int i, long l
   } else if (first_token + s.tokens > p.max_tokens) {
     s.status = TOPLOC_SEQ_BATCH_FULL;
   } else {
-    const long long after = (kv + p.page_size - 1) / p.page_size;
+    const int after = pages_for((int)kv, p.page_size);
     if (after > p.max_pages) {
       s.status = TOPLOC_SEQ_TABLE_FULL;
     } else {
-      s.pages_before = (int)(((long long)s.cached + p.page_size - 1) / p.page_size);
-      s.pages_needed = (int)after - s.pages_before;
+      s.pages_before = pages_for(s.cached, p.page_size);
+      s.pages_needed = after - s.pages_before;
     }
   }
   return s;
@@ -163,45 +169,66 @@ __global__ void __launch_bounds__(kPlanThreads) toploc_plan_pages_kernel(const P
     for (int j = tid & 31; j < s.pages_needed; j += 32) row[j] = p.free_pages[page + j];
   }
 
-  // slots and positions: consecutive rows to consecutive threads
+  // slots and positions: four consecutive rows a thread, which as a rule are one sequence's and in one page
   PlannedSeq s;
   s.first_token = 0;
   s.tokens = 0;
   s.status = TOPLOC_SEQ_OK;
   int seq = 0;
   const long long rows = min(total_tokens, p.max_tokens);
-  const long long step = (long long)gridDim.x * kPlanThreads;
-  for (long long r = (long long)blockIdx.x * kPlanThreads + tid; r < p.max_tokens; r += step) {
-    if (r >= rows) {
-      p.slots[r] = -1;
-      p.positions[r] = 0;
-      continue;
-    }
-    if (r >= s.first_token + s.tokens) {  // find the row's sequence: its run, then within the run
-      int lo = 0, hi = kPlanThreads;      // run_token[lo] <= r < run_token[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (run_token[mid] <= r) lo = mid; else hi = mid;
+  const long long step = (long long)gridDim.x * kPlanThreads * 4;
+  for (long long r0 = ((long long)blockIdx.x * kPlanThreads + tid) * 4; r0 < p.max_tokens; r0 += step) {
+    long long slot[4];
+    int position[4];
+    int page_end = 0;  // positions of this sequence from the last one on up to here lie in the last slot's page
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const long long r = r0 + e;
+      slot[e] = -1;
+      position[e] = 0;
+      if (r >= rows) continue;
+      if (r >= s.first_token + s.tokens) {  // find the row's sequence: its run, then within the run
+        int lo = 0, hi = kPlanThreads;      // run_token[lo] <= r < run_token[hi]
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (run_token[mid] <= r) lo = mid; else hi = mid;
+        }
+        long long token = run_token[lo], page = run_page[lo];
+        for (seq = lo * per; seq < p.num_seqs; ++seq) {
+          s = look_at(p, seq, token);
+          if (r < token + s.tokens) break;
+          token += s.tokens;
+          page += s.pages_needed;
+        }
+        place(p, s, page);
+        page_end = 0;
       }
-      long long token = run_token[lo], page = run_page[lo];
-      for (seq = lo * per; seq < p.num_seqs; ++seq) {
-        s = look_at(p, seq, token);
-        if (r < token + s.tokens) break;
-        token += s.tokens;
-        page += s.pages_needed;
+      const int pos = (int)((long long)s.cached + (r - s.first_token));
+      position[e] = pos;
+      if (s.status != TOPLOC_SEQ_OK) continue;
+      if (e > 0 && pos < page_end) {
+        if (slot[e - 1] >= 0) slot[e] = slot[e - 1] + 1;
+        continue;
       }
-      place(p, s, page);
-    }
-    const int pos = (int)((long long)s.cached + (r - s.first_token));
-    long long slot = -1;
-    if (s.status == TOPLOC_SEQ_OK) {
-      const int col = pos / p.page_size;
+      const int col = (int)((unsigned)pos / (unsigned)p.page_size);
       const int held = col < s.pages_before ? p.table[seq * p.table_stride + col]
                                             : p.free_pages[s.first_page + (col - s.pages_before)];
-      if (held >= 0) slot = (long long)held * p.page_size + (pos - col * p.page_size);
+      if (held >= 0) slot[e] = (long long)held * p.page_size + (pos - col * p.page_size);
+      page_end = (int)min((long long)(col + 1) * p.page_size, 0x7FFFFFFFll);
     }
-    p.slots[r] = slot;
-    p.positions[r] = pos;
+    if (r0 + 4 <= p.max_tokens && p.wide) {
+      *reinterpret_cast<longlong2*>(p.slots + r0) = make_longlong2(slot[0], slot[1]);
+      *reinterpret_cast<longlong2*>(p.slots + r0 + 2) = make_longlong2(slot[2], slot[3]);
+      *reinterpret_cast<int4*>(p.positions + r0) = make_int4(position[0], position[1], position[2], position[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (r0 + e < p.max_tokens) {
+          p.slots[r0 + e] = slot[e];
+          p.positions[r0 + e] = position[e];
+        }
+      }
+    }
   }
 }
 
@@ -271,11 +298,11 @@ extern "C" int toploc_plan_pages(const int32_t* d_cached_lens, const int32_t* d_
   if (const int rc = check_device(&sms)) return rc;
   const PlanParams p = {d_cached_lens, d_new_lens, d_free_pages, d_first_free, d_block_table, d_seq_offsets, d_kv_lens,
                         d_slots, d_positions, d_next_free, d_status, table_stride, max_tokens, num_seqs, num_free,
-                        page_size, max_pages};
-  // a thread per row and a warp per sequence, up to two blocks an SM
-  const long long wanted = max((long long)(max_tokens + kPlanThreads - 1) / kPlanThreads,
+                        page_size, max_pages, aligned(d_slots, 16) && aligned(d_positions, 16)};
+  // four rows a thread and a warp per sequence, up to four blocks an SM (each repeats the prefix sums)
+  const long long wanted = max((long long)(max_tokens + 4 * kPlanThreads - 1) / (4 * kPlanThreads),
                                (long long)(num_seqs + kPlanThreads / 32 - 1) / (kPlanThreads / 32));
-  const int blocks = (int)max(1ll, min(wanted, 2ll * sms));
+  const int blocks = (int)max(1ll, min(wanted, 4ll * sms));
   toploc_plan_pages_kernel<<<blocks, kPlanThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
   return launched();
 }

@@ -94,15 +94,17 @@ def _need(condition, what):
 
 def _device(name, *tensors):
     """All tensors (None: absent) on one CUDA device, which is returned."""
-    dev = tensors[0].device
+    index = tensors[0].get_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device != dev):
-            raise ToplocError("%s needs CUDA tensors of one device" % name)
-    return dev
+        if t is not None and t.get_device() != index:
+            index = -1
+    if index < 0:  # the CPU's number
+        raise ToplocError("%s needs CUDA tensors of one device" % name)
+    return tensors[0].device
 
 
 def _vector(t, dtype, length, what):
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != length or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != (length,) or not t.is_contiguous():
         raise ToplocError("%s must be a contiguous %s tensor of %d entries" % (what, dtype, length))
 
 
@@ -112,13 +114,13 @@ def _ptr(t):
 
 def _call(fn, name, dev, stream, *args):
     """fn(*args, stream) with `dev` current; raises on a non-zero return code."""
-    if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    if dev.index == torch.cuda.current_device():
-        rc = fn(*args, stream.cuda_stream)
+    index = dev.index
+    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if index == torch._C._cuda_getDevice():
+        rc = fn(*args, raw)
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, stream.cuda_stream)
+            rc = fn(*args, raw)
     if rc != 0:
         raise ToplocError("%s failed: %s (%d)" % (name, binding.toploc_error_string(rc), rc))
 
@@ -130,14 +132,16 @@ def toploc_plan_pages(cached_lens, new_lens, free_pages, first_free, block_table
     [max_tokens]; slots int64 [max_tokens], status uint8 [n].  The last six are written, and the block table."""
     dev = _device("toploc_plan_pages", cached_lens, new_lens, free_pages, first_free, block_table, seq_offsets, kv_lens,
                   slots, positions, next_free, status)
-    n, tokens, i32 = cached_lens.shape[0], slots.shape[0], torch.int32
-    for t, dtype, length, what in ((cached_lens, i32, n, "cached_lens"), (new_lens, i32, n, "new_lens"),
-                                   (free_pages, i32, free_pages.shape[0], "free_pages"),
-                                   (first_free, i32, 1, "first_free"), (seq_offsets, i32, n + 1, "seq_offsets"),
-                                   (kv_lens, i32, n, "kv_lens"), (slots, torch.int64, tokens, "slots"),
-                                   (positions, i32, tokens, "positions"), (next_free, i32, 1, "next_free"),
-                                   (status, torch.uint8, n, "status")):
-        _vector(t, dtype, length, what)
+    n, tokens, i32 = cached_lens.numel(), slots.numel(), torch.int32
+    if not (cached_lens.dtype is new_lens.dtype is free_pages.dtype is first_free.dtype is seq_offsets.dtype is
+            kv_lens.dtype is positions.dtype is next_free.dtype is i32 and
+            new_lens.shape == kv_lens.shape == status.shape == (n,) and seq_offsets.shape == (n + 1,) and
+            positions.shape == (tokens,) and first_free.shape == next_free.shape == (1,) and free_pages.dim() == 1 and
+            slots.dtype is torch.int64 and status.dtype is torch.uint8):
+        raise ToplocError("toploc_plan_pages: int32 cached_lens, new_lens, kv_lens [n], free_pages, first_free and "
+                          "next_free [1], seq_offsets [n + 1], positions [tokens]; int64 slots [tokens], uint8 status [n]")
+    for t in (cached_lens, new_lens, free_pages, seq_offsets, kv_lens, slots, positions, status):
+        _need(t.is_contiguous(), "toploc_plan_pages needs contiguous vectors")
     _need(block_table.dtype == i32 and block_table.dim() == 2 and block_table.shape[0] == n and
           (block_table.stride(1) == 1 or block_table.shape[1] <= 1 or n == 0), "block_table must be int32 [n, max_pages]")
     width = block_table.shape[1]
