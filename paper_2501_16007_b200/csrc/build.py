@@ -13,13 +13,14 @@ _INCLUDE = os.path.join(_ROOT, "include")
 PROOF_SOURCES = [os.path.join(_HERE, "toploc.cu"), os.path.join(_HERE, "toploc_direct.cu"),
                  os.path.join(_HERE, "toploc_producer.cu")]
 MODEL_SOURCES = [os.path.join(_HERE, "toploc_pages.cu"), os.path.join(_HERE, "toploc_norm.cu"),
-                 os.path.join(_HERE, "toploc_attention.cu"), os.path.join(_HERE, "toploc_attention_tc.cu")]
+                 os.path.join(_HERE, "toploc_attention.cu"), os.path.join(_HERE, "toploc_attention_tc.cu"),
+                 os.path.join(_HERE, "toploc_attention_few.cu")]
 SOURCES = PROOF_SOURCES + MODEL_SOURCES
 PROOF_HEADERS = [os.path.join(_INCLUDE, "toploc.h"), os.path.join(_INCLUDE, "toploc_device.cuh"),
                  os.path.join(_HERE, "nearest_ratio.cuh")]
 MODEL_HEADERS = [os.path.join(_INCLUDE, "toploc.h"), os.path.join(_INCLUDE, "toploc_model.h"),
                  os.path.join(_HERE, "model_common.cuh"), os.path.join(_HERE, "attention_common.cuh"),
-                 os.path.join(_HERE, "sm100.cuh")]
+                 os.path.join(_HERE, "attention_tc.cuh"), os.path.join(_HERE, "sm100.cuh")]
 HEADERS = PROOF_HEADERS + MODEL_HEADERS
 LIBRARY = os.path.join(_HERE, "libtoploc.so")
 

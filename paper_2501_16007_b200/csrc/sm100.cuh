@@ -168,6 +168,20 @@ __device__ __forceinline__ void tmem_ready(uint32_t (&r)[32]) {
                  "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]),
                  "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
 }
+__device__ __forceinline__ void tmem_load(uint32_t (&r)[16], uint32_t addr) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, "
+               "%13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                 "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
+                 "=r"(r[15])
+               : "r"(addr));
+}
+__device__ __forceinline__ void tmem_ready(uint32_t (&r)[16]) {
+  asm volatile(""
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]),
+                 "+r"(r[15]));
+}
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -181,25 +195,32 @@ __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence
 __device__ __forceinline__ uint32_t operand_low(uint32_t address, uint32_t block_step) {
   return ((address & 0x3FFFF) >> 4) | (block_step >> 4) << 16;
 }
-constexpr uint32_t kOperandHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
+constexpr uint32_t kSwizzledHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
 
-// Instruction word: bf16 x bf16 -> fp32, 128 x n; b_by_rows: B's rows run along K (its n index is contiguous).
-__host__ __device__ constexpr uint32_t bf16_product(uint32_t n, bool b_by_rows) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | ((b_by_rows ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+// The upper word of an operand without a swizzle whose rows run along K: cores of 8 elements (16 bytes) x 8 rows,
+// block_step (lower word) from 8 rows to the next 8, core_step from 8 elements to the next.
+__host__ __device__ constexpr uint32_t plain_high(uint32_t core_step) { return (core_step >> 4) | 1u << 14; }
+
+// Instruction word: bf16 x bf16 -> fp32, 128 x n; by_rows: the operand's rows run along K (its m or n index is
+// contiguous).
+__host__ __device__ constexpr uint32_t bf16_product(uint32_t n, bool a_by_rows, bool b_by_rows) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((a_by_rows ? 1u : 0u) << 15) | ((b_by_rows ? 1u : 0u) << 16) |
+         ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
-// D (tensor memory) = A B (+ D), K = 16; A in shared memory (its descriptor's lower word, B's too).
+// D (tensor memory) = A B (+ D), K = 16; operands in shared memory by the lower words of their descriptors.
+template <uint32_t kHighA = kSwizzledHigh, uint32_t kHighB = kSwizzledHigh>
 __device__ __forceinline__ void mma_shared(uint32_t d, uint32_t a, uint32_t b, uint32_t word, bool add) {
   asm volatile(
       "{\n\t"
       ".reg .pred p;\n\t"
       ".reg .b64 da, db;\n\t"
-      "setp.ne.b32 p, %5, 0;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
       "mov.b64 da, {%1, %4};\n\t"
-      "mov.b64 db, {%2, %4};\n\t"
+      "mov.b64 db, {%2, %5};\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t"
       "}" ::"r"(d),
-      "r"(a), "r"(b), "r"(word), "r"(kOperandHigh), "r"((uint32_t)add)
+      "r"(a), "r"(b), "r"(word), "r"(kHighA), "r"(kHighB), "r"((uint32_t)add)
       : "memory");
 }
 
@@ -213,7 +234,7 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b, uin
       "mov.b64 db, {%2, %4};\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t"
       "}" ::"r"(d),
-      "r"(a), "r"(b), "r"(word), "r"(kOperandHigh), "r"((uint32_t)add)
+      "r"(a), "r"(b), "r"(word), "r"(kSwizzledHigh), "r"((uint32_t)add)
       : "memory");
 }
 

@@ -1,0 +1,447 @@
+// Attention on the tensor cores where a sequence brings few rows (up to 16 or 32 packed ones: a token or a few, all heads
+// of a key head), bf16, head_dim 64 or 128.  Bound by reading the keys and values.
+//
+//   S^T = K Q^T (128 keys x N rows),  P^T = 2^(scale S^T - m),  O^T += V^T P^T (head_dim x N)
+//
+// With so few rows the other order would leave most of a product's 128 rows and of the softmax threads empty.  Here a
+// thread has a key and weighs it for all N rows (N exponentials, not 128), and the products are N wide.  A row's maximum
+// and sum run over threads, but seldom: the maximum of the first tile stays the reference for the whole item unless a
+// score exceeds it by 2^64 (weights, sums and outputs share it, and fp32 and bf16 have the range; the quotient is the
+// same), so a tile needs one vote, and the threads' own sums are added up once at the end.
+//
+// Two blocks share an SM, three tiles of 32 KB in flight each (head_dim 128).  A block: four warps of softmax, a warp
+// that feeds keys (and finds the items), one that feeds values, one that issues the products; the scores of the next tile
+// are computed while the weights of this one are.
+#include "attention_tc.cuh"
+
+namespace {
+
+constexpr int kFewThreads = 224;
+constexpr float kFewLimit = 64.0f;
+
+template <int D, int N>
+struct FewShared {
+  static constexpr int kHalves = D / 64;
+  static constexpr int kTileBytes = kHalves * kBlockBytes;
+  static constexpr int kStages = D == 128 ? 3 : 6;
+  static constexpr int kQueryBytes = N * 128 * kHalves, kWeightBytes = kKeyTile * N * 2;
+  struct Head {
+    uint64_t full[kStages], empty[kStages];
+    uint64_t s_full[2], p_full, o_full;
+    uint64_t q_full, q_empty, drain;
+    uint64_t group;  // the four warps of the softmax
+    uint64_t item_full[kItems], item_empty[kItems];
+    Item items[kItems];
+    uint32_t tmem;
+    int gave_up;
+    int bad_values[2];    // number of the item (by parity) in whose hidden keys' tiles a value was not finite
+    uint32_t exceeds[2];  // number of the tile (by parity) with a score over the limit
+    float rows[4][N];     // by warp: maxima, or sums
+  };
+  static constexpr int kHeadBytes = 1024;
+  static_assert(sizeof(Head) <= kHeadBytes, "head");
+  static constexpr int kBytes = kHeadBytes + kStages * kTileBytes + kQueryBytes + kWeightBytes;
+  static_assert(kBytes <= 115712, "shared memory of half an SM");
+};
+
+template <int D, int N>
+__global__ void __launch_bounds__(kFewThreads, 2)
+toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorMap map_q,
+                            const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  using S = FewShared<D, N>;
+  constexpr int kStages = S::kStages, kHalves = S::kHalves;
+  extern __shared__ __align__(1024) unsigned char base[];
+  const AttentionParams& p = tp.p;
+  typename S::Head& sh = *reinterpret_cast<typename S::Head*>(base);
+  unsigned char* ring = base + S::kHeadBytes;
+  unsigned char* queries = ring + kStages * S::kTileBytes;
+  unsigned char* weights = queries + S::kQueryBytes;
+  const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  volatile int* gave_up = &sh.gave_up;
+
+  asm volatile("griddepcontrol.launch_dependents;");  // the join waits for this grid to end
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      barrier_init(shared_address(&sh.full[i]), 1);
+      barrier_init(shared_address(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      barrier_init(shared_address(&sh.s_full[i]), 1);
+      sh.bad_values[i] = -1;
+      sh.exceeds[i] = 0;
+    }
+    barrier_init(shared_address(&sh.p_full), 4);
+    barrier_init(shared_address(&sh.o_full), 1);
+    barrier_init(shared_address(&sh.q_full), 1);
+    barrier_init(shared_address(&sh.q_empty), 1);
+    barrier_init(shared_address(&sh.drain), 1);
+    barrier_init(shared_address(&sh.group), 4);
+    for (int i = 0; i < kItems; ++i) {
+      barrier_init(shared_address(&sh.item_full[i]), 1);
+      barrier_init(shared_address(&sh.item_empty[i]), 6);
+    }
+    sh.gave_up = 0;
+    barrier_init_fence();
+  }
+  constexpr uint32_t kColumns = 4 * N;  // tensor memory: two tiles of scores, the outputs (a power of two at least 32)
+  if (warp == 5) tmem_alloc(shared_address(&sh.tmem), kColumns);
+  long long* run_cost = reinterpret_cast<long long*>(ring);  // where the ring's first tile comes later
+  lay_line<kFewThreads>(tp, run_cost);
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, sh.tmem, 0);
+  constexpr uint32_t kOut = 2 * N;  // scores of tile j at N (j % 2), outputs at 2 N
+
+  if (warp == 4) {
+    // ---- feeding: finds the items, copies queries and keys ----
+    if (lane == 0) {
+      prefetch_map(&map_q);
+      prefetch_map(&map_k);
+      prefetch_map(&map_v);
+    }
+    Walk walk(tp, find_place<kFewThreads>(tp, run_cost, blockIdx.x), find_place<kFewThreads>(tp, run_cost, blockIdx.x + 1));
+    __syncwarp();  // run_cost has been read: the ring's place is free
+    uint32_t q_uses = 0;
+    Feeder<S> keys(tp, &map_k, sh, ring, gave_up);
+    for (uint32_t number = 0;; ++number) {
+      const uint32_t slot = number % kItems;
+      if (!warp_wait(sh.item_empty[slot], ((number / kItems) & 1) ^ 1, gave_up)) break;
+      Item im;
+      const bool more = walk.next(im);
+      im = uniform(im);
+      if (lane == 0) {
+        sh.items[slot] = im;
+        barrier_arrive(shared_address(&sh.item_full[slot]));
+      }
+      __syncwarp();
+      if (!more) break;
+      if (im.n0 == 0) continue;
+      if (!warp_wait(sh.q_empty, (q_uses & 1) ^ 1, gave_up)) break;
+      ++q_uses;
+      if (elect_one()) {
+        const uint32_t bar = shared_address(&sh.q_full);
+        barrier_arrive_expect(bar, tp.q_bytes);
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h)
+          copy_3d(shared_address(queries + h * N * 128), &map_q, bar, h * 64, im.head * p.group, im.first);
+      }
+      __syncwarp();
+      keys.item(im, im.n0);
+      for (int j = 0; j < im.n0 && keys.fine; ++j) keys.feed(j, key_place(false, j));
+      if (!keys.fine) break;
+    }
+    if (*gave_up) {  // copies in flight have to land before the block ends
+      if (q_uses > 0) barrier_drain(shared_address(&sh.q_full), (q_uses - 1) & 1);
+      keys.drain();
+    }
+  } else if (warp == 6) {
+    // ---- feeding: values ----
+    Feeder<S> values(tp, &map_v, sh, ring, gave_up);
+    for (uint32_t number = 0;; ++number) {
+      const uint32_t slot = number % kItems;
+      if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
+      const Item im = uniform(sh.items[slot]);
+      __syncwarp();
+      if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
+      if (im.seq < 0) break;
+      values.item(im, im.n0);
+      for (int j = 0; j < im.n0 && values.fine; ++j) values.feed(j, value_place(false, j, im.n0));
+      if (!values.fine) break;
+    }
+    if (*gave_up) values.drain();
+  } else if (warp == 5) {
+    // ---- products: the whole warp follows, one lane issues ----
+    constexpr uint32_t kScores = bf16_product(N, false, false), kValues = bf16_product(N, true, true);
+    // (head_dim 64: the upper 64 rows of the second product repeat the lower ones and are not read)
+    const uint32_t k_low = operand_low(shared_address(ring), 16);
+    const uint32_t v_low = operand_low(shared_address(ring), D == 128 ? kBlockBytes : 0);
+    const uint32_t q_low = operand_low(shared_address(queries), 16), w_low = operand_low(shared_address(weights), 128);
+    uint32_t used = 0, q_uses = 0, p_uses = 0;
+    const auto full = [&](uint32_t n) {
+      const bool ok = warp_wait(sh.full[ring_stage(n, kStages)], ring_parity(n, kStages), gave_up);
+      tmem_fence_after();
+      return ok;
+    };
+    const auto release = [&](uint32_t n) {
+      if (elect_one()) mma_commit(shared_address(&sh.empty[ring_stage(n, kStages)]));
+    };
+    const auto scores = [&](int j, uint32_t n) {
+      const uint32_t a = k_low + ring_stage(n, kStages) * (S::kTileBytes / 16);
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          mma_shared(tmem + N * (j & 1), a + ((k / 4) * kBlockBytes + (k % 4) * 32) / 16,
+                     q_low + ((k / 4) * N * 128 + (k % 4) * 32) / 16, kScores, k > 0);
+        mma_commit(shared_address(&sh.s_full[j & 1]));
+      }
+    };
+    const auto values = [&](uint32_t n, bool add) {
+      const uint32_t a = v_low + ring_stage(n, kStages) * (S::kTileBytes / 16);
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < kKeyTile / 16; ++k)
+          mma_shared<kSwizzledHigh, plain_high(2048)>(tmem + kOut, a + k * (2048 / 16), w_low + k * (256 / 16), kValues,
+                                                      add || k > 0);
+        mma_commit(shared_address(&sh.o_full));
+      }
+    };
+    for (uint32_t number = 0;; ++number) {
+      const uint32_t slot = number % kItems;
+      if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
+      const int seq = __shfl_sync(0xFFFFFFFFu, sh.items[slot].seq, 0), n = __shfl_sync(0xFFFFFFFFu, sh.items[slot].n0, 0);
+      __syncwarp();
+      if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
+      if (seq < 0) break;
+      if (n == 0) continue;
+      bool ok = warp_wait(sh.q_full, q_uses++ & 1, gave_up);
+      ok = ok && full(used);
+      if (!ok) break;
+      scores(0, used);
+      release(used);
+      for (int j = 0; ok && j < n; ++j) {
+        if (j + 1 < n) {
+          const uint32_t at = used + key_place(false, j + 1);
+          ok = full(at);
+          if (!ok) break;
+          scores(j + 1, at);
+          release(at);
+        } else if (elect_one()) {
+          mma_commit(shared_address(&sh.q_empty));
+        }
+        const uint32_t at = used + value_place(false, j, n);
+        ok = full(at) && warp_wait(sh.p_full, p_uses++ & 1, gave_up);
+        if (!ok) break;
+        tmem_fence_after();
+        values(at, j > 0);
+        release(at);
+      }
+      if (!ok) break;
+      used += 2 * n;
+    }
+    if (*gave_up && lane == 0) {  // products in flight have to end before tensor memory is freed
+      mma_commit(shared_address(&sh.drain));
+      barrier_drain(shared_address(&sh.drain), 0);
+    }
+    __syncwarp();
+  } else {
+    // ---- softmax: a thread per key; at the end a thread per channel ----
+    const int me = threadIdx.x;  // 0 .. 127
+    const uint32_t lanes = (uint32_t)warp << 21;
+    const float scale = p.scale_log2;
+    uint32_t used = 0, s_uses[2] = {0, 0}, pv = 0, syncs = 0, tiles_done = 0;
+    const auto sync = [&] {  // the four warps
+      __syncwarp();
+      if (lane == 0) barrier_arrive(shared_address(&sh.group));
+      return warp_wait(sh.group, syncs++ & 1, gave_up);
+    };
+    for (uint32_t number = 0;; ++number) {
+      const uint32_t slot = number % kItems;
+      if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
+      const Item im = uniform(sh.items[slot]);
+      __syncwarp();
+      if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
+      if (im.seq < 0) break;
+      const int n = im.n0, rows = im.rows;
+      const int hidden_from = max(im.behind + 1, 0);  // first key hidden from a row of the item
+      float ref[N], l[N];
+#pragma unroll
+      for (int r = 0; r < N; ++r) ref[r] = -INFINITY, l[r] = 0.f;
+      bool ok = true;
+      for (int j = 0; j < n; ++j) {
+        const int key0 = im.kbegin + j * kKeyTile, key = key0 + me, buffer = j & 1;
+        const bool masked = key0 + kKeyTile - 1 > im.behind;
+        ok = warp_wait(sh.s_full[buffer], s_uses[buffer]++ & 1, gave_up);
+        if (!ok) break;
+        tmem_fence_after();
+        uint32_t x[N];
+        tmem_load(x, tmem + lanes + N * buffer);
+        tmem_wait_load();
+        tmem_ready(x);
+        float s[N];
+#pragma unroll
+        for (int r = 0; r < N; ++r) s[r] = __uint_as_float(x[r]) * scale;
+        if (masked) {
+          int newest = im.behind, head = 0;  // of row r's token
+#pragma unroll
+          for (int r = 0; r < N; ++r) {
+            if (key > newest) s[r] = -INFINITY;  // whatever was there
+            if (++head == p.group) head = 0, ++newest;
+          }
+        }
+        // does a score exceed its reference by too much? (tile 0: there is none yet)
+        bool renew = j == 0;
+        ++tiles_done;
+        if (j > 0) {
+          bool over = false;
+#pragma unroll
+          for (int r = 0; r < N; ++r)
+            if (r < rows) over = over || s[r] - ref[r] > kFewLimit;
+          if (__any_sync(0xFFFFFFFFu, over) && lane == 0) *(volatile uint32_t*)&sh.exceeds[tiles_done & 1] = tiles_done;
+          ok = sync();
+          if (!ok) break;
+          renew = *(volatile uint32_t*)&sh.exceeds[tiles_done & 1] == tiles_done;
+        }
+        if (renew) {
+#pragma unroll
+          for (int r = 0; r < N; ++r) {
+            if (r < rows) {
+              float top = s[r];
+#pragma unroll
+              for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, off));
+              if (lane == 0) sh.rows[warp][r] = top;
+            }
+          }
+          ok = sync();
+          if (!ok) break;
+          float shrink[N];
+#pragma unroll
+          for (int r = 0; r < N; ++r) {
+            shrink[r] = 0.f;
+            if (r < rows) {
+              const float top = fmaxf(fmaxf(sh.rows[0][r], sh.rows[1][r]), fmaxf(sh.rows[2][r], sh.rows[3][r]));
+              const float now = fmaxf(ref[r], top);
+              shrink[r] = now == -INFINITY ? 0.f : exp2_approx(ref[r] - now);
+              ref[r] = now == -INFINITY ? 0.f : now;
+              l[r] *= shrink[r];
+            }
+          }
+          ok = sync();  // the maxima have been read
+          if (!ok) break;
+          if (j > 0) {
+            ok = warp_wait(sh.o_full, (pv - 1) & 1, gave_up);
+            if (!ok) break;
+            tmem_fence_after();
+            tmem_load(x, tmem + lanes + kOut);
+            tmem_wait_load();
+            tmem_ready(x);
+#pragma unroll
+            for (int r = 0; r < N; ++r) x[r] = __float_as_uint(__uint_as_float(x[r]) * shrink[r]);
+            tmem_store(tmem + lanes + kOut, x);
+            tmem_wait_store();
+          }
+        }
+        uint32_t packed[N / 2];
+#pragma unroll
+        for (int r = 0; r < N; r += 2) {
+          float a = 0.f, b = 0.f;
+          if (r < rows) a = exp2_approx(s[r] - ref[r]);
+          if (r + 1 < rows) b = exp2_approx(s[r + 1] - ref[r + 1]);
+          l[r] += a;
+          l[r + 1] += b;
+          packed[r / 2] = pack_bf16(a, b);
+        }
+        if (j > 0) {  // the weights of the tile before have been used
+          ok = warp_wait(sh.o_full, (pv - 1) & 1, gave_up);
+          if (!ok) break;
+        }
+        // 8 rows of a key are 16 bytes, keys side by side
+#pragma unroll
+        for (int c = 0; c < N / 8; ++c)
+          *reinterpret_cast<uint4*>(weights + c * 2048 + me * 16) =
+              make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
+        if (masked) {
+          const uint32_t place = used + value_place(false, j, n), stage = ring_stage(place, kStages);
+          ok = warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up);
+          if (!ok) break;
+          clean_values<kHalves>(ring + stage * S::kTileBytes, max(hidden_from - key0, 0), im.kend - key0,
+                                &sh.bad_values[number & 1], (int)number);
+        }
+        fence_async_shared();
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) barrier_arrive(shared_address(&sh.p_full));
+        ++pv;
+      }
+      if (!ok) break;
+      used += 2 * n;
+
+      // ---- the rows' results ----
+#pragma unroll
+      for (int r = 0; r < N; ++r) {
+        if (r < rows) {
+#pragma unroll
+          for (int off = 16; off > 0; off >>= 1) l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], off);
+          if (lane == 0) sh.rows[warp][r] = l[r];
+        }
+      }
+      ok = sync();
+      if (ok && n > 0) ok = warp_wait(sh.o_full, (pv - 1) & 1, gave_up);
+      if (!ok) break;
+      tmem_fence_after();
+      uint32_t x[N];
+      if (n > 0) {
+        tmem_load(x, tmem + lanes + kOut);
+        tmem_wait_load();
+        tmem_ready(x);
+      }
+      const bool repair = *(volatile int*)&sh.bad_values[number & 1] == (int)number;
+      int token = 0, head = 0;
+#pragma unroll
+      for (int r = 0; r < N; ++r) {
+        if (r < rows) {
+          const float total = sh.rows[0][r] + sh.rows[1][r] + sh.rows[2][r] + sh.rows[3][r];
+          const bool any_keys = total != 0.f;
+          float o = any_keys ? __uint_as_float(x[r]) : 0.f;
+          if (repair && me < D) {  // values that were taken out of tiles with hidden keys: back to the rows that see them
+            for (int key = max(im.kbegin, hidden_from); key <= min(im.behind + token, im.kend - 1); ++key) {
+              const __nv_bfloat16* v = value_of(p, im, key);
+              const float f = v == nullptr ? 0.f : __bfloat162float(v[me]);
+              if (!(fabsf(f) < INFINITY)) o += f;
+            }
+          }
+          o *= any_keys ? 1.f / total : 0.f;
+          const float lse2 = any_keys ? ref[r] + log2f(total) : -INFINITY;
+          if (im.slot >= 0) {
+            const long long part = ((long long)blockIdx.x * 2 + im.slot) * tp.item_rows + r;
+            if (me < D) p.part_out[part * D + me] = o;
+            if (me == r) p.part_lse[part] = lse2;
+          } else {
+            const int q_head = im.head * p.group + head;
+            if (me < D)
+              static_cast<__nv_bfloat16*>(p.out)[(im.first + token) * p.out_token + q_head * p.out_head + me] =
+                  __float2bfloat16_rn(o);
+            if (me == r && p.lse) p.lse[(long long)(im.first + token) * p.q_heads + q_head] = lse2 * kLn2;
+          }
+        }
+        if (++head == p.group) head = 0, ++token;
+      }
+      tmem_fence_before();
+      if (!sync()) break;  // all have read: the next item may overwrite
+    }
+  }
+  __syncthreads();
+  if (sh.gave_up && p.status && threadIdx.x == 0) {
+    for (int i = blockIdx.x; i < p.num_seqs; i += gridDim.x) p.status[i] = TOPLOC_SEQ_WAIT_EXPIRED;
+  }
+  if (warp == 5) tmem_free(tmem, kColumns);
+}
+
+template <int D, int N>
+int launch(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int blocks,
+           cudaStream_t stream) {
+  constexpr int kBytes = FewShared<D, N>::kBytes;
+  if (cudaFuncSetAttribute(toploc_attention_few_kernel<D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) !=
+      cudaSuccess)
+    return TOPLOC_ERR_CUDA;
+  toploc_attention_few_kernel<D, N><<<blocks, kFewThreads, kBytes, stream>>>(tp, q, k, v);
+  return launched();
+}
+
+}  // namespace
+
+namespace toploc_model {
+
+int launch_few_rows(const void* params, const void* map_q, const void* map_k, const void* map_v, int blocks,
+                    cudaStream_t stream) {
+  const TcParams& tp = *static_cast<const TcParams*>(params);
+  const CUtensorMap& q = *static_cast<const CUtensorMap*>(map_q);
+  const CUtensorMap& k = *static_cast<const CUtensorMap*>(map_k);
+  const CUtensorMap& v = *static_cast<const CUtensorMap*>(map_v);
+  const bool sixteen = tp.item_rows <= 16;
+  if (tp.p.head_dim == 128)
+    return sixteen ? launch<128, 16>(tp, q, k, v, blocks, stream) : launch<128, 32>(tp, q, k, v, blocks, stream);
+  return sixteen ? launch<64, 16>(tp, q, k, v, blocks, stream) : launch<64, 32>(tp, q, k, v, blocks, stream);
+}
+
+}  // namespace toploc_model

@@ -23,42 +23,15 @@
 //
 // The output is not rescaled whenever the maximum grows but only where it grew by more than 2^8: P then stays
 // below 2^8, and O, the sum and P share the same reference, so the quotient is the same.
-#include "attention_common.cuh"
-#include "sm100.cuh"
+#include "attention_tc.cuh"
 
 namespace {
 
-using namespace toploc_model;
-using namespace sm100;
-
 constexpr int kTcThreads = 384;            // two groups of softmax, and one whose first two warps feed and issue
-constexpr int kItems = 4;                  // items announced ahead
 // Registers move from the third group of warps to the softmax, whose threads hold a row of 128 scores.  The block is
 // launched with 168 a thread (65536 / 384, in steps of 8); 2 * 216 + 72 = 3 * 168.
 constexpr int kSoftmaxRegisters = 216, kOtherRegisters = 72;
 constexpr float kLazyLog2 = 8.0f;
-constexpr int kBlockBytes = 128 * 128;     // 128 rows of 64 elements
-
-// One piece of work: two tiles of rows (or the one that is left) of a sequence and key head against a range of keys.
-struct Item {
-  int seq;     // -1: no more work
-  int head;    // key head
-  int slot;    // where the result goes: -1 the output, 0 a part whose row tile began in an earlier block, 1 in this one
-  int first;   // row of the packed tensors its sequence starts at
-  int behind;  // keys in front of the sequence's first new token (may be negative)
-  int row0;    // first packed row (token * group + head in group)
-  int rows;    // packed rows of the sequence
-  int kbegin;  // keys kbegin .. kend - 1, kbegin a multiple of the tile
-  int kend;
-  int two;     // two row tiles
-  int n0, n1;  // key tiles of the two groups, or n0 in all
-};
-
-// The parts a block leaves, for the join.
-struct Part {
-  int seq, head, row0, first, rows;  // seq -1: none
-  int last;                          // slot 0: the row tile's keys end here
-};
 
 template <int D>
 struct Shared {
@@ -81,12 +54,6 @@ struct Shared {
   static constexpr int kBytes = kHeadBytes + kExchangeBytes + (2 + kStages) * kTileBytes;
   static_assert(kBytes <= 232448, "shared memory of a block");
 };
-
-__device__ __forceinline__ float exp2_approx(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 __device__ __forceinline__ void store_32_bytes(void* at, const uint32_t* v) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]),
@@ -119,209 +86,6 @@ __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
-}
-
-__device__ __forceinline__ uint32_t ring_stage(uint32_t n, int stages) { return n % (uint32_t)stages; }
-__device__ __forceinline__ uint32_t ring_parity(uint32_t n, int stages) { return (n / (uint32_t)stages) & 1u; }
-
-// A wait of a whole warp: all lanes or none go on.
-__device__ __forceinline__ bool warp_wait(const uint64_t& bar, uint32_t parity, volatile int* gave_up) {
-  return __all_sync(0xFFFFFFFFu, barrier_wait(shared_address(&bar), parity, gave_up));
-}
-
-struct TcParams {
-  AttentionParams p;
-  int tile_rows;  // packed rows of a row tile: 128 rounded down to whole tokens
-  int box_rows;   // rows of a key copy
-  int q_bytes;    // bytes of a query tile's copy
-  bool wide_out;  // rows of the output at multiples of 32 bytes
-  Part* parts;    // [blocks][2]
-};
-
-// Tiles of the ring an item takes, and the places of key and value tile j among them.
-__device__ __forceinline__ int item_tiles(const Item& im) { return im.two ? max(im.n0, im.n1) : im.n0; }
-__device__ __forceinline__ int key_place(bool two, int j) { return two ? 2 * j : max(2 * j - 1, 0); }
-__device__ __forceinline__ int value_place(bool two, int j, int n) {
-  return two ? 2 * j + 1 : min(n, j + 2) + j;  // K0 V0 K1 V1 .. or K0 K1 V0 K2 V1 ..
-}
-
-// ---- the line of work ----------------------------------------------------------------------------
-//
-// A sequence of T rows and c keys in front of them has L levels of rows_item rows per key head; a level stands for
-// kLevelCost (what an item costs beside its keys, in keys) + c + the tokens up to its end.  Sequences follow one
-// another, in them key heads, in them levels.
-
-constexpr long long kLevelCost = 192;
-constexpr long long kLeastShare = 6 * kKeyTile;  // less is not worth a block of its own
-
-struct Line {
-  long long front;  // kLevelCost + keys in front
-  int rows_item, tokens_item, tokens, levels;
-  __device__ Line(const TcParams& tp, const SeqRange& s)
-      : front(kLevelCost + max(s.keys - s.rows, 0)), rows_item(2 * tp.tile_rows), tokens_item(rows_item / tp.p.group),
-        tokens(s.rows), levels((s.rows + tokens_item - 1) / tokens_item) {}
-  __device__ long long upto(int level) const {  // of levels 0 .. level - 1
-    const long long whole = level * front + (long long)tokens_item * level * (level + 1) / 2;
-    return level < levels ? whole : whole - ((long long)levels * tokens_item - tokens);
-  }
-};
-
-// A place on the line: a key tile of a level.
-struct Place {
-  int seq, head, level, tile;
-};
-
-__device__ __forceinline__ bool before(const Place& a, const Place& b) {
-  if (a.seq != b.seq) return a.seq < b.seq;
-  if (a.head != b.head) return a.head < b.head;
-  if (a.level != b.level) return a.level < b.level;
-  return a.tile < b.tile;
-}
-
-// Key tiles that a level's rows see in all.
-__device__ __forceinline__ int tiles_seen(const SeqRange& s, int tokens_upto) {
-  const int seen = min(s.keys, s.keys - s.rows + tokens_upto);
-  return seen > 0 ? (seen + kKeyTile - 1) / kKeyTile : 0;
-}
-
-// One warp's copies into the ring: the keys, or the values, of item after item.
-template <int D>
-struct Feeder {
-  using S = Shared<D>;
-  static constexpr int kStages = S::kStages;
-  const TcParams& tp;
-  const CUtensorMap* map;
-  typename S::Head& sh;
-  uint32_t ring, base = 0;             // places in front of the item
-  uint32_t fed = 0, fed_parity = 0;    // by stage: this warp's last copy there
-  volatile int* gave_up;
-  Item im;
-  int tiles = 0, page = 0, next = 0, lane = threadIdx.x & 31;
-  bool fine = true;
-
-  __device__ Feeder(const TcParams& tp, const CUtensorMap* map, typename S::Head& sh, void* ring, volatile int* gave_up)
-      : tp(tp), map(map), sh(sh), ring(shared_address(ring)), gave_up(gave_up) {}
-
-  // The page of this lane's copy of tile j, as the table has it (looked up ahead of its use).
-  __device__ int page_of(int j) const {
-    const int key = im.kbegin + j * kKeyTile + lane * tp.box_rows;
-    const bool copied = tp.p.kv_lens && j < tiles && lane * tp.box_rows < kKeyTile && key < im.kend;
-    return copied ? tp.p.table[im.seq * tp.p.table_stride + key / tp.p.page_size] : 0;
-  }
-
-  __device__ void item(const Item& next_item, int n) {
-    base += 2 * tiles;
-    im = next_item;
-    tiles = n;
-    page = page_of(0);
-    next = page_of(1);
-  }
-
-  __device__ void feed(int j, int at) {
-    const uint32_t place = base + at, stage = ring_stage(place, kStages);
-    const uint32_t bar = shared_address(&sh.full[stage]), dst = ring + stage * S::kTileBytes;
-    const int after = page_of(j + 2);
-    fine = warp_wait(sh.empty[stage], ring_parity(place, kStages) ^ 1, gave_up);
-    if (!fine) return;
-    fed |= 1u << stage;
-    fed_parity = (fed_parity & ~(1u << stage)) | ring_parity(place, kStages) << stage;
-    const int key0 = im.kbegin + j * kKeyTile;
-    if (tp.p.kv_lens) {
-      if (page < 0 || page >= tp.p.num_pages) {
-        if (tp.p.status) tp.p.status[im.seq] = TOPLOC_SEQ_BAD_PAGE;
-        page = tp.p.num_pages;  // past the end: the copy fills zeros
-      }
-      const int copies = (min(kKeyTile, im.kend - key0) + tp.box_rows - 1) / tp.box_rows;
-      const int in_page = tp.box_rows < kKeyTile ? 0 : key0 % tp.p.page_size;
-      if (elect_one()) barrier_arrive_expect(bar, copies * S::kHalves * tp.box_rows * 128);
-      __syncwarp();
-      for (int c = 0; c < copies; ++c) {
-        const int which = __shfl_sync(0xFFFFFFFFu, page, c);
-        if (elect_one()) {
-#pragma unroll
-          for (int h = 0; h < S::kHalves; ++h)
-            copy_4d(dst + h * kBlockBytes + c * tp.box_rows * 128, map, bar, h * 64, in_page, im.head, which);
-        }
-      }
-    } else if (elect_one()) {
-      barrier_arrive_expect(bar, S::kTileBytes);
-#pragma unroll
-      for (int h = 0; h < S::kHalves; ++h)
-        copy_4d(dst + h * kBlockBytes, map, bar, h * 64, im.first + key0, im.head, 0);
-    }
-    __syncwarp();
-    page = next;
-    next = after;
-  }
-
-  // After a wait gave up: no copy of this warp is in flight when it returns.
-  __device__ void drain() const {
-    for (int i = 0; i < kStages; ++i)
-      if (fed >> i & 1) barrier_drain(shared_address(&sh.full[i]), fed_parity >> i & 1);
-  }
-};
-
-__device__ __forceinline__ Item uniform(const Item& im) {  // the same for every lane, and known to be
-  Item r;
-  r.seq = __shfl_sync(0xFFFFFFFFu, im.seq, 0);
-  r.head = __shfl_sync(0xFFFFFFFFu, im.head, 0);
-  r.slot = __shfl_sync(0xFFFFFFFFu, im.slot, 0);
-  r.first = __shfl_sync(0xFFFFFFFFu, im.first, 0);
-  r.behind = __shfl_sync(0xFFFFFFFFu, im.behind, 0);
-  r.row0 = __shfl_sync(0xFFFFFFFFu, im.row0, 0);
-  r.rows = __shfl_sync(0xFFFFFFFFu, im.rows, 0);
-  r.kbegin = __shfl_sync(0xFFFFFFFFu, im.kbegin, 0);
-  r.kend = __shfl_sync(0xFFFFFFFFu, im.kend, 0);
-  r.two = __shfl_sync(0xFFFFFFFFu, im.two, 0);
-  r.n0 = __shfl_sync(0xFFFFFFFFu, im.n0, 0);
-  r.n1 = __shfl_sync(0xFFFFFFFFu, im.n1, 0);
-  return r;
-}
-
-constexpr int kRuns = kTcThreads;
-
-// Where position `at` of the line falls; a cut in front of a level's second tile or behind its last but one moves to the
-// level's ends.
-__device__ __forceinline__ Place find_place(const TcParams& tp, const long long* run_cost, int per, long long at) {
-  const AttentionParams& p = tp.p;
-  if (at >= run_cost[kRuns]) return Place{p.num_seqs, 0, 0, 0};
-  int lo = 0, hi = kRuns;  // run_cost[lo] <= at < run_cost[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (run_cost[mid] <= at) lo = mid; else hi = mid;
-  }
-  at -= run_cost[lo];
-  for (int i = lo * per; i < p.num_seqs; ++i) {
-    const SeqRange s = sequence(p, i);
-    const Line line(tp, s);
-    const long long one = line.upto(line.levels), all = one * p.kv_heads;
-    if (at >= all) {
-      at -= all;
-      continue;
-    }
-    Place place = {i, (int)(at / one), 0, 0};
-    at -= place.head * one;
-    int a = 0, b = line.levels;  // upto(a) <= at < upto(b)
-    while (b - a > 1) {
-      const int mid = (a + b) >> 1;
-      if (line.upto(mid) <= at) a = mid; else b = mid;
-    }
-    place.level = a;
-    at -= line.upto(a);
-    const int n = tiles_seen(s, min((a + 1) * line.tokens_item, line.tokens));
-    const long long tile = (at - kLevelCost + kKeyTile / 2) / kKeyTile;
-    if (at <= kLevelCost || tile <= 1) return place;
-    if (tile >= n - 1) {
-      if (++place.level == line.levels) {
-        place.level = 0;
-        if (++place.head == p.kv_heads) return Place{i + 1, 0, 0, 0};
-      }
-      return place;
-    }
-    place.tile = (int)tile;
-    return place;
-  }
-  return Place{p.num_seqs, 0, 0, 0};
 }
 
 template <int D>
@@ -365,32 +129,8 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
     barrier_init_fence();
   }
   if (warp == 9) tmem_alloc(shared_address(&sh.tmem), 512);
-  // the line: a run of sequences per thread, and the work in front of every run (kept where the ring comes later)
-  long long* run_cost = reinterpret_cast<long long*>(ring);
-  long long* warp_cost = run_cost + kRuns + 1;
-  const int per = (p.num_seqs + kRuns - 1) / kRuns;
-  {
-    long long cost = 0;
-    for (int i = threadIdx.x * per; i < min(((int)threadIdx.x + 1) * per, p.num_seqs); ++i) {
-      const SeqRange s = sequence(p, i);
-      if (s.bad && p.status && blockIdx.x == 0) p.status[i] = TOPLOC_SEQ_BAD_LENGTH;
-      const Line line(tp, s);
-      cost += line.upto(line.levels) * p.kv_heads;
-    }
-    long long incl = cost;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const long long up = __shfl_up_sync(0xFFFFFFFFu, incl, off);
-      if (lane >= off) incl += up;
-    }
-    if (lane == 31) warp_cost[warp] = incl;
-    __syncthreads();
-    long long in_front = incl - cost;
-    for (int w = 0; w < warp; ++w) in_front += warp_cost[w];
-    run_cost[threadIdx.x] = in_front;
-    if (threadIdx.x == kRuns - 1) run_cost[kRuns] = in_front + cost;
-    fence_async_shared();  // tensor copies write there next
-  }
+  long long* run_cost = reinterpret_cast<long long*>(ring);  // where the ring's first tile comes later
+  lay_line<kTcThreads>(tp, run_cost);
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
@@ -405,64 +145,15 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       prefetch_map(&map_k);
       prefetch_map(&map_v);
     }
-    const int rows_item = 2 * tp.tile_rows, tokens_item = rows_item / p.group;
-    const long long all = run_cost[kRuns];
-    const long long share = max((all + gridDim.x - 1) / gridDim.x, kLeastShare);
-    Place at = find_place(tp, run_cost, per, share * blockIdx.x);
-    const Place end = find_place(tp, run_cost, per, share * (blockIdx.x + 1));
+    Walk walk(tp, find_place<kTcThreads>(tp, run_cost, blockIdx.x), find_place<kTcThreads>(tp, run_cost, blockIdx.x + 1));
     __syncwarp();  // run_cost has been read: the ring's place is free
-    SeqRange s = {0, 0, 0, false};
-    int s_of = -1;
     uint32_t q_uses = 0;
-    Feeder<D> keys(tp, &map_k, sh, ring, gave_up);
-    if (lane < 2) tp.parts[2 * blockIdx.x + lane].seq = -1;
-    __syncwarp();
+    Feeder<S> keys(tp, &map_k, sh, ring, gave_up);
     for (uint32_t number = 0;; ++number) {
-      while (before(at, end)) {  // the sequence of the next item, past those without rows
-        if (s_of != at.seq) {
-          s = sequence(p, at.seq);
-          s_of = at.seq;
-        }
-        if (s.rows > 0) break;
-        at = Place{at.seq + 1, 0, 0, 0};
-      }
-      const bool more = before(at, end);
       const uint32_t slot = number % kItems;
       if (!warp_wait(sh.item_empty[slot], ((number / kItems) & 1) ^ 1, gave_up)) break;
-      Item im = {};
-      im.seq = -1;
-      if (more) {
-        im.seq = at.seq;
-        im.head = at.head;
-        im.first = s.first;
-        im.behind = s.keys - s.rows;
-        im.row0 = at.level * rows_item;
-        im.rows = s.rows * p.group;
-        const int tokens = min((at.level + 1) * tokens_item, s.rows);
-        const int all_tiles = tiles_seen(s, tokens);
-        const bool ends_here = end.seq == at.seq && end.head == at.head && end.level == at.level;
-        const int tile_end = ends_here ? end.tile : all_tiles;
-        im.kbegin = at.tile * kKeyTile;
-        im.kend = min(min(s.keys, im.behind + tokens), tile_end * kKeyTile);
-        im.two = im.row0 + tp.tile_rows < im.rows;
-        if (im.two) {
-          const int first = tiles_seen(s, at.level * tokens_item + tokens_item / 2);
-          im.n0 = max(min(first, tile_end) - at.tile, 0);
-          im.n1 = max(tile_end - at.tile, 0);
-        } else {
-          im.n0 = max(tile_end - at.tile, 0);
-        }
-        im.slot = at.tile > 0 ? 0 : ends_here ? 1 : -1;
-        if (im.slot >= 0 && lane == 0)
-          tp.parts[2 * blockIdx.x + im.slot] = Part{im.seq, im.head, im.row0, im.first, im.rows, ends_here ? 0 : 1};
-        at.tile = 0;  // the next item
-        if (ends_here) {
-          at = end;
-        } else if (rows_item * (++at.level) >= im.rows) {
-          at.level = 0;
-          if (++at.head == p.kv_heads) at = Place{at.seq + 1, 0, 0, 0};
-        }
-      }
+      Item im;
+      const bool more = walk.next(im);
       im = uniform(im);
       if (lane == 0) {
         sh.items[slot] = im;
@@ -499,7 +190,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
   } else if (warp == 10) {
     lower_registers<kOtherRegisters>();
     // ---- feeding: values ----
-    Feeder<D> values(tp, &map_v, sh, ring, gave_up);
+    Feeder<S> values(tp, &map_v, sh, ring, gave_up);
     for (uint32_t number = 0;; ++number) {
       const uint32_t slot = number % kItems;
       if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
@@ -516,7 +207,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
   } else if (warp == 9) {
     lower_registers<kOtherRegisters>();
     // ---- products: the whole warp follows, one lane issues ----
-    constexpr uint32_t kScores = bf16_product(128, false), kValues = bf16_product(D, true);
+    constexpr uint32_t kScores = bf16_product(128, false, false), kValues = bf16_product(D, false, true);
     const uint32_t q_low = operand_low(shared_address(q_tiles), 16);
     const uint32_t k_low = operand_low(shared_address(ring), 16), v_low = operand_low(shared_address(ring), kBlockBytes);
     uint32_t used = 0, q_uses = 0, p_uses[2] = {0, 0};
@@ -666,40 +357,11 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       const int hidden_from = max(im.behind + im.row0 / p.group + 1, 0);     // first key hidden from a row of the item
       const bool live = __any_sync(0xFFFFFFFFu, valid);                      // else nobody reads the warp's rows
       const int tiles = two ? (w ? im.n1 : im.n0) : (n + 1 - w) / 2;
-      // Before the products of a tile with hidden keys:
-      const auto clean_values = [&](int j, int key0) {
-        // Values of hidden keys meet weights of zero, and 0 * NaN is NaN: rows past the item's keys (never
-        // loaded, or another sequence's) become zero; a value in front of them that is not finite too, and
-        // the rows that do see it get it back at the end.
+      const auto clean = [&](int j, int key0) {
         const uint32_t place = used + value_place(two, j, n), stage = ring_stage(place, kStages);
         if (!warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up)) return false;
-        const int from = max(hidden_from - key0, 0);
-        unsigned char* tile = ring + stage * S::kTileBytes;
-        for (int e = r; e < (kKeyTile - from) * 8; e += 128) {
-          const int j_row = from + (e >> 3);
-          const bool past = key0 + j_row >= im.kend;
-#pragma unroll
-          for (int h = 0; h < kHalves; ++h) {
-            uint4* at = reinterpret_cast<uint4*>(tile + h * kBlockBytes + j_row * 128 + (e & 7) * 16);
-            uint4 v = make_uint4(0, 0, 0, 0);
-            bool write = past;
-            if (!past) {
-              v = *at;
-              uint32_t* x = &v.x;
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                if ((x[q] & 0x7F80u) == 0x7F80u) x[q] &= 0xFFFF0000u, write = true;
-                if ((x[q] & 0x7F800000u) == 0x7F800000u) x[q] &= 0xFFFFu, write = true;
-              }
-              if (write) {
-                *(volatile int*)&sh.bad_values[number & 1] = (int)number;
-                __threadfence_block();
-              }
-            }
-            if (write) *at = v;
-          }
-        }
-        fence_async_shared();
+        clean_values<kHalves>(ring + stage * S::kTileBytes, max(hidden_from - key0, 0), im.kend - key0,
+                              &sh.bad_values[number & 1], (int)number);
         return true;
       };
       float m = -INFINITY, l = 0.f;
@@ -797,7 +459,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
         } else if (!masked && lane == 0) {
           barrier_arrive(shared_address(&sh.p_most[w]));
         }
-        if (masked && !clean_values(j, key0)) {
+        if (masked && !clean(j, key0)) {
           ok = false;
           break;
         }
@@ -833,7 +495,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       const int head = im.head * p.group + row - token * p.group;
       const long long at = (long long)(im.first + token) * p.q_heads + head;
       // where the row's part of a split tile goes
-      const long long part = ((long long)blockIdx.x * 2 + im.slot) * (2 * tp.tile_rows) + (row - im.row0);
+      const long long part = ((long long)blockIdx.x * 2 + im.slot) * tp.item_rows + (row - im.row0);
       // two row tiles: a group writes its rows; one: each group writes half of the channels
       const int width = two ? D : D / 2, c0 = two ? 0 : w * width;
       const bool mine = (two ? tiles : n) > 0, others = !two && n > 1;
@@ -870,17 +532,11 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
         if (repair) {  // values that were taken out of tiles with hidden keys: back to the rows that see them
           const int begin = max(im.kbegin, hidden_from);
           for (int key = begin; key <= min(newest, im.kend - 1); ++key) {
-            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + (long long)im.head * p.v_head + c;
-            if (p.kv_lens) {
-              const int col = key / p.page_size, page = p.table[im.seq * p.table_stride + col];
-              if (page < 0 || page >= p.num_pages) continue;
-              v += page * p.v_page + (long long)(key - col * p.page_size) * p.v_token;
-            } else {
-              v += (long long)(im.first + key) * p.v_token;
-            }
+            const __nv_bfloat16* v = value_of(p, im, key);
+            if (v == nullptr) continue;
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-              const float f = __bfloat162float(v[e]);
+              const float f = __bfloat162float(v[c + e]);
               if (!(fabsf(f) < INFINITY)) o[e] += f;
             }
           }
@@ -939,7 +595,7 @@ template <int D>
 __global__ void __launch_bounds__(128) toploc_attention_tc_join_kernel(const TcParams tp) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const AttentionParams& p = tp.p;
-  const int b = blockIdx.x, lane = threadIdx.x & 31, rows_item = 2 * tp.tile_rows;
+  const int b = blockIdx.x, lane = threadIdx.x & 31, rows_item = tp.item_rows;
   const Part part = tp.parts[2 * b + 1];
   if (part.seq < 0) return;
   int end = b + 1;  // the last block with a part
@@ -1022,17 +678,10 @@ bool make_map(CUtensorMap* map, const void* at, int rank, const int64_t* extent,
 }
 
 template <int D>
-int launch(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int blocks,
-           cudaStream_t stream) {
-  constexpr int kBytes = Shared<D>::kBytes;
-  if (cudaFuncSetAttribute(toploc_attention_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) !=
-      cudaSuccess)
-    return TOPLOC_ERR_CUDA;
-  toploc_attention_tc_kernel<D><<<blocks, kTcThreads, kBytes, stream>>>(tp, q, k, v);
-  if (const int rc = launched()) return rc;
+int launch_join(const TcParams& tp, int blocks, cudaStream_t stream) {
   if (blocks == 1) return TOPLOC_OK;
   cudaLaunchConfig_t config = {};
-  config.gridDim = dim3((unsigned)blocks, (unsigned)((2 * tp.tile_rows + kJoinRows - 1) / kJoinRows));
+  config.gridDim = dim3((unsigned)blocks, (unsigned)((tp.item_rows + kJoinRows - 1) / kJoinRows));
   config.blockDim = dim3(128);
   config.stream = stream;
   cudaLaunchAttribute early;
@@ -1041,6 +690,17 @@ int launch(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const
   config.attrs = &early;
   config.numAttrs = 1;
   return cudaLaunchKernelEx(&config, toploc_attention_tc_join_kernel<D>, tp) == cudaSuccess ? TOPLOC_OK : TOPLOC_ERR_CUDA;
+}
+
+template <int D>
+int launch(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int blocks,
+           cudaStream_t stream) {
+  constexpr int kBytes = Shared<D>::kBytes;
+  if (cudaFuncSetAttribute(toploc_attention_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) !=
+      cudaSuccess)
+    return TOPLOC_ERR_CUDA;
+  toploc_attention_tc_kernel<D><<<blocks, kTcThreads, kBytes, stream>>>(tp, q, k, v);
+  return launched();
 }
 
 }  // namespace
@@ -1064,26 +724,30 @@ bool tensor_cores_take(const toploc_attention_layout* lay, const toploc_kv_layou
          (page == 0 || (step(kv->k_page_stride, kv->num_pages) && step(kv->v_page_stride, kv->num_pages)));
 }
 
-// Parts (outputs, lse, who they belong to) of two row tiles a block.
+// Parts (outputs, lse, who they belong to) of two row tiles a block; the kernel for few rows has twice the blocks and at
+// most kFewRows rows of an item.
 size_t tensor_core_workspace_bytes(const toploc_attention_layout* lay) {
   const int group = lay->q_heads / lay->kv_heads;
-  return (size_t)2 * kSms * (2 * (128 / group * group) * (size_t)(lay->head_dim + 1) * 4 + sizeof(Part));
+  return (size_t)2 * kSms * (2 * (128 / group * group) * (size_t)(lay->head_dim + 1) * 4 + 2 * sizeof(Part));
 }
 
 int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, const toploc_kv_layout* kv, void* workspace,
                         cudaStream_t stream) {
   if (encode_tiled() == nullptr) return TOPLOC_ERR_CUDA;
   const int page = kv->page_size;
-  const int tokens = min(128 / p.group, p.max_new);  // of a query copy
   int sms = 0;
   if (const int rc = check_device(&sms)) return rc;
-  const int blocks = min(sms, kSms);
+  sms = min(sms, kSms);
+  const bool few = (long long)p.max_new * p.group <= kFewRows;
+  const int blocks = few ? 2 * sms : sms, tokens = min(128 / p.group, p.max_new);  // tokens of a query copy
   TcParams tp;
-  tp.tile_rows = 128 / p.group * p.group;
+  tp.tile_rows = few ? p.max_new * p.group : 128 / p.group * p.group;
+  tp.item_rows = few ? tp.tile_rows : 2 * tp.tile_rows;
+  tp.least_share = few ? 3 * kKeyTile : 6 * kKeyTile;
   tp.box_rows = page > 0 ? min(page, kKeyTile) : kKeyTile;
   tp.q_bytes = p.head_dim * 2 * p.group * tokens;
   tp.wide_out = aligned(p.out, 32) && p.out_token % 16 == 0 && p.out_head % 16 == 0;
-  const long long part_rows = (long long)2 * blocks * 2 * tp.tile_rows;
+  const long long part_rows = (long long)2 * blocks * tp.item_rows;
   p.part_out = static_cast<float*>(workspace);
   p.part_lse = p.part_out + part_rows * p.head_dim;
   tp.parts = reinterpret_cast<Part*>(p.part_lse + part_rows);
@@ -1097,7 +761,10 @@ int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, 
   if (!make_map(&q, p.q, 3, q_extent, q_stride, q_box) || !make_map(&k, p.k, 4, kv_extent, k_stride, kv_box) ||
       !make_map(&v, p.v, 4, kv_extent, v_stride, kv_box))
     return TOPLOC_ERR_CUDA;
-  return p.head_dim == 128 ? launch<128>(tp, q, k, v, blocks, stream) : launch<64>(tp, q, k, v, blocks, stream);
+  const int rc = few ? launch_few_rows(&tp, &q, &k, &v, blocks, stream)
+                 : p.head_dim == 128 ? launch<128>(tp, q, k, v, blocks, stream) : launch<64>(tp, q, k, v, blocks, stream);
+  if (rc != TOPLOC_OK) return rc;
+  return p.head_dim == 128 ? launch_join<128>(tp, blocks, stream) : launch_join<64>(tp, blocks, stream);
 }
 
 }  // namespace toploc_model
