@@ -37,9 +37,12 @@ struct Part {
 struct TcParams {
   AttentionParams p;
   int tile_rows;  // packed rows of a row tile: 128 rounded down to whole tokens
+  int tile_tokens, item_tokens;  // tokens of a row tile, of an item
   int item_rows;  // packed rows of an item: two tiles (a few rows: all that a sequence can bring)
-  int least_share;  // keys that are worth a block
+  float least_share;  // keys that are worth a block
   int box_rows;   // rows of a key copy
+  int page_shift, page_tiles;  // pages below a tile: log2 of their size; others: tiles a page
+  float share_scale;  // 1 / blocks
   int q_bytes;    // bytes of a query tile's copy
   bool wide_out;  // rows of the output at multiples of 32 bytes
   Part* parts;    // [blocks][2]
@@ -48,6 +51,17 @@ struct TcParams {
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ float reciprocal(float x) {  // within an ulp
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float log2_approx(float x) {  // within 2^-22
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
@@ -72,17 +86,24 @@ __device__ __forceinline__ int value_place(bool two, int j, int n) {
 // kLevelCost (what an item costs beside its keys, in keys) + c + the tokens up to its end.  Sequences follow one
 // another, in them key heads, in them levels.
 
-constexpr long long kLevelCost = 192;
+//
+// In fp32: the line decides only where it is cut, every block computes the same numbers, and code is what the start of
+// these kernels waits for (instruction caches that are empty at a launch; 64-bit arithmetic and divisions were most of it).
+
+constexpr float kLevelCost = 192.f;
 
 struct Line {
-  long long front;  // kLevelCost + keys in front
-  int rows_item, tokens_item, tokens, levels;
+  float front;  // kLevelCost + keys in front
+  float tokens_item, cut;  // cut: tokens that the last level lacks
+  int levels;
   __device__ Line(const TcParams& tp, const SeqRange& s)
-      : front(kLevelCost + max(s.keys - s.rows, 0)), rows_item(tp.item_rows), tokens_item(rows_item / tp.p.group),
-        tokens(s.rows), levels((s.rows + tokens_item - 1) / tokens_item) {}
-  __device__ long long upto(int level) const {  // of levels 0 .. level - 1
-    const long long whole = level * front + (long long)tokens_item * level * (level + 1) / 2;
-    return level < levels ? whole : whole - ((long long)levels * tokens_item - tokens);
+      : front(kLevelCost + (float)max(s.keys - s.rows, 0)), tokens_item((float)tp.item_tokens),
+        levels((s.rows + tp.item_tokens - 1) / tp.item_tokens) {
+    cut = (float)levels * tokens_item - (float)s.rows;
+  }
+  __device__ float upto(int level) const {  // of levels 0 .. level - 1
+    const float n = (float)level;
+    return n * (front + 0.5f * tokens_item * (n + 1.f)) - (level < levels ? 0.f : cut);
   }
 };
 
@@ -105,80 +126,96 @@ __device__ __forceinline__ int tiles_seen(const SeqRange& s, int tokens_upto) {
 }
 
 // The line's beginning: a run of sequences per thread (kRuns threads), the work in front of every run in run_cost and the
-// whole in run_cost[kRuns] (kRuns + 1 + kRuns / 32 entries in shared memory).  Ends with the writes on their way; a
-// __syncthreads has to follow.
+// whole in run_cost[kRuns] (kRuns + 1 + kRuns / 32 entries in shared memory).  A __syncthreads has to follow.
 template <int kRuns>
-__device__ __forceinline__ void lay_line(const TcParams& tp, long long* run_cost) {
+__device__ __forceinline__ void lay_line(const TcParams& tp, float* run_cost) {
   const AttentionParams& p = tp.p;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = (p.num_seqs + kRuns - 1) / kRuns;
-  long long* warp_cost = run_cost + kRuns + 1;
-  long long cost = 0;
+  float* warp_cost = run_cost + kRuns + 1;
+  float cost = 0.f;
+#pragma unroll 1
   for (int i = threadIdx.x * per; i < min(((int)threadIdx.x + 1) * per, p.num_seqs); ++i) {
     const SeqRange s = sequence(p, i);
     if (s.bad && p.status && blockIdx.x == 0) p.status[i] = TOPLOC_SEQ_BAD_LENGTH;
     const Line line(tp, s);
-    cost += line.upto(line.levels) * p.kv_heads;
+    cost += line.upto(line.levels) * (float)p.kv_heads;
   }
-  long long incl = cost;
+  float incl = cost;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
-    const long long up = __shfl_up_sync(0xFFFFFFFFu, incl, off);
+    const float up = __shfl_up_sync(0xFFFFFFFFu, incl, off);
     if (lane >= off) incl += up;
   }
+  const float before_lane = __shfl_up_sync(0xFFFFFFFFu, incl, 1);
   if (lane == 31) warp_cost[warp] = incl;
   __syncthreads();
-  long long in_front = incl - cost;
+  float in_front = 0.f;
+#pragma unroll 1
   for (int w = 0; w < warp; ++w) in_front += warp_cost[w];
-  run_cost[threadIdx.x] = in_front;
-  if (threadIdx.x == kRuns - 1) run_cost[kRuns] = in_front + cost;
+  run_cost[threadIdx.x] = in_front + (lane > 0 ? before_lane : 0.f);
+  if (threadIdx.x == kRuns - 1) run_cost[kRuns] = in_front + incl;
   fence_async_shared();  // tensor copies write there next
 }
 
-// Where the stretch of a block begins; a cut in front of a level's second tile or behind its last but one moves to the
-// level's ends.
+// Where the stretches of this block and of the next one begin (lane 0 and 1 of a warp look for one each; all get both).
+// A cut in front of a level's second tile or behind its last but one moves to the level's ends.
+struct Stretch {
+  Place begin, end;
+};
+
 template <int kRuns>
-__device__ __forceinline__ Place find_place(const TcParams& tp, const long long* run_cost, int block) {
+__device__ __forceinline__ Stretch find_stretch(const TcParams& tp, const float* run_cost) {
   const AttentionParams& p = tp.p;
-  const int per = (p.num_seqs + kRuns - 1) / kRuns;
-  long long at = max((run_cost[kRuns] + gridDim.x - 1) / gridDim.x, (long long)tp.least_share) * block;
-  if (at >= run_cost[kRuns]) return Place{p.num_seqs, 0, 0, 0};
-  int lo = 0, hi = kRuns;  // run_cost[lo] <= at < run_cost[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (run_cost[mid] <= at) lo = mid; else hi = mid;
-  }
-  at -= run_cost[lo];
-  for (int i = lo * per; i < p.num_seqs; ++i) {
-    const SeqRange s = sequence(p, i);
-    const Line line(tp, s);
-    const long long one = line.upto(line.levels), all = one * p.kv_heads;
-    if (at >= all) {
-      at -= all;
-      continue;
+  const int per = (p.num_seqs + kRuns - 1) / kRuns, lane = threadIdx.x & 31;
+  const int block = blockIdx.x + min(lane, 1);
+  const float all_work = run_cost[kRuns];
+  float at = max(all_work * tp.share_scale, tp.least_share) * (float)block;
+  Place place = {p.num_seqs, 0, 0, 0};
+  if (at < all_work && block < gridDim.x) {  // (the last block's stretch ends with the line, whatever the rounding)
+    int lo = 0, hi = kRuns;                  // run_cost[lo] <= at < run_cost[hi]
+#pragma unroll 1
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (run_cost[mid] <= at) lo = mid; else hi = mid;
     }
-    Place place = {i, (int)(at / one), 0, 0};
-    at -= place.head * one;
-    int a = 0, b = line.levels;  // upto(a) <= at < upto(b)
-    while (b - a > 1) {
-      const int mid = (a + b) >> 1;
-      if (line.upto(mid) <= at) a = mid; else b = mid;
-    }
-    place.level = a;
-    at -= line.upto(a);
-    const int n = tiles_seen(s, min((a + 1) * line.tokens_item, line.tokens));
-    const long long tile = (at - kLevelCost + kKeyTile / 2) / kKeyTile;
-    if (at <= kLevelCost || tile <= 1) return place;
-    if (tile >= n - 1) {
-      if (++place.level == line.levels) {
-        place.level = 0;
-        if (++place.head == p.kv_heads) return Place{i + 1, 0, 0, 0};
+    at -= run_cost[lo];
+#pragma unroll 1
+    for (int i = lo * per; i < p.num_seqs; ++i) {
+      const SeqRange s = sequence(p, i);
+      const Line line(tp, s);
+      const float one = line.upto(line.levels), all = one * (float)p.kv_heads;
+      if (at >= all) {
+        at -= all;
+        continue;
       }
-      return place;
+      const int head = min((int)__fdividef(at, one), p.kv_heads - 1);
+      at = max(at - (float)head * one, 0.f);
+      int a = 0, b = line.levels;  // upto(a) <= at < upto(b)
+#pragma unroll 1
+      while (b - a > 1) {
+        const int mid = (a + b) >> 1;
+        if (line.upto(mid) <= at) a = mid; else b = mid;
+      }
+      at -= line.upto(a);
+      const int n = tiles_seen(s, min((a + 1) * tp.item_tokens, s.rows));
+      const int tile = (int)max((at - kLevelCost) * (1.f / kKeyTile) + 0.5f, 0.f);
+      place = Place{i, head, a, tile <= 1 ? 0 : tile};
+      if (tile > 1 && tile >= n - 1) {
+        place.tile = 0;
+        if (++place.level == line.levels) {
+          place.level = 0;
+          if (++place.head == p.kv_heads) place = Place{i + 1, 0, 0, 0};
+        }
+      }
+      break;
     }
-    place.tile = (int)tile;
-    return place;
   }
-  return Place{p.num_seqs, 0, 0, 0};
+  __syncwarp();
+  const auto of = [&](int l) {
+    return Place{__shfl_sync(0xFFFFFFFFu, place.seq, l), __shfl_sync(0xFFFFFFFFu, place.head, l),
+                 __shfl_sync(0xFFFFFFFFu, place.level, l), __shfl_sync(0xFFFFFFFFu, place.tile, l)};
+  };
+  return Stretch{of(0), of(1)};
 }
 
 // A warp's walk over its block's stretch: the items one after the other.
@@ -188,7 +225,7 @@ struct Walk {
   SeqRange s = {0, 0, 0, false};
   int s_of = -1;
 
-  __device__ Walk(const TcParams& tp, const Place& begin, const Place& end) : tp(tp), at(begin), end(end) {
+  __device__ Walk(const TcParams& tp, const Stretch& stretch) : tp(tp), at(stretch.begin), end(stretch.end) {
     if ((threadIdx.x & 31) < 2) tp.parts[2 * blockIdx.x + (threadIdx.x & 31)].seq = -1;
     __syncwarp();
   }
@@ -198,6 +235,7 @@ struct Walk {
     const AttentionParams& p = tp.p;
     im = Item{};
     im.seq = -1;
+#pragma unroll 1
     while (before(at, end)) {  // past the sequences without rows
       if (s_of != at.seq) {
         s = sequence(p, at.seq);
@@ -207,7 +245,7 @@ struct Walk {
       at = Place{at.seq + 1, 0, 0, 0};
     }
     if (!before(at, end)) return false;
-    const int tokens_item = tp.item_rows / p.group, tokens = min((at.level + 1) * tokens_item, s.rows);
+    const int tokens = min((at.level + 1) * tp.item_tokens, s.rows);
     im.seq = at.seq;
     im.head = at.head;
     im.first = s.first;
@@ -220,7 +258,7 @@ struct Walk {
     im.kend = min(min(s.keys, im.behind + tokens), tile_end * kKeyTile);
     im.two = im.row0 + tp.tile_rows < im.rows;
     if (im.two) {
-      const int first = tiles_seen(s, at.level * tokens_item + tp.tile_rows / p.group);
+      const int first = tiles_seen(s, at.level * tp.item_tokens + tp.tile_tokens);
       im.n0 = max(min(first, tile_end) - at.tile, 0);
       im.n1 = max(tile_end - at.tile, 0);
     } else {
@@ -261,15 +299,19 @@ struct Feeder {
   __device__ int page_of(int j) const {
     const int key = im.kbegin + j * kKeyTile + lane * tp.box_rows;
     const bool copied = tp.p.kv_lens && j < tiles && lane * tp.box_rows < kKeyTile && key < im.kend;
-    return copied ? tp.p.table[im.seq * tp.p.table_stride + key / tp.p.page_size] : 0;
+    const int col = tp.box_rows < kKeyTile ? key >> tp.page_shift : (unsigned)(key / kKeyTile) / (unsigned)tp.page_tiles;
+    return copied ? tp.p.table[im.seq * tp.p.table_stride + col] : 0;
   }
 
   __device__ void item(const Item& next_item, int n) {
     base += 2 * tiles;
     im = next_item;
     tiles = n;
-    page = page_of(0);
-    next = page_of(1);
+#pragma unroll 1
+    for (int j = 0; j < 2; ++j) {
+      page = next;
+      next = page_of(j);
+    }
   }
 
   __device__ void feed(int j, int at) {
@@ -287,9 +329,10 @@ struct Feeder {
         page = tp.p.num_pages;  // past the end: the copy fills zeros
       }
       const int copies = (min(kKeyTile, im.kend - key0) + tp.box_rows - 1) / tp.box_rows;
-      const int in_page = tp.box_rows < kKeyTile ? 0 : key0 % tp.p.page_size;
+      const int in_page = tp.page_tiles > 1 ? (unsigned)(key0 / kKeyTile) % (unsigned)tp.page_tiles * kKeyTile : 0;
       if (elect_one()) barrier_arrive_expect(bar, copies * S::kHalves * tp.box_rows * 128);
       __syncwarp();
+#pragma unroll 1
       for (int c = 0; c < copies; ++c) {
         const int which = __shfl_sync(0xFFFFFFFFu, page, c);
         if (elect_one()) {
@@ -311,6 +354,7 @@ struct Feeder {
 
   // After a wait gave up: no copy of this warp is in flight when it returns.
   __device__ void drain() const {
+#pragma unroll 1
     for (int i = 0; i < kStages; ++i)
       if (fed >> i & 1) barrier_drain(shared_address(&sh.full[i]), fed_parity >> i & 1);
   }
@@ -339,6 +383,7 @@ __device__ __forceinline__ Item uniform(const Item& im) {  // the same for every
 // 128 threads, each for its share; what follows has to wait for them all.
 template <int kHalves>
 __device__ __forceinline__ void clean_values(unsigned char* tile, int from, int keys, int* bad, int number) {
+#pragma unroll 1
   for (int e = threadIdx.x & 127; e < (kKeyTile - from) * 8; e += 128) {
     const int row = from + (e >> 3);
     const bool past = row >= keys;
@@ -366,13 +411,26 @@ __device__ __forceinline__ void clean_values(unsigned char* tile, int from, int 
   fence_async_shared();
 }
 
-// Value [key] of a sequence and key head (first channel), NULL where its page lies outside the cache.
-__device__ __forceinline__ const __nv_bfloat16* value_of(const AttentionParams& p, const Item& im, int key) {
-  const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + (long long)im.head * p.v_head;
-  if (p.kv_lens == nullptr) return v + (long long)(im.first + key) * p.v_token;
-  const int col = key / p.page_size, page = p.table[im.seq * p.table_stride + col];
-  if (page < 0 || page >= p.num_pages) return nullptr;
-  return v + page * p.v_page + (long long)(key - col * p.page_size) * p.v_token;
+// Adds what clean_values took out of the values of keys begin .. end - 1 (NaN and infinities, as a rule nothing) to the
+// channels c .. c + count - 1 of a row that sees these keys.  Not inlined: as good as never called.
+__device__ __noinline__ void give_back(const AttentionParams& p, int seq, int key_head, int first, int begin, int end,
+                                       int c, int count, float* out) {
+#pragma unroll 1
+  for (int key = begin; key < end; ++key) {
+    const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(p.v) + (long long)key_head * p.v_head + c;
+    if (p.kv_lens == nullptr) {
+      v += (long long)(first + key) * p.v_token;
+    } else {
+      const int col = key / p.page_size, page = p.table[seq * p.table_stride + col];
+      if (page < 0 || page >= p.num_pages) continue;
+      v += page * p.v_page + (long long)(key - col * p.page_size) * p.v_token;
+    }
+#pragma unroll 1
+    for (int e = 0; e < count; ++e) {
+      const float f = __bfloat162float(v[e]);
+      if (!(fabsf(f) < INFINITY)) out[e] += f;
+    }
+  }
 }
 
 }  // namespace

@@ -47,24 +47,38 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
 // longest wait that is due ends in milliseconds) it gives up.
 constexpr int kWaitTries = 2000000;
 
-__device__ __forceinline__ bool barrier_wait_slow(uint32_t bar, uint32_t parity, volatile int* gave_up) {
-  for (int i = 0; i < kWaitTries; ++i) {
-    if (barrier_try(bar, parity)) return true;
-    if ((i & 31) == 31 && *gave_up) return false;
-  }
-  *gave_up = 1;
-  return false;
-}
-
 // True when the phase of `parity` is complete; false after the limit, or where another wait of the block
-// gave up (*gave_up, in shared memory).
+// gave up (*gave_up, in shared memory).  One small loop in assembly: the kernels wait in some forty places,
+// and code that does not fit the instruction caches costs them more than the waits.
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
-  if (barrier_try(bar, parity)) return true;
-  return barrier_wait_slow(bar, parity, gave_up);
+  uint32_t done;
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p, q;\n\t"
+      ".reg .u32 n, g;\n\t"
+      "mov.u32 n, 0;\n"
+      "again:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000;\n\t"
+      "@p bra end;\n\t"
+      "ld.volatile.shared.u32 g, [%3];\n\t"
+      "setp.ne.u32 q, g, 0;\n\t"
+      "@q bra end;\n\t"
+      "add.u32 n, n, 1;\n\t"
+      "setp.lt.u32 q, n, %4;\n\t"
+      "@q bra again;\n\t"
+      "st.volatile.shared.u32 [%3], 1;\n"
+      "end:\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity), "r"(shared_address((const void*)gave_up)), "n"(kWaitTries)
+      : "memory");
+  return done != 0;
 }
 
 // Waits for the block's own copies or products in flight before it ends early; bounded all the same.
 __device__ __forceinline__ void barrier_drain(uint32_t bar, uint32_t parity) {
+#pragma unroll 1
   for (int i = 0; i < kWaitTries && !barrier_try(bar, parity); ++i) {
   }
 }
@@ -181,6 +195,34 @@ __device__ __forceinline__ void tmem_ready(uint32_t (&r)[16]) {
                : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
                  "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]),
                  "+r"(r[15]));
+}
+__device__ __forceinline__ void tmem_load(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ void tmem_ready(uint32_t (&r)[4]) {
+  asm volatile(""
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]));
+}
+__device__ __forceinline__ void tmem_load(uint32_t (&r)[8], uint32_t addr) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(addr));
+}
+__device__ __forceinline__ void tmem_ready(uint32_t (&r)[8]) {
+  asm volatile(""
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]));
+}
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};"
+               :
+               : "r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]));
+}
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               :
+               : "r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]));
 }
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }

@@ -4,7 +4,9 @@
 //   S^T = K Q^T (128 keys x N rows),  P^T = 2^(scale S^T - m),  O^T += V^T P^T (head_dim x N)
 //
 // With so few rows the other order would leave most of a product's 128 rows and of the softmax threads empty.  Here a
-// thread has a key and weighs it for all N rows (N exponentials, not 128), and the products are N wide.  A row's maximum
+// thread has a key and weighs it for all N rows (R exponentials, not 128), and the products are N wide.
+// R is 4, 8, 16 or 32, N is R and at least 16: loops over rows are unrolled, and code for rows that are not there would
+// only crowd the instruction caches.  A row's maximum
 // and sum run over threads, but seldom: the maximum of the first tile stays the reference for the whole item unless a
 // score exceeds it by 2^64 (weights, sums and outputs share it, and fp32 and bf16 have the range; the quotient is the
 // same), so a tile needs one vote, and the threads' own sums are added up once at the end.
@@ -44,10 +46,11 @@ struct FewShared {
   static_assert(kBytes <= 115712, "shared memory of half an SM");
 };
 
-template <int D, int N>
+template <int D, int R>
 __global__ void __launch_bounds__(kFewThreads, 2)
-toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorMap map_q,
+toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_constant__ CUtensorMap map_q,
                             const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  constexpr int N = R < 16 ? 16 : R;  // rows of the products
   using S = FewShared<D, N>;
   constexpr int kStages = S::kStages, kHalves = S::kHalves;
   extern __shared__ __align__(1024) unsigned char base[];
@@ -61,6 +64,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
 
   asm volatile("griddepcontrol.launch_dependents;");  // the join waits for this grid to end
   if (threadIdx.x == 0) {
+#pragma unroll 1
     for (int i = 0; i < kStages; ++i) {
       barrier_init(shared_address(&sh.full[i]), 1);
       barrier_init(shared_address(&sh.empty[i]), 1);
@@ -76,6 +80,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
     barrier_init(shared_address(&sh.q_empty), 1);
     barrier_init(shared_address(&sh.drain), 1);
     barrier_init(shared_address(&sh.group), 4);
+#pragma unroll 1
     for (int i = 0; i < kItems; ++i) {
       barrier_init(shared_address(&sh.item_full[i]), 1);
       barrier_init(shared_address(&sh.item_empty[i]), 6);
@@ -85,7 +90,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
   }
   constexpr uint32_t kColumns = 4 * N;  // tensor memory: two tiles of scores, the outputs (a power of two at least 32)
   if (warp == 5) tmem_alloc(shared_address(&sh.tmem), kColumns);
-  long long* run_cost = reinterpret_cast<long long*>(ring);  // where the ring's first tile comes later
+  float* run_cost = reinterpret_cast<float*>(ring);  // where the ring's first tile comes later
   lay_line<kFewThreads>(tp, run_cost);
   tmem_fence_before();
   __syncthreads();
@@ -100,10 +105,11 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
       prefetch_map(&map_k);
       prefetch_map(&map_v);
     }
-    Walk walk(tp, find_place<kFewThreads>(tp, run_cost, blockIdx.x), find_place<kFewThreads>(tp, run_cost, blockIdx.x + 1));
+    Walk walk(tp, find_stretch<kFewThreads>(tp, run_cost));
     __syncwarp();  // run_cost has been read: the ring's place is free
     uint32_t q_uses = 0;
     Feeder<S> keys(tp, &map_k, sh, ring, gave_up);
+#pragma unroll 1
     for (uint32_t number = 0;; ++number) {
       const uint32_t slot = number % kItems;
       if (!warp_wait(sh.item_empty[slot], ((number / kItems) & 1) ^ 1, gave_up)) break;
@@ -128,6 +134,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
       }
       __syncwarp();
       keys.item(im, im.n0);
+#pragma unroll 1
       for (int j = 0; j < im.n0 && keys.fine; ++j) keys.feed(j, key_place(false, j));
       if (!keys.fine) break;
     }
@@ -138,6 +145,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
   } else if (warp == 6) {
     // ---- feeding: values ----
     Feeder<S> values(tp, &map_v, sh, ring, gave_up);
+#pragma unroll 1
     for (uint32_t number = 0;; ++number) {
       const uint32_t slot = number % kItems;
       if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
@@ -186,6 +194,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
         mma_commit(shared_address(&sh.o_full));
       }
     };
+#pragma unroll 1
     for (uint32_t number = 0;; ++number) {
       const uint32_t slot = number % kItems;
       if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
@@ -199,6 +208,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
       if (!ok) break;
       scores(0, used);
       release(used);
+#pragma unroll 1
       for (int j = 0; ok && j < n; ++j) {
         if (j + 1 < n) {
           const uint32_t at = used + key_place(false, j + 1);
@@ -235,6 +245,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
       if (lane == 0) barrier_arrive(shared_address(&sh.group));
       return warp_wait(sh.group, syncs++ & 1, gave_up);
     };
+#pragma unroll 1
     for (uint32_t number = 0;; ++number) {
       const uint32_t slot = number % kItems;
       if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
@@ -244,27 +255,28 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
       if (im.seq < 0) break;
       const int n = im.n0, rows = im.rows;
       const int hidden_from = max(im.behind + 1, 0);  // first key hidden from a row of the item
-      float ref[N], l[N];
+      float ref[R], l[R];
 #pragma unroll
-      for (int r = 0; r < N; ++r) ref[r] = -INFINITY, l[r] = 0.f;
+      for (int r = 0; r < R; ++r) ref[r] = -INFINITY, l[r] = 0.f;
       bool ok = true;
+#pragma unroll 1
       for (int j = 0; j < n; ++j) {
         const int key0 = im.kbegin + j * kKeyTile, key = key0 + me, buffer = j & 1;
         const bool masked = key0 + kKeyTile - 1 > im.behind;
         ok = warp_wait(sh.s_full[buffer], s_uses[buffer]++ & 1, gave_up);
         if (!ok) break;
         tmem_fence_after();
-        uint32_t x[N];
+        uint32_t x[R];
         tmem_load(x, tmem + lanes + N * buffer);
         tmem_wait_load();
         tmem_ready(x);
-        float s[N];
+        float s[R];
 #pragma unroll
-        for (int r = 0; r < N; ++r) s[r] = __uint_as_float(x[r]) * scale;
+        for (int r = 0; r < R; ++r) s[r] = __uint_as_float(x[r]) * scale;
         if (masked) {
           int newest = im.behind, head = 0;  // of row r's token
 #pragma unroll
-          for (int r = 0; r < N; ++r) {
+          for (int r = 0; r < R; ++r) {
             if (key > newest) s[r] = -INFINITY;  // whatever was there
             if (++head == p.group) head = 0, ++newest;
           }
@@ -275,7 +287,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
         if (j > 0) {
           bool over = false;
 #pragma unroll
-          for (int r = 0; r < N; ++r)
+          for (int r = 0; r < R; ++r)
             if (r < rows) over = over || s[r] - ref[r] > kFewLimit;
           if (__any_sync(0xFFFFFFFFu, over) && lane == 0) *(volatile uint32_t*)&sh.exceeds[tiles_done & 1] = tiles_done;
           ok = sync();
@@ -284,7 +296,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
         }
         if (renew) {
 #pragma unroll
-          for (int r = 0; r < N; ++r) {
+          for (int r = 0; r < R; ++r) {
             if (r < rows) {
               float top = s[r];
 #pragma unroll
@@ -294,9 +306,9 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
           }
           ok = sync();
           if (!ok) break;
-          float shrink[N];
+          float shrink[R];
 #pragma unroll
-          for (int r = 0; r < N; ++r) {
+          for (int r = 0; r < R; ++r) {
             shrink[r] = 0.f;
             if (r < rows) {
               const float top = fmaxf(fmaxf(sh.rows[0][r], sh.rows[1][r]), fmaxf(sh.rows[2][r], sh.rows[3][r]));
@@ -316,14 +328,16 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
             tmem_wait_load();
             tmem_ready(x);
 #pragma unroll
-            for (int r = 0; r < N; ++r) x[r] = __float_as_uint(__uint_as_float(x[r]) * shrink[r]);
+            for (int r = 0; r < R; ++r) x[r] = __float_as_uint(__uint_as_float(x[r]) * shrink[r]);
             tmem_store(tmem + lanes + kOut, x);
             tmem_wait_store();
           }
         }
         uint32_t packed[N / 2];
 #pragma unroll
-        for (int r = 0; r < N; r += 2) {
+        for (int r = 0; r < N / 2; ++r) packed[r] = 0u;
+#pragma unroll
+        for (int r = 0; r < R; r += 2) {
           float a = 0.f, b = 0.f;
           if (r < rows) a = exp2_approx(s[r] - ref[r]);
           if (r + 1 < rows) b = exp2_approx(s[r + 1] - ref[r + 1]);
@@ -337,7 +351,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
         }
         // 8 rows of a key are 16 bytes, keys side by side
 #pragma unroll
-        for (int c = 0; c < N / 8; ++c)
+        for (int c = 0; c < (R + 7) / 8; ++c)
           *reinterpret_cast<uint4*>(weights + c * 2048 + me * 16) =
               make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
         if (masked) {
@@ -358,7 +372,7 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
 
       // ---- the rows' results ----
 #pragma unroll
-      for (int r = 0; r < N; ++r) {
+      for (int r = 0; r < R; ++r) {
         if (r < rows) {
 #pragma unroll
           for (int off = 16; off > 0; off >>= 1) l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], off);
@@ -369,42 +383,54 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
       if (ok && n > 0) ok = warp_wait(sh.o_full, (pv - 1) & 1, gave_up);
       if (!ok) break;
       tmem_fence_after();
-      uint32_t x[N];
+      uint32_t x[R];
       if (n > 0) {
         tmem_load(x, tmem + lanes + kOut);
         tmem_wait_load();
         tmem_ready(x);
       }
       const bool repair = *(volatile int*)&sh.bad_values[number & 1] == (int)number;
-      int token = 0, head = 0;
+      float o[R];
 #pragma unroll
-      for (int r = 0; r < N; ++r) {
+      for (int r = 0; r < R; ++r) o[r] = n > 0 ? __uint_as_float(x[r]) : 0.f;
+      if (repair && me < D) {  // values that were taken out of tiles with hidden keys: back to the rows that see them
+        float copy[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) copy[r] = o[r];
+#pragma unroll 1
+        for (int r = 0; r < rows; ++r)
+          give_back(p, im.seq, im.head, im.first, max(im.kbegin, hidden_from), min(im.behind + r / p.group + 1, im.kend),
+                    me, 1, copy + r);
+#pragma unroll
+        for (int r = 0; r < R; ++r) o[r] = copy[r];
+      }
+      // row r's place: of the output, or of the block's part
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + im.first * p.out_token + im.head * p.group * p.out_head + me;
+      float* lse = p.lse + (long long)im.first * p.q_heads + im.head * p.group;
+      const long long part = ((long long)blockIdx.x * 2 + im.slot) * tp.item_rows;
+      int head = 0;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
         if (r < rows) {
           const float total = sh.rows[0][r] + sh.rows[1][r] + sh.rows[2][r] + sh.rows[3][r];
           const bool any_keys = total != 0.f;
-          float o = any_keys ? __uint_as_float(x[r]) : 0.f;
-          if (repair && me < D) {  // values that were taken out of tiles with hidden keys: back to the rows that see them
-            for (int key = max(im.kbegin, hidden_from); key <= min(im.behind + token, im.kend - 1); ++key) {
-              const __nv_bfloat16* v = value_of(p, im, key);
-              const float f = v == nullptr ? 0.f : __bfloat162float(v[me]);
-              if (!(fabsf(f) < INFINITY)) o += f;
-            }
-          }
-          o *= any_keys ? 1.f / total : 0.f;
-          const float lse2 = any_keys ? ref[r] + log2f(total) : -INFINITY;
+          const float value = any_keys ? o[r] * reciprocal(total) : 0.f;
+          const float lse2 = any_keys ? ref[r] + log2_approx(total) : -INFINITY;
           if (im.slot >= 0) {
-            const long long part = ((long long)blockIdx.x * 2 + im.slot) * tp.item_rows + r;
-            if (me < D) p.part_out[part * D + me] = o;
-            if (me == r) p.part_lse[part] = lse2;
+            if (me < D) p.part_out[(part + r) * D + me] = value;
+            if (me == r) p.part_lse[part + r] = lse2;
           } else {
-            const int q_head = im.head * p.group + head;
-            if (me < D)
-              static_cast<__nv_bfloat16*>(p.out)[(im.first + token) * p.out_token + q_head * p.out_head + me] =
-                  __float2bfloat16_rn(o);
-            if (me == r && p.lse) p.lse[(long long)(im.first + token) * p.q_heads + q_head] = lse2 * kLn2;
+            if (me < D) *out = __float2bfloat16_rn(value);
+            if (me == r && p.lse) *lse = lse2 * kLn2;
           }
         }
-        if (++head == p.group) head = 0, ++token;
+        out += p.out_head;
+        ++lse;
+        if (++head == p.group) {  // the next token
+          head = 0;
+          out += p.out_token - p.group * p.out_head;
+          lse += p.q_heads - p.group;
+        }
       }
       tmem_fence_before();
       if (!sync()) break;  // all have read: the next item may overwrite
@@ -417,15 +443,24 @@ toploc_attention_few_kernel(const TcParams tp, const __grid_constant__ CUtensorM
   if (warp == 5) tmem_free(tmem, kColumns);
 }
 
-template <int D, int N>
+template <int D, int R>
 int launch(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int blocks,
            cudaStream_t stream) {
-  constexpr int kBytes = FewShared<D, N>::kBytes;
-  if (cudaFuncSetAttribute(toploc_attention_few_kernel<D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) !=
+  constexpr int kBytes = FewShared<D, R < 16 ? 16 : R>::kBytes;
+  if (cudaFuncSetAttribute(toploc_attention_few_kernel<D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) !=
       cudaSuccess)
     return TOPLOC_ERR_CUDA;
-  toploc_attention_few_kernel<D, N><<<blocks, kFewThreads, kBytes, stream>>>(tp, q, k, v);
+  toploc_attention_few_kernel<D, R><<<blocks, kFewThreads, kBytes, stream>>>(tp, q, k, v);
   return launched();
+}
+
+template <int D>
+int launch_rows(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int blocks,
+                cudaStream_t stream) {
+  if (tp.item_rows <= 4) return launch<D, 4>(tp, q, k, v, blocks, stream);
+  if (tp.item_rows <= 8) return launch<D, 8>(tp, q, k, v, blocks, stream);
+  if (tp.item_rows <= 16) return launch<D, 16>(tp, q, k, v, blocks, stream);
+  return launch<D, 32>(tp, q, k, v, blocks, stream);
 }
 
 }  // namespace
@@ -438,10 +473,8 @@ int launch_few_rows(const void* params, const void* map_q, const void* map_k, co
   const CUtensorMap& q = *static_cast<const CUtensorMap*>(map_q);
   const CUtensorMap& k = *static_cast<const CUtensorMap*>(map_k);
   const CUtensorMap& v = *static_cast<const CUtensorMap*>(map_v);
-  const bool sixteen = tp.item_rows <= 16;
-  if (tp.p.head_dim == 128)
-    return sixteen ? launch<128, 16>(tp, q, k, v, blocks, stream) : launch<128, 32>(tp, q, k, v, blocks, stream);
-  return sixteen ? launch<64, 16>(tp, q, k, v, blocks, stream) : launch<64, 32>(tp, q, k, v, blocks, stream);
+  return tp.p.head_dim == 128 ? launch_rows<128>(tp, q, k, v, blocks, stream)
+                              : launch_rows<64>(tp, q, k, v, blocks, stream);
 }
 
 }  // namespace toploc_model

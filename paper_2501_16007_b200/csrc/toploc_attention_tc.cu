@@ -90,7 +90,7 @@ __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
 
 template <int D>
 __global__ void __launch_bounds__(kTcThreads, 1)
-toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMap map_q,
+toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_constant__ CUtensorMap map_q,
                            const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   using S = Shared<D>;
   constexpr int kStages = S::kStages, kHalves = S::kHalves;
@@ -106,6 +106,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
   // tell the join kernel that it may be scheduled (it waits for this grid to end)
   asm volatile("griddepcontrol.launch_dependents;");
   if (threadIdx.x == 0) {
+#pragma unroll 1
     for (int i = 0; i < kStages; ++i) {
       barrier_init(shared_address(&sh.full[i]), 1);
       barrier_init(shared_address(&sh.empty[i]), 1);
@@ -121,6 +122,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
     barrier_init(shared_address(&sh.q_empty), 1);
     barrier_init(shared_address(&sh.drain), 1);
     barrier_init(shared_address(&sh.join), 8);
+#pragma unroll 1
     for (int i = 0; i < kItems; ++i) {
       barrier_init(shared_address(&sh.item_full[i]), 1);
       barrier_init(shared_address(&sh.item_empty[i]), 10);
@@ -129,7 +131,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
     barrier_init_fence();
   }
   if (warp == 9) tmem_alloc(shared_address(&sh.tmem), 512);
-  long long* run_cost = reinterpret_cast<long long*>(ring);  // where the ring's first tile comes later
+  float* run_cost = reinterpret_cast<float*>(ring);  // where the ring's first tile comes later
   lay_line<kTcThreads>(tp, run_cost);
   tmem_fence_before();
   __syncthreads();
@@ -145,10 +147,11 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       prefetch_map(&map_k);
       prefetch_map(&map_v);
     }
-    Walk walk(tp, find_place<kTcThreads>(tp, run_cost, blockIdx.x), find_place<kTcThreads>(tp, run_cost, blockIdx.x + 1));
+    Walk walk(tp, find_stretch<kTcThreads>(tp, run_cost));
     __syncwarp();  // run_cost has been read: the ring's place is free
     uint32_t q_uses = 0;
     Feeder<S> keys(tp, &map_k, sh, ring, gave_up);
+#pragma unroll 1
     for (uint32_t number = 0;; ++number) {
       const uint32_t slot = number % kItems;
       if (!warp_wait(sh.item_empty[slot], ((number / kItems) & 1) ^ 1, gave_up)) break;
@@ -175,11 +178,12 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
 #pragma unroll
           for (int h = 0; h < kHalves; ++h)
             copy_3d(shared_address(q_tiles + w * S::kTileBytes + h * kBlockBytes), &map_q, q_bar, h * 64,
-                    im.head * p.group, im.first + (im.row0 + w * tp.tile_rows) / p.group);
+                    im.head * p.group, im.first + im.row0 / tp.item_rows * tp.item_tokens + w * tp.tile_tokens);
       }
       __syncwarp();
 
       keys.item(im, n);
+#pragma unroll 1
       for (int j = 0; j < n && keys.fine; ++j) keys.feed(j, key_place(im.two, j));
       if (!keys.fine) break;
     }
@@ -191,6 +195,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
     lower_registers<kOtherRegisters>();
     // ---- feeding: values ----
     Feeder<S> values(tp, &map_v, sh, ring, gave_up);
+#pragma unroll 1
     for (uint32_t number = 0;; ++number) {
       const uint32_t slot = number % kItems;
       if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
@@ -200,6 +205,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       if (im.seq < 0) break;
       const int n = item_tiles(im);
       values.item(im, n);
+#pragma unroll 1
       for (int j = 0; j < n && values.fine; ++j) values.feed(j, value_place(im.two, j, n));
       if (!values.fine) break;
     }
@@ -253,6 +259,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
     const auto queries_used = [&] {
       if (elect_one()) mma_commit(shared_address(&sh.q_empty));
     };
+#pragma unroll 1
     for (uint32_t number = 0;; ++number) {
       const uint32_t slot = number % kItems;
       if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
@@ -274,6 +281,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
         if (n1 > 0) scores(1, used, true);
         release(used);
         if (n == 1) queries_used();
+#pragma unroll 1
         for (int j = 0; ok && j < n; ++j) {
           const uint32_t v_at = used + 2 * j + 1, k_at = v_at + 1;
           ok = full(v_at) && (j + 1 >= n || full(k_at));
@@ -294,6 +302,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
         }
       } else {
         uint32_t at = used;
+#pragma unroll 1
         for (int w = 0; ok && w < min(n, 2); ++w, ++at) {
           ok = full(at);
           if (!ok) break;
@@ -301,6 +310,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
           release(at);
         }
         if (n <= 2 && ok) queries_used();
+#pragma unroll 1
         for (int j = 0; ok && j < n; ++j) {
           const int w = j & 1;
           ok = full(at) && values(w, at, j >= 2);
@@ -339,6 +349,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       if (lane == 0) barrier_arrive(shared_address(&sh.join));
       return warp_wait(sh.join, joins++ & 1, gave_up);
     };
+#pragma unroll 1
     for (uint32_t number = 0;; ++number) {
       const uint32_t slot = number % kItems;
       if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
@@ -366,6 +377,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
       };
       float m = -INFINITY, l = 0.f;
       bool ok = true;
+#pragma unroll 1
       for (int i = 0; i < tiles; ++i) {
         const int j = two ? i : 2 * i + w;
         const int key0 = im.kbegin + j * kKeyTile;
@@ -491,7 +503,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
         if (a.y != a.y || b.y != b.y) total = NAN;  // a NaN score leaves no trace in a maximum
       }
       const bool any_keys = total != 0.f;
-      const float inv = any_keys ? 1.f / total : 0.f;
+      const float inv = any_keys ? reciprocal(total) : 0.f;
       const int head = im.head * p.group + row - token * p.group;
       const long long at = (long long)(im.first + token) * p.q_heads + head;
       // where the row's part of a split tile goes
@@ -530,16 +542,12 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
           for (int e = 0; e < 32; ++e) o[e] = 0.f;
         }
         if (repair) {  // values that were taken out of tiles with hidden keys: back to the rows that see them
-          const int begin = max(im.kbegin, hidden_from);
-          for (int key = begin; key <= min(newest, im.kend - 1); ++key) {
-            const __nv_bfloat16* v = value_of(p, im, key);
-            if (v == nullptr) continue;
+          float copy[32];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float f = __bfloat162float(v[c + e]);
-              if (!(fabsf(f) < INFINITY)) o[e] += f;
-            }
-          }
+          for (int e = 0; e < 32; ++e) copy[e] = o[e];
+          give_back(p, im.seq, im.head, im.first, max(im.kbegin, hidden_from), min(newest + 1, im.kend), c, 32, copy);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = copy[e];
         }
         if (im.slot < 0) {
           uint32_t packed[16];
@@ -565,7 +573,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
         }
       }
       if (valid && (two || w == 0)) {
-        const float lse2 = any_keys ? (top == -INFINITY ? 0.f : top) * scale + log2f(total) : -INFINITY;
+        const float lse2 = any_keys ? (top == -INFINITY ? 0.f : top) * scale + log2_approx(total) : -INFINITY;
         if (im.slot >= 0)
           p.part_lse[part] = lse2;
         else if (p.lse)
@@ -592,7 +600,7 @@ toploc_attention_tc_kernel(const TcParams tp, const __grid_constant__ CUtensorMa
 constexpr int kJoinRows = 8;  // rows of a block
 
 template <int D>
-__global__ void __launch_bounds__(128) toploc_attention_tc_join_kernel(const TcParams tp) {
+__global__ void __launch_bounds__(128) toploc_attention_tc_join_kernel(const __grid_constant__ TcParams tp) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const AttentionParams& p = tp.p;
   const int b = blockIdx.x, lane = threadIdx.x & 31, rows_item = tp.item_rows;
@@ -743,7 +751,13 @@ int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, 
   TcParams tp;
   tp.tile_rows = few ? p.max_new * p.group : 128 / p.group * p.group;
   tp.item_rows = few ? tp.tile_rows : 2 * tp.tile_rows;
-  tp.least_share = few ? 3 * kKeyTile : 6 * kKeyTile;
+  tp.tile_tokens = tp.tile_rows / p.group;
+  tp.item_tokens = tp.item_rows / p.group;
+  tp.least_share = few ? 3.f * kKeyTile : 6.f * kKeyTile;
+  tp.share_scale = 1.f / (float)blocks;
+  tp.page_shift = 0;
+  while (page >> (tp.page_shift + 1) > 0) ++tp.page_shift;
+  tp.page_tiles = page > kKeyTile ? page / kKeyTile : 1;
   tp.box_rows = page > 0 ? min(page, kKeyTile) : kKeyTile;
   tp.q_bytes = p.head_dim * 2 * p.group * tokens;
   tp.wide_out = aligned(p.out, 32) && p.out_token % 16 == 0 && p.out_head % 16 == 0;
