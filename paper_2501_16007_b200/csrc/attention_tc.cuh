@@ -26,6 +26,7 @@ struct Item {
   int kend;
   int two;     // two row tiles
   int n0, n1;  // key tiles of the two groups, or n0 in all
+  int clean;   // tiles from here on hold keys that are hidden from a row (or none at all at their end)
 };
 
 // The parts a block leaves, for the join.
@@ -264,6 +265,7 @@ struct Walk {
     } else {
       im.n0 = max(tile_end - at.tile, 0);
     }
+    im.clean = max(im.behind + at.level * tp.item_tokens + 1 - im.kbegin, 0) / kKeyTile;
     im.slot = at.tile > 0 ? 0 : ends_here ? 1 : -1;
     if (im.slot >= 0 && (threadIdx.x & 31) == 0)
       tp.parts[2 * blockIdx.x + im.slot] = Part{im.seq, im.head, im.row0, im.first, im.rows, ends_here ? 0 : 1};
@@ -374,38 +376,38 @@ __device__ __forceinline__ Item uniform(const Item& im) {  // the same for every
   r.two = __shfl_sync(0xFFFFFFFFu, im.two, 0);
   r.n0 = __shfl_sync(0xFFFFFFFFu, im.n0, 0);
   r.n1 = __shfl_sync(0xFFFFFFFFu, im.n1, 0);
+  r.clean = __shfl_sync(0xFFFFFFFFu, im.clean, 0);
   return r;
 }
 
 // Values of hidden keys meet weights of zero, and 0 * NaN is NaN.  Rows of a value tile past the item's keys (never
 // loaded, or another sequence's: rows `keys` and on) become zero.  So does, in rows from `from` on, a value that is not
-// finite; *bad gets the item's number then, and the rows that do see the key get the value back at the end.  Called by
-// 128 threads, each for its share; what follows has to wait for them all.
-template <int kHalves>
-__device__ __forceinline__ void clean_values(unsigned char* tile, int from, int keys, int* bad, int number) {
+// finite; *bad gets the item's number then, and the rows that do see the key get the value back at the end.  By kThreads
+// threads, number `me` of them this one; what follows has to wait for them all.
+template <int kHalves, int kThreads>
+__device__ __forceinline__ void clean_values(unsigned char* tile, int from, int keys, int me, int* bad, int number) {
 #pragma unroll 1
-  for (int e = threadIdx.x & 127; e < (kKeyTile - from) * 8; e += 128) {
+  for (int e = me; e < (kKeyTile - from) * 8; e += kThreads) {
     const int row = from + (e >> 3);
-    const bool past = row >= keys;
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
       uint4* at = reinterpret_cast<uint4*>(tile + h * kBlockBytes + row * 128 + (e & 7) * 16);
-      uint4 v = make_uint4(0, 0, 0, 0);
-      bool write = past;
-      if (!past) {
-        v = *at;
-        uint32_t* x = &v.x;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if ((x[q] & 0x7F80u) == 0x7F80u) x[q] &= 0xFFFF0000u, write = true;
-          if ((x[q] & 0x7F800000u) == 0x7F800000u) x[q] &= 0xFFFFu, write = true;
-        }
-        if (write) {
+      if (row >= keys) {
+        *at = make_uint4(0, 0, 0, 0);
+      } else {
+        const uint4 v = *at;
+        // an exponent of all ones carries into the sign's place
+        const uint32_t ones = ((v.x & 0x7F807F80u) + 0x00800080u) | ((v.y & 0x7F807F80u) + 0x00800080u) |
+                              ((v.z & 0x7F807F80u) + 0x00800080u) | ((v.w & 0x7F807F80u) + 0x00800080u);
+        if (ones & 0x80008000u) {
           *(volatile int*)bad = number;
           __threadfence_block();
+          uint16_t* x = reinterpret_cast<uint16_t*>(at);
+#pragma unroll 1
+          for (int i = 0; i < 8; ++i)
+            if ((x[i] & 0x7F80u) == 0x7F80u) x[i] = 0;
         }
       }
-      if (write) *at = v;
     }
   }
   fence_async_shared();

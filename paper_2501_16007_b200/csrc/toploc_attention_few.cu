@@ -358,8 +358,8 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
           const uint32_t place = used + value_place(false, j, n), stage = ring_stage(place, kStages);
           ok = warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up);
           if (!ok) break;
-          clean_values<kHalves>(ring + stage * S::kTileBytes, max(hidden_from - key0, 0), im.kend - key0,
-                                &sh.bad_values[number & 1], (int)number);
+          clean_values<kHalves, 128>(ring + stage * S::kTileBytes, max(hidden_from - key0, 0), im.kend - key0, me,
+                                     &sh.bad_values[number & 1], (int)number);
         }
         fence_async_shared();
         tmem_fence_before();

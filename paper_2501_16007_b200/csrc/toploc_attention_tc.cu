@@ -25,6 +25,8 @@
 // below 2^8, and O, the sum and P share the same reference, so the quotient is the same.
 #include "attention_tc.cuh"
 
+#include <type_traits>
+
 namespace {
 
 constexpr int kTcThreads = 384;            // two groups of softmax, and one whose first two warps feed and issue
@@ -47,7 +49,8 @@ struct Shared {
     Item items[kItems];
     uint32_t tmem;
     int gave_up;
-    int bad_values[2];  // number of the item (by parity) in whose hidden keys' tiles a value was not finite
+    uint64_t cleaned[kStages];  // the stage's value tile, one with hidden keys, may be used
+    int bad_values[8];  // number of the item (of 8) in whose hidden keys' tiles a value was not finite
   };
   static constexpr int kHeadBytes = 1024, kExchangeBytes = 2 * 128 * 8;
   static_assert(sizeof(Head) <= kHeadBytes, "head");
@@ -66,6 +69,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
+}
+
+// Scores beyond column `last` become minus infinity, whatever was there.
+__device__ __forceinline__ void hide(uint32_t (&x)[32], int last) {
+#pragma unroll
+  for (int e = 0; e < 32; ++e)
+    if (e > last) x[e] = 0xFF800000u;
 }
 
 // Two fp32 products and sums in one instruction.
@@ -110,13 +120,13 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
     for (int i = 0; i < kStages; ++i) {
       barrier_init(shared_address(&sh.full[i]), 1);
       barrier_init(shared_address(&sh.empty[i]), 1);
+      barrier_init(shared_address(&sh.cleaned[i]), 1);
     }
     for (int w = 0; w < 2; ++w) {
       barrier_init(shared_address(&sh.s_full[w]), 1);
       barrier_init(shared_address(&sh.p_most[w]), 4);
       barrier_init(shared_address(&sh.p_full[w]), 4);
       barrier_init(shared_address(&sh.o_full[w]), 1);
-      sh.bad_values[w] = -1;
     }
     barrier_init(shared_address(&sh.q_full), 1);
     barrier_init(shared_address(&sh.q_empty), 1);
@@ -127,6 +137,8 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       barrier_init(shared_address(&sh.item_full[i]), 1);
       barrier_init(shared_address(&sh.item_empty[i]), 10);
     }
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) sh.bad_values[i] = -1;
     sh.gave_up = 0;
     barrier_init_fence();
   }
@@ -203,10 +215,24 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       __syncwarp();
       if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
       if (im.seq < 0) break;
-      const int n = item_tiles(im);
+      const int n = item_tiles(im), hidden_from = max(im.behind + im.row0 / p.group + 1, 0);
       values.item(im, n);
+      // Tiles with hidden keys are cleaned one behind the copies: at once when a tile has landed would hold up the copies,
+      // later would hold up the ring.
 #pragma unroll 1
-      for (int j = 0; j < n && values.fine; ++j) values.feed(j, value_place(im.two, j, n));
+      for (int j = 0; j <= n && values.fine; ++j) {
+        if (j < n) values.feed(j, value_place(im.two, j, n));
+        const int landed = j - 1;
+        if (!values.fine || landed < im.clean || landed < 0) continue;
+        const uint32_t place = values.base + value_place(im.two, landed, n), stage = ring_stage(place, kStages);
+        values.fine = warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up);
+        if (!values.fine) break;
+        const int key0 = im.kbegin + landed * kKeyTile;
+        clean_values<kHalves, 32>(ring + stage * S::kTileBytes, max(hidden_from - key0, 0), im.kend - key0, lane,
+                                  &sh.bad_values[number & 7], (int)number);
+        __syncwarp();
+        if (lane == 0) barrier_arrive(shared_address(&sh.cleaned[stage]));
+      }
       if (!values.fine) break;
     }
     if (*gave_up) values.drain();
@@ -216,7 +242,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
     constexpr uint32_t kScores = bf16_product(128, false, false), kValues = bf16_product(D, false, true);
     const uint32_t q_low = operand_low(shared_address(q_tiles), 16);
     const uint32_t k_low = operand_low(shared_address(ring), 16), v_low = operand_low(shared_address(ring), kBlockBytes);
-    uint32_t used = 0, q_uses = 0, p_uses[2] = {0, 0};
+    uint32_t used = 0, q_uses = 0, p_uses[2] = {0, 0}, cleans = 0;  // cleans: by stage, the parity of its next cleaning
     const auto full = [&](uint32_t n) {
       const bool ok = warp_wait(sh.full[ring_stage(n, kStages)], ring_parity(n, kStages), gave_up);
       tmem_fence_after();
@@ -266,6 +292,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       // (through a shuffle: the same for every lane, and known to be)
       const int seq = __shfl_sync(0xFFFFFFFFu, sh.items[slot].seq, 0);
       const int n0 = __shfl_sync(0xFFFFFFFFu, sh.items[slot].n0, 0), n1 = __shfl_sync(0xFFFFFFFFu, sh.items[slot].n1, 0);
+      const int clean = __shfl_sync(0xFFFFFFFFu, sh.items[slot].clean, 0);
       const bool two = __shfl_sync(0xFFFFFFFFu, sh.items[slot].two, 0);
       __syncwarp();
       if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
@@ -273,55 +300,38 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       const int n = two ? max(n0, n1) : n0;
       if (n == 0) continue;
       bool ok = warp_wait(sh.q_full, q_uses++ & 1, gave_up);
-      tmem_fence_after();
-      if (two) {
-        ok = ok && full(used);
-        if (!ok) break;
-        if (n0 > 0) scores(0, used, true);
-        if (n1 > 0) scores(1, used, true);
-        release(used);
-        if (n == 1) queries_used();
+      // Round by round, group by group: the group's weights of a tile times the values, then its scores of the tile it
+      // takes next (two row tiles: both groups take every tile, group 1 after group 0; one: tiles in turn).  The first
+      // round has only scores.
+      const int rounds = two ? n : (n + 1) / 2;
+      int cleaned_to = clean;
 #pragma unroll 1
-        for (int j = 0; ok && j < n; ++j) {
-          const uint32_t v_at = used + 2 * j + 1, k_at = v_at + 1;
-          ok = full(v_at) && (j + 1 >= n || full(k_at));
+      for (int round = -1; ok && round < rounds; ++round) {
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            const int nw = w ? n1 : n0;
-            if (!ok || j >= nw) continue;
-            ok = values(w, v_at, j > 0);
-            if (!ok) break;
-            if (j + 1 < nw) scores(w, k_at, true);
+        for (int w = 0; w < 2; ++w) {
+          const int tiles = two ? (w ? n1 : n0) : n;
+          const int j = two ? round : 2 * round + w, next = j + (two ? 1 : 2);
+          const bool weigh = round >= 0 && j < tiles, score = next < tiles;
+          const uint32_t v_at = used + value_place(two, j, n), k_at = used + key_place(two, next);
+          // (group 1 of two row tiles meets what group 0 has waited for, unless group 0 has no such tile)
+          if (weigh && (w == 0 || !two || j >= n0)) ok = ok && full(v_at);
+          if (score && (w == 0 || !two || next >= n0)) ok = ok && full(k_at);
+          if (weigh && j >= cleaned_to) {
+            const uint32_t stage = ring_stage(v_at, kStages);
+            ok = ok && warp_wait(sh.cleaned[stage], cleans >> stage & 1, gave_up);
+            cleans ^= 1u << stage;
+            cleaned_to = j + 1;
           }
-          if (!ok) break;
-          release(v_at);
-          if (j + 1 < n) {
-            release(k_at);
-            if (j + 2 == n) queries_used();
+          if (weigh) {
+            ok = ok && values(w, v_at, j >= (two ? 1 : 2));
+            if (ok && (w == 1 || !two)) release(v_at);
           }
-        }
-      } else {
-        uint32_t at = used;
-#pragma unroll 1
-        for (int w = 0; ok && w < min(n, 2); ++w, ++at) {
-          ok = full(at);
-          if (!ok) break;
-          scores(w, at, false);
-          release(at);
-        }
-        if (n <= 2 && ok) queries_used();
-#pragma unroll 1
-        for (int j = 0; ok && j < n; ++j) {
-          const int w = j & 1;
-          ok = full(at) && values(w, at, j >= 2);
-          if (!ok) break;
-          release(at++);
-          if (j + 2 < n) {
-            ok = full(at);
-            if (!ok) break;
-            scores(w, at, false);
-            release(at++);
-            if (j + 3 == n) queries_used();
+          if (score && ok) {
+            scores(w, k_at, two);
+            if (w == 1 || !two) {
+              release(k_at);
+              if (next == n - 1) queries_used();
+            }
           }
         }
       }
@@ -341,7 +351,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
     const int w = warp >> 2, r = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 rows of tensor memory
     const uint32_t s_at = tmem + lanes + 128 * w;
-    uint32_t used = 0, s_uses = 0, pv[2] = {0, 0};
+    uint32_t s_uses = 0, pv[2] = {0, 0};
     const float scale = p.scale_log2;
     uint32_t joins = 0;
     const auto join = [&] {  // both groups are here
@@ -368,13 +378,6 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       const int hidden_from = max(im.behind + im.row0 / p.group + 1, 0);     // first key hidden from a row of the item
       const bool live = __any_sync(0xFFFFFFFFu, valid);                      // else nobody reads the warp's rows
       const int tiles = two ? (w ? im.n1 : im.n0) : (n + 1 - w) / 2;
-      const auto clean = [&](int j, int key0) {
-        const uint32_t place = used + value_place(two, j, n), stage = ring_stage(place, kStages);
-        if (!warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up)) return false;
-        clean_values<kHalves>(ring + stage * S::kTileBytes, max(hidden_from - key0, 0), im.kend - key0,
-                              &sh.bad_values[number & 1], (int)number);
-        return true;
-      };
       float m = -INFINITY, l = 0.f;
       bool ok = true;
 #pragma unroll 1
@@ -385,30 +388,37 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
         ok = warp_wait(sh.s_full[w], s_uses++ & 1, gave_up);
         if (!ok) break;
         if (live) {
+          // columns up to `seen` are seen by every row of the warp (that counts), none from `upto` on by any
+          const int last = newest - key0;
+          int seen = kKeyTile, upto = kKeyTile;
+          if (masked) {
+            seen = __reduce_min_sync(0xFFFFFFFFu, valid ? last : kKeyTile);
+            upto = min(__reduce_max_sync(0xFFFFFFFFu, valid ? last : -1) + 1, kKeyTile);
+          }
           // Loops over quarters of the row, not unrolled: the warps of a group run through them together out of the
           // instruction caches, which the unrolled 128 columns overflow (single tokens 102 -> @@ us).
           tmem_fence_after();
           float peak = -INFINITY;
-#pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
+          // (tiles with hidden keys have loops of their own: branches in the ordinary ones cost 6 % of the kernel)
+          const auto highest = [&](int c, auto hiding) {
             uint32_t x[32];
             tmem_load(x, s_at + 32 * c);
             tmem_wait_load();
             tmem_ready(x);
-            if (masked) {
-              const int last = newest - key0 - 32 * c;
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (e > last) x[e] = 0xFF800000u;  // -inf, whatever was there
-              tmem_store(s_at + 32 * c, x);
-            }
+            if (decltype(hiding)::value && 32 * c + 31 > seen) hide(x, last - 32 * c);
             float top[4] = {peak, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int e = 0; e < 32; e += 2)
               top[e / 2 % 4] = max3(top[e / 2 % 4], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
             peak = max3(max3(top[0], top[1], top[2]), top[3], -INFINITY);
+          };
+          if (!masked) {
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) highest(c, std::false_type());
+          } else {
+#pragma unroll 1
+            for (int c = 0; 32 * c < upto; ++c) highest(c, std::true_type());
           }
-          if (masked) tmem_wait_store();
           // (peak - m) * scale > the limit, also where m is -inf; not where both are
           const bool grow = valid && peak > m && !((peak - m) * scale <= kLazyLog2);
           if (__any_sync(0xFFFFFFFFu, grow)) {
@@ -440,51 +450,64 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
           const float ref = m == -INFINITY ? 0.f : m * scale;
           const uint64_t scales = pair(scale, scale), refs = pair(-ref, -ref);
           uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
+          const auto weigh = [&](int c, auto hiding) {
             uint32_t x[32], packed[16];
             tmem_load(x, s_at + 32 * c);  // (weights go where scores have been read: 16 columns of every 32)
             tmem_wait_load();
             tmem_ready(x);
+            if (decltype(hiding)::value && 32 * c + 31 > seen) hide(x, last - 32 * c);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
+              const uint64_t t =
+                  fma_pair(pair(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), scales, refs);
               float a, b;
-              unpair(fma_pair(pair(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), scales, refs), a, b);
+              unpair(t, a, b);
               a = exp2_approx(a);
               b = exp2_approx(b);
               sum[e & 1] = add_pair(sum[e & 1], pair(a, b));
               packed[e] = pack_bf16(a, b);
             }
             tmem_store(s_at + 16 * c, packed);
-            if (c == 2 && !masked) {  // three quarters of the weights go ahead: their product runs during the last one
-              tmem_wait_store();
-              tmem_fence_before();
-              __syncwarp();
-              if (lane == 0) barrier_arrive(shared_address(&sh.p_most[w]));
+          };
+          const auto hand_over = [&](uint64_t& bar) {
+            tmem_wait_store();
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) barrier_arrive(shared_address(&bar));
+          };
+          // three quarters of the weights go ahead: their product runs during the last one
+          if (!masked) {
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              weigh(c, std::false_type());
+              if (c == 2) hand_over(sh.p_most[w]);
+            }
+          } else {
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              if (32 * c < upto) {
+                weigh(c, std::true_type());
+              } else {
+                uint32_t none[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) none[e] = 0u;
+                tmem_store(s_at + 16 * c, none);
+              }
+              if (c == 2) hand_over(sh.p_most[w]);
             }
           }
           float a, b;
           unpair(add_pair(sum[0], sum[1]), a, b);
           l += a + b;
           if (!(peak < INFINITY)) l = NAN;  // a NaN or infinity among the scores: the softmax of the row is NaN
-          tmem_wait_store();
-        } else if (!masked && lane == 0) {
+          hand_over(sh.p_full[w]);
+        } else if (lane == 0) {
           barrier_arrive(shared_address(&sh.p_most[w]));
-        }
-        if (masked && !clean(j, key0)) {
-          ok = false;
-          break;
-        }
-        tmem_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          if (masked) barrier_arrive(shared_address(&sh.p_most[w]));
           barrier_arrive(shared_address(&sh.p_full[w]));
         }
         ++pv[w];
       }
       if (!ok) break;
-      used += 2 * n;
 
       // ---- the rows' results ----
       pv[w ^ 1] += two ? (w ? im.n0 : im.n1) : (n + 1 - (w ^ 1)) / 2;  // the other group's products
@@ -516,7 +539,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       if (two ? mine && w == 1 : others) ok = ok && warp_wait(sh.o_full[1], (pv[1] - 1) & 1, gave_up);
       if (!ok) break;
       tmem_fence_after();
-      const bool repair = *(volatile int*)&sh.bad_values[number & 1] == (int)number;
+      const bool repair = *(volatile int*)&sh.bad_values[number & 7] == (int)number;
 #pragma unroll 1
       for (int c = c0; c < c0 + width; c += 32) {
         float o[32];
