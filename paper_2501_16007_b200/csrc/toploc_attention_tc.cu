@@ -395,8 +395,9 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
             seen = __reduce_min_sync(0xFFFFFFFFu, valid ? last : kKeyTile);
             upto = min(__reduce_max_sync(0xFFFFFFFFu, valid ? last : -1) + 1, kKeyTile);
           }
-          // Loops over quarters of the row, not unrolled: the warps of a group run through them together out of the
-          // instruction caches, which the unrolled 128 columns overflow (single tokens 102 -> @@ us).
+          // Loops over quarters of the row, not unrolled, the scores read twice: unrolled code for 128 columns takes as
+          // long where tiles are many and overflows the instruction caches where they are few (short prompts 47 us so,
+          // 51 us with half of the row kept in registers).
           tmem_fence_after();
           float peak = -INFINITY;
           // (tiles with hidden keys have loops of their own: branches in the ordinary ones cost 6 % of the kernel)
@@ -620,59 +621,65 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
 // Block (b, y) looks after the row tile that block b of the first kernel began and did not finish: its parts are that
 // block's slot 1 and slot 0 of the next ones up to the one that finished it.  Part i has out_i = sum p v / sum p and
 // lse_i over its keys; the whole is sum_i w_i out_i / sum_i w_i, w_i = 2^(lse_i - max).  A warp per row, parts in order.
-constexpr int kJoinRows = 8;  // rows of a block
+constexpr int kJoinRows = 8, kJoinThreads = 256;  // rows of a block: one a warp
 
 template <int D>
-__global__ void __launch_bounds__(128) toploc_attention_tc_join_kernel(const __grid_constant__ TcParams tp) {
+__global__ void __launch_bounds__(kJoinThreads) toploc_attention_tc_join_kernel(const __grid_constant__ TcParams tp) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const AttentionParams& p = tp.p;
   const int b = blockIdx.x, lane = threadIdx.x & 31, rows_item = tp.item_rows;
   const Part part = tp.parts[2 * b + 1];
   if (part.seq < 0) return;
-  int end = b + 1;  // the last block with a part
-  while (end < (int)gridDim.x - 1 && tp.parts[2 * end].seq >= 0 && !tp.parts[2 * end].last) ++end;
-  const int begin_row = blockIdx.y * kJoinRows + (threadIdx.x >> 5);
-  for (int r = begin_row; r < (int)(blockIdx.y + 1) * kJoinRows; r += 4) {
-    const int row = part.row0 + r;
-    if (r >= rows_item || row >= part.rows) break;
-    const auto place = [&](int i) { return (long long)(i == b ? 2 * b + 1 : 2 * i) * rows_item + r; };
-    float top = -INFINITY;
-    for (int i = b + lane; i <= end; i += 32) top = fmaxf(top, p.part_lse[place(i)]);
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, off));
-    const float ref = top == -INFINITY ? 0.f : top;
-    // 16 bytes a lane: D / 4 lanes cover a row, so a warp takes 128 / D parts at once, and several in flight
-    constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes;
-    float sum = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int i = b + lane / kLanes; i <= end; i += kAtOnce) {
-      const float w = exp2f(p.part_lse[place(i)] - ref);
-      const float4 from = *reinterpret_cast<const float4*>(p.part_out + place(i) * D + lane % kLanes * 4);
-      sum += w;
-      if (w != 0.f) {
-        o.x = fmaf(w, from.x, o.x);
-        o.y = fmaf(w, from.y, o.y);
-        o.z = fmaf(w, from.z, o.z);
-        o.w = fmaf(w, from.w, o.w);
-      }
-    }
-    if (kAtOnce == 2) {
-      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
-      o.x += __shfl_xor_sync(0xFFFFFFFFu, o.x, 16);
-      o.y += __shfl_xor_sync(0xFFFFFFFFu, o.y, 16);
-      o.z += __shfl_xor_sync(0xFFFFFFFFu, o.z, 16);
-      o.w += __shfl_xor_sync(0xFFFFFFFFu, o.w, 16);
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int token = row / p.group, head = part.head * p.group + row - token * p.group;
-    if (lane < kLanes) {
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + (part.first + token) * p.out_token + head * p.out_head;
-      reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-    }
-    if (p.lse && lane == 0)
-      p.lse[(long long)(part.first + token) * p.q_heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+  // the last block with a part: 32 at a time
+  int end = b;
+  for (bool more = true; more;) {
+    const int i = end + 1 + lane;
+    const bool stop = i >= (int)gridDim.x || tp.parts[2 * i].seq < 0 || tp.parts[2 * i].last;
+    const unsigned stops = __ballot_sync(0xFFFFFFFFu, stop);
+    more = stops == 0;
+    end += more ? 32 : __ffs(stops);
   }
+  end = min(end, (int)gridDim.x - 1);
+  const int r = blockIdx.y * kJoinRows + (threadIdx.x >> 5), row = part.row0 + r;
+  if (r >= rows_item || row >= part.rows) return;
+  // 16 bytes a lane: D / 4 lanes cover a row, so a warp takes 128 / D parts at once, and eight of those in flight (nothing
+  // is loaded that waits for another load: the maximum runs along)
+  constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes;
+  const auto place = [&](int i) { return (long long)(i == b ? 2 * b + 1 : 2 * i) * rows_item + r; };
+  float top = -INFINITY, sum = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  const auto add = [&](float lse, float4 from) {
+    const float now = fmaxf(top, lse), ref = now == -INFINITY ? 0.f : now;
+    const float shrink = exp2f(top - ref), w = exp2f(lse - ref);
+    top = now;
+    sum = fmaf(sum, shrink, w);
+    o.x = fmaf(o.x, shrink, w * from.x);
+    o.y = fmaf(o.y, shrink, w * from.y);
+    o.z = fmaf(o.z, shrink, w * from.z);
+    o.w = fmaf(o.w, shrink, w * from.w);
+  };
+#pragma unroll 8
+  for (int i = b + lane / kLanes; i <= end; i += kAtOnce)
+    add(p.part_lse[place(i)], *reinterpret_cast<const float4*>(p.part_out + place(i) * D + lane % kLanes * 4));
+  if (kAtOnce == 2) {  // the other half's parts, in the same order for both
+    const float other_top = __shfl_xor_sync(0xFFFFFFFFu, top, 16), other_sum = __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
+    const float4 other = make_float4(__shfl_xor_sync(0xFFFFFFFFu, o.x, 16), __shfl_xor_sync(0xFFFFFFFFu, o.y, 16),
+                                     __shfl_xor_sync(0xFFFFFFFFu, o.z, 16), __shfl_xor_sync(0xFFFFFFFFu, o.w, 16));
+    const float now = fmaxf(top, other_top), ref = now == -INFINITY ? 0.f : now;
+    const float mine = exp2f(top - ref), theirs = exp2f(other_top - ref);
+    top = now;
+    sum = sum * mine + other_sum * theirs;
+    o = make_float4(o.x * mine + other.x * theirs, o.y * mine + other.y * theirs, o.z * mine + other.z * theirs,
+                    o.w * mine + other.w * theirs);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int token = row / p.group, head = part.head * p.group + row - token * p.group;
+  if (lane < kLanes) {
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + (part.first + token) * p.out_token + head * p.out_head;
+    reinterpret_cast<uint2*>(out)[lane] = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+  }
+  if (p.lse && lane == 0)
+    p.lse[(long long)(part.first + token) * p.q_heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -713,7 +720,7 @@ int launch_join(const TcParams& tp, int blocks, cudaStream_t stream) {
   if (blocks == 1) return TOPLOC_OK;
   cudaLaunchConfig_t config = {};
   config.gridDim = dim3((unsigned)blocks, (unsigned)((tp.item_rows + kJoinRows - 1) / kJoinRows));
-  config.blockDim = dim3(128);
+  config.blockDim = dim3(kJoinThreads);
   config.stream = stream;
   cudaLaunchAttribute early;
   early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
