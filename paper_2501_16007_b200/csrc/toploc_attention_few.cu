@@ -447,9 +447,8 @@ template <int D, int R>
 int launch(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int blocks,
            cudaStream_t stream) {
   constexpr int kBytes = FewShared<D, R < 16 ? 16 : R>::kBytes;
-  if (cudaFuncSetAttribute(toploc_attention_few_kernel<D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) !=
-      cudaSuccess)
-    return TOPLOC_ERR_CUDA;
+  static std::atomic<uint64_t> allowed{0};
+  if (const int rc = allow_shared(reinterpret_cast<const void*>(toploc_attention_few_kernel<D, R>), kBytes, allowed)) return rc;
   toploc_attention_few_kernel<D, R><<<blocks, kFewThreads, kBytes, stream>>>(tp, q, k, v);
   return launched();
 }

@@ -527,7 +527,9 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
         if (a.y != a.y || b.y != b.y) total = NAN;  // a NaN score leaves no trace in a maximum
       }
       const bool any_keys = total != 0.f;
+      // 1 / sum, with the groups' weights; 0 where their outputs do not count (and may be anything)
       const float inv = any_keys ? reciprocal(total) : 0.f;
+      const float factor[2] = {weight[0] * inv, weight[1] * inv};
       const int head = im.head * p.group + row - token * p.group;
       const long long at = (long long)(im.first + token) * p.q_heads + head;
       // where the row's part of a split tile goes
@@ -544,27 +546,28 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
 #pragma unroll 1
       for (int c = c0; c < c0 + width; c += 32) {
         float o[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = 0.f;
         if (live && mine) {
           uint32_t x[32];
           tmem_load(x, o_at + c);
           tmem_wait_load();
           tmem_ready(x);
+          if (factor[0] != 0.f) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = weight[0] == 0.f ? 0.f : __uint_as_float(x[e]) * weight[0];
+            for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(x[e]) * factor[0];
+          }
           if (others) {
             tmem_load(x, o_at + D + c);
             tmem_wait_load();
             tmem_ready(x);
+            if (factor[1] != 0.f) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (weight[1] != 0.f) o[e] = fmaf(__uint_as_float(x[e]), weight[1], o[e]);
+              for (int e = 0; e < 32; ++e) o[e] = fmaf(__uint_as_float(x[e]), factor[1], o[e]);
+            }
           }
         }
         if (!valid) continue;
-        if (!any_keys) {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
-        }
         if (repair) {  // values that were taken out of tiles with hidden keys: back to the rows that see them
           float copy[32];
 #pragma unroll
@@ -576,7 +579,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
         if (im.slot < 0) {
           uint32_t packed[16];
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) packed[e / 2] = pack_bf16(o[e] * inv, o[e + 1] * inv);
+          for (int e = 0; e < 32; e += 2) packed[e / 2] = pack_bf16(o[e], o[e + 1]);
           __nv_bfloat16* out =
               static_cast<__nv_bfloat16*>(p.out) + (im.first + token) * p.out_token + head * p.out_head + c;
           if (tp.wide_out) {
@@ -591,7 +594,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
         } else {
           uint32_t words[32];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) words[e] = __float_as_uint(o[e] * inv);
+          for (int e = 0; e < 32; ++e) words[e] = __float_as_uint(o[e]);
 #pragma unroll
           for (int e = 0; e < 32; e += 8) store_32_bytes(p.part_out + part * D + c + e, words + e);
         }
@@ -734,9 +737,8 @@ template <int D>
 int launch(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int blocks,
            cudaStream_t stream) {
   constexpr int kBytes = Shared<D>::kBytes;
-  if (cudaFuncSetAttribute(toploc_attention_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) !=
-      cudaSuccess)
-    return TOPLOC_ERR_CUDA;
+  static std::atomic<uint64_t> allowed{0};
+  if (const int rc = allow_shared(reinterpret_cast<const void*>(toploc_attention_tc_kernel<D>), kBytes, allowed)) return rc;
   toploc_attention_tc_kernel<D><<<blocks, kTcThreads, kBytes, stream>>>(tp, q, k, v);
   return launched();
 }

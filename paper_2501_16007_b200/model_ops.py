@@ -185,9 +185,9 @@ def _attention_layout(q, kv_heads, num_seqs, max_new_tokens, scale, out, lse):
     _need(out.shape == q.shape and out.dtype == q.dtype and out.stride(2) == 1, "out must have q's shape and type")
     _need(lse is None or (lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous()),
           "lse must be a contiguous float32 [tokens, q_heads]")
+    (qt, qh, _), (ot, oh, _) = q.stride(), out.stride()
     return ToplocAttentionLayout(_DTYPES[q.dtype], dim, heads, kv_heads, num_seqs, max_new_tokens, tokens,
-                                 dim ** -0.5 if scale is None else scale, 0, q.stride(0), q.stride(1), out.stride(0),
-                                 out.stride(1))
+                                 dim ** -0.5 if scale is None else scale, 0, qt, qh, ot, oh)
 
 
 def _attention_workspace(lib, lay_p, kv_p, workspace, dev):
