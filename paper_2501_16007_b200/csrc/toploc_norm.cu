@@ -56,8 +56,9 @@ __device__ __forceinline__ float scale_of(float amax) {
 // Bound by memory: x and residual are read once, residual_out and y written once.  A block takes a row and keeps it in
 // registers between the two passes, 16 bytes an access where rows allow it.  What has to be in flight on an SM (50 KB and
 // more) comes from its many threads, not from many values a thread: 16 values a thread and 32 registers (2048 threads an
-// SM) take 620 us for 65536 x 8192 bf16 with e4m3 groups of 128 (6.1 TB/s), 32 values 715 us.  Rows that are no vectors:
-// 1024 threads of up to 8 values (4095 x 5001 fp32: 64 us, with 32 values 135).
+// SM) take 620 us for 65536 x 8192 bf16 with e4m3 groups of 128 (6.1 TB/s), 32 values 715 us.  Rows that begin
+// anywhere (an odd hidden size) move as vectors too where all tensors share the odd place (4095 x 5001 fp32: 62 us, 5.3
+// TB/s; element by element 78 us, with 32 values a thread 135 us).
 //
 // kVec elements an access, kPer accesses a thread, access v of a row to thread v % threads.
 enum Mode { kSame, kRowScale, kGroupScale };
@@ -108,8 +109,34 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, const float* v) {
   }
 }
 
-template <typename T, int kVec, int kPer, Mode kMode>
-__global__ void __launch_bounds__(kVec > 1 || kPer > 8 ? 512 : 1024, kVec * kPer > 16 ? 1 : kVec > 1 ? 4 : kPer <= 5 ? 2 : 1)
+// Access of kVec elements from c on of a row of `hidden`, which may begin in front of the row or end behind it (kShift).
+template <typename T, int kVec, bool kShift>
+__device__ __forceinline__ void load_part(const T* p, int c, int hidden, float* v) {
+  if (!kShift || (c >= 0 && c + kVec <= hidden)) {
+    load_values<T, kVec>(p + c, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) v[e] = c + e >= 0 && c + e < hidden ? to_float(p[c + e]) : 0.f;
+  }
+}
+
+template <typename T, int kVec, bool kShift>
+__device__ __forceinline__ void store_part(T* p, int c, int hidden, const float* v) {
+  if (!kShift || (c >= 0 && c + kVec <= hidden)) {
+    store_values<T, kVec>(p + c, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e)
+      if (c + e >= 0 && c + e < hidden) store_as(p + c + e, v[e]);
+  }
+}
+
+// kShift: rows that do not begin at a vector's place, but all tensors' rows at the same distance from one: the accesses
+// are laid from that place on, the first and the last partly outside (the weights, whose rows begin elsewhere, are read
+// element by element).
+template <typename T, int kVec, int kPer, Mode kMode, bool kShift>
+__global__ void __launch_bounds__(kVec > 1 || kPer > 8 ? 512 : 1024,
+                                  kVec * kPer > 16 ? 1 : kShift ? 2 : kVec > 1 ? 4 : kPer <= 5 ? 2 : 1)
     toploc_rmsnorm_rows_kernel(const NormParams p) {
   __shared__ float partial[32], partial_max[32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
@@ -118,21 +145,23 @@ __global__ void __launch_bounds__(kVec > 1 || kPer > 8 ? 512 : 1024, kVec * kPer
   const T* r = static_cast<const T*>(p.residual) + row * p.residual_stride;
   T* ro = static_cast<T*>(p.residual_out) + row * p.residual_out_stride;
   const T* w = static_cast<const T*>(p.weight);
+  // elements in front of the row in its first access
+  const int shift = kShift ? (int)((reinterpret_cast<uintptr_t>(x) / sizeof(T)) % kVec) : 0;
   float h[kPer][kVec];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int c = (tid + i * threads) * kVec;
+    const int c = (tid + i * threads) * kVec - shift;
 #pragma unroll
     for (int e = 0; e < kVec; ++e) h[i][e] = 0.f;
-    if (c < p.hidden) load_values<T, kVec>(x + c, h[i]);
+    if (c < p.hidden) load_part<T, kVec, kShift>(x, c, p.hidden, h[i]);
   }
   if (p.residual) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int c = (tid + i * threads) * kVec;
+      const int c = (tid + i * threads) * kVec - shift;
       if (c < p.hidden) {
         float v[kVec];
-        load_values<T, kVec>(r + c, v);
+        load_part<T, kVec, kShift>(r, c, p.hidden, v);
 #pragma unroll
         for (int e = 0; e < kVec; ++e) h[i][e] += v[e];
       }
@@ -148,8 +177,8 @@ __global__ void __launch_bounds__(kVec > 1 || kPer > 8 ? 512 : 1024, kVec * kPer
   if (p.residual_out) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int c = (tid + i * threads) * kVec;
-      if (c < p.hidden) store_values<T, kVec>(ro + c, h[i]);
+      const int c = (tid + i * threads) * kVec - shift;
+      if (c < p.hidden) store_part<T, kVec, kShift>(ro, c, p.hidden, h[i]);
     }
   }
   __syncthreads();
@@ -157,10 +186,15 @@ __global__ void __launch_bounds__(kVec > 1 || kPer > 8 ? 512 : 1024, kVec * kPer
   const float scale = rsqrtf(fmaf(total, p.per_channel, p.eps));
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int c = (tid + i * threads) * kVec;
+    const int c = (tid + i * threads) * kVec - shift;
     if (c < p.hidden) {
       float v[kVec];
-      load_values<T, kVec>(w + c, v);
+      if constexpr (kShift) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = c + e >= 0 && c + e < p.hidden ? to_float(w[c + e]) : 0.f;
+      } else {
+        load_values<T, kVec>(w + c, v);
+      }
 #pragma unroll
       for (int e = 0; e < kVec; ++e) h[i][e] = h[i][e] * scale * v[e];
     }
@@ -169,8 +203,8 @@ __global__ void __launch_bounds__(kVec > 1 || kPer > 8 ? 512 : 1024, kVec * kPer
     T* y = static_cast<T*>(p.y) + row * p.y_stride;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int c = (tid + i * threads) * kVec;
-      if (c < p.hidden) store_values<T, kVec>(y + c, h[i]);
+      const int c = (tid + i * threads) * kVec - shift;
+      if (c < p.hidden) store_part<T, kVec, kShift>(y, c, p.hidden, h[i]);
     }
   } else {
     uint8_t* y = static_cast<uint8_t*>(p.y) + row * p.y_stride;
@@ -272,23 +306,25 @@ int launch_any(const NormParams& p, cudaStream_t stream) {
 }
 
 template <typename T, int kVec, int kPer>
-int launch_rows(const NormParams& p, Mode mode, int threads, cudaStream_t stream) {
+int launch_rows(const NormParams& p, Mode mode, bool shifted, int threads, cudaStream_t stream) {
   const unsigned rows = (unsigned)p.rows;
-  if (mode == kSame)
-    toploc_rmsnorm_rows_kernel<T, kVec, kPer, kSame><<<rows, threads, 0, stream>>>(p);
+  if (kVec > 1 && shifted)
+    toploc_rmsnorm_rows_kernel<T, kVec, kPer, kSame, (kVec > 1)><<<rows, threads, 0, stream>>>(p);
+  else if (mode == kSame)
+    toploc_rmsnorm_rows_kernel<T, kVec, kPer, kSame, false><<<rows, threads, 0, stream>>>(p);
   else if (mode == kRowScale)
-    toploc_rmsnorm_rows_kernel<T, kVec, kPer, kRowScale><<<rows, threads, 0, stream>>>(p);
+    toploc_rmsnorm_rows_kernel<T, kVec, kPer, kRowScale, false><<<rows, threads, 0, stream>>>(p);
   else
-    toploc_rmsnorm_rows_kernel<T, kVec, kPer, kGroupScale><<<rows, threads, 0, stream>>>(p);
+    toploc_rmsnorm_rows_kernel<T, kVec, kPer, kGroupScale, false><<<rows, threads, 0, stream>>>(p);
   return launched();
 }
 
 // The row in registers where it fits 512 threads of 32 values (and a group's lanes are neighbours), else in shared
 // memory.
 template <typename T>
-int launch(NormParams& p, bool quant, bool vectors, cudaStream_t stream) {
+int launch(NormParams& p, bool quant, bool vectors, bool shifted, cudaStream_t stream) {
   constexpr int kWide = 16 / sizeof(T);
-  const int vec = vectors ? kWide : 1, accesses = (p.hidden + vec - 1) / vec;
+  const int vec = vectors || shifted ? kWide : 1, accesses = (p.hidden + (shifted ? vec - 1 : 0) + vec - 1) / vec;
   const Mode mode = !quant ? kSame : p.groups == 1 ? kRowScale : kGroupScale;
   const int lanes = p.group / vec;  // of a group
   const bool fits = accesses <= 512 * (32 / vec) &&
@@ -296,28 +332,28 @@ int launch(NormParams& p, bool quant, bool vectors, cudaStream_t stream) {
   if (!fits) return quant ? launch_any<T, true>(p, stream) : launch_any<T, false>(p, stream);
   while (1 << p.group_shift < lanes && p.group_shift < 5) ++p.group_shift;
   int per = 1;
-  if (vectors) {
+  if (vec > 1) {
     while (per * 512 < accesses) per *= 2;
   } else {
     for (const int more : {2, 3, 5, 8, 32})
       if (per * (per > 8 ? 512 : 1024) < accesses) per = more;
   }
   const int threads = ((accesses + per - 1) / per + 31) / 32 * 32;
-  if (vectors) {
+  if (vec > 1) {
     switch (per) {
-      case 1: return launch_rows<T, kWide, 1>(p, mode, threads, stream);
-      case 2: return launch_rows<T, kWide, 2>(p, mode, threads, stream);
-      case 4: return launch_rows<T, kWide, 4>(p, mode, threads, stream);
-      default: return launch_rows<T, kWide, 32 / kWide>(p, mode, threads, stream);
+      case 1: return launch_rows<T, kWide, 1>(p, mode, shifted, threads, stream);
+      case 2: return launch_rows<T, kWide, 2>(p, mode, shifted, threads, stream);
+      case 4: return launch_rows<T, kWide, 4>(p, mode, shifted, threads, stream);
+      default: return launch_rows<T, kWide, 32 / kWide>(p, mode, shifted, threads, stream);
     }
   }
   switch (per) {
-    case 1: return launch_rows<T, 1, 1>(p, mode, threads, stream);
-    case 2: return launch_rows<T, 1, 2>(p, mode, threads, stream);
-    case 3: return launch_rows<T, 1, 3>(p, mode, threads, stream);
-    case 5: return launch_rows<T, 1, 5>(p, mode, threads, stream);
-    case 8: return launch_rows<T, 1, 8>(p, mode, threads, stream);
-    default: return launch_rows<T, 1, 32>(p, mode, threads, stream);
+    case 1: return launch_rows<T, 1, 1>(p, mode, shifted, threads, stream);
+    case 2: return launch_rows<T, 1, 2>(p, mode, shifted, threads, stream);
+    case 3: return launch_rows<T, 1, 3>(p, mode, shifted, threads, stream);
+    case 5: return launch_rows<T, 1, 5>(p, mode, shifted, threads, stream);
+    case 8: return launch_rows<T, 1, 8>(p, mode, shifted, threads, stream);
+    default: return launch_rows<T, 1, 32>(p, mode, shifted, threads, stream);
   }
 }
 
@@ -352,6 +388,13 @@ extern "C" int toploc_rmsnorm_residual(const void* d_x, const void* d_residual_o
   if (d_residual_opt) vectors = vectors && p.residual_stride % per == 0 && aligned(d_residual_opt, 16);
   if (d_residual_out_opt) vectors = vectors && p.residual_out_stride % per == 0 && aligned(d_residual_out_opt, 16);
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  return lay->dtype == TOPLOC_DTYPE_BF16 ? launch<__nv_bfloat16>(p, quant, vectors, stream)
-                                         : launch<float>(p, quant, vectors, stream);
+  // rows that begin anywhere, but all tensors' rows at the same distance from a vector's place (one unaligned stride)
+  const auto away = [&](const void* at, int64_t stride) {
+    return !at || (reinterpret_cast<uintptr_t>(at) % 16 == reinterpret_cast<uintptr_t>(d_x) % 16 &&
+                   (stride - p.x_stride) % per == 0);
+  };
+  const bool shifted = !vectors && !quant && p.hidden >= 256 && away(d_residual_opt, p.residual_stride) &&
+                       away(d_residual_out_opt, p.residual_out_stride) && away(d_y, p.y_stride);
+  return lay->dtype == TOPLOC_DTYPE_BF16 ? launch<__nv_bfloat16>(p, quant, vectors, shifted, stream)
+                                         : launch<float>(p, quant, vectors, shifted, stream);
 }

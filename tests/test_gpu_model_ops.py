@@ -445,7 +445,8 @@ def norm_reference(x, r, w, eps):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("rows,hidden,pad", [(1, 1, 0), (3, 7, 0), (64, 4096, 0), (5, 8192, 8), (9, 5001, 1),
-                                             (2, 1000, 24), (33, 128, 0), (2, 49152, 0), (4, 12296, 0), (700, 2048, 0)])
+                                             (2, 1000, 24), (33, 128, 0), (2, 49152, 0), (4, 12296, 0), (700, 2048, 0),
+                                             (33, 5001, 0), (3, 16381, 0), (5, 257, 0), (4, 8193, 0)])
 @pytest.mark.parametrize("group", [None, 0, 128, 48])
 def test_norm(dtype, rows, hidden, pad, group):
     g = generator(rows + hidden)
