@@ -340,6 +340,62 @@ def test_paged_hidden_keys_have_no_influence(bad, dtype):
     assert (torch.isnan(seen) if bad != bad else (seen == bad)).all()
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_paged_hidden_keys_few_rows(dim):
+    """The same where a sequence brings few rows."""
+    g = generator(17)
+    caches, table, contents = build_cache(g, [150], 2, dim, 16, torch.bfloat16)
+    q = normal(g, 4, 8, dim)
+    for which, token in ((0, 149), (1, 148)):
+        contents[0][which][token, :, 5] = float("nan")
+        caches[which][int(table[0, token // 16]), token % 16, :, 5] = float("nan")
+    out, lse = tl.toploc_attention_paged(q, *caches, table, ints([0, 4]), ints([150]), 4, want_lse=True)
+    torch.cuda.synchronize()
+    k, v = (torch.nan_to_num(t) for t in contents[0])
+    clean = attention_reference(q[:3], k, v, 0, 146, dim ** -0.5)
+    others = [c for c in range(dim) if c != 5]
+    assert_near(lse[:3], clean[1], clean[3], "lse")
+    assert_near(out[:3][..., others], clean[0][..., others], clean[2][..., others], "other channels")
+    assert_near(out[:2, :, 5], clean[0][:2, :, 5], clean[2][:2, :, 5], "rows in front of it")
+    assert torch.isnan(out[2, :, 5]).all() and torch.isnan(out[3]).all() and torch.isnan(lse[3]).all()
+
+
+def test_paged_few_rows_without_keys():
+    check_paged([0, 5, 1, 3], [1, 2, 2, 0], 8, 2, 128, 16, torch.bfloat16)
+    check_paged([0, 5, 1, 3], [1, 4, 6, 0], 4, 4, 64, 32, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dim,heads,kv_heads,dtype", [(128, 16, 2, torch.bfloat16), (64, 8, 2, torch.bfloat16),
+                                                      (128, 8, 2, torch.float32)])
+def test_paged_mixture(dim, heads, kv_heads, dtype):
+    """Long and short, many rows and one, idle ones between: cuts of the work fall anywhere."""
+    check_paged([3000, 70, 1025, 0, 129, 2500], [64, 1, 7, 0, 33, 20], heads, kv_heads, dim, 16, dtype)
+    check_paged([4000, 1, 999, 64, 2222], [3, 1, 2, 0, 1], heads, kv_heads, dim, 64, dtype)
+
+
+def test_paged_cache_beyond_32_bits():
+    """Pages whose elements, and slots, lie past 2^31 elements and 2^32 bytes of a cache."""
+    page, heads, dim = 16, 8, 128
+    pages = (1 << 31) // (page * heads * dim) + 3000
+    caches = [torch.empty((pages, page, heads, dim), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    g = generator(23)
+    kv, new = 100, 100
+    k, v, q = normal(g, kv, heads, dim), normal(g, kv, heads, dim), normal(g, kv, 16, dim)
+    chosen = [pages - 1, 5, pages - 2000, pages - 7, 0, pages - 3, 77]
+    table = ints([chosen]).view(1, -1)
+    at = torch.arange(kv, device=DEV)
+    slots = table[0, at // page].to(torch.int64) * page + at % page
+    tl.toploc_cache_write(k, v, slots, *caches)
+    for cache, rows in zip(caches, (k, v)):
+        assert torch.equal(cache[pages - 1, 0], rows[0]) and torch.equal(cache[pages - 2000, 3], rows[2 * page + 3])
+    for tokens in (new, 1):
+        out, lse = tl.toploc_attention_paged(q[-tokens:], *caches, table, ints([0, tokens]), ints([kv]), tokens,
+                                             want_lse=True)
+        want = attention_reference(q[-tokens:], k, v, 0, kv - tokens, dim ** -0.5)
+        assert_near(out, want[0], want[2], "out")
+        assert_near(lse, want[1], want[3], "lse")
+
+
 def test_paged_promises_that_are_not_kept():
     """Lengths over their bounds and pages outside the cache: flagged, nothing outside is read, the others are right."""
     g = generator(5)
@@ -388,6 +444,11 @@ def check_prompt(lens, heads, kv_heads, dim, dtype, fused=True, pad=0, seed=0, m
 @pytest.mark.parametrize("heads,kv_heads", [(4, 1), (2, 2), (6, 2)])
 def test_prompt_lengths(dtype, dim, heads, kv_heads):
     check_prompt([1, 0, 33, 128, 2, 129, 64], heads, kv_heads, dim, dtype)
+
+
+def test_prompt_long():
+    check_prompt([900, 1, 1500], 4, 2, 128, torch.bfloat16)
+    check_prompt([1300, 300], 6, 1, 64, torch.bfloat16)
 
 
 def test_prompt_layouts():
