@@ -42,7 +42,7 @@ struct TcParams {
   int tile_rows;  // packed rows of a row tile: 128 rounded down to whole tokens
   int tile_tokens, item_tokens;  // tokens of a row tile, of an item
   int item_rows;  // packed rows of an item: two tiles (a few rows: all that a sequence can bring)
-  float least_share;  // keys that are worth a block
+  int piece;      // tiles (a power of two): where a block's share is short, row tiles are cut at multiples only
   int box_rows;   // rows of a key copy
   int page_shift, page_tiles;  // pages below a tile: log2 of their size; others: tiles a page
   float share_scale;  // 1 / blocks
@@ -161,7 +161,8 @@ __device__ __forceinline__ void lay_line(const TcParams& tp, float* run_cost) {
 }
 
 // Where the stretches of this block and of the next one begin (lane 0 and 1 of a warp look for one each; all get both).
-// A cut in front of a level's second tile or behind its last but one moves to the level's ends.
+// A cut in front of a level's second tile or behind its last but one moves to the level's ends (so a level of three tiles
+// is never cut).
 struct Stretch {
   Place begin, end;
 };
@@ -172,7 +173,9 @@ __device__ __forceinline__ Stretch find_stretch(const TcParams& tp, const float*
   const int per = (p.num_seqs + kRuns - 1) / kRuns, lane = threadIdx.x & 31;
   const int block = blockIdx.x + min(lane, 1);
   const float all_work = run_cost[kRuns];
-  float at = max(all_work * tp.share_scale, tp.least_share) * (float)block;
+  const float share = all_work * tp.share_scale;
+  const int piece = share >= (float)(4 * kKeyTile * tp.piece) ? 1 : tp.piece;
+  float at = share * (float)block;
   Place place = {p.num_seqs, 0, 0, 0};
   if (at < all_work && block < gridDim.x) {  // (the last block's stretch ends with the line, whatever the rounding)
     int lo = 0, hi = kRuns;                  // run_cost[lo] <= at < run_cost[hi]
@@ -201,7 +204,7 @@ __device__ __forceinline__ Stretch find_stretch(const TcParams& tp, const float*
       }
       at -= line.upto(a);
       const int n = tiles_seen(s, min((a + 1) * tp.item_tokens, s.rows));
-      const int tile = (int)max((at - kLevelCost) * (1.f / kKeyTile) + 0.5f, 0.f);
+      const int near = (int)max((at - kLevelCost) * (1.f / kKeyTile) + 0.5f, 0.f), tile = (near + piece / 2) & -piece;
       place = Place{i, head, a, tile <= 1 ? 0 : tile};
       if (tile > 1 && tile >= n - 1) {
         place.tile = 0;

@@ -633,11 +633,11 @@ __global__ void __launch_bounds__(kJoinThreads) toploc_attention_tc_join_kernel(
   const int b = blockIdx.x, lane = threadIdx.x & 31, rows_item = tp.item_rows;
   const Part part = tp.parts[2 * b + 1];
   if (part.seq < 0) return;
-  // the last block with a part: 32 at a time
+  // the block with the last part, 32 at a time (blocks between may have had nothing to do)
   int end = b;
   for (bool more = true; more;) {
     const int i = end + 1 + lane;
-    const bool stop = i >= (int)gridDim.x || tp.parts[2 * i].seq < 0 || tp.parts[2 * i].last;
+    const bool stop = i >= (int)gridDim.x || (tp.parts[2 * i].seq >= 0 && tp.parts[2 * i].last);
     const unsigned stops = __ballot_sync(0xFFFFFFFFu, stop);
     more = stops == 0;
     end += more ? 32 : __ffs(stops);
@@ -662,8 +662,12 @@ __global__ void __launch_bounds__(kJoinThreads) toploc_attention_tc_join_kernel(
     o.w = fmaf(o.w, shrink, w * from.w);
   };
 #pragma unroll 8
-  for (int i = b + lane / kLanes; i <= end; i += kAtOnce)
-    add(p.part_lse[place(i)], *reinterpret_cast<const float4*>(p.part_out + place(i) * D + lane % kLanes * 4));
+  for (int i = b + lane / kLanes; i <= end; i += kAtOnce) {
+    const bool there = i == b || tp.parts[2 * i].seq >= 0;
+    const float lse = p.part_lse[place(i)];
+    const float4 from = *reinterpret_cast<const float4*>(p.part_out + place(i) * D + lane % kLanes * 4);
+    if (there) add(lse, from);
+  }
   if (kAtOnce == 2) {  // the other half's parts, in the same order for both
     const float other_top = __shfl_xor_sync(0xFFFFFFFFu, top, 16), other_sum = __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
     const float4 other = make_float4(__shfl_xor_sync(0xFFFFFFFFu, o.x, 16), __shfl_xor_sync(0xFFFFFFFFu, o.y, 16),
@@ -785,7 +789,7 @@ int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, 
   tp.item_rows = few ? tp.tile_rows : 2 * tp.tile_rows;
   tp.tile_tokens = tp.tile_rows / p.group;
   tp.item_tokens = tp.item_rows / p.group;
-  tp.least_share = few ? 3.f * kKeyTile : 6.f * kKeyTile;
+  tp.piece = few ? 2 : 4;
   tp.share_scale = 1.f / (float)blocks;
   tp.page_shift = 0;
   while (page >> (tp.page_shift + 1) > 0) ++tp.page_shift;
@@ -810,6 +814,9 @@ int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, 
   const int rc = few ? launch_few_rows(&tp, &q, &k, &v, blocks, stream)
                  : p.head_dim == 128 ? launch<128>(tp, q, k, v, blocks, stream) : launch<64>(tp, q, k, v, blocks, stream);
   if (rc != TOPLOC_OK) return rc;
+  // rows that see three tiles of keys at most are never cut: nothing to join
+  const long long most_keys = page > 0 ? min((long long)kv->max_pages * page, (long long)INT32_MAX) : p.max_new;
+  if (most_keys <= 3 * kKeyTile) return TOPLOC_OK;
   return p.head_dim == 128 ? launch_join<128>(tp, blocks, stream) : launch_join<64>(tp, blocks, stream);
 }
 
