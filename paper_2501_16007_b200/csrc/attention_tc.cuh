@@ -231,9 +231,15 @@ struct Walk {
   SeqRange s = {0, 0, 0, false};
   int s_of = -1;
 
-  __device__ Walk(const TcParams& tp, const Stretch& stretch) : tp(tp), at(stretch.begin), end(stretch.end) {
+  __device__ Walk(const TcParams& tp) : tp(tp), at{0, 0, 0, 0}, end{0, 0, 0, 0} {}
+
+  template <int kRuns>
+  __device__ void begin(const float* run_cost) {
+    const Stretch stretch = find_stretch<kRuns>(tp, run_cost);
+    at = stretch.begin;
+    end = stretch.end;
     if ((threadIdx.x & 31) < 2) tp.parts[2 * blockIdx.x + (threadIdx.x & 31)].seq = -1;
-    __syncwarp();
+    __syncwarp();  // (run_cost has been read: the ring's place is free)
   }
 
   // The next item (seq -1 and false: there is none), the same in every lane; notes the part that it leaves.

@@ -98,66 +98,56 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, sh.tmem, 0);
   constexpr uint32_t kOut = 2 * N;  // scores of tile j at N (j % 2), outputs at 2 N
 
-  if (warp == 4) {
-    // ---- feeding: finds the items, copies queries and keys ----
-    if (lane == 0) {
-      prefetch_map(&map_q);
-      prefetch_map(&map_k);
-      prefetch_map(&map_v);
+  if (warp == 4 || warp == 6) {
+    // ---- feeding: warp 4 finds the items, copies queries and keys, warp 6 values (one code for both: less to fetch) ----
+    const bool keys = warp == 4;
+    Walk walk(tp);
+    if (keys) {
+      if (lane == 0) {
+        prefetch_map(&map_q);
+        prefetch_map(&map_k);
+        prefetch_map(&map_v);
+      }
+      walk.begin<kFewThreads>(run_cost);
     }
-    Walk walk(tp, find_stretch<kFewThreads>(tp, run_cost));
-    __syncwarp();  // run_cost has been read: the ring's place is free
     uint32_t q_uses = 0;
-    Feeder<S> keys(tp, &map_k, sh, ring, gave_up);
+    Feeder<S> feeder(tp, keys ? &map_k : &map_v, sh, ring, gave_up);
 #pragma unroll 1
     for (uint32_t number = 0;; ++number) {
-      const uint32_t slot = number % kItems;
-      if (!warp_wait(sh.item_empty[slot], ((number / kItems) & 1) ^ 1, gave_up)) break;
+      const uint32_t slot = number % kItems, parity = (number / kItems) & 1;
+      if (!warp_wait(keys ? sh.item_empty[slot] : sh.item_full[slot], keys ? parity ^ 1 : parity, gave_up)) break;
       Item im;
-      const bool more = walk.next(im);
+      if (keys)
+        walk.next(im);
+      else
+        im = sh.items[slot];
       im = uniform(im);
-      if (lane == 0) {
-        sh.items[slot] = im;
-        barrier_arrive(shared_address(&sh.item_full[slot]));
-      }
+      if (keys && lane == 0) sh.items[slot] = im;
       __syncwarp();
-      if (!more) break;
-      if (im.n0 == 0) continue;
-      if (!warp_wait(sh.q_empty, (q_uses & 1) ^ 1, gave_up)) break;
-      ++q_uses;
-      if (elect_one()) {
-        const uint32_t bar = shared_address(&sh.q_full);
-        barrier_arrive_expect(bar, tp.q_bytes);
+      if (lane == 0) barrier_arrive(shared_address(keys ? &sh.item_full[slot] : &sh.item_empty[slot]));
+      if (im.seq < 0) break;
+      if (keys && im.n0 > 0) {
+        if (!warp_wait(sh.q_empty, (q_uses & 1) ^ 1, gave_up)) break;
+        ++q_uses;
+        if (elect_one()) {
+          const uint32_t bar = shared_address(&sh.q_full);
+          barrier_arrive_expect(bar, tp.q_bytes);
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h)
-          copy_3d(shared_address(queries + h * N * 128), &map_q, bar, h * 64, im.head * p.group, im.first);
+          for (int h = 0; h < kHalves; ++h)
+            copy_3d(shared_address(queries + h * N * 128), &map_q, bar, h * 64, im.head * p.group, im.first);
+        }
+        __syncwarp();
       }
-      __syncwarp();
-      keys.item(im, im.n0);
+      feeder.item(im, im.n0);
 #pragma unroll 1
-      for (int j = 0; j < im.n0 && keys.fine; ++j) keys.feed(j, key_place(false, j));
-      if (!keys.fine) break;
+      for (int j = 0; j < im.n0 && feeder.fine; ++j)
+        feeder.feed(j, keys ? key_place(false, j) : value_place(false, j, im.n0));
+      if (!feeder.fine) break;
     }
     if (*gave_up) {  // copies in flight have to land before the block ends
       if (q_uses > 0) barrier_drain(shared_address(&sh.q_full), (q_uses - 1) & 1);
-      keys.drain();
+      feeder.drain();
     }
-  } else if (warp == 6) {
-    // ---- feeding: values ----
-    Feeder<S> values(tp, &map_v, sh, ring, gave_up);
-#pragma unroll 1
-    for (uint32_t number = 0;; ++number) {
-      const uint32_t slot = number % kItems;
-      if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
-      const Item im = uniform(sh.items[slot]);
-      __syncwarp();
-      if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
-      if (im.seq < 0) break;
-      values.item(im, im.n0);
-      for (int j = 0; j < im.n0 && values.fine; ++j) values.feed(j, value_place(false, j, im.n0));
-      if (!values.fine) break;
-    }
-    if (*gave_up) values.drain();
   } else if (warp == 5) {
     // ---- products: the whole warp follows, one lane issues ----
     constexpr uint32_t kScores = bf16_product(N, false, false), kValues = bf16_product(N, true, true);

@@ -151,91 +151,75 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, sh.tmem, 0);
   constexpr uint32_t kOut = 256;  // scores of group w at 128 w, outputs at 256 + D w
 
-  if (warp == 8) {
+  if (warp == 8 || warp == 10) {
     lower_registers<kOtherRegisters>();
-    // ---- feeding: finds the items, copies queries, keys and values ----
-    if (lane == 0) {
-      prefetch_map(&map_q);
-      prefetch_map(&map_k);
-      prefetch_map(&map_v);
-    }
-    Walk walk(tp, find_stretch<kTcThreads>(tp, run_cost));
-    __syncwarp();  // run_cost has been read: the ring's place is free
-    uint32_t q_uses = 0;
-    Feeder<S> keys(tp, &map_k, sh, ring, gave_up);
-#pragma unroll 1
-    for (uint32_t number = 0;; ++number) {
-      const uint32_t slot = number % kItems;
-      if (!warp_wait(sh.item_empty[slot], ((number / kItems) & 1) ^ 1, gave_up)) break;
-      Item im;
-      const bool more = walk.next(im);
-      im = uniform(im);
+    // ---- feeding: warp 8 finds the items, copies queries and keys, warp 10 values (one code for both: less to fetch) ----
+    const bool keys = warp == 8;
+    Walk walk(tp);
+    if (keys) {
       if (lane == 0) {
-        sh.items[slot] = im;
-        barrier_arrive(shared_address(&sh.item_full[slot]));
+        prefetch_map(&map_q);
+        prefetch_map(&map_k);
+        prefetch_map(&map_v);
       }
-      __syncwarp();
-      if (!more) break;
-      const int n = item_tiles(im);
-      if (n == 0) continue;
-
-      // queries: each tile in blocks of 64 channels
-      if (!warp_wait(sh.q_empty, (q_uses & 1) ^ 1, gave_up)) break;
-      ++q_uses;
-      const uint32_t q_bar = shared_address(&sh.q_full);
-      if (elect_one()) {
-        const int tiles = im.two ? 2 : 1;
-        barrier_arrive_expect(q_bar, tiles * tp.q_bytes);
-        for (int w = 0; w < tiles; ++w)
-#pragma unroll
-          for (int h = 0; h < kHalves; ++h)
-            copy_3d(shared_address(q_tiles + w * S::kTileBytes + h * kBlockBytes), &map_q, q_bar, h * 64,
-                    im.head * p.group, im.first + im.row0 / tp.item_rows * tp.item_tokens + w * tp.tile_tokens);
-      }
-      __syncwarp();
-
-      keys.item(im, n);
-#pragma unroll 1
-      for (int j = 0; j < n && keys.fine; ++j) keys.feed(j, key_place(im.two, j));
-      if (!keys.fine) break;
+      walk.begin<kTcThreads>(run_cost);
     }
-    if (*gave_up) {  // copies in flight have to land before the block ends
-      if (q_uses > 0) barrier_drain(shared_address(&sh.q_full), (q_uses - 1) & 1);
-      keys.drain();
-    }
-  } else if (warp == 10) {
-    lower_registers<kOtherRegisters>();
-    // ---- feeding: values ----
-    Feeder<S> values(tp, &map_v, sh, ring, gave_up);
+    uint32_t q_uses = 0;
+    Feeder<S> feeder(tp, keys ? &map_k : &map_v, sh, ring, gave_up);
 #pragma unroll 1
     for (uint32_t number = 0;; ++number) {
-      const uint32_t slot = number % kItems;
-      if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
-      const Item im = uniform(sh.items[slot]);
+      const uint32_t slot = number % kItems, parity = (number / kItems) & 1;
+      if (!warp_wait(keys ? sh.item_empty[slot] : sh.item_full[slot], keys ? parity ^ 1 : parity, gave_up)) break;
+      Item im;
+      if (keys)
+        walk.next(im);
+      else
+        im = sh.items[slot];
+      im = uniform(im);
+      if (keys && lane == 0) sh.items[slot] = im;
       __syncwarp();
-      if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
+      if (lane == 0) barrier_arrive(shared_address(keys ? &sh.item_full[slot] : &sh.item_empty[slot]));
       if (im.seq < 0) break;
       const int n = item_tiles(im), hidden_from = max(im.behind + im.row0 / p.group + 1, 0);
-      values.item(im, n);
-      // Tiles with hidden keys are cleaned one behind the copies: at once when a tile has landed would hold up the copies,
-      // later would hold up the ring.
+      if (keys && n > 0) {  // queries: each tile in blocks of 64 channels
+        if (!warp_wait(sh.q_empty, (q_uses & 1) ^ 1, gave_up)) break;
+        ++q_uses;
+        const uint32_t q_bar = shared_address(&sh.q_full);
+        if (elect_one()) {
+          const int tiles = im.two ? 2 : 1;
+          barrier_arrive_expect(q_bar, tiles * tp.q_bytes);
 #pragma unroll 1
-      for (int j = 0; j <= n && values.fine; ++j) {
-        if (j < n) values.feed(j, value_place(im.two, j, n));
+          for (int w = 0; w < tiles; ++w)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h)
+              copy_3d(shared_address(q_tiles + w * S::kTileBytes + h * kBlockBytes), &map_q, q_bar, h * 64,
+                      im.head * p.group, im.first + im.row0 / tp.item_rows * tp.item_tokens + w * tp.tile_tokens);
+        }
+        __syncwarp();
+      }
+      feeder.item(im, n);
+      // Value tiles with hidden keys are cleaned one behind the copies: at once when a tile has landed would hold up the
+      // copies, later would hold up the ring.
+#pragma unroll 1
+      for (int j = 0; j <= n && feeder.fine; ++j) {
+        if (j < n) feeder.feed(j, keys ? key_place(im.two, j) : value_place(im.two, j, n));
         const int landed = j - 1;
-        if (!values.fine || landed < im.clean || landed < 0) continue;
-        const uint32_t place = values.base + value_place(im.two, landed, n), stage = ring_stage(place, kStages);
-        values.fine = warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up);
-        if (!values.fine) break;
+        if (keys || !feeder.fine || landed < im.clean || landed < 0) continue;
+        const uint32_t place = feeder.base + value_place(im.two, landed, n), stage = ring_stage(place, kStages);
+        feeder.fine = warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up);
+        if (!feeder.fine) break;
         const int key0 = im.kbegin + landed * kKeyTile;
         clean_values<kHalves, 32>(ring + stage * S::kTileBytes, max(hidden_from - key0, 0), im.kend - key0, lane,
                                   &sh.bad_values[number & 7], (int)number);
         __syncwarp();
         if (lane == 0) barrier_arrive(shared_address(&sh.cleaned[stage]));
       }
-      if (!values.fine) break;
+      if (!feeder.fine) break;
     }
-    if (*gave_up) values.drain();
+    if (*gave_up) {  // copies in flight have to land before the block ends
+      if (q_uses > 0) barrier_drain(shared_address(&sh.q_full), (q_uses - 1) & 1);
+      feeder.drain();
+    }
   } else if (warp == 9) {
     lower_registers<kOtherRegisters>();
     // ---- products: the whole warp follows, one lane issues ----

@@ -5,6 +5,7 @@ device memory and streams.  Wrong arguments raise ToplocError before anything is
 only the device can see comes back in status tensors (TOPLOC_SEQ_*).
 """
 import ctypes
+import struct
 
 import torch
 
@@ -51,6 +52,10 @@ class ToplocNormLayout(ctypes.Structure):
                 ("x_stride", _i64), ("residual_stride", _i64), ("residual_out_stride", _i64), ("y_stride", _i64)]
 
 
+# The three structures as the wrappers pass them: their bytes (packing is several times as fast as ctypes fields, and a
+# decode step's call is short)
+_KV, _ATTENTION, _NORM = struct.Struct("=4i7q"), struct.Struct("=6iqfi4q"), struct.Struct("=4i5q")
+
 _LIB = None
 
 
@@ -59,7 +64,7 @@ def _library():
     global _LIB
     if _LIB is None:
         lib = binding.load_library()
-        kv_p, att_p = ctypes.POINTER(ToplocKvLayout), ctypes.POINTER(ToplocAttentionLayout)
+        kv_p = att_p = norm_p = _vp  # a structure by reference, or its bytes
         lib.toploc_sequence_status_string.restype = ctypes.c_char_p
         lib.toploc_sequence_status_string.argtypes = [ctypes.c_int]
         lib.toploc_plan_pages.restype = ctypes.c_int
@@ -77,7 +82,7 @@ def _library():
         lib.toploc_attention_prompt.argtypes = [_vp, _vp, _vp, att_p, kv_p, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t,
                                                 _vp]
         lib.toploc_rmsnorm_residual.restype = ctypes.c_int
-        lib.toploc_rmsnorm_residual.argtypes = [_vp, _vp, _vp, ctypes.c_float, ctypes.POINTER(ToplocNormLayout), _vp,
+        lib.toploc_rmsnorm_residual.argtypes = [_vp, _vp, _vp, ctypes.c_float, norm_p, _vp,
                                                 _vp, _vp, _vp]
         _LIB = lib
     return _LIB
@@ -110,6 +115,13 @@ def _vector(t, dtype, length, what):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _pack(layout, *fields):
+    try:
+        return layout.pack(*fields)
+    except struct.error as e:  # a number that does not fit its field
+        raise ToplocError("a size, bound or stride is out of range: %s" % e)
 
 
 def _call(fn, name, dev, stream, *args):
@@ -160,7 +172,7 @@ def _cache_layout(k_cache, v_cache, block_table=None):
     stride = 0 if block_table is None else block_table.stride(0) if block_table.shape[0] > 1 else width
     kp, kt, kh, _ = k_cache.stride()
     vp, vt, vh, _ = v_cache.stride()
-    return ToplocKvLayout(k_cache.shape[1], k_cache.shape[0], width, 0, stride, kp, kt, kh, vp, vt, vh)
+    return _pack(_KV, k_cache.shape[1], k_cache.shape[0], width, 0, stride, kp, kt, kh, vp, vt, vh)
 
 
 def toploc_cache_write(k, v, slots, k_cache, v_cache, stream=None):
@@ -175,7 +187,7 @@ def toploc_cache_write(k, v, slots, k_cache, v_cache, stream=None):
     _vector(slots, torch.int64, k.shape[0], "slots")
     _call(_library().toploc_cache_write, "toploc_cache_write", dev, stream, _ptr(k), _ptr(v), k.stride(0), k.stride(1),
           v.stride(0), v.stride(1), _ptr(slots), k.shape[0], _DTYPES[k.dtype], k.shape[1], k.shape[2], _ptr(k_cache),
-          _ptr(v_cache), ctypes.byref(kv))
+          _ptr(v_cache), kv)
 
 
 def _attention_layout(q, kv_heads, num_seqs, max_new_tokens, scale, out, lse):
@@ -186,13 +198,13 @@ def _attention_layout(q, kv_heads, num_seqs, max_new_tokens, scale, out, lse):
     _need(lse is None or (lse.dtype == torch.float32 and lse.shape == q.shape[:2] and lse.is_contiguous()),
           "lse must be a contiguous float32 [tokens, q_heads]")
     (qt, qh, _), (ot, oh, _) = q.stride(), out.stride()
-    return ToplocAttentionLayout(_DTYPES[q.dtype], dim, heads, kv_heads, num_seqs, max_new_tokens, tokens,
-                                 dim ** -0.5 if scale is None else scale, 0, qt, qh, ot, oh)
+    return _pack(_ATTENTION, _DTYPES[q.dtype], dim, heads, kv_heads, num_seqs, max_new_tokens, tokens,
+                 dim ** -0.5 if scale is None else scale, 0, qt, qh, ot, oh)
 
 
-def _attention_workspace(lib, lay_p, kv_p, workspace, dev):
+def _attention_workspace(lib, lay, kv, workspace, dev):
     if workspace is None:
-        need = lib.toploc_attention_workspace_bytes(lay_p, kv_p)
+        need = lib.toploc_attention_workspace_bytes(lay, kv)
         if need == 0:
             return None, 0
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
@@ -203,7 +215,7 @@ def toploc_attention_workspace_bytes(q, k_cache, v_cache, block_table, max_new_t
     """Bytes of workspace toploc_attention_paged needs for these tensors (0: none)."""
     lay = _attention_layout(q, k_cache.shape[2], block_table.shape[0], max_new_tokens, None, q, None)
     kv = _cache_layout(k_cache, v_cache, block_table)
-    return int(_library().toploc_attention_workspace_bytes(ctypes.byref(lay), ctypes.byref(kv)))
+    return int(_library().toploc_attention_workspace_bytes(lay, kv))
 
 
 def toploc_attention_paged(q, k_cache, v_cache, block_table, seq_offsets, kv_lens, max_new_tokens, scale=None,
@@ -229,10 +241,9 @@ def toploc_attention_paged(q, k_cache, v_cache, block_table, seq_offsets, kv_len
     kv = _cache_layout(k_cache, v_cache, block_table)
     _need(k_cache.dtype == q.dtype and k_cache.shape[3] == q.shape[2], "the caches must have q's type and head_dim")
     lib = _library()
-    lay_p, kv_p = ctypes.byref(lay), ctypes.byref(kv)
-    workspace, size = _attention_workspace(lib, lay_p, kv_p, workspace, dev)
+    workspace, size = _attention_workspace(lib, lay, kv, workspace, dev)
     _call(lib.toploc_attention_paged, "toploc_attention_paged", dev, stream, _ptr(q), _ptr(k_cache), _ptr(v_cache),
-          lay_p, kv_p, _ptr(block_table), _ptr(seq_offsets), _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(status),
+          lay, kv, _ptr(block_table), _ptr(seq_offsets), _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(status),
           _ptr(workspace), size)
     return out, lse
 
@@ -256,11 +267,10 @@ def toploc_attention_prompt(q, k, v, seq_offsets, max_tokens, scale=None, out=No
           v.stride(2) == 1 and k.shape[0] == q.shape[0] and k.shape[2] == q.shape[2],
           "k and v must be [tokens, kv_heads, head_dim] of q's type, the last dimension contiguous")
     lay = _attention_layout(q, k.shape[1], n, max_tokens, scale, out, lse)
-    kv = ToplocKvLayout(0, 0, 0, 0, 0, 0, k.stride(0), k.stride(1), 0, v.stride(0), v.stride(1))
+    kv = _pack(_KV, 0, 0, 0, 0, 0, 0, k.stride(0), k.stride(1), 0, v.stride(0), v.stride(1))
     lib = _library()
-    lay_p, kv_p = ctypes.byref(lay), ctypes.byref(kv)
-    workspace, size = _attention_workspace(lib, lay_p, kv_p, workspace, dev)
-    _call(lib.toploc_attention_prompt, "toploc_attention_prompt", dev, stream, _ptr(q), _ptr(k), _ptr(v), lay_p, kv_p,
+    workspace, size = _attention_workspace(lib, lay, kv, workspace, dev)
+    _call(lib.toploc_attention_prompt, "toploc_attention_prompt", dev, stream, _ptr(q), _ptr(k), _ptr(v), lay, kv,
           _ptr(seq_offsets), _ptr(out), _ptr(lse), _ptr(status), _ptr(workspace), size)
     return out, lse
 
@@ -295,8 +305,8 @@ def toploc_rmsnorm_residual(x, residual, weight, eps, residual_out=None, y=None,
         _need(scales.dtype == torch.float32 and scales.is_contiguous() and
               scales.shape == (rows, 1 if group == 0 else -(-hidden // group)),
               "scales must be contiguous float32 [rows, groups]")
-    lay = ToplocNormLayout(_DTYPES[x.dtype], TOPLOC_NORM_OUT_E4M3 if quant else TOPLOC_NORM_OUT_SAME, group, hidden,
-                           rows, strides[0], strides[1], strides[2], y.stride(0) if rows > 1 else hidden)
+    lay = _pack(_NORM, _DTYPES[x.dtype], TOPLOC_NORM_OUT_E4M3 if quant else TOPLOC_NORM_OUT_SAME, group, hidden, rows,
+                strides[0], strides[1], strides[2], y.stride(0) if rows > 1 else hidden)
     _call(_library().toploc_rmsnorm_residual, "toploc_rmsnorm_residual", dev, stream, _ptr(x), _ptr(residual),
-          _ptr(weight), eps, ctypes.byref(lay), _ptr(residual_out), _ptr(y), _ptr(scales) if quant else None)
+          _ptr(weight), eps, lay, _ptr(residual_out), _ptr(y), _ptr(scales) if quant else None)
     return y, residual_out, scales if quant else None

@@ -194,3 +194,13 @@ def test_wrappers_refuse_host_tensors_and_wrong_shapes():
     i = torch.zeros(1, dtype=torch.int32)
     with pytest.raises(tl.ToplocError, match="CUDA"):
         tl.toploc_plan_pages(i, i, i, i, table, 16, i, i, i.long(), i, i, i.byte())
+
+
+def test_wrappers_refuse_numbers_that_do_not_fit():
+    from paper_2501_16007_b200 import model_ops
+    q = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
+    with pytest.raises(tl.ToplocError, match="out of range"):
+        model_ops._attention_layout(q, 2, 1, 1 << 40, None, q, None)
+    lay = tl.ToplocAttentionLayout.from_buffer_copy(model_ops._attention_layout(q, 2, 3, 4, 0.25, q, None))
+    assert (lay.head_dim, lay.q_heads, lay.kv_heads, lay.num_seqs, lay.max_new_tokens, lay.total_tokens, lay.scale,
+            lay.q_token_stride, lay.out_head_stride) == (64, 2, 2, 3, 4, 4, 0.25, 128, 64)
