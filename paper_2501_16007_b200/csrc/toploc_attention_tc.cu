@@ -226,7 +226,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
     constexpr uint32_t kScores = bf16_product(128, false, false), kValues = bf16_product(D, false, true);
     const uint32_t q_low = operand_low(shared_address(q_tiles), 16);
     const uint32_t k_low = operand_low(shared_address(ring), 16), v_low = operand_low(shared_address(ring), kBlockBytes);
-    uint32_t used = 0, q_uses = 0, p_uses[2] = {0, 0}, cleans = 0;  // cleans: by stage, the parity of its next cleaning
+    uint32_t used = 0, q_uses = 0, p_parity = 0, cleans = 0;  // cleans: by stage, the parity of its next cleaning
     const auto full = [&](uint32_t n) {
       const bool ok = warp_wait(sh.full[ring_stage(n, kStages)], ring_parity(n, kStages), gave_up);
       tmem_fence_after();
@@ -248,7 +248,8 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       }
     };
     const auto values = [&](int w, uint32_t n, bool add) {  // as the group's weights come into tensor memory
-      const uint32_t b = v_low + ring_stage(n, kStages) * (S::kTileBytes / 16), parity = p_uses[w]++ & 1;
+      const uint32_t b = v_low + ring_stage(n, kStages) * (S::kTileBytes / 16), parity = p_parity >> w & 1;
+      p_parity ^= 1u << w;
       if (!warp_wait(sh.p_most[w], parity, gave_up)) return false;
       tmem_fence_after();
       if (elect_one()) {
@@ -291,7 +292,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       int cleaned_to = clean;
 #pragma unroll 1
       for (int round = -1; ok && round < rounds; ++round) {
-#pragma unroll
+#pragma unroll 1
         for (int w = 0; w < 2; ++w) {
           const int tiles = two ? (w ? n1 : n0) : n;
           const int j = two ? round : 2 * round + w, next = j + (two ? 1 : 2);
