@@ -27,7 +27,7 @@ struct AttentionParams {
   long long k_page, k_token, k_head, v_page, v_token, v_head, table_stride;
   float scale_log2;
   int head_dim, q_heads, kv_heads, group, num_seqs, max_new;
-  int page_size, num_pages, max_pages;
+  int page_size, num_pages, max_pages, most_keys;
   int row_tiles, splits;
 };
 
@@ -37,21 +37,19 @@ struct SeqRange {
   bool bad;
 };
 
+// (32 bits are enough: total_tokens, and most_keys = max_pages * page_size, are held below 2^31 by the entry points)
 __device__ __forceinline__ SeqRange sequence(const AttentionParams& p, int i) {
+  const int a = p.offsets[i], b = p.offsets[i + 1], total = (int)p.total_tokens;
   SeqRange s;
-  const int a = p.offsets[i], b = p.offsets[i + 1];
   s.first = max(a, 0);
-  long long rows = min((long long)b, p.total_tokens) - s.first;
-  s.bad = a < 0 || b < a || b > p.total_tokens || rows > p.max_new;
-  rows = max(0ll, min(rows, (long long)p.max_new));
-  s.rows = (int)rows;
-  if (p.kv_lens == nullptr) {
-    s.keys = s.rows;
-  } else {
+  const int rows = b > s.first ? min(b, total) - s.first : 0;
+  s.bad = a < 0 || b < a || b > total || rows > p.max_new;
+  s.rows = max(min(rows, p.max_new), 0);
+  s.keys = s.rows;
+  if (p.kv_lens != nullptr) {
     const int kv = p.kv_lens[i];
-    const long long most = (long long)p.max_pages * p.page_size;
-    s.bad = s.bad || kv < 0 || kv > most;
-    s.keys = (int)max(0ll, min((long long)kv, most));
+    s.bad = s.bad || kv < 0 || kv > p.most_keys;
+    s.keys = max(min(kv, p.most_keys), 0);
   }
   return s;
 }

@@ -116,10 +116,9 @@ struct Place {
 };
 
 __device__ __forceinline__ bool before(const Place& a, const Place& b) {
-  if (a.seq != b.seq) return a.seq < b.seq;
-  if (a.head != b.head) return a.head < b.head;
-  if (a.level != b.level) return a.level < b.level;
-  return a.tile < b.tile;
+  const int d = a.seq != b.seq ? a.seq - b.seq : a.head != b.head ? a.head - b.head
+                : a.level != b.level ? a.level - b.level : a.tile - b.tile;
+  return d < 0;
 }
 
 // Key tiles that a level's rows see in all.
@@ -248,15 +247,14 @@ struct Walk {
     im = Item{};
     im.seq = -1;
 #pragma unroll 1
-    while (before(at, end)) {  // past the sequences without rows
+    for (;; at = Place{at.seq + 1, 0, 0, 0}) {  // past the sequences without rows
+      if (!before(at, end)) return false;
       if (s_of != at.seq) {
         s = sequence(p, at.seq);
         s_of = at.seq;
       }
       if (s.rows > 0) break;
-      at = Place{at.seq + 1, 0, 0, 0};
     }
-    if (!before(at, end)) return false;
     const int tokens = min((at.level + 1) * tp.item_tokens, s.rows);
     im.seq = at.seq;
     im.head = at.head;

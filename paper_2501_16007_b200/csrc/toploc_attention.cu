@@ -284,6 +284,7 @@ int attention(const void* d_q, const void* d_k, const void* d_v, const toploc_at
   p.group = lay->q_heads / lay->kv_heads;
   p.num_seqs = lay->num_seqs; p.max_new = lay->max_new_tokens;
   p.page_size = kv->page_size; p.num_pages = kv->num_pages; p.max_pages = kv->max_pages;
+  p.most_keys = kv->page_size > 0 ? kv->max_pages * kv->page_size : 0;  // (check_layout: fits)
   const bool tensor_cores = tensor_cores_take(lay, kv, d_q, d_k, d_v, d_out);
   const size_t need = workspace_bytes_of(lay, kv, tensor_cores);
   if (need > 0 && (!workspace || workspace_bytes < need)) return TOPLOC_ERR_WORKSPACE;
