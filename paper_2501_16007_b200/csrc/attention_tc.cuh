@@ -460,7 +460,7 @@ inline int allow_shared(const void* kernel, int bytes, std::atomic<uint64_t>& do
 
 namespace toploc_model {
 
-constexpr int kFewRows = 32;  // packed rows of a sequence that the kernel for few rows takes
+constexpr int kFewRows = 8;  // packed rows of a sequence that the kernel for few rows takes (figures: there)
 // (tp: a TcParams, maps: CUtensorMap)
 int launch_few_rows(const void* tp, const void* map_q, const void* map_k, const void* map_v, int blocks,
                     cudaStream_t stream);

@@ -1,19 +1,23 @@
-// Attention on the tensor cores where a sequence brings few rows (up to 16 or 32 packed ones: a token or a few, all heads
-// of a key head), bf16, head_dim 64 or 128.  Bound by reading the keys and values.
+// Attention on the tensor cores where a sequence brings few rows (up to 8 packed ones: a token, perhaps two, all heads of a
+// key head), bf16, head_dim 64 or 128.  Bound by reading the keys and values.
 //
-//   S^T = K Q^T (128 keys x N rows),  P^T = 2^(scale S^T - m),  O^T += V^T P^T (head_dim x N)
+//   S^T = K Q^T (128 keys x 16 rows),  P^T = 2^(scale S^T - m),  O^T += V^T P^T (head_dim x 16)
 //
-// With so few rows the other order would leave most of a product's 128 rows and of the softmax threads empty.  Here a
-// thread has a key and weighs it for all N rows (R exponentials, not 128), and the products are N wide.
-// R is 4, 8, 16 or 32, N is R and at least 16: loops over rows are unrolled, and code for rows that are not there would
-// only crowd the instruction caches.  A row's maximum
-// and sum run over threads, but seldom: the maximum of the first tile stays the reference for the whole item unless a
-// score exceeds it by 2^64 (weights, sums and outputs share it, and fp32 and bf16 have the range; the quotient is the
-// same), so a tile needs one vote, and the threads' own sums are added up once at the end.
+// With so few rows the other order (rows along a product's 128) would leave most of the products and of the softmax
+// threads empty.  Here a thread has a key and weighs it for all R rows (R exponentials, not 128), and the products are 16
+// wide, the least there is.  R is 4 or 8: loops over rows are unrolled, and code for rows that are not there would only
+// crowd the instruction caches (98 us with code for 16 rows where there are four).  A row's maximum and sum run over
+// threads, but seldom: the maximum of the first tile stays the reference for the whole item unless a score exceeds it by
+// 2^64 (weights, sums and outputs share it, and fp32 and bf16 have the range; the quotient is the same), so a tile needs
+// one vote, and the threads' own sums are added up once at the end.
 //
-// Two blocks share an SM, three tiles of 32 KB in flight each (head_dim 128).  A block: four warps of softmax, a warp
-// that feeds keys (and finds the items), one that feeds values, one that issues the products; the scores of the next tile
-// are computed while the weights of this one are.
+// Two blocks share an SM, three tiles of 32 KB in flight each (head_dim 128).  A block: four warps of softmax, a warp that
+// finds the items and copies queries and keys, one that copies values, one that issues the products; the scores of the
+// next tile are computed while the weights of this one are.  The work is cut as in the kernel for many rows.
+//
+// 64 sequences of up to 2048 keys (286 MB), 4 rows: 59 us, 4.9 TB/s, 0.74 of the measured copy (the kernel for many rows:
+// 69); 8 rows: 62 (70); 16 rows 85 (72), 32 rows 156 (74), so the other kernel takes those.  Four times the keys: 200 us,
+// 5.6 TB/s.  What is missing is the start (6 us until the first tile lands) and the join.
 #include "attention_tc.cuh"
 
 namespace {
@@ -21,8 +25,9 @@ namespace {
 constexpr int kFewThreads = 224;
 constexpr float kFewLimit = 64.0f;
 
-template <int D, int N>
+template <int D>
 struct FewShared {
+  static constexpr int N = 16;  // rows of the products
   static constexpr int kHalves = D / 64;
   static constexpr int kTileBytes = kHalves * kBlockBytes;
   static constexpr int kStages = D == 128 ? 3 : 6;
@@ -50,8 +55,8 @@ template <int D, int R>
 __global__ void __launch_bounds__(kFewThreads, 2)
 toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_constant__ CUtensorMap map_q,
                             const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
-  constexpr int N = R < 16 ? 16 : R;  // rows of the products
-  using S = FewShared<D, N>;
+  using S = FewShared<D>;
+  constexpr int N = S::N;
   constexpr int kStages = S::kStages, kHalves = S::kHalves;
   extern __shared__ __align__(1024) unsigned char base[];
   const AttentionParams& p = tp.p;
@@ -323,9 +328,9 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
             tmem_wait_store();
           }
         }
-        uint32_t packed[N / 2];
+        uint32_t packed[4];  // of 8 rows
 #pragma unroll
-        for (int r = 0; r < N / 2; ++r) packed[r] = 0u;
+        for (int r = 0; r < 4; ++r) packed[r] = 0u;
 #pragma unroll
         for (int r = 0; r < R; r += 2) {
           float a = 0.f, b = 0.f;
@@ -339,11 +344,8 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
           ok = warp_wait(sh.o_full, (pv - 1) & 1, gave_up);
           if (!ok) break;
         }
-        // 8 rows of a key are 16 bytes, keys side by side
-#pragma unroll
-        for (int c = 0; c < (R + 7) / 8; ++c)
-          *reinterpret_cast<uint4*>(weights + c * 2048 + me * 16) =
-              make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
+        // 8 rows of a key are 16 bytes, keys side by side (the other 8 rows of the product come out as anything)
+        *reinterpret_cast<uint4*>(weights + me * 16) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
         if (masked) {
           const uint32_t place = used + value_place(false, j, n), stage = ring_stage(place, kStages);
           ok = warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up);
@@ -436,7 +438,7 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
 template <int D, int R>
 int launch(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int blocks,
            cudaStream_t stream) {
-  constexpr int kBytes = FewShared<D, R < 16 ? 16 : R>::kBytes;
+  constexpr int kBytes = FewShared<D>::kBytes;
   static std::atomic<uint64_t> allowed{0};
   if (const int rc = allow_shared(reinterpret_cast<const void*>(toploc_attention_few_kernel<D, R>), kBytes, allowed)) return rc;
   toploc_attention_few_kernel<D, R><<<blocks, kFewThreads, kBytes, stream>>>(tp, q, k, v);
@@ -446,10 +448,7 @@ int launch(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const
 template <int D>
 int launch_rows(const TcParams& tp, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int blocks,
                 cudaStream_t stream) {
-  if (tp.item_rows <= 4) return launch<D, 4>(tp, q, k, v, blocks, stream);
-  if (tp.item_rows <= 8) return launch<D, 8>(tp, q, k, v, blocks, stream);
-  if (tp.item_rows <= 16) return launch<D, 16>(tp, q, k, v, blocks, stream);
-  return launch<D, 32>(tp, q, k, v, blocks, stream);
+  return tp.item_rows <= 4 ? launch<D, 4>(tp, q, k, v, blocks, stream) : launch<D, 8>(tp, q, k, v, blocks, stream);
 }
 
 }  // namespace

@@ -7,19 +7,31 @@
 // has its heads side by side.
 //
 // A block has two groups of four warps that do the softmax, a thread per row (no exchange between threads: the
-// running maximum and sum of a row live in one), a warp that feeds keys and values through a ring of tiles by tensor
-// copies, and one that issues the products.  While one group works on its scores the tensor cores run the other
-// group's products.  The groups hold, item by item,
+// running maximum and sum of a row live in one), a warp that finds the work and copies queries and keys into a ring of
+// tiles, one that copies values, and one that issues the products.  While one group works on its scores the tensor cores
+// run the other group's products.  The groups hold, item by item,
 //   two row tiles against the same keys      (more than 128 rows), or
-//   one row tile against every other key tile (few rows, single tokens among them: bound by reading the keys, so both
-//                                              groups serve the stream and join at the end).
+//   one row tile against every other key tile (fewer rows: bound by reading the keys, so both groups serve the stream and
+//                                              join at the end).
 //
 // The work is cut evenly, not by items: the keys that all row tiles see, one after the other, are one long line, and
 // each of the persistent blocks (one an SM) takes an equal stretch of it.  A tile whose keys lie in several stretches
 // leaves partial results (normalised outputs and lse) that a second kernel joins, always in the same order.  So a
 // single long sequence and a batch of ragged ones both keep every SM busy to the end, whatever the lengths on the
-// device are; there is no bound on them to tune by.  The feeding warp runs ahead into the next item while the last one
+// device are; there is no bound on them to tune by.  The feeding warps run ahead into the next item while the last one
 // is finished.
+//
+// What bounds it.  A pair of row tiles against a tile of keys (head_dim 128) needs 2048 clocks of the tensor cores and as
+// many of the special-function units (256 * 128 exponentials, 16 a clock); it takes about 3300: a group's softmax (2200)
+// and then its two products (1100 to 1300) are one chain, two groups in turn hide half of it, and tensor memory (2 * 128
+// columns of scores, 2 * 128 of outputs) has no room for scores ahead.  Packed prompts of 16383 rows: 770 us, 1.1 PFLOP/s
+// (0.69 of the measured bf16 rate); one sequence of 131000 keys and 17 tokens: 134 us.  Instruction fetch is the other
+// bound: eleven warps run seven different pieces of code, and the kernel gained more from small code (loops that are not
+// unrolled, one code for both feeding warps, rare branches out of line: 76 to 57 KB, 143 to 134 us, prompts 840 to 770)
+// than from fewer instructions.  Tried and not kept: two threads a row with 16 softmax warps (the same time, short
+// prompts 52 against 46 us: the maxima have to be exchanged), a share of the exponentials as a polynomial on the fp32 units
+// (3 to 10 % slower, the more the larger the share), the row's scores kept in registers between maximum and weights
+// (the same where tiles are many, 10 % slower on short prompts: its code is unrolled).
 //
 // The output is not rescaled whenever the maximum grows but only where it grew by more than 2^8: P then stays
 // below 2^8, and O, the sum and P share the same reference, so the quotient is the same.
@@ -29,9 +41,9 @@
 
 namespace {
 
-constexpr int kTcThreads = 384;            // two groups of softmax, and one whose first two warps feed and issue
-// Registers move from the third group of warps to the softmax, whose threads hold a row of 128 scores.  The block is
-// launched with 168 a thread (65536 / 384, in steps of 8); 2 * 216 + 72 = 3 * 168.
+constexpr int kTcThreads = 384;  // two groups of softmax, and one whose first three warps feed and issue
+// Registers move from the third group of warps to the softmax.  The block is launched with 168 a thread (65536 / 384, in
+// steps of 8); 2 * 216 + 72 = 3 * 168.
 constexpr int kSoftmaxRegisters = 216, kOtherRegisters = 72;
 constexpr float kLazyLog2 = 8.0f;
 
@@ -380,9 +392,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
             seen = __reduce_min_sync(0xFFFFFFFFu, valid ? last : kKeyTile);
             upto = min(__reduce_max_sync(0xFFFFFFFFu, valid ? last : -1) + 1, kKeyTile);
           }
-          // Loops over quarters of the row, not unrolled, the scores read twice: unrolled code for 128 columns takes as
-          // long where tiles are many and overflows the instruction caches where they are few (short prompts 47 us so,
-          // 51 us with half of the row kept in registers).
+          // loops over quarters of the row, not unrolled, the scores read twice (see above)
           tmem_fence_after();
           float peak = -INFINITY;
           // (tiles with hidden keys have loops of their own: branches in the ordinary ones cost 6 % of the kernel)
