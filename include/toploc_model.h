@@ -162,8 +162,10 @@ typedef struct {
  *
  * Variants, by a rule on types and layout: bf16 with head_dim 64 or 128, rows
  * and strides of 16-byte multiples, and a page_size that is a multiple of 8 and
- * divides 128 (or a multiple of 128) takes the tensor-core kernel, all else
- * (fp32 among it) a kernel on the fp32 units.
+ * divides 128 (or a multiple of 128) takes the tensor cores, all else (fp32
+ * among it) a kernel on the fp32 units.  On the tensor cores, calls whose
+ * max_new_tokens * q_heads / kv_heads is at most 8 (single tokens, as a rule) take
+ * a kernel of their own that holds keys instead of rows along a product.
  */
 size_t toploc_attention_workspace_bytes(const toploc_attention_layout* lay, const toploc_kv_layout* kv);
 int toploc_attention_paged(const void* d_q, const void* d_k_cache, const void* d_v_cache,

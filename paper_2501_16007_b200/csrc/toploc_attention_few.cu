@@ -6,8 +6,8 @@
 // With so few rows the other order (rows along a product's 128) would leave most of the products and of the softmax
 // threads empty.  Here a thread has a key and weighs it for all R rows (R exponentials, not 128), and the products are 16
 // wide, the least there is.  R is 4 or 8: loops over rows are unrolled, and code for rows that are not there would only
-// crowd the instruction caches (98 us with code for 16 rows where there are four).  A row's maximum and sum run over
-// threads, but seldom: the maximum of the first tile stays the reference for the whole item unless a score exceeds it by
+// crowd the instruction caches (with that and other code made small at once, 98 to 59 us at four rows).  A row's
+// maximum and sum run over threads, but seldom: the maximum of the first tile stays the reference for the whole item unless a score exceeds it by
 // 2^64 (weights, sums and outputs share it, and fp32 and bf16 have the range; the quotient is the same), so a tile needs
 // one vote, and the threads' own sums are added up once at the end.
 //
@@ -16,8 +16,8 @@
 // next tile are computed while the weights of this one are.  The work is cut as in the kernel for many rows.
 //
 // 64 sequences of up to 2048 keys (286 MB), 4 rows: 59 us, 4.9 TB/s, 0.74 of the measured copy (the kernel for many rows:
-// 69); 8 rows: 62 (70); 16 rows 85 (72), 32 rows 156 (74), so the other kernel takes those.  Four times the keys: 200 us,
-// 5.6 TB/s.  What is missing is the start (6 us until the first tile lands) and the join.
+// 69); 8 rows: 62 (70); 16 rows 85 (72), 32 rows 156 (74), so the other kernel takes those.  Four times the keys: 183 us,
+// 6.2 TB/s: what is missing at the smaller size is the start and end of the kernel, and the join.
 #include "attention_tc.cuh"
 
 namespace {

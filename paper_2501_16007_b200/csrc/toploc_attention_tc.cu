@@ -22,16 +22,16 @@
 // is finished.
 //
 // What bounds it.  A pair of row tiles against a tile of keys (head_dim 128) needs 2048 clocks of the tensor cores and as
-// many of the special-function units (256 * 128 exponentials, 16 a clock); it takes about 3300: a group's softmax (2200)
-// and then its two products (1100 to 1300) are one chain, two groups in turn hide half of it, and tensor memory (2 * 128
-// columns of scores, 2 * 128 of outputs) has no room for scores ahead.  Packed prompts of 16383 rows: 770 us, 1.1 PFLOP/s
-// (0.69 of the measured bf16 rate); one sequence of 131000 keys and 17 tokens: 134 us.  Instruction fetch is the other
-// bound: eleven warps run seven different pieces of code, and the kernel gained more from small code (loops that are not
-// unrolled, one code for both feeding warps, rare branches out of line: 76 to 57 KB, 143 to 134 us, prompts 840 to 770)
-// than from fewer instructions.  Tried and not kept: two threads a row with 16 softmax warps (the same time, short
-// prompts 52 against 46 us: the maxima have to be exchanged), a share of the exponentials as a polynomial on the fp32 units
-// (3 to 10 % slower, the more the larger the share), the row's scores kept in registers between maximum and weights
-// (the same where tiles are many, 10 % slower on short prompts: its code is unrolled).
+// many of the special-function units (256 * 128 exponentials, 16 a clock); it takes about 3300.  A group's softmax and
+// then its two products are one chain (2400 and 1700 clocks in a trace of an earlier, slower version), two groups in turn
+// hide half of it, and tensor memory (2 * 128 columns of scores, 2 * 128 of outputs) has no room for scores ahead.
+// Packed prompts of 16383 rows: 770 us, 1.1 PFLOP/s (0.69 of the measured bf16 rate); one sequence of 131000 keys and 17
+// tokens: 136 us.  Instruction fetch is the other bound: eleven warps run seven different pieces of code, and the kernel
+// gained more from small code (loops that are not unrolled, one code for both feeding warps, rare branches out of line: 76
+// to 57 KB, 146 to 136 us, prompts 840 to 770) than from fewer instructions.  Tried and not kept: two threads a row with
+// 16 softmax warps (the same time, short prompts 52 against 46 us: the maxima have to be exchanged), a share of the
+// exponentials as a polynomial on the fp32 units (2 to 10 % slower), the row's scores kept in registers between maximum
+// and weights (the same where tiles are many, 10 % slower on short prompts: its code is unrolled).
 //
 // The output is not rescaled whenever the maximum grows but only where it grew by more than 2^8: P then stays
 // below 2^8, and O, the sum and P share the same reference, so the quotient is the same.
