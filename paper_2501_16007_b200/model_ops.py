@@ -2,7 +2,8 @@
 
 The operators of the passes that produce the activations a proof commits to.  torch is used for
 device memory and streams.  Wrong arguments raise ToplocError before anything is enqueued; what
-only the device can see comes back in status tensors (TOPLOC_SEQ_*).
+only the device can see comes back in status tensors (TOPLOC_SEQ_*).  What a call allocates (outputs
+that are not given, its workspace) is memory of the stream it runs on.
 """
 import ctypes
 import struct
@@ -117,6 +118,19 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _empty(shape, dtype, device, stream, hidden=False):
+    """A tensor that work on `stream` (None: torch's current one) may write at once: its memory is one of that stream's, so
+    that neither what the current stream still does with a block freed there, nor the next allocation after this tensor is
+    gone, can meet the call.  hidden: the caller never sees it; else it may be read, and dropped, on the current stream."""
+    if stream is None or stream == torch.cuda.current_stream(device):
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if not hidden:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _pack(layout, *fields):
     try:
         return layout.pack(*fields)
@@ -202,12 +216,12 @@ def _attention_layout(q, kv_heads, num_seqs, max_new_tokens, scale, out, lse):
                  dim ** -0.5 if scale is None else scale, 0, qt, qh, ot, oh)
 
 
-def _attention_workspace(lib, lay, kv, workspace, dev):
+def _attention_workspace(lib, lay, kv, workspace, dev, stream):
     if workspace is None:
         need = lib.toploc_attention_workspace_bytes(lay, kv)
         if need == 0:
             return None, 0
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = _empty((need,), torch.uint8, dev, stream, hidden=True)
     return workspace, workspace.numel() * workspace.element_size()
 
 
@@ -225,9 +239,9 @@ def toploc_attention_paged(q, k_cache, v_cache, block_table, seq_offsets, kv_len
     kv_lens int32 [n]; max_new_tokens bounds a sequence's new tokens; scale: 1 / sqrt(head_dim) by default; status:
     uint8 [n], set where a sequence is not as promised.  Returns (out, lse or None)."""
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     if lse is None and want_lse:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        lse = _empty(q.shape[:2], torch.float32, q.device, stream)
     dev = _device("toploc_attention_paged", q, k_cache, v_cache, block_table, seq_offsets, kv_lens, out, lse, status,
                   workspace)
     n = kv_lens.shape[0]
@@ -241,7 +255,7 @@ def toploc_attention_paged(q, k_cache, v_cache, block_table, seq_offsets, kv_len
     kv = _cache_layout(k_cache, v_cache, block_table)
     _need(k_cache.dtype == q.dtype and k_cache.shape[3] == q.shape[2], "the caches must have q's type and head_dim")
     lib = _library()
-    workspace, size = _attention_workspace(lib, lay, kv, workspace, dev)
+    workspace, size = _attention_workspace(lib, lay, kv, workspace, dev, stream)
     _call(lib.toploc_attention_paged, "toploc_attention_paged", dev, stream, _ptr(q), _ptr(k_cache), _ptr(v_cache),
           lay, kv, _ptr(block_table), _ptr(seq_offsets), _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(status),
           _ptr(workspace), size)
@@ -254,9 +268,9 @@ def toploc_attention_prompt(q, k, v, seq_offsets, max_tokens, scale=None, out=No
     (views of one tensor are fine), seq_offsets int32 [n + 1], max_tokens bounds a sequence's length.  Returns
     (out, lse or None)."""
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     if lse is None and want_lse:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        lse = _empty(q.shape[:2], torch.float32, q.device, stream)
     dev = _device("toploc_attention_prompt", q, k, v, seq_offsets, out, lse, status, workspace)
     n = seq_offsets.shape[0] - 1
     _need(n >= 0, "seq_offsets must have num_seqs + 1 entries")
@@ -269,7 +283,7 @@ def toploc_attention_prompt(q, k, v, seq_offsets, max_tokens, scale=None, out=No
     lay = _attention_layout(q, k.shape[1], n, max_tokens, scale, out, lse)
     kv = _pack(_KV, 0, 0, 0, 0, 0, 0, k.stride(0), k.stride(1), 0, v.stride(0), v.stride(1))
     lib = _library()
-    workspace, size = _attention_workspace(lib, lay, kv, workspace, dev)
+    workspace, size = _attention_workspace(lib, lay, kv, workspace, dev, stream)
     _call(lib.toploc_attention_prompt, "toploc_attention_prompt", dev, stream, _ptr(q), _ptr(k), _ptr(v), lay, kv,
           _ptr(seq_offsets), _ptr(out), _ptr(lse), _ptr(status), _ptr(workspace), size)
     return out, lse
@@ -285,13 +299,13 @@ def toploc_rmsnorm_residual(x, residual, weight, eps, residual_out=None, y=None,
     _need(x.dtype in _DTYPES and x.dim() == 2 and x.stride(1) == 1, "x must be bfloat16 or float32 [rows, hidden]")
     rows, hidden = x.shape
     if y is None:
-        y = torch.empty((rows, hidden), dtype=torch.float8_e4m3fn if quantize else x.dtype, device=x.device)
+        y = _empty((rows, hidden), torch.float8_e4m3fn if quantize else x.dtype, x.device, stream)
     quant = y.dtype == torch.float8_e4m3fn
     _need(group >= 0, "group must not be negative")
     if quant and scales is None:
-        scales = torch.empty((rows, 1 if group == 0 else -(-hidden // group)), dtype=torch.float32, device=x.device)
+        scales = _empty((rows, 1 if group == 0 else -(-hidden // group)), torch.float32, x.device, stream)
     if residual is not None and residual_out is None:
-        residual_out = torch.empty((rows, hidden), dtype=x.dtype, device=x.device)
+        residual_out = _empty((rows, hidden), x.dtype, x.device, stream)
     dev = _device("toploc_rmsnorm_residual", x, residual, weight, residual_out, y, scales)
     strides = []
     for t, what in ((x, "x"), (residual, "residual"), (residual_out, "residual_out")):

@@ -1,0 +1,76 @@
+"""Memory that a call allocates belongs to the stream it was given (no GPU: the allocator's streams are stood in for).
+
+A block allocated on torch's current stream and dropped on return would go to the next allocation of the current stream,
+while the kernels on the given stream still write to it."""
+import contextlib
+
+import pytest
+import torch
+
+import paper_2501_16007_b200 as tl
+from paper_2501_16007_b200 import model_ops
+
+CURRENT, SIDE = "current", "side"
+
+
+@pytest.fixture
+def allocations(monkeypatch):
+    """[(shape, stream that was current at the allocation, streams recorded later)]"""
+    made, now, empty = [], [CURRENT], torch.empty
+
+    @contextlib.contextmanager
+    def on(stream):
+        now.append(stream)
+        yield
+        now.pop()
+
+    def recorded_empty(*shape, **kw):
+        t = empty(*shape, **dict(kw, device="cpu"))
+        made.append((t, now[-1], []))
+        return t
+
+    def record(t, stream):
+        for other, _, streams in made:
+            if other is t:
+                streams.append(stream)
+
+    monkeypatch.setattr(torch, "empty", recorded_empty)
+    monkeypatch.setattr(torch, "empty_like", lambda t, **kw: recorded_empty(t.shape, dtype=t.dtype))
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: now[-1])
+    monkeypatch.setattr(torch.Tensor, "record_stream", record)
+    return made
+
+
+def check(made, shapes, stream):
+    """All allocations were made on `stream`; what the caller gets is also kept for the current one."""
+    assert sorted(tuple(t.shape) for t, _, _ in made) == sorted(shapes)
+    for t, where, recorded in made:
+        assert where == stream, "%s allocated on the %s stream" % (tuple(t.shape), where)
+        if stream != CURRENT:
+            assert recorded == ([] if t.shape == (640,) else [CURRENT]), tuple(t.shape)   # 640: the workspace
+
+
+class Library:
+    def __getattr__(self, name):
+        return lambda *args: 640 if name.endswith("bytes") else 0
+
+
+@pytest.mark.parametrize("given,expected", [(None, CURRENT), (CURRENT, CURRENT), (SIDE, SIDE)])
+def test_model_operators(monkeypatch, allocations, given, expected):
+    monkeypatch.setattr(model_ops, "_library", Library)
+    monkeypatch.setattr(model_ops, "_device", lambda name, *tensors: tensors[0].device)
+    monkeypatch.setattr(model_ops, "_call", lambda *args: None)
+    q, kv = torch.zeros((4, 8, 64), dtype=torch.bfloat16), torch.zeros((4, 2, 64), dtype=torch.bfloat16)
+    cache, i32 = torch.zeros((3, 16, 2, 64), dtype=torch.bfloat16), torch.int32
+    table, offsets, lens = torch.zeros((1, 3), dtype=i32), torch.zeros(2, dtype=i32), torch.zeros(1, dtype=i32)
+    del allocations[:]
+    tl.toploc_attention_paged(q, cache, cache, table, offsets, lens, 4, want_lse=True, stream=given)
+    check(allocations, [(4, 8, 64), (4, 8), (640,)], expected)
+    del allocations[:]
+    tl.toploc_attention_prompt(q, kv, kv, offsets, 4, want_lse=True, stream=given)
+    check(allocations, [(4, 8, 64), (4, 8), (640,)], expected)
+    x, w = torch.zeros((4, 512), dtype=torch.bfloat16), torch.zeros(512, dtype=torch.bfloat16)
+    del allocations[:]
+    tl.toploc_rmsnorm_residual(x, x, w, 1e-5, quantize=True, group=128, stream=given)
+    check(allocations, [(4, 512), (4, 512), (4, 4)], expected)
