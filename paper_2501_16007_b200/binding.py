@@ -2,7 +2,8 @@
 
 Every step of the proof path runs in the CUDA library (csrc/libtoploc.so).  torch is
 used for device memory and streams, nothing else.  There is no fallback: if the library
-is missing or the arguments are wrong, the call raises.
+is missing or the arguments are wrong, the call raises.  What a call allocates (outputs that are
+not given, its workspace) is memory of the stream it runs on.
 """
 import ctypes
 import os
@@ -221,10 +222,23 @@ def _dev_ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
-def _workspace(lay, workspace, device):
+def _empty(shape, dtype, device, stream, hidden=False):
+    """A tensor that work on `stream` (None: torch's current one) may write at once: its memory is one of that stream's, so
+    that neither what the current stream still does with a block freed there, nor the next allocation after this tensor is
+    gone, can meet the call.  hidden: the caller never sees it; else it may be read, and dropped, on the current stream."""
+    if stream is None or stream == torch.cuda.current_stream(device):
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if not hidden:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _workspace(lay, workspace, device, stream):
     need = toploc_workspace_bytes(lay)
     if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = _empty((need,), torch.uint8, device, stream, hidden=True)
     return workspace, (0 if workspace is None else workspace.numel() * workspace.element_size())
 
 
@@ -239,15 +253,15 @@ def toploc_build_proofs(act, lay, proofs=None, status=None, indices=None, worksp
     pb = toploc_layout_proof_bytes(lay)
     dev = act.device
     if proofs is None:
-        proofs = torch.empty((n, pb), dtype=torch.uint8, device=dev)
+        proofs = _empty((n, pb), torch.uint8, dev, stream)
     if status is None:
-        status = torch.empty((n,), dtype=torch.uint8, device=dev)
+        status = _empty((n,), torch.uint8, dev, stream)
     if indices is None and want_indices:
-        indices = torch.empty((n, lay.k), dtype=torch.int32, device=dev)
+        indices = _empty((n, lay.k), torch.int32, dev, stream)
     assert proofs.is_contiguous() and proofs.numel() == n * pb and status.numel() == n
     assert indices is None or (indices.is_contiguous() and indices.numel() == n * lay.k
                                and indices.dtype == torch.int32)
-    workspace, wbytes = _workspace(lay, workspace, dev)
+    workspace, wbytes = _workspace(lay, workspace, dev, stream)
     with torch.cuda.device(dev):
         rc = load_library().toploc_build_proofs(
             _dev_ptr(act), ctypes.byref(lay), _dev_ptr(proofs), _dev_ptr(status), _dev_ptr(indices),
@@ -266,12 +280,12 @@ def toploc_verify_proofs(act, lay, proofs, thresholds=None, results=None, gen_in
     dev = act.device
     thr = thresholds if thresholds is not None else default_thresholds()
     if results is None:
-        results = torch.empty((n, RESULT_DTYPE.itemsize), dtype=torch.uint8, device=dev)
+        results = _empty((n, RESULT_DTYPE.itemsize), torch.uint8, dev, stream)
     assert proofs.is_contiguous() and proofs.numel() == n * toploc_layout_proof_bytes(lay)
     assert results.is_contiguous() and results.numel() == n * RESULT_DTYPE.itemsize
     assert gen_indices is None or (gen_indices.is_contiguous() and gen_indices.dtype == torch.int32
                                    and gen_indices.numel() == n * lay.k)
-    workspace, wbytes = _workspace(lay, workspace, dev)
+    workspace, wbytes = _workspace(lay, workspace, dev, stream)
     with torch.cuda.device(dev):
         rc = load_library().toploc_verify_proofs(
             _dev_ptr(act), ctypes.byref(lay), _dev_ptr(proofs), ctypes.byref(thr), _dev_ptr(results),
@@ -316,11 +330,11 @@ def toploc_verify_proofs_per_chunk_thresholds(act, lay, proofs, thresholds, resu
     n = toploc_num_chunks(lay)
     dev = act.device
     if results is None:
-        results = torch.empty((n, RESULT_DTYPE.itemsize), dtype=torch.uint8, device=dev)
+        results = _empty((n, RESULT_DTYPE.itemsize), torch.uint8, dev, stream)
     assert proofs.is_contiguous() and proofs.numel() == n * toploc_layout_proof_bytes(lay)
     assert thresholds.is_contiguous() and thresholds.numel() * thresholds.element_size() == n * THRESHOLDS_DTYPE.itemsize
     assert results.is_contiguous() and results.numel() == n * RESULT_DTYPE.itemsize
-    workspace, wbytes = _workspace(lay, workspace, dev)
+    workspace, wbytes = _workspace(lay, workspace, dev, stream)
     with torch.cuda.device(dev):
         rc = load_library().toploc_verify_proofs_per_chunk_thresholds(
             _dev_ptr(act), ctypes.byref(lay), _dev_ptr(proofs), _dev_ptr(thresholds), _dev_ptr(results),
@@ -381,14 +395,14 @@ def toploc_select_topk(act, lay, sel_indices=None, sel_patterns=None, status=Non
     n = toploc_num_chunks(lay)
     dev = act.device
     if sel_indices is None:
-        sel_indices = torch.empty((n, lay.k), dtype=torch.int32, device=dev)
+        sel_indices = _empty((n, lay.k), torch.int32, dev, stream)
     if sel_patterns is None:
-        sel_patterns = torch.empty((n, lay.k), dtype=torch.int16, device=dev)
+        sel_patterns = _empty((n, lay.k), torch.int16, dev, stream)
     if status is None:
-        status = torch.empty((n,), dtype=torch.uint8, device=dev)
+        status = _empty((n,), torch.uint8, dev, stream)
     if ranked_indices is None and want_ranked:
-        ranked_indices = torch.empty((n, lay.k), dtype=torch.int32, device=dev)
-    workspace, wbytes = _workspace(lay, workspace, dev)
+        ranked_indices = _empty((n, lay.k), torch.int32, dev, stream)
+    workspace, wbytes = _workspace(lay, workspace, dev, stream)
     with torch.cuda.device(dev):
         rc = load_library().toploc_select_topk(
             _dev_ptr(act), ctypes.byref(lay), _dev_ptr(sel_indices), _dev_ptr(sel_patterns), _dev_ptr(status),
@@ -431,13 +445,13 @@ def toploc_stream_finish(state, lay, proofs=None, status=None, indices=None, wor
     dev = state.device
     n, pb = lay.num_seqs, toploc_layout_proof_bytes(lay)
     if proofs is None:
-        proofs = torch.empty((n, pb), dtype=torch.uint8, device=dev)
+        proofs = _empty((n, pb), torch.uint8, dev, stream)
     if status is None:
-        status = torch.empty((n,), dtype=torch.uint8, device=dev)
+        status = _empty((n,), torch.uint8, dev, stream)
     if indices is None and want_indices:
-        indices = torch.empty((n, lay.k), dtype=torch.int32, device=dev)
+        indices = _empty((n, lay.k), torch.int32, dev, stream)
     if workspace is None:
-        workspace = torch.empty(max(16, toploc_stream_workspace_bytes(lay)), dtype=torch.uint8, device=dev)
+        workspace = _empty((max(16, toploc_stream_workspace_bytes(lay)),), torch.uint8, dev, stream, hidden=True)
     with torch.cuda.device(dev):
         rc = load_library().toploc_stream_finish(
             _dev_ptr(state), ctypes.byref(lay), _dev_ptr(proofs), _dev_ptr(status), _dev_ptr(indices),
@@ -462,9 +476,9 @@ def toploc_commit_direct(act, lay, commits=None, status=None, stream=None):
         raise ToplocError("toploc_commit_direct needs a CUDA tensor")
     n, dev = _direct_chunks(lay), act.device
     if commits is None:
-        commits = torch.empty((n, 6 * lay.k), dtype=torch.uint8, device=dev)
+        commits = _empty((n, 6 * lay.k), torch.uint8, dev, stream)
     if status is None:
-        status = torch.empty((n,), dtype=torch.uint8, device=dev)
+        status = _empty((n,), torch.uint8, dev, stream)
     assert commits.is_contiguous() and commits.numel() == n * 6 * lay.k and status.numel() == n
     with torch.cuda.device(dev):
         rc = load_library().toploc_commit_direct(_dev_ptr(act), ctypes.byref(lay), _dev_ptr(commits),
@@ -482,9 +496,9 @@ def toploc_verify_direct(act, lay, commits, thresholds=None, results=None, exp_d
     n, dev = _direct_chunks(lay), act.device
     thr = thresholds if thresholds is not None else default_thresholds(lay.k)
     if results is None:
-        results = torch.empty((n, RESULT_DTYPE.itemsize), dtype=torch.uint8, device=dev)
+        results = _empty((n, RESULT_DTYPE.itemsize), torch.uint8, dev, stream)
     if exp_dev is None and want_exp_dev:
-        exp_dev = torch.empty((n, 9), dtype=torch.int32, device=dev)
+        exp_dev = _empty((n, 9), torch.int32, dev, stream)
     assert commits.is_contiguous() and commits.numel() == n * 6 * lay.k
     assert results.is_contiguous() and results.numel() == n * RESULT_DTYPE.itemsize
     with torch.cuda.device(dev):
@@ -502,9 +516,9 @@ def toploc_verify_direct_per_chunk_thresholds(act, lay, commits, thresholds, res
         raise ToplocError("toploc_verify_direct_per_chunk_thresholds needs CUDA tensors")
     n, dev = _direct_chunks(lay), act.device
     if results is None:
-        results = torch.empty((n, RESULT_DTYPE.itemsize), dtype=torch.uint8, device=dev)
+        results = _empty((n, RESULT_DTYPE.itemsize), torch.uint8, dev, stream)
     if exp_dev is None and want_exp_dev:
-        exp_dev = torch.empty((n, 9), dtype=torch.int32, device=dev)
+        exp_dev = _empty((n, 9), torch.int32, dev, stream)
     assert commits.is_contiguous() and commits.numel() == n * 6 * lay.k
     assert thresholds.is_contiguous() and thresholds.numel() * thresholds.element_size() == n * THRESHOLDS_DTYPE.itemsize
     with torch.cuda.device(dev):

@@ -11,7 +11,7 @@ import struct
 import torch
 
 from . import binding
-from .binding import TOPLOC_DTYPE_BF16, TOPLOC_DTYPE_FP32, ToplocError
+from .binding import TOPLOC_DTYPE_BF16, TOPLOC_DTYPE_FP32, ToplocError, _empty
 
 __all__ = [
     "TOPLOC_SEQ_OK", "TOPLOC_SEQ_BAD_LENGTH", "TOPLOC_SEQ_NO_PAGES", "TOPLOC_SEQ_TABLE_FULL", "TOPLOC_SEQ_BATCH_FULL",
@@ -116,19 +116,6 @@ def _vector(t, dtype, length, what):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
-
-
-def _empty(shape, dtype, device, stream, hidden=False):
-    """A tensor that work on `stream` (None: torch's current one) may write at once: its memory is one of that stream's, so
-    that neither what the current stream still does with a block freed there, nor the next allocation after this tensor is
-    gone, can meet the call.  hidden: the caller never sees it; else it may be read, and dropped, on the current stream."""
-    if stream is None or stream == torch.cuda.current_stream(device):
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    if not hidden:
-        t.record_stream(torch.cuda.current_stream(device))
-    return t
 
 
 def _pack(layout, *fields):

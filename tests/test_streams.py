@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2501_16007_b200 as tl
-from paper_2501_16007_b200 import model_ops
+from paper_2501_16007_b200 import binding, model_ops
 
 CURRENT, SIDE = "current", "side"
 
@@ -74,3 +74,35 @@ def test_model_operators(monkeypatch, allocations, given, expected):
     del allocations[:]
     tl.toploc_rmsnorm_residual(x, x, w, 1e-5, quantize=True, group=128, stream=given)
     check(allocations, [(4, 512), (4, 512), (4, 4)], expected)
+
+
+@pytest.mark.parametrize("given,expected", [(None, CURRENT), (CURRENT, CURRENT), (SIDE, SIDE)])
+def test_proof_path(monkeypatch, allocations, given, expected):
+    monkeypatch.setattr(binding, "load_library", Library)
+    monkeypatch.setattr(binding, "toploc_num_chunks", lambda lay: 2)
+    monkeypatch.setattr(binding, "toploc_stream_workspace_bytes", lambda lay: 640)
+    monkeypatch.setattr(binding, "_stream_ptr", lambda stream: None)
+    monkeypatch.setattr(torch.cuda, "device", lambda dev: contextlib.nullcontext())
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True, raising=False)
+    act = torch.zeros((64, 256), dtype=torch.bfloat16)
+    lay, _ = tl.make_layout(act, 32, 16, 2, 32)
+    proofs, thr = torch.zeros((2, 640), dtype=torch.uint8), tl.ToplocThresholds()
+    per_chunk = torch.zeros((2, 24), dtype=torch.uint8)
+    state = torch.zeros(64, dtype=torch.uint8)
+    commits = torch.zeros((2, 96), dtype=torch.uint8)
+    for call, shapes in [
+            (lambda: tl.toploc_build_proofs(act, lay, want_indices=True, stream=given), [(2, 640), (2,), (2, 16), (640,)]),
+            (lambda: tl.toploc_verify_proofs(act, lay, proofs, thr, stream=given), [(2, 40), (640,)]),
+            (lambda: tl.toploc_verify_proofs_per_chunk_thresholds(act, lay, proofs, per_chunk, stream=given),
+             [(2, 40), (640,)]),
+            (lambda: tl.toploc_select_topk(act, lay, want_ranked=True, stream=given),
+             [(2, 16), (2, 16), (2,), (2, 16), (640,)]),
+            (lambda: tl.toploc_stream_finish(state, lay, want_indices=True, stream=given),
+             [(2, 640), (2,), (2, 16), (640,)]),
+            (lambda: tl.toploc_commit_direct(act, lay, stream=given), [(2, 96), (2,)]),
+            (lambda: tl.toploc_verify_direct(act, lay, commits, thr, stream=given), [(2, 40), (2, 9)]),
+            (lambda: tl.toploc_verify_direct_per_chunk_thresholds(act, lay, commits, per_chunk, stream=given),
+             [(2, 40), (2, 9)])]:
+        del allocations[:]
+        call()
+        check(allocations, shapes, expected)
