@@ -120,7 +120,8 @@ typedef struct {
   int32_t max_new_tokens; /* no sequence brings more (a bound; it sizes the launch) */
   int64_t total_tokens;   /* rows of q, out and lse */
   float scale;            /* > 0, finite; 1 / sqrt(head_dim) as a rule */
-  int32_t reserved;       /* 0 */
+  int32_t wait_tries;     /* 0; else the tries (4 us each) after which a wait inside the kernel gives up, by default
+                             8 s in all (see TOPLOC_SEQ_WAIT_EXPIRED) */
   int64_t q_token_stride, q_head_stride;     /* elements; the last dimension is contiguous */
   int64_t out_token_stride, out_head_stride;
 } toploc_attention_layout;

@@ -47,6 +47,7 @@ struct TcParams {
   int page_shift, page_tiles;  // pages below a tile: log2 of their size; others: tiles a page
   float share_scale;  // 1 / blocks
   int q_bytes;    // bytes of a query tile's copy
+  int wait_tries; // limit of a wait
   bool wide_out;  // rows of the output at multiples of 32 bytes
   Part* parts;    // [blocks][2]
 };
@@ -297,7 +298,6 @@ struct Feeder {
   const CUtensorMap* map;
   typename S::Head& sh;
   uint32_t ring, base = 0;             // places in front of the item
-  uint32_t fed = 0, fed_parity = 0;    // by stage: this warp's last copy there
   volatile int* gave_up;
   Item im;
   int tiles = 0, page = 0, next = 0, lane = threadIdx.x & 31;
@@ -331,8 +331,7 @@ struct Feeder {
     const int after = page_of(j + 2);
     fine = warp_wait(sh.empty[stage], ring_parity(place, kStages) ^ 1, gave_up);
     if (!fine) return;
-    fed |= 1u << stage;
-    fed_parity = (fed_parity & ~(1u << stage)) | ring_parity(place, kStages) << stage;
+    if (lane == 0) sh.fed[stage] = place + 1;  // (the other feeding warp's word too: a stage's copies follow one another)
     const int key0 = im.kbegin + j * kKeyTile;
     if (tp.p.kv_lens) {
       if (page < 0 || page >= tp.p.num_pages) {
@@ -362,14 +361,20 @@ struct Feeder {
     page = next;
     next = after;
   }
-
-  // After a wait gave up: no copy of this warp is in flight when it returns.
-  __device__ void drain() const {
-#pragma unroll 1
-    for (int i = 0; i < kStages; ++i)
-      if (fed >> i & 1) barrier_drain(shared_address(&sh.full[i]), fed_parity >> i & 1);
-  }
 };
+
+// The block ends early: a wait gave up, in whatever role, and all roles have left their loops (the threads are
+// synchronised in front of this and behind it).  Copies have to land before the block ends, products to end before tensor
+// memory is freed.  By a whole warp, the one that issued the products.
+template <typename S>
+__device__ __noinline__ void drain_block(typename S::Head& sh) {
+  if (sh.queries_fed > 0) barrier_drain(shared_address(&sh.q_full), (sh.queries_fed - 1) & 1);
+#pragma unroll 1
+  for (int i = 0; i < S::kStages; ++i)  // (a stage's last copy: what the other feeding warp had there before has been used)
+    if (sh.fed[i] > 0) barrier_drain(shared_address(&sh.full[i]), ring_parity(sh.fed[i] - 1, S::kStages));
+  if (elect_one()) mma_commit(shared_address(&sh.drain));
+  barrier_drain(shared_address(&sh.drain), 0);
+}
 
 __device__ __forceinline__ Item uniform(const Item& im) {  // the same for every lane, and known to be
   Item r;

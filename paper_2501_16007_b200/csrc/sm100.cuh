@@ -43,40 +43,43 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
   return done != 0;
 }
 
-// No wait is endless: after this many tries (each up to about a microsecond, a second or two in all; the
-// longest wait that is due ends in milliseconds) it gives up.
+// No wait is endless: after so many tries it gives up.  A try that fails takes 4 us (measured, whatever limit of its own it
+// is given), so this is 8 s; the longest wait that is due is for a warp that passes idle sequences one by one (a million of
+// them in 0.2 s).
 constexpr int kWaitTries = 2000000;
 
 // True when the phase of `parity` is complete; false after the limit, or where another wait of the block
-// gave up (*gave_up, in shared memory).  One small loop in assembly: the kernels wait in some forty places,
+// gave up.  gave_up: two words of shared memory at an 8-byte aligned place, whether a wait gave up and the limit.
+// One small loop in assembly: the kernels wait in some forty places,
 // and code that does not fit the instruction caches costs them more than the waits.
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile int* gave_up) {
   uint32_t done;
   asm volatile(
       "{\n\t"
       ".reg .pred p, q;\n\t"
-      ".reg .u32 n, g;\n\t"
+      ".reg .u32 n, g, m;\n\t"
       "mov.u32 n, 0;\n"
       "again:\n\t"
       "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000;\n\t"
       "@p bra end;\n\t"
-      "ld.volatile.shared.u32 g, [%3];\n\t"
+      "ld.volatile.shared.v2.u32 {g, m}, [%3];\n\t"
       "setp.ne.u32 q, g, 0;\n\t"
       "@q bra end;\n\t"
       "add.u32 n, n, 1;\n\t"
-      "setp.lt.u32 q, n, %4;\n\t"
+      "setp.lt.u32 q, n, m;\n\t"
       "@q bra again;\n\t"
       "st.volatile.shared.u32 [%3], 1;\n"
       "end:\n\t"
       "selp.u32 %0, 1, 0, p;\n\t"
       "}"
       : "=r"(done)
-      : "r"(bar), "r"(parity), "r"(shared_address((const void*)gave_up)), "n"(kWaitTries)
+      : "r"(bar), "r"(parity), "r"(shared_address((const void*)gave_up))
       : "memory");
   return done != 0;
 }
 
-// Waits for the block's own copies or products in flight before it ends early; bounded all the same.
+// Waits for the block's own copies or products in flight before it ends early; bounded all the same, by a limit of its
+// own.
 __device__ __forceinline__ void barrier_drain(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
   for (int i = 0; i < kWaitTries && !barrier_try(bar, parity); ++i) {

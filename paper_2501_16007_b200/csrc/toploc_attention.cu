@@ -212,7 +212,7 @@ int splits_of(const toploc_attention_layout* lay, const toploc_kv_layout* kv) {
 int check_layout(const toploc_attention_layout* lay, const toploc_kv_layout* kv) {
   if (!lay || !kv || lay->num_seqs < 0 || lay->max_new_tokens < 0 || lay->total_tokens < 0 || lay->q_heads <= 0 ||
       lay->kv_heads <= 0 || lay->head_dim <= 0 || !(lay->scale > 0.f) || !(lay->scale < INFINITY) || kv->page_size < 0 ||
-      lay->q_heads % lay->kv_heads != 0)
+      lay->wait_tries < 0 || lay->q_heads % lay->kv_heads != 0)
     return TOPLOC_ERR_INVALID_ARGUMENT;
   if (kv->page_size > 0 && (kv->num_pages < 0 || kv->max_pages < 0 || kv->table_stride < kv->max_pages))
     return TOPLOC_ERR_INVALID_ARGUMENT;

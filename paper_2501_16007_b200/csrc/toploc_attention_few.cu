@@ -40,7 +40,9 @@ struct FewShared {
     uint64_t item_full[kItems], item_empty[kItems];
     Item items[kItems];
     uint32_t tmem;
-    int gave_up;
+    alignas(8) int gave_up[2];  // a wait ran out; the limit of a wait
+    uint32_t fed[kStages];      // by stage: place of the last copy there + 1
+    uint32_t queries_fed;       // copies of queries
     int bad_values[2];    // number of the item (by parity) in whose hidden keys' tiles a value was not finite
     uint32_t exceeds[2];  // number of the tile (by parity) with a score over the limit
     float rows[4][N];     // by warp: maxima, or sums
@@ -65,7 +67,7 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
   unsigned char* queries = ring + kStages * S::kTileBytes;
   unsigned char* weights = queries + S::kQueryBytes;
   const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  volatile int* gave_up = &sh.gave_up;
+  volatile int* gave_up = sh.gave_up;
 
   asm volatile("griddepcontrol.launch_dependents;");  // the join waits for this grid to end
   if (threadIdx.x == 0) {
@@ -73,6 +75,7 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
     for (int i = 0; i < kStages; ++i) {
       barrier_init(shared_address(&sh.full[i]), 1);
       barrier_init(shared_address(&sh.empty[i]), 1);
+      sh.fed[i] = 0;
     }
     for (int i = 0; i < 2; ++i) {
       barrier_init(shared_address(&sh.s_full[i]), 1);
@@ -90,7 +93,8 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
       barrier_init(shared_address(&sh.item_full[i]), 1);
       barrier_init(shared_address(&sh.item_empty[i]), 6);
     }
-    sh.gave_up = 0;
+    sh.gave_up[0] = 0;
+    sh.gave_up[1] = tp.wait_tries;
     barrier_init_fence();
   }
   constexpr uint32_t kColumns = 4 * N;  // tensor memory: two tiles of scores, the outputs (a power of two at least 32)
@@ -149,10 +153,7 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
         feeder.feed(j, keys ? key_place(false, j) : value_place(false, j, im.n0));
       if (!feeder.fine) break;
     }
-    if (*gave_up) {  // copies in flight have to land before the block ends
-      if (q_uses > 0) barrier_drain(shared_address(&sh.q_full), (q_uses - 1) & 1);
-      feeder.drain();
-    }
+    if (keys && lane == 0) sh.queries_fed = q_uses;
   } else if (warp == 5) {
     // ---- products: the whole warp follows, one lane issues ----
     constexpr uint32_t kScores = bf16_product(N, false, false), kValues = bf16_product(N, true, true);
@@ -224,11 +225,6 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
       if (!ok) break;
       used += 2 * n;
     }
-    if (*gave_up && lane == 0) {  // products in flight have to end before tensor memory is freed
-      mma_commit(shared_address(&sh.drain));
-      barrier_drain(shared_address(&sh.drain), 0);
-    }
-    __syncwarp();
   } else {
     // ---- softmax: a thread per key; at the end a thread per channel ----
     const int me = threadIdx.x;  // 0 .. 127
@@ -429,8 +425,12 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
     }
   }
   __syncthreads();
-  if (sh.gave_up && p.status && threadIdx.x == 0) {
-    for (int i = blockIdx.x; i < p.num_seqs; i += gridDim.x) p.status[i] = TOPLOC_SEQ_WAIT_EXPIRED;
+  if (sh.gave_up[0]) {  // the same for all threads
+    if (warp == 5) drain_block<S>(sh);
+    if (p.status && threadIdx.x == 0) {
+      for (int i = blockIdx.x; i < p.num_seqs; i += gridDim.x) p.status[i] = TOPLOC_SEQ_WAIT_EXPIRED;
+    }
+    __syncthreads();
   }
   if (warp == 5) tmem_free(tmem, kColumns);
 }

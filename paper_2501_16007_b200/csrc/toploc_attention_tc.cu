@@ -60,7 +60,9 @@ struct Shared {
     uint64_t item_full[kItems], item_empty[kItems];
     Item items[kItems];
     uint32_t tmem;
-    int gave_up;
+    alignas(8) int gave_up[2];  // a wait ran out; the limit of a wait
+    uint32_t fed[kStages];      // by stage: place of the last copy there + 1
+    uint32_t queries_fed;       // copies of queries
     uint64_t cleaned[kStages];  // the stage's value tile, one with hidden keys, may be used
     int bad_values[8];  // number of the item (of 8) in whose hidden keys' tiles a value was not finite
   };
@@ -123,7 +125,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
   unsigned char* q_tiles = base + S::kHeadBytes + S::kExchangeBytes;
   unsigned char* ring = q_tiles + 2 * S::kTileBytes;
   const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  volatile int* gave_up = &sh.gave_up;
+  volatile int* gave_up = sh.gave_up;
 
   // tell the join kernel that it may be scheduled (it waits for this grid to end)
   asm volatile("griddepcontrol.launch_dependents;");
@@ -133,6 +135,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       barrier_init(shared_address(&sh.full[i]), 1);
       barrier_init(shared_address(&sh.empty[i]), 1);
       barrier_init(shared_address(&sh.cleaned[i]), 1);
+      sh.fed[i] = 0;
     }
     for (int w = 0; w < 2; ++w) {
       barrier_init(shared_address(&sh.s_full[w]), 1);
@@ -151,7 +154,8 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
     }
 #pragma unroll 1
     for (int i = 0; i < 8; ++i) sh.bad_values[i] = -1;
-    sh.gave_up = 0;
+    sh.gave_up[0] = 0;
+    sh.gave_up[1] = tp.wait_tries;
     barrier_init_fence();
   }
   if (warp == 9) tmem_alloc(shared_address(&sh.tmem), 512);
@@ -228,10 +232,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       }
       if (!feeder.fine) break;
     }
-    if (*gave_up) {  // copies in flight have to land before the block ends
-      if (q_uses > 0) barrier_drain(shared_address(&sh.q_full), (q_uses - 1) & 1);
-      feeder.drain();
-    }
+    if (keys && lane == 0) sh.queries_fed = q_uses;
   } else if (warp == 9) {
     lower_registers<kOtherRegisters>();
     // ---- products: the whole warp follows, one lane issues ----
@@ -335,11 +336,6 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       if (!ok) break;
       used += 2 * n;
     }
-    if (*gave_up && lane == 0) {  // products in flight have to end before tensor memory is freed
-      mma_commit(shared_address(&sh.drain));
-      barrier_drain(shared_address(&sh.drain), 0);
-    }
-    __syncwarp();
   } else if (warp == 11) {
     lower_registers<kOtherRegisters>();
   } else {
@@ -608,8 +604,12 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
     }
   }
   __syncthreads();
-  if (sh.gave_up && p.status && blockIdx.x < (unsigned)p.num_seqs && threadIdx.x == 0) {
-    for (int i = blockIdx.x; i < p.num_seqs; i += gridDim.x) p.status[i] = TOPLOC_SEQ_WAIT_EXPIRED;
+  if (sh.gave_up[0]) {  // the same for all threads
+    if (warp == 9) drain_block<S>(sh);
+    if (p.status && blockIdx.x < (unsigned)p.num_seqs && threadIdx.x == 0) {
+      for (int i = blockIdx.x; i < p.num_seqs; i += gridDim.x) p.status[i] = TOPLOC_SEQ_WAIT_EXPIRED;
+    }
+    __syncthreads();
   }
   if (warp == 9) tmem_free(tmem, 512);
 }
@@ -786,6 +786,7 @@ int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, 
   tp.item_tokens = tp.item_rows / p.group;
   tp.piece = few ? 2 : 4;
   tp.share_scale = 1.f / (float)blocks;
+  tp.wait_tries = lay->wait_tries > 0 ? lay->wait_tries : kWaitTries;
   tp.page_shift = 0;
   while (page >> (tp.page_shift + 1) > 0) ++tp.page_shift;
   tp.page_tiles = page > kKeyTile ? page / kKeyTile : 1;

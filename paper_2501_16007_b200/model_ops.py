@@ -43,7 +43,7 @@ class ToplocKvLayout(ctypes.Structure):
 
 class ToplocAttentionLayout(ctypes.Structure):
     _fields_ = [("dtype", _i32), ("head_dim", _i32), ("q_heads", _i32), ("kv_heads", _i32), ("num_seqs", _i32),
-                ("max_new_tokens", _i32), ("total_tokens", _i64), ("scale", ctypes.c_float), ("reserved", _i32),
+                ("max_new_tokens", _i32), ("total_tokens", _i64), ("scale", ctypes.c_float), ("wait_tries", _i32),
                 ("q_token_stride", _i64), ("q_head_stride", _i64), ("out_token_stride", _i64),
                 ("out_head_stride", _i64)]
 

@@ -204,3 +204,8 @@ def test_wrappers_refuse_numbers_that_do_not_fit():
     lay = tl.ToplocAttentionLayout.from_buffer_copy(model_ops._attention_layout(q, 2, 3, 4, 0.25, q, None))
     assert (lay.head_dim, lay.q_heads, lay.kv_heads, lay.num_seqs, lay.max_new_tokens, lay.total_tokens, lay.scale,
             lay.q_token_stride, lay.out_head_stride) == (64, 2, 2, 3, 4, 4, 0.25, 128, 64)
+
+
+def test_wait_limit_refusals(lib):
+    assert paged(lib, attention_layout(wait_tries=-1)) == INVALID
+    assert paged(lib, attention_layout(wait_tries=5, num_seqs=0)) == 0
