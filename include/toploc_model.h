@@ -31,7 +31,7 @@ extern "C" {
 #define TOPLOC_SEQ_TABLE_FULL 3 /* more pages than a row of the block table holds */
 #define TOPLOC_SEQ_BATCH_FULL 4 /* the sequence's tokens end beyond the token buffers */
 #define TOPLOC_SEQ_BAD_PAGE 5   /* a block table entry outside the cache */
-#define TOPLOC_SEQ_WAIT_EXPIRED 6 /* a wait inside the kernel ran out of its limit; the rows are not valid */
+#define TOPLOC_SEQ_WAIT_EXPIRED 6 /* a wait inside the kernel ran out of its limit; rows that were not finished are NaN */
 
 const char* toploc_sequence_status_string(int sequence_status);
 

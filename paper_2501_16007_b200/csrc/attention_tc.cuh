@@ -290,6 +290,35 @@ struct Walk {
   }
 };
 
+// The block ends early: nothing in its stretch counts.  The sequences of the stretch are flagged and their rows there become
+// NaN, so that the failure shows without a status too; of a row tile that other blocks share in, the part's lse does, which
+// makes the joined rows NaN whatever an earlier call has left in the workspace (the records of the parts are written again:
+// the block may have given up in front of them).  By a whole warp, all roles having left their loops.
+__device__ __noinline__ void abandon(const TcParams& tp, const Stretch& stretch) {
+  const AttentionParams& p = tp.p;
+  const int lane = threadIdx.x & 31;
+  Walk walk(tp);
+  walk.at = stretch.begin;
+  walk.end = stretch.end;
+  Item im;
+#pragma unroll 1
+  while (walk.next(im)) {
+    if (p.status && lane == 0) p.status[im.seq] = TOPLOC_SEQ_WAIT_EXPIRED;
+#pragma unroll 1
+    for (int r = lane; r < min(tp.item_rows, im.rows - im.row0); r += 32) {
+      if (im.slot >= 0) {
+        p.part_lse[((long long)blockIdx.x * 2 + im.slot) * tp.item_rows + r] = NAN;
+        continue;
+      }
+      const int token = (im.row0 + r) / p.group, head = im.head * p.group + im.row0 + r - token * p.group;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + (im.first + token) * p.out_token + head * p.out_head;
+#pragma unroll 1
+      for (int c = 0; c < p.head_dim; ++c) out[c] = __float2bfloat16_rn(NAN);
+      if (p.lse) p.lse[(long long)(im.first + token) * p.q_heads + head] = NAN;
+    }
+  }
+}
+
 // One warp's copies into the ring: the keys, or the values, of item after item.
 template <typename S>
 struct Feeder {

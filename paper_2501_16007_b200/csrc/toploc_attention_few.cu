@@ -43,6 +43,7 @@ struct FewShared {
     alignas(8) int gave_up[2];  // a wait ran out; the limit of a wait
     uint32_t fed[kStages];      // by stage: place of the last copy there + 1
     uint32_t queries_fed;       // copies of queries
+    Stretch stretch;            // of the block's work
     int bad_values[2];    // number of the item (by parity) in whose hidden keys' tiles a value was not finite
     uint32_t exceeds[2];  // number of the tile (by parity) with a score over the limit
     float rows[4][N];     // by warp: maxima, or sums
@@ -118,6 +119,7 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
         prefetch_map(&map_v);
       }
       walk.begin<kFewThreads>(run_cost);
+      if (lane == 0) sh.stretch = Stretch{walk.at, walk.end};
     }
     uint32_t q_uses = 0;
     Feeder<S> feeder(tp, keys ? &map_k : &map_v, sh, ring, gave_up);
@@ -427,9 +429,7 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
   __syncthreads();
   if (sh.gave_up[0]) {  // the same for all threads
     if (warp == 5) drain_block<S>(sh);
-    if (p.status && threadIdx.x == 0) {
-      for (int i = blockIdx.x; i < p.num_seqs; i += gridDim.x) p.status[i] = TOPLOC_SEQ_WAIT_EXPIRED;
-    }
+    if (warp == 0) abandon(tp, sh.stretch);
     __syncthreads();
   }
   if (warp == 5) tmem_free(tmem, kColumns);

@@ -63,6 +63,7 @@ struct Shared {
     alignas(8) int gave_up[2];  // a wait ran out; the limit of a wait
     uint32_t fed[kStages];      // by stage: place of the last copy there + 1
     uint32_t queries_fed;       // copies of queries
+    Stretch stretch;            // of the block's work
     uint64_t cleaned[kStages];  // the stage's value tile, one with hidden keys, may be used
     int bad_values[8];  // number of the item (of 8) in whose hidden keys' tiles a value was not finite
   };
@@ -179,6 +180,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
         prefetch_map(&map_v);
       }
       walk.begin<kTcThreads>(run_cost);
+      if (lane == 0) sh.stretch = Stretch{walk.at, walk.end};
     }
     uint32_t q_uses = 0;
     Feeder<S> feeder(tp, keys ? &map_k : &map_v, sh, ring, gave_up);
@@ -606,9 +608,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
   __syncthreads();
   if (sh.gave_up[0]) {  // the same for all threads
     if (warp == 9) drain_block<S>(sh);
-    if (p.status && blockIdx.x < (unsigned)p.num_seqs && threadIdx.x == 0) {
-      for (int i = blockIdx.x; i < p.num_seqs; i += gridDim.x) p.status[i] = TOPLOC_SEQ_WAIT_EXPIRED;
-    }
+    if (warp == 0) abandon(tp, sh.stretch);
     __syncthreads();
   }
   if (warp == 9) tmem_free(tmem, 512);

@@ -78,3 +78,25 @@ def test_the_call_returns_and_the_next_one_is_right(case):
         p.call(0)
         assert not p.status.any()
         assert torch.equal(p.out, want[0]) and torch.equal(p.lse, want[1])
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_expired_waits_show_on_the_rows_and_sequences_they_spoil(case):
+    p = Paged(*CASES[case])
+    p.call(0)
+    want_out, want_lse = p.out.clone(), p.lse.clone()
+    assert not p.status.any() and not torch.isnan(want_lse).any()
+    lens = p.offsets[1:] - p.offsets[:-1]
+    sequence = torch.repeat_interleave(torch.arange(p.n), lens).to(DEV)       # of every row
+    for _ in range(5):
+        p.work.fill_(0x3C)                                # what an earlier call may have left there
+        p.call(1)
+        flagged = p.status == tl.TOPLOC_SEQ_WAIT_EXPIRED
+        assert flagged.any() and ((p.status == 0) | flagged).all()
+        assert (lens.to(DEV)[flagged] > 0).all(), "a sequence without rows is flagged"
+        nan = torch.isnan(p.lse)
+        assert torch.equal(torch.where(nan, want_lse, p.lse), want_lse), "a row neither right nor NaN"
+        assert torch.equal(torch.where(nan[:, :, None], want_out, p.out), want_out)
+        assert torch.isnan(p.out[nan]).all()
+        assert flagged[sequence[nan.any(1)]].all(), "a spoilt row whose sequence is not flagged"
+        assert nan.any()
