@@ -170,29 +170,29 @@ __global__ void __launch_bounds__(128) toploc_attention_fp32_kernel(const Attent
 
 // ---- joining the parts -----------------------------------------------------------------------------
 //
-// Part s has out_s = sum p v / sum p and lse_s over its keys; the whole is sum_s w_s out_s / sum_s w_s
-// with w_s = 2^(lse_s - max).  A warp per row, parts in order: the result does not depend on timing.
+// Part i has out_i = sum p v / sum p and lse_i over its keys; the whole is sum_i w_i out_i / sum_i w_i
+// with w_i = 2^(lse_i - max).  A warp per row, parts in order: the result does not depend on timing.
 template <typename T>
-__global__ void __launch_bounds__(128) toploc_attention_join_kernel(const AttentionParams p) {
-  const int lane = threadIdx.x & 31;
-  const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const long long all = p.total_tokens * p.q_heads;
-  if (at >= all) return;
-  const long long token = at / p.q_heads;
-  const int h = (int)(at - token * p.q_heads);
-  if (token >= p.offsets[p.num_seqs]) return;  // rows of no sequence
+__global__ void __launch_bounds__(128) toploc_attention_join_kernel(const AttentionParams p, int blocks_a_seq) {
+  const int lane = threadIdx.x & 31, seq = blockIdx.x / blocks_a_seq;
+  const SeqRange s = sequence(p, seq);  // the rows that the kernel before has written, no others
+  const int r = (blockIdx.x - seq * blocks_a_seq) * 4 + (threadIdx.x >> 5);
+  if (r >= s.rows * p.q_heads) return;
+  const long long token = s.first + r / p.q_heads;
+  const int h = r % p.q_heads;
+  const long long at = token * p.q_heads + h, all = p.total_tokens * p.q_heads;
   float top = -INFINITY;
-  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_lse[s * all + at]);
+  for (int i = 0; i < p.splits; ++i) top = fmaxf(top, p.part_lse[i * all + at]);
   const float ref = top == -INFINITY ? 0.f : top;
   float sum = 0.f;
-  for (int s = 0; s < p.splits; ++s) sum += exp2f(p.part_lse[s * all + at] - ref);
+  for (int i = 0; i < p.splits; ++i) sum += exp2f(p.part_lse[i * all + at] - ref);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T* out = static_cast<T*>(p.out) + token * p.out_token + h * p.out_head;
   for (int c = lane; c < p.head_dim; c += 32) {
     float o = 0.f;
-    for (int s = 0; s < p.splits; ++s) {
-      const float w = exp2f(p.part_lse[s * all + at] - ref);
-      if (w != 0.f) o = fmaf(w, p.part_out[(s * all + at) * p.head_dim + c], o);
+    for (int i = 0; i < p.splits; ++i) {
+      const float w = exp2f(p.part_lse[i * all + at] - ref);
+      if (w != 0.f) o = fmaf(w, p.part_out[(i * all + at) * p.head_dim + c], o);
     }
     store_as(out + c, o * inv);
   }
@@ -257,8 +257,9 @@ int launch_all(AttentionParams& p, cudaStream_t stream) {
   const int rc = p.head_dim <= 64 ? launch_fp32<T, 2>(p, stream)
            : p.head_dim <= 128 ? launch_fp32<T, 4>(p, stream) : launch_fp32<T, 8>(p, stream);
   if (rc != TOPLOC_OK || p.splits == 1) return rc;
-  const long long rows = p.total_tokens * p.q_heads;
-  toploc_attention_join_kernel<T><<<(unsigned)((rows + 3) / 4), 128, 0, stream>>>(p);
+  // (splits_of: where keys are split, all sequences together bring few rows)
+  const int blocks_a_seq = (p.max_new * p.q_heads + 3) / 4;
+  toploc_attention_join_kernel<T><<<(unsigned)(p.num_seqs * blocks_a_seq), 128, 0, stream>>>(p, blocks_a_seq);
   return launched();
 }
 
