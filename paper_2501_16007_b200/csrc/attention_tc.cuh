@@ -5,8 +5,6 @@
 #include "attention_common.cuh"
 #include "sm100.cuh"
 
-#include <atomic>
-
 namespace {
 
 using namespace toploc_model;
@@ -476,18 +474,6 @@ __device__ __noinline__ void give_back(const AttentionParams& p, int seq, int ke
       if (!(fabsf(f) < INFINITY)) out[e] += f;
     }
   }
-}
-
-// Lets a kernel have `bytes` of shared memory on the current device; once per kernel and device (a bit of `done` each).
-inline int allow_shared(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return TOPLOC_ERR_CUDA;
-  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
-  if (done.load(std::memory_order_relaxed) & bit) return TOPLOC_OK;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
-    return TOPLOC_ERR_CUDA;
-  done.fetch_or(bit, std::memory_order_relaxed);
-  return TOPLOC_OK;
 }
 
 }  // namespace

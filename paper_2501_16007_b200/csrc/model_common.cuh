@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "toploc_model.h"
 
 namespace toploc_model {
@@ -24,6 +26,20 @@ inline int check_device(int* sm_count = nullptr) {
   if (major != 10) return TOPLOC_ERR_ARCH;
   if (sm_count && cudaDeviceGetAttribute(sm_count, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return TOPLOC_ERR_CUDA;
+  return TOPLOC_OK;
+}
+
+// Lets a kernel have `bytes` of shared memory, the most that any of its launches takes, on the current device; once per
+// kernel and device (a bit of `done` each).  Not this launch's bytes: the limit is the kernel's, and a thread that set a
+// smaller one between another thread's call and launch would make that launch fail.
+inline int allow_shared(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return TOPLOC_ERR_CUDA;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return TOPLOC_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
+    return TOPLOC_ERR_CUDA;
+  done.fetch_or(bit, std::memory_order_relaxed);
   return TOPLOC_OK;
 }
 

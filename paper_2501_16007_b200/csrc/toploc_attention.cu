@@ -241,13 +241,14 @@ size_t workspace_bytes_of(const toploc_attention_layout* lay, const toploc_kv_la
 
 template <typename T, int CHUNKS>
 int launch_fp32(const AttentionParams& p, cudaStream_t stream) {
-  const int bytes = (kRows + 2 * kKeys) * (p.head_dim + 4) * 4;
-  if (cudaFuncSetAttribute(toploc_attention_fp32_kernel<T, CHUNKS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           bytes) != cudaSuccess)
-    return TOPLOC_ERR_CUDA;
+  const auto bytes = [](int head_dim) { return (kRows + 2 * kKeys) * (head_dim + 4) * 4; };
+  static std::atomic<uint64_t> allowed{0};
+  if (const int rc = allow_shared(reinterpret_cast<const void*>(toploc_attention_fp32_kernel<T, CHUNKS>),
+                                  bytes(32 * CHUNKS), allowed))
+    return rc;
   const long long blocks = (long long)p.num_seqs * p.kv_heads * p.row_tiles * p.splits;
   if (blocks > 0x7FFFFFFF) return TOPLOC_ERR_UNSUPPORTED;
-  toploc_attention_fp32_kernel<T, CHUNKS><<<(unsigned)blocks, 128, bytes, stream>>>(p);
+  toploc_attention_fp32_kernel<T, CHUNKS><<<(unsigned)blocks, 128, bytes(p.head_dim), stream>>>(p);
   return launched();
 }
 

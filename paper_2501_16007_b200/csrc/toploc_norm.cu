@@ -7,6 +7,7 @@ namespace {
 
 using namespace toploc_model;
 
+constexpr int kMostHidden = 49152;  // channels of a row (its fp32 values fit shared memory)
 constexpr float kE4m3Max = 448.0f;
 constexpr float kSmallestScale = 1.17549435e-38f;  // 2^-126: a zero group divides by it and stores zeros
 
@@ -298,9 +299,10 @@ __global__ void __launch_bounds__(256) toploc_rmsnorm_residual_kernel(const Norm
 template <typename T, bool QUANT>
 int launch_any(const NormParams& p, cudaStream_t stream) {
   const size_t bytes = (size_t)p.hidden * 4;
-  if (bytes > 40 * 1024 && cudaFuncSetAttribute(toploc_rmsnorm_residual_kernel<T, QUANT>,
-                                                cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess)
-    return TOPLOC_ERR_CUDA;
+  static std::atomic<uint64_t> allowed{0};
+  if (const int rc = allow_shared(reinterpret_cast<const void*>(toploc_rmsnorm_residual_kernel<T, QUANT>), kMostHidden * 4,
+                                  allowed))
+    return rc;
   toploc_rmsnorm_residual_kernel<T, QUANT><<<(unsigned)p.rows, 256, bytes, stream>>>(p);
   return launched();
 }
@@ -365,7 +367,7 @@ extern "C" int toploc_rmsnorm_residual(const void* d_x, const void* d_residual_o
   if (!lay || lay->hidden <= 0 || lay->rows < 0 || lay->group < 0 || !(eps >= 0.f)) return TOPLOC_ERR_INVALID_ARGUMENT;
   const int size = element_bytes(lay->dtype);
   const bool quant = lay->out_kind == TOPLOC_NORM_OUT_E4M3;
-  if (size == 0 || (!quant && lay->out_kind != TOPLOC_NORM_OUT_SAME) || lay->hidden > 49152 || lay->rows > 0x7FFFFFFF)
+  if (size == 0 || (!quant && lay->out_kind != TOPLOC_NORM_OUT_SAME) || lay->hidden > kMostHidden || lay->rows > 0x7FFFFFFF)
     return TOPLOC_ERR_UNSUPPORTED;
   if (lay->rows == 0) return TOPLOC_OK;
   if (!d_x || !d_weight || !d_y || (quant && !d_scales_opt)) return TOPLOC_ERR_INVALID_ARGUMENT;
