@@ -109,15 +109,17 @@ extern "C" int toploc_rmsnorm_append(const void* d_x, int64_t x_row_stride, cons
       reinterpret_cast<uintptr_t>(d_weight) % 16 != 0 || reinterpret_cast<uintptr_t>(d_state_opt) % 16 != 0)
     return TOPLOC_ERR_INVALID_ARGUMENT;
   const size_t row_bytes = (size_t)lay->hidden * 2;
-  if (row_bytes > 160 * 1024) return TOPLOC_ERR_UNSUPPORTED;  // the row must fit shared memory beside the scratch
+  constexpr size_t kMostRowBytes = 160 * 1024;  // the row must fit shared memory beside the scratch
+  if (row_bytes > kMostRowBytes) return TOPLOC_ERR_UNSUPPORTED;
   int dev = 0, major = 0;
   if (cudaGetDevice(&dev) != cudaSuccess ||
       cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess)
     return TOPLOC_ERR_CUDA;
   if (major != 10) return TOPLOC_ERR_ARCH;
+  // (the most that any call takes: the limit is the kernel's, and another thread's call may be between this and its launch)
   if (row_bytes > 32 * 1024 &&
       cudaFuncSetAttribute(toploc_rmsnorm_append_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)row_bytes) != cudaSuccess)
+                           (int)kMostRowBytes) != cudaSuccess)
     return TOPLOC_ERR_CUDA;
   toploc_rmsnorm_append_kernel<<<(unsigned)lay->num_seqs, kNormThreads, row_bytes, static_cast<cudaStream_t>(cuda_stream)>>>(
       static_cast<const uint4*>(d_x), x_row_stride / 8, static_cast<const uint4*>(d_weight), eps,

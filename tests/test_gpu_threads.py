@@ -58,3 +58,16 @@ def test_norm_of_two_hidden_sizes():
         bodies.append(lambda x=x, w=w, y=y, s=scales: tl.toploc_rmsnorm_residual(x, None, w, 1e-5, y=y, scales=s, group=48))
     assert not together(*bodies)
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(outs, wants))
+
+
+def test_final_norm_of_two_hidden_sizes():
+    bodies, outs, wants = [], [], []
+    for hidden in (20480, 81920, 40960):
+        x, w = torch.randn((2, hidden), device=DEV).to(torch.bfloat16), torch.ones(hidden, device=DEV, dtype=torch.bfloat16)
+        lay, _ = tl.make_layout(x, 1, 16, 2, 1)
+        y = torch.empty_like(x)
+        wants.append(tl.toploc_rmsnorm_append(x, w, 1e-5, lay, 0, torch.empty_like(x)))
+        outs.append(y)
+        bodies.append(lambda x=x, w=w, y=y, lay=lay: tl.toploc_rmsnorm_append(x, w, 1e-5, lay, 0, y))
+    assert not together(*bodies)
+    assert all(torch.equal(a, b) for a, b in zip(outs, wants))
