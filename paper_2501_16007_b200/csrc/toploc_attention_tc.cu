@@ -168,179 +168,7 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
   const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, sh.tmem, 0);
   constexpr uint32_t kOut = 256;  // scores of group w at 128 w, outputs at 256 + D w
 
-  if (warp == 8 || warp == 10) {
-    lower_registers<kOtherRegisters>();
-    // ---- feeding: warp 8 finds the items, copies queries and keys, warp 10 values (one code for both: less to fetch) ----
-    const bool keys = warp == 8;
-    Walk walk(tp);
-    if (keys) {
-      if (lane == 0) {
-        prefetch_map(&map_q);
-        prefetch_map(&map_k);
-        prefetch_map(&map_v);
-      }
-      walk.begin<kTcThreads>(run_cost);
-      if (lane == 0) sh.stretch = Stretch{walk.at, walk.end};
-    }
-    uint32_t q_uses = 0;
-    Feeder<S> feeder(tp, keys ? &map_k : &map_v, sh, ring, gave_up);
-#pragma unroll 1
-    for (uint32_t number = 0;; ++number) {
-      const uint32_t slot = number % kItems, parity = (number / kItems) & 1;
-      if (!warp_wait(keys ? sh.item_empty[slot] : sh.item_full[slot], keys ? parity ^ 1 : parity, gave_up)) break;
-      Item im;
-      if (keys)
-        walk.next(im);
-      else
-        im = sh.items[slot];
-      im = uniform(im);
-      if (keys && lane == 0) sh.items[slot] = im;
-      __syncwarp();
-      if (lane == 0) barrier_arrive(shared_address(keys ? &sh.item_full[slot] : &sh.item_empty[slot]));
-      if (im.seq < 0) break;
-      const int n = item_tiles(im), hidden_from = max(im.behind + im.row0 / p.group + 1, 0);
-      if (keys && n > 0) {  // queries: each tile in blocks of 64 channels
-        if (!warp_wait(sh.q_empty, (q_uses & 1) ^ 1, gave_up)) break;
-        ++q_uses;
-        const uint32_t q_bar = shared_address(&sh.q_full);
-        if (elect_one()) {
-          const int tiles = im.two ? 2 : 1;
-          barrier_arrive_expect(q_bar, tiles * tp.q_bytes);
-#pragma unroll 1
-          for (int w = 0; w < tiles; ++w)
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h)
-              copy_3d(shared_address(q_tiles + w * S::kTileBytes + h * kBlockBytes), &map_q, q_bar, h * 64,
-                      im.head * p.group, im.first + im.row0 / tp.item_rows * tp.item_tokens + w * tp.tile_tokens);
-        }
-        __syncwarp();
-      }
-      feeder.item(im, n);
-      // Value tiles with hidden keys are cleaned one behind the copies: at once when a tile has landed would hold up the
-      // copies, later would hold up the ring.
-#pragma unroll 1
-      for (int j = 0; j <= n && feeder.fine; ++j) {
-        if (j < n) feeder.feed(j, keys ? key_place(im.two, j) : value_place(im.two, j, n));
-        const int landed = j - 1;
-        if (keys || !feeder.fine || landed < im.clean || landed < 0) continue;
-        const uint32_t place = feeder.base + value_place(im.two, landed, n), stage = ring_stage(place, kStages);
-        feeder.fine = warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up);
-        if (!feeder.fine) break;
-        const int key0 = im.kbegin + landed * kKeyTile;
-        clean_values<kHalves, 32>(ring + stage * S::kTileBytes, max(hidden_from - key0, 0), im.kend - key0, lane,
-                                  &sh.bad_values[number & 7], (int)number);
-        __syncwarp();
-        if (lane == 0) barrier_arrive(shared_address(&sh.cleaned[stage]));
-      }
-      if (!feeder.fine) break;
-    }
-    if (keys && lane == 0) sh.queries_fed = q_uses;
-  } else if (warp == 9) {
-    lower_registers<kOtherRegisters>();
-    // ---- products: the whole warp follows, one lane issues ----
-    constexpr uint32_t kScores = bf16_product(128, false, false), kValues = bf16_product(D, false, true);
-    const uint32_t q_low = operand_low(shared_address(q_tiles), 16);
-    const uint32_t k_low = operand_low(shared_address(ring), 16), v_low = operand_low(shared_address(ring), kBlockBytes);
-    uint32_t used = 0, q_uses = 0, p_parity = 0, cleans = 0;  // cleans: by stage, the parity of its next cleaning
-    const auto full = [&](uint32_t n) {
-      const bool ok = warp_wait(sh.full[ring_stage(n, kStages)], ring_parity(n, kStages), gave_up);
-      tmem_fence_after();
-      return ok;
-    };
-    const auto release = [&](uint32_t n) {
-      if (elect_one()) mma_commit(shared_address(&sh.empty[ring_stage(n, kStages)]));
-    };
-    const auto scores = [&](int w, uint32_t n, bool two) {  // scores of group w against the key tile at place n
-      const uint32_t a = q_low + (two ? w : 0) * (S::kTileBytes / 16);
-      const uint32_t b = k_low + ring_stage(n, kStages) * (S::kTileBytes / 16);
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint32_t at = ((k / 4) * kBlockBytes + (k % 4) * 32) / 16;
-          mma_shared(tmem + 128 * w, a + at, b + at, kScores, k > 0);
-        }
-        mma_commit(shared_address(&sh.s_full[w]));
-      }
-    };
-    const auto values = [&](int w, uint32_t n, bool add) {  // as the group's weights come into tensor memory
-      const uint32_t b = v_low + ring_stage(n, kStages) * (S::kTileBytes / 16), parity = p_parity >> w & 1;
-      p_parity ^= 1u << w;
-      if (!warp_wait(sh.p_most[w], parity, gave_up)) return false;
-      tmem_fence_after();
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < 6; ++k)
-          mma_tmem(tmem + kOut + D * w, tmem + 128 * w + 8 * k, b + k * (2048 / 16), kValues, add || k > 0);
-      }
-      if (!warp_wait(sh.p_full[w], parity, gave_up)) return false;
-      tmem_fence_after();
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 6; k < 8; ++k)
-          mma_tmem(tmem + kOut + D * w, tmem + 128 * w + 8 * k, b + k * (2048 / 16), kValues, true);
-        mma_commit(shared_address(&sh.o_full[w]));
-      }
-      return true;
-    };
-    const auto queries_used = [&] {
-      if (elect_one()) mma_commit(shared_address(&sh.q_empty));
-    };
-#pragma unroll 1
-    for (uint32_t number = 0;; ++number) {
-      const uint32_t slot = number % kItems;
-      if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
-      // (through a shuffle: the same for every lane, and known to be)
-      const int seq = __shfl_sync(0xFFFFFFFFu, sh.items[slot].seq, 0);
-      const int n0 = __shfl_sync(0xFFFFFFFFu, sh.items[slot].n0, 0), n1 = __shfl_sync(0xFFFFFFFFu, sh.items[slot].n1, 0);
-      const int clean = __shfl_sync(0xFFFFFFFFu, sh.items[slot].clean, 0);
-      const bool two = __shfl_sync(0xFFFFFFFFu, sh.items[slot].two, 0);
-      __syncwarp();
-      if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
-      if (seq < 0) break;
-      const int n = two ? max(n0, n1) : n0;
-      if (n == 0) continue;
-      bool ok = warp_wait(sh.q_full, q_uses++ & 1, gave_up);
-      // Round by round, group by group: the group's weights of a tile times the values, then its scores of the tile it
-      // takes next (two row tiles: both groups take every tile, group 1 after group 0; one: tiles in turn).  The first
-      // round has only scores.
-      const int rounds = two ? n : (n + 1) / 2;
-      int cleaned_to = clean;
-#pragma unroll 1
-      for (int round = -1; ok && round < rounds; ++round) {
-#pragma unroll 1
-        for (int w = 0; w < 2; ++w) {
-          const int tiles = two ? (w ? n1 : n0) : n;
-          const int j = two ? round : 2 * round + w, next = j + (two ? 1 : 2);
-          const bool weigh = round >= 0 && j < tiles, score = next < tiles;
-          const uint32_t v_at = used + value_place(two, j, n), k_at = used + key_place(two, next);
-          // (group 1 of two row tiles meets what group 0 has waited for, unless group 0 has no such tile)
-          if (weigh && (w == 0 || !two || j >= n0)) ok = ok && full(v_at);
-          if (score && (w == 0 || !two || next >= n0)) ok = ok && full(k_at);
-          if (weigh && j >= cleaned_to) {
-            const uint32_t stage = ring_stage(v_at, kStages);
-            ok = ok && warp_wait(sh.cleaned[stage], cleans >> stage & 1, gave_up);
-            cleans ^= 1u << stage;
-            cleaned_to = j + 1;
-          }
-          if (weigh) {
-            ok = ok && values(w, v_at, j >= (two ? 1 : 2));
-            if (ok && (w == 1 || !two)) release(v_at);
-          }
-          if (score && ok) {
-            scores(w, k_at, two);
-            if (w == 1 || !two) {
-              release(k_at);
-              if (next == n - 1) queries_used();
-            }
-          }
-        }
-      }
-      if (!ok) break;
-      used += 2 * n;
-    }
-  } else if (warp == 11) {
-    lower_registers<kOtherRegisters>();
-  } else {
+  if (warp < 8) {  // (first: behind the other roles it made the prompts 1.5 % slower)
     raise_registers<kSoftmaxRegisters>();
     // ---- softmax: a thread per row ----
     const int w = warp >> 2, r = threadIdx.x & 127;
@@ -602,6 +430,177 @@ toploc_attention_tc_kernel(const __grid_constant__ TcParams tp, const __grid_con
       if (!two) {  // both have read: the next item may overwrite
         tmem_fence_before();
         if (!join()) break;
+      }
+    }
+  } else {  // the third group of warps: all four hand in their registers together (the last has no other part)
+    lower_registers<kOtherRegisters>();
+    if (warp == 8 || warp == 10) {
+      // ---- feeding: warp 8 finds the items, copies queries and keys, warp 10 values (one code for both: less to fetch) ----
+      const bool keys = warp == 8;
+      Walk walk(tp);
+      if (keys) {
+        if (lane == 0) {
+          prefetch_map(&map_q);
+          prefetch_map(&map_k);
+          prefetch_map(&map_v);
+        }
+        walk.begin<kTcThreads>(run_cost);
+        if (lane == 0) sh.stretch = Stretch{walk.at, walk.end};
+      }
+      uint32_t q_uses = 0;
+      Feeder<S> feeder(tp, keys ? &map_k : &map_v, sh, ring, gave_up);
+  #pragma unroll 1
+      for (uint32_t number = 0;; ++number) {
+        const uint32_t slot = number % kItems, parity = (number / kItems) & 1;
+        if (!warp_wait(keys ? sh.item_empty[slot] : sh.item_full[slot], keys ? parity ^ 1 : parity, gave_up)) break;
+        Item im;
+        if (keys)
+          walk.next(im);
+        else
+          im = sh.items[slot];
+        im = uniform(im);
+        if (keys && lane == 0) sh.items[slot] = im;
+        __syncwarp();
+        if (lane == 0) barrier_arrive(shared_address(keys ? &sh.item_full[slot] : &sh.item_empty[slot]));
+        if (im.seq < 0) break;
+        const int n = item_tiles(im), hidden_from = max(im.behind + im.row0 / p.group + 1, 0);
+        if (keys && n > 0) {  // queries: each tile in blocks of 64 channels
+          if (!warp_wait(sh.q_empty, (q_uses & 1) ^ 1, gave_up)) break;
+          ++q_uses;
+          const uint32_t q_bar = shared_address(&sh.q_full);
+          if (elect_one()) {
+            const int tiles = im.two ? 2 : 1;
+            barrier_arrive_expect(q_bar, tiles * tp.q_bytes);
+  #pragma unroll 1
+            for (int w = 0; w < tiles; ++w)
+  #pragma unroll
+              for (int h = 0; h < kHalves; ++h)
+                copy_3d(shared_address(q_tiles + w * S::kTileBytes + h * kBlockBytes), &map_q, q_bar, h * 64,
+                        im.head * p.group, im.first + im.row0 / tp.item_rows * tp.item_tokens + w * tp.tile_tokens);
+          }
+          __syncwarp();
+        }
+        feeder.item(im, n);
+        // Value tiles with hidden keys are cleaned one behind the copies: at once when a tile has landed would hold up the
+        // copies, later would hold up the ring.
+  #pragma unroll 1
+        for (int j = 0; j <= n && feeder.fine; ++j) {
+          if (j < n) feeder.feed(j, keys ? key_place(im.two, j) : value_place(im.two, j, n));
+          const int landed = j - 1;
+          if (keys || !feeder.fine || landed < im.clean || landed < 0) continue;
+          const uint32_t place = feeder.base + value_place(im.two, landed, n), stage = ring_stage(place, kStages);
+          feeder.fine = warp_wait(sh.full[stage], ring_parity(place, kStages), gave_up);
+          if (!feeder.fine) break;
+          const int key0 = im.kbegin + landed * kKeyTile;
+          clean_values<kHalves, 32>(ring + stage * S::kTileBytes, max(hidden_from - key0, 0), im.kend - key0, lane,
+                                    &sh.bad_values[number & 7], (int)number);
+          __syncwarp();
+          if (lane == 0) barrier_arrive(shared_address(&sh.cleaned[stage]));
+        }
+        if (!feeder.fine) break;
+      }
+      if (keys && lane == 0) sh.queries_fed = q_uses;
+    } else if (warp == 9) {
+      // ---- products: the whole warp follows, one lane issues ----
+      constexpr uint32_t kScores = bf16_product(128, false, false), kValues = bf16_product(D, false, true);
+      const uint32_t q_low = operand_low(shared_address(q_tiles), 16);
+      const uint32_t k_low = operand_low(shared_address(ring), 16), v_low = operand_low(shared_address(ring), kBlockBytes);
+      uint32_t used = 0, q_uses = 0, p_parity = 0, cleans = 0;  // cleans: by stage, the parity of its next cleaning
+      const auto full = [&](uint32_t n) {
+        const bool ok = warp_wait(sh.full[ring_stage(n, kStages)], ring_parity(n, kStages), gave_up);
+        tmem_fence_after();
+        return ok;
+      };
+      const auto release = [&](uint32_t n) {
+        if (elect_one()) mma_commit(shared_address(&sh.empty[ring_stage(n, kStages)]));
+      };
+      const auto scores = [&](int w, uint32_t n, bool two) {  // scores of group w against the key tile at place n
+        const uint32_t a = q_low + (two ? w : 0) * (S::kTileBytes / 16);
+        const uint32_t b = k_low + ring_stage(n, kStages) * (S::kTileBytes / 16);
+        if (elect_one()) {
+  #pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t at = ((k / 4) * kBlockBytes + (k % 4) * 32) / 16;
+            mma_shared(tmem + 128 * w, a + at, b + at, kScores, k > 0);
+          }
+          mma_commit(shared_address(&sh.s_full[w]));
+        }
+      };
+      const auto values = [&](int w, uint32_t n, bool add) {  // as the group's weights come into tensor memory
+        const uint32_t b = v_low + ring_stage(n, kStages) * (S::kTileBytes / 16), parity = p_parity >> w & 1;
+        p_parity ^= 1u << w;
+        if (!warp_wait(sh.p_most[w], parity, gave_up)) return false;
+        tmem_fence_after();
+        if (elect_one()) {
+  #pragma unroll
+          for (int k = 0; k < 6; ++k)
+            mma_tmem(tmem + kOut + D * w, tmem + 128 * w + 8 * k, b + k * (2048 / 16), kValues, add || k > 0);
+        }
+        if (!warp_wait(sh.p_full[w], parity, gave_up)) return false;
+        tmem_fence_after();
+        if (elect_one()) {
+  #pragma unroll
+          for (int k = 6; k < 8; ++k)
+            mma_tmem(tmem + kOut + D * w, tmem + 128 * w + 8 * k, b + k * (2048 / 16), kValues, true);
+          mma_commit(shared_address(&sh.o_full[w]));
+        }
+        return true;
+      };
+      const auto queries_used = [&] {
+        if (elect_one()) mma_commit(shared_address(&sh.q_empty));
+      };
+  #pragma unroll 1
+      for (uint32_t number = 0;; ++number) {
+        const uint32_t slot = number % kItems;
+        if (!warp_wait(sh.item_full[slot], (number / kItems) & 1, gave_up)) break;
+        // (through a shuffle: the same for every lane, and known to be)
+        const int seq = __shfl_sync(0xFFFFFFFFu, sh.items[slot].seq, 0);
+        const int n0 = __shfl_sync(0xFFFFFFFFu, sh.items[slot].n0, 0), n1 = __shfl_sync(0xFFFFFFFFu, sh.items[slot].n1, 0);
+        const int clean = __shfl_sync(0xFFFFFFFFu, sh.items[slot].clean, 0);
+        const bool two = __shfl_sync(0xFFFFFFFFu, sh.items[slot].two, 0);
+        __syncwarp();
+        if (lane == 0) barrier_arrive(shared_address(&sh.item_empty[slot]));
+        if (seq < 0) break;
+        const int n = two ? max(n0, n1) : n0;
+        if (n == 0) continue;
+        bool ok = warp_wait(sh.q_full, q_uses++ & 1, gave_up);
+        // Round by round, group by group: the group's weights of a tile times the values, then its scores of the tile it
+        // takes next (two row tiles: both groups take every tile, group 1 after group 0; one: tiles in turn).  The first
+        // round has only scores.
+        const int rounds = two ? n : (n + 1) / 2;
+        int cleaned_to = clean;
+  #pragma unroll 1
+        for (int round = -1; ok && round < rounds; ++round) {
+  #pragma unroll 1
+          for (int w = 0; w < 2; ++w) {
+            const int tiles = two ? (w ? n1 : n0) : n;
+            const int j = two ? round : 2 * round + w, next = j + (two ? 1 : 2);
+            const bool weigh = round >= 0 && j < tiles, score = next < tiles;
+            const uint32_t v_at = used + value_place(two, j, n), k_at = used + key_place(two, next);
+            // (group 1 of two row tiles meets what group 0 has waited for, unless group 0 has no such tile)
+            if (weigh && (w == 0 || !two || j >= n0)) ok = ok && full(v_at);
+            if (score && (w == 0 || !two || next >= n0)) ok = ok && full(k_at);
+            if (weigh && j >= cleaned_to) {
+              const uint32_t stage = ring_stage(v_at, kStages);
+              ok = ok && warp_wait(sh.cleaned[stage], cleans >> stage & 1, gave_up);
+              cleans ^= 1u << stage;
+              cleaned_to = j + 1;
+            }
+            if (weigh) {
+              ok = ok && values(w, v_at, j >= (two ? 1 : 2));
+              if (ok && (w == 1 || !two)) release(v_at);
+            }
+            if (score && ok) {
+              scores(w, k_at, two);
+              if (w == 1 || !two) {
+                release(k_at);
+                if (next == n - 1) queries_used();
+              }
+            }
+          }
+        }
+        if (!ok) break;
+        used += 2 * n;
       }
     }
   }
