@@ -24,6 +24,9 @@ namespace {
 
 constexpr int kFewThreads = 224;
 constexpr float kFewLimit = 64.0f;
+// The reference of a row that has met no score but minus infinity: any other score exceeds it by more than the limit, and
+// the weights of minus infinities against it are 0.
+constexpr float kNoScore = -3e38f;
 
 template <int D>
 struct FewShared {
@@ -250,7 +253,7 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
       const int hidden_from = max(im.behind + 1, 0);  // first key hidden from a row of the item
       float ref[R], l[R];
 #pragma unroll
-      for (int r = 0; r < R; ++r) ref[r] = -INFINITY, l[r] = 0.f;
+      for (int r = 0; r < R; ++r) ref[r] = kNoScore, l[r] = 0.f;
       bool ok = true;
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
@@ -306,8 +309,8 @@ toploc_attention_few_kernel(const __grid_constant__ TcParams tp, const __grid_co
             if (r < rows) {
               const float top = fmaxf(fmaxf(sh.rows[0][r], sh.rows[1][r]), fmaxf(sh.rows[2][r], sh.rows[3][r]));
               const float now = fmaxf(ref[r], top);
-              shrink[r] = now == -INFINITY ? 0.f : exp2_approx(ref[r] - now);
-              ref[r] = now == -INFINITY ? 0.f : now;
+              shrink[r] = exp2_approx(ref[r] - now);
+              ref[r] = now;
               l[r] *= shrink[r];
             }
           }
