@@ -138,7 +138,8 @@ typedef struct {
  * the cache past kv_lens[i], NaN included, has no influence on any result; nor
  * has a key that the mask hides from a row on that row.
  *
- * Scores, maxima, sums and outputs are accumulated in fp32; bf16 inputs take
+ * Scores, maxima, sums and outputs are accumulated in fp32 (the outputs' sums
+ * with weights up to 2^8, so values up to about 2^120 / keys are safe); bf16 inputs take
  * the weights p_j rounded to bf16 into the second product (8 bits, as v_j has;
  * the sum in the denominator uses them unrounded).
  *

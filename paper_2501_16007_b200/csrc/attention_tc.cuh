@@ -11,6 +11,10 @@ using namespace toploc_model;
 using namespace sm100;
 
 constexpr int kItems = 4;                  // items announced ahead
+// A row's reference is renewed where a score exceeds it by more than this factor of 2^8: weights stay below 2^8, and the
+// output, the sum and the weights share the reference, so the quotient is the same.  (Sums of weighted values are fp32: up
+// to 2^8 times the keys times the values has to fit it.)
+constexpr float kLazyLog2 = 8.0f;
 constexpr int kBlockBytes = 128 * 128;     // 128 rows of 64 elements
 
 // One piece of work: two tiles of rows (or the one that is left) of a sequence and key head against a range of keys.

@@ -7,8 +7,8 @@
 // threads empty.  Here a thread has a key and weighs it for all R rows (R exponentials, not 128), and the products are 16
 // wide, the least there is.  R is 4 or 8: loops over rows are unrolled, and code for rows that are not there would only
 // crowd the instruction caches (with that and other code made small at once, 98 to 59 us at four rows).  A row's
-// maximum and sum run over threads, but seldom: the maximum of the first tile stays the reference for the whole item unless a score exceeds it by
-// 2^64 (weights, sums and outputs share it, and fp32 and bf16 have the range; the quotient is the same), so a tile needs
+// maximum and sum run over threads, but seldom: the maximum of the first tile stays the reference for the whole item
+// unless a score exceeds it by more than the limit that the kernel for many rows has too, so a tile needs
 // one vote, and the threads' own sums are added up once at the end.
 //
 // Two blocks share an SM, three tiles of 32 KB in flight each (head_dim 128).  A block: four warps of softmax, a warp that
@@ -23,7 +23,7 @@
 namespace {
 
 constexpr int kFewThreads = 224;
-constexpr float kFewLimit = 64.0f;
+constexpr float kFewLimit = kLazyLog2;
 // The reference of a row that has met no score but minus infinity: any other score exceeds it by more than the limit, and
 // the weights of minus infinities against it are 0.
 constexpr float kNoScore = -3e38f;

@@ -33,8 +33,7 @@
 // exponentials as a polynomial on the fp32 units (2 to 10 % slower), the row's scores kept in registers between maximum
 // and weights (the same where tiles are many, 10 % slower on short prompts: its code is unrolled).
 //
-// The output is not rescaled whenever the maximum grows but only where it grew by more than 2^8: P then stays
-// below 2^8, and O, the sum and P share the same reference, so the quotient is the same.
+// The output is not rescaled whenever the maximum grows but only where it grew by more than kLazyLog2.
 #include "attention_tc.cuh"
 
 #include <type_traits>
@@ -45,7 +44,6 @@ constexpr int kTcThreads = 384;  // two groups of softmax, and one whose first t
 // Registers move from the third group of warps to the softmax.  The block is launched with 168 a thread (65536 / 384, in
 // steps of 8); 2 * 216 + 72 = 3 * 168.
 constexpr int kSoftmaxRegisters = 216, kOtherRegisters = 72;
-constexpr float kLazyLog2 = 8.0f;
 
 template <int D>
 struct Shared {

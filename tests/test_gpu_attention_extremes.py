@@ -48,3 +48,28 @@ def test_a_first_tile_of_minus_infinities(dtype, new, heads, kv_heads, level):
     # equal scores: equal weights, exact (up to the score's own error, a few fp32 roundings of |level|, that all share)
     assert ((lse - want_lse).abs() <= U32 * (16 + 16 * want_lse.abs()) + U32 * (keys + 16)).all()
     assert ((out - want).abs() <= u * want.abs() + (u + U32 * (keys + 16)) * v.double().abs().mean() * 4).all()
+
+
+@pytest.mark.parametrize("dtype,new,heads,kv_heads", KERNELS)
+@pytest.mark.parametrize("rise", [5.0, 40.0])
+def test_large_values_behind_scores_that_rise(dtype, new, heads, kv_heads, rise):
+    """Finite results from values of 1e30 whose scores exceed the first tile's by e^rise."""
+    keys, dim = 1000, 128
+    g = torch.Generator(device=DEV)
+    g.manual_seed(8)
+    q = torch.ones((new, heads, dim), dtype=dtype, device=DEV)
+    k = torch.randn((keys, kv_heads, dim), generator=g, device=DEV).mul_(0.25).to(dtype)
+    k[200:, :, :64] += rise / 64 * dim ** 0.5
+    v = (torch.randn((keys, kv_heads, dim), generator=g, device=DEV) * 1e30).to(dtype)
+    out, lse, want, want_lse = run(dtype, new, heads, kv_heads, k, v, q)
+    assert torch.isfinite(out).all()
+    half = dtype == torch.bfloat16
+    # a score is off by dim roundings of its partial sums and a few of its own; a weight by twice that and, for bf16, its
+    # own rounding
+    score = U32 * ((dim + 4) * k.double().abs().sum(2).max() * dim ** -0.5 + 8)
+    weight = 2 * score + U32 * (keys + 16) + (U16 if half else 0)
+    scores = torch.einsum("thd,jd->thj", q.double(), k[:, 0].double()) * dim ** -0.5
+    hidden = torch.arange(keys, device=DEV)[None] > torch.arange(keys - new, keys, device=DEV)[:, None]
+    spread = torch.softmax(torch.where(hidden[:, None], float("-inf"), scores), -1) @ v[:, 0].double().abs()
+    assert ((out - want).abs() <= (U16 if half else U32) * want.abs() + 1.05 * weight * spread).all()
+    assert ((lse - want_lse).abs() <= 2 * score + U32 * (keys + 16 + 4 * want_lse.abs())).all()
