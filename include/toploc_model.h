@@ -54,8 +54,7 @@ const char* toploc_sequence_status_string(int sequence_status);
  *   d_positions   [max_tokens]    c_i + row - offset_i (rotary angle), 0 for
  *                                 rows past the last token
  *   d_next_free   [1]             first_free + pages taken: the next step's
- *                                 d_first_free (two buffers used in turn; it
- *                                 must not be this call's d_first_free)
+ *                                 d_first_free (two buffers used in turn)
  *   d_status      [num_seqs]      TOPLOC_SEQ_*
  *
  * A sequence whose status is not OK takes no pages, gets kv_len 0 (attention
@@ -66,7 +65,9 @@ const char* toploc_sequence_status_string(int sequence_status);
  * t_i counts as 0.  The same inputs give the same outputs, and a repeated call
  * changes nothing.
  *
- * All arrays DEVICE; int32 4-byte, int64 8-byte aligned.  page_size > 0,
+ * All arrays DEVICE; int32 4-byte, int64 8-byte aligned.  What is written must
+ * not lie in what is read (d_kv_lens is not d_cached_lens: two buffers used in
+ * turn; refused), nor in another output.  page_size > 0,
  * table_stride >= max_pages (elements between rows of the table),
  * num_seqs and max_tokens >= 0, num_seqs <= 2^24, max_tokens < 2^31.
  */

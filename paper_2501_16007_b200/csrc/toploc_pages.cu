@@ -232,6 +232,23 @@ __global__ void __launch_bounds__(kPlanThreads) toploc_plan_pages_kernel(const P
   }
 }
 
+// Memory of an argument: rows of `bytes`, a step apart (a vector is one row).
+struct Rows {
+  const void* at;
+  long long bytes, rows, step;
+  Rows(const void* at, long long bytes, long long rows = 1, long long step = 0)
+      : at(at), bytes(bytes), rows(rows), step(rows > 1 ? step : bytes) {}
+};
+
+// Whether a vector and rows share memory.
+bool overlap(const Rows& vector, const Rows& r) {
+  if (vector.bytes <= 0 || r.bytes <= 0 || r.rows <= 0) return false;
+  const long long from = (long long)(reinterpret_cast<uintptr_t>(vector.at) - reinterpret_cast<uintptr_t>(r.at));
+  // the first row that ends behind the vector's beginning has to begin in front of its end
+  const long long row = from < r.bytes ? 0 : (from - r.bytes) / r.step + 1;
+  return row < r.rows && row * r.step < from + vector.bytes;
+}
+
 struct WriteParams {
   const unsigned char* src[2];
   unsigned char* cache[2];
@@ -294,6 +311,15 @@ extern "C" int toploc_plan_pages(const int32_t* d_cached_lens, const int32_t* d_
                         (const void*)d_kv_lens, (const void*)d_positions, (const void*)d_next_free})
     if (!aligned(q, 4)) return TOPLOC_ERR_INVALID_ARGUMENT;
   if (!aligned(d_slots, 8)) return TOPLOC_ERR_INVALID_ARGUMENT;
+  // every block reads the inputs several times while others write: nothing that is written may lie in them
+  const Rows inputs[] = {{d_cached_lens, num_seqs * 4ll}, {d_new_lens, num_seqs * 4ll}, {d_free_pages, num_free * 4ll},
+                         {d_first_free, 4}};
+  const Rows outputs[] = {{d_block_table, max_pages * 4ll, num_seqs, min((long long)table_stride, 1ll << 56) * 4},
+                          {d_seq_offsets, (num_seqs + 1ll) * 4}, {d_kv_lens, num_seqs * 4ll}, {d_slots, max_tokens * 8},
+                          {d_positions, max_tokens * 4}, {d_next_free, 4}, {d_status, num_seqs}};
+  for (const Rows& in : inputs)
+    for (const Rows& out : outputs)
+      if (overlap(in, out)) return TOPLOC_ERR_INVALID_ARGUMENT;
   int sms = 0;
   if (const int rc = check_device(&sms)) return rc;
   const PlanParams p = {d_cached_lens, d_new_lens, d_free_pages, d_first_free, d_block_table, d_seq_offsets, d_kv_lens,

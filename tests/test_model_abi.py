@@ -209,3 +209,33 @@ def test_wrappers_refuse_numbers_that_do_not_fit():
 def test_wait_limit_refusals(lib):
     assert paged(lib, attention_layout(wait_tries=-1)) == INVALID
     assert paged(lib, attention_layout(wait_tries=5, num_seqs=0)) == 0
+
+
+def test_plan_refuses_outputs_in_inputs(lib):
+    """Blocks read the lengths and the free list again while others write."""
+    def call(**kw):                        # every array a megabyte from the next; 1000 sequences, tokens and pages
+        names = ("cached", "new", "free", "first", "table", "offs", "kv", "slots", "pos", "nxt", "status")
+        a = {name: at((2 + i) << 20) for i, name in enumerate(names)}
+        a.update(kw)
+        order = dict(cached=a["cached"], new=a["new"], n=1000, free=a["free"], num_free=1000, first=a["first"], page=16,
+                     table=a["table"], width=4, stride=a.get("stride", 8), offs=a["offs"], kv=a["kv"], slots=a["slots"],
+                     pos=a["pos"], tokens=1000, nxt=a["nxt"], status=a["status"])
+        return lib.toploc_plan_pages(*order.values(), None)
+
+    if not torch.cuda.is_available():                                   # (else they would run)
+        assert call() not in (0, INVALID, UNSUPPORTED)                  # as far as the device
+        for beside in (-1000, 1000):
+            assert call(kv=at((2 << 20) + 4 * beside)) not in (0, INVALID)
+        assert call(table=at(64 << 20), stride=1 << 62) not in (0, INVALID)
+        # a vector between the rows of a table (of 4 entries, 4096 apart) shares nothing with it
+        assert call(table=at(64 << 20), stride=4096, cached=at((64 << 20) + 64)) not in (0, INVALID)
+    for name in ("cached", "new", "free"):
+        where = (2 + ("cached", "new", "free").index(name)) << 20
+        for out in ("offs", "kv", "slots", "pos", "nxt", "status", "table"):
+            assert call(**{out: at(where)}) == INVALID, (name, out)
+            assert call(**{out: at(where + 4 * 999 // 8 * 8)}) == INVALID, (name, out)
+        assert call(kv=at(where - 4 * 999)) == INVALID and call(slots=at(where - 8 * 999)) == INVALID
+        assert call(table=at(where - (8 * 999 + 3) * 4)) == INVALID
+    first = 5 << 20
+    for out in ("offs", "kv", "nxt", "status"):
+        assert call(**{out: at(first)}) == INVALID
