@@ -72,6 +72,13 @@ def rotate(x, positions):
     return torch.cat([a * cos - b * sin, a * sin + b * cos], dim=-1).to(x.dtype)
 
 
+def check_status(status):
+    """Raises where a call has flagged a sequence.  Waits for the GPU: once behind many steps is enough."""
+    for i, code in enumerate(status.tolist()):
+        if code != tl.TOPLOC_SEQ_OK:
+            raise tl.ToplocError("sequence %d: %s" % (i, tl.toploc_sequence_status_string(code)))
+
+
 class Provider:
     """Ragged prompts in, GENERATED tokens a sequence and their proofs out."""
 
@@ -84,6 +91,7 @@ class Provider:
         self.table = torch.full((num_seqs, self.width), -1, dtype=torch.int32, device=device)
         self.free = torch.randperm(pages, device=device).to(torch.int32)
         self.heads = [torch.zeros(1, dtype=torch.int32, device=device) for _ in range(2)]   # of the free list, in turn
+        self.planned, self.status = (torch.zeros(num_seqs, dtype=torch.uint8, device=device) for _ in range(2))
 
     def step(self, tokens, cached, new, longest):
         """One step: packed new tokens behind `cached` ones of every sequence; the last hidden states of all rows."""
@@ -92,15 +100,16 @@ class Provider:
         kv_lens = torch.empty(self.n, dtype=i32, device=dev)
         slots = torch.empty(rows, dtype=torch.int64, device=dev)
         positions = torch.empty(rows, dtype=i32, device=dev)
-        self.status = torch.empty(self.n, dtype=torch.uint8, device=dev)
         tl.toploc_plan_pages(cached, new, self.free, self.heads[0], self.table, PAGE, offsets, kv_lens, slots, positions,
-                             self.heads[1], self.status)
+                             self.heads[1], self.planned)
+        torch.maximum(self.status, self.planned, out=self.status)      # what any step flags stays
         self.heads.reverse()
 
         def attend(layer, q, k, v):
             k_cache, v_cache = self.caches[layer]
             tl.toploc_cache_write(k, v, slots, k_cache, v_cache)
-            return tl.toploc_attention_paged(q, k_cache, v_cache, self.table, offsets, kv_lens, longest)[0]
+            return tl.toploc_attention_paged(q, k_cache, v_cache, self.table, offsets, kv_lens, longest,
+                                             status=self.status)[0]
 
         return self.model.forward(tokens, positions, attend), offsets, kv_lens
 
@@ -121,6 +130,7 @@ class Provider:
             last, _, cached = self.step(generated[-1], cached, one, 1)
             tl.toploc_stream_append(last, layout, t, state)
         proofs, _, _ = tl.toploc_stream_finish(state, layout)
+        check_status(self.status)
         return torch.stack(generated, dim=1), proofs
 
 
@@ -133,10 +143,13 @@ def validate(model, prompts, generated, proofs):
     tokens = torch.tensor([t for w in whole for t in w], device=dev)
     positions = torch.cat([torch.arange(len(w)) for w in whole]).to(dev)
 
+    status = torch.zeros(len(whole), dtype=torch.uint8, device=dev)
+
     def attend(layer, q, k, v):
-        return tl.toploc_attention_prompt(q, k, v, offsets, max(len(w) for w in whole))[0]
+        return tl.toploc_attention_prompt(q, k, v, offsets, max(len(w) for w in whole), status=status)[0]
 
     hidden = model.forward(tokens, positions, attend)
+    check_status(status)
     rows = torch.cat([torch.arange(int(e) - GENERATED, int(e)) for e in ends[1:]]).to(dev)
     recomputed = hidden[rows]
     layout, _ = tl.make_layout(recomputed, GENERATED, K, len(prompts), GENERATED)

@@ -156,7 +156,8 @@ typedef struct {
  *                where a sequence is not as promised (BAD_LENGTH: t_i over
  *                max_new_tokens or kv_lens[i] over the table, counted as the
  *                largest possible; BAD_PAGE; WAIT_EXPIRED), else left as it is;
- *                nothing outside the cache is read in any case
+ *                nothing outside the cache is read in any case.  With NULL the
+ *                first two have no sign, and WAIT_EXPIRED only the NaN rows
  * d_workspace    DEVICE toploc_attention_workspace_bytes, 32-byte aligned:
  *                partial results of rows whose keys are split over blocks
  *                (always joined in the same order); contents are undefined

@@ -224,7 +224,9 @@ def toploc_attention_paged(q, k_cache, v_cache, block_table, seq_offsets, kv_len
     """Causal attention of packed new tokens q [tokens, q_heads, head_dim] over the caches [num_pages, page_size,
     kv_heads, head_dim] that already hold them.  block_table int32 [n, max_pages], seq_offsets int32 [n + 1],
     kv_lens int32 [n]; max_new_tokens bounds a sequence's new tokens; scale: 1 / sqrt(head_dim) by default; status:
-    uint8 [n], set where a sequence is not as promised.  Returns (out, lse or None)."""
+    uint8 [n], set where a sequence is not as promised (zeroed by the caller; one tensor may collect many calls).
+    Without it lengths over their bounds and pages outside the cache go unnoticed, and a wait inside the kernel that
+    ran out shows only as NaN rows.  Returns (out, lse or None)."""
     if out is None:
         out = _empty(q.shape, q.dtype, q.device, stream)
     if lse is None and want_lse:
@@ -252,8 +254,8 @@ def toploc_attention_paged(q, k_cache, v_cache, block_table, seq_offsets, kv_len
 def toploc_attention_prompt(q, k, v, seq_offsets, max_tokens, scale=None, out=None, lse=None, want_lse=False,
                             status=None, workspace=None, stream=None):
     """Causal attention over packed prompts: q [tokens, q_heads, head_dim], k and v [tokens, kv_heads, head_dim]
-    (views of one tensor are fine), seq_offsets int32 [n + 1], max_tokens bounds a sequence's length.  Returns
-    (out, lse or None)."""
+    (views of one tensor are fine), seq_offsets int32 [n + 1], max_tokens bounds a sequence's length; status as for
+    toploc_attention_paged.  Returns (out, lse or None)."""
     if out is None:
         out = _empty(q.shape, q.dtype, q.device, stream)
     if lse is None and want_lse:
