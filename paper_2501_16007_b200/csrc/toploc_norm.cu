@@ -59,7 +59,8 @@ __device__ __forceinline__ float scale_of(float amax) {
 // more) comes from its many threads, not from many values a thread: 16 values a thread and 32 registers (2048 threads an
 // SM) take 620 us for 65536 x 8192 bf16 with e4m3 groups of 128 (6.1 TB/s), 32 values 715 us.  Rows that begin
 // anywhere (an odd hidden size) move as vectors too where all tensors share the odd place (4095 x 5001 fp32: 62 us, 5.3
-// TB/s; element by element 78 us, with 32 values a thread 135 us).
+// TB/s; element by element 78 us, with 32 values a thread 135 us).  Where they do not (or 8 bits come out), single elements:
+// 4096 x 12289 in fp32 154 us, 5.2 TB/s, to e4m3 152, bf16 133 and 154 (2.3 to 3.0 TB/s).
 //
 // kVec elements an access, kPer accesses a thread, access v of a row to thread v % threads.
 enum Mode { kSame, kRowScale, kGroupScale };
@@ -136,11 +137,13 @@ __device__ __forceinline__ void store_part(T* p, int c, int hidden, const float*
 // are laid from that place on, the first and the last partly outside (the weights, whose rows begin elsewhere, are read
 // element by element).
 template <typename T, int kVec, int kPer, Mode kMode, bool kShift>
-__global__ void __launch_bounds__(kVec > 1 || kPer > 8 ? 512 : 1024,
+__global__ void __launch_bounds__(kVec > 1 ? 512 : 1024,
                                   kVec * kPer > 16 ? 1 : kShift ? 2 : kVec > 1 ? 4 : kPer <= 5 ? 2 : 1)
     toploc_rmsnorm_rows_kernel(const NormParams p) {
   __shared__ float partial[32], partial_max[32];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
+  // (a constant where a thread has many accesses: their places then differ by constants, and nothing spills)
+  const int threads = kPer > 8 ? 1024 : blockDim.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
   const long long row = blockIdx.x;
   const T* x = static_cast<const T*>(p.x) + row * p.x_stride;
   const T* r = static_cast<const T*>(p.residual) + row * p.residual_stride;
@@ -321,8 +324,8 @@ int launch_rows(const NormParams& p, Mode mode, bool shifted, int threads, cudaS
   return launched();
 }
 
-// The row in registers where it fits 512 threads of 32 values (and a group's lanes are neighbours), else in shared
-// memory.
+// The row in registers where it fits 512 threads of 32 values, or 1024 of 16 single ones (and a group's lanes are
+// neighbours), else in shared memory.
 template <typename T>
 int launch(NormParams& p, bool quant, bool vectors, bool shifted, cudaStream_t stream) {
   constexpr int kWide = 16 / sizeof(T);
@@ -337,10 +340,10 @@ int launch(NormParams& p, bool quant, bool vectors, bool shifted, cudaStream_t s
   if (vec > 1) {
     while (per * 512 < accesses) per *= 2;
   } else {
-    for (const int more : {2, 3, 5, 8, 32})
-      if (per * (per > 8 ? 512 : 1024) < accesses) per = more;
+    for (const int more : {2, 3, 5, 8, 16})
+      if (per * 1024 < accesses) per = more;
   }
-  const int threads = ((accesses + per - 1) / per + 31) / 32 * 32;
+  const int threads = per > 8 ? 1024 : ((accesses + per - 1) / per + 31) / 32 * 32;
   if (vec > 1) {
     switch (per) {
       case 1: return launch_rows<T, kWide, 1>(p, mode, shifted, threads, stream);
@@ -355,7 +358,7 @@ int launch(NormParams& p, bool quant, bool vectors, bool shifted, cudaStream_t s
     case 3: return launch_rows<T, 1, 3>(p, mode, shifted, threads, stream);
     case 5: return launch_rows<T, 1, 5>(p, mode, shifted, threads, stream);
     case 8: return launch_rows<T, 1, 8>(p, mode, shifted, threads, stream);
-    default: return launch_rows<T, 1, 32>(p, mode, shifted, threads, stream);
+    default: return launch_rows<T, 1, 16>(p, mode, shifted, threads, stream);
   }
 }
 
