@@ -59,7 +59,7 @@ __device__ __forceinline__ SeqRange sequence(const AttentionParams& p, int i) {
 // Whether the tensor-core kernel takes these types, pointers and strides.
 bool tensor_cores_take(const toploc_attention_layout* lay, const toploc_kv_layout* kv, const void* q, const void* k,
                        const void* v, const void* out);
-size_t tensor_core_workspace_bytes(const toploc_attention_layout* lay);
+size_t tensor_core_workspace_bytes(const toploc_attention_layout* lay, const toploc_kv_layout* kv);
 int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, const toploc_kv_layout* kv, void* workspace,
                         cudaStream_t stream);
 

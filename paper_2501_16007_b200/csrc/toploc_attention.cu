@@ -234,7 +234,7 @@ bool tensor_core_types(const toploc_attention_layout* lay) {
 
 size_t workspace_bytes_of(const toploc_attention_layout* lay, const toploc_kv_layout* kv, bool tensor_cores) {
   if (lay->num_seqs == 0 || lay->total_tokens == 0 || lay->max_new_tokens == 0) return 0;
-  if (tensor_cores) return tensor_core_workspace_bytes(lay);
+  if (tensor_cores) return tensor_core_workspace_bytes(lay, kv);
   const int splits = splits_of(lay, kv);
   return splits <= 1 ? 0 : (size_t)splits * lay->total_tokens * lay->q_heads * (lay->head_dim + 1) * 4;
 }

@@ -760,11 +760,18 @@ bool tensor_cores_take(const toploc_attention_layout* lay, const toploc_kv_layou
          (page == 0 || (step(kv->k_page_stride, kv->num_pages) && step(kv->v_page_stride, kv->num_pages)));
 }
 
+// Whether a row tile's keys can lie in two blocks' stretches: three tiles of keys are never cut (find_stretch).
+static bool can_be_cut(const toploc_attention_layout* lay, const toploc_kv_layout* kv) {
+  const long long most_keys = kv->page_size > 0 ? (long long)kv->max_pages * kv->page_size : lay->max_new_tokens;
+  return most_keys > 3 * kKeyTile;
+}
+
 // Parts (outputs, lse, who they belong to) of two row tiles a block; the kernel for few rows has twice the blocks and at
-// most kFewRows rows of an item.
-size_t tensor_core_workspace_bytes(const toploc_attention_layout* lay) {
+// most kFewRows rows of an item.  Where nothing can be cut, the records alone.
+size_t tensor_core_workspace_bytes(const toploc_attention_layout* lay, const toploc_kv_layout* kv) {
   const int group = lay->q_heads / lay->kv_heads;
-  return (size_t)2 * kSms * (2 * (128 / group * group) * (size_t)(lay->head_dim + 1) * 4 + 2 * sizeof(Part));
+  const size_t rows = can_be_cut(lay, kv) ? 2 * (128 / group * group) : 0;
+  return (size_t)2 * kSms * (rows * (size_t)(lay->head_dim + 1) * 4 + 2 * sizeof(Part));
 }
 
 int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, const toploc_kv_layout* kv, void* workspace,
@@ -790,7 +797,8 @@ int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, 
   tp.box_rows = page > 0 ? min(page, kKeyTile) : kKeyTile;
   tp.q_bytes = p.head_dim * 2 * p.group * tokens;
   tp.wide_out = aligned(p.out, 32) && p.out_token % 16 == 0 && p.out_head % 16 == 0;
-  const long long part_rows = (long long)2 * blocks * tp.item_rows;
+  const bool cut = can_be_cut(lay, kv);
+  const long long part_rows = cut ? (long long)2 * blocks * tp.item_rows : 0;
   p.part_out = static_cast<float*>(workspace);
   p.part_lse = p.part_out + part_rows * p.head_dim;
   tp.parts = reinterpret_cast<Part*>(p.part_lse + part_rows);
@@ -807,9 +815,7 @@ int launch_tensor_cores(AttentionParams& p, const toploc_attention_layout* lay, 
   const int rc = few ? launch_few_rows(&tp, &q, &k, &v, blocks, stream)
                  : p.head_dim == 128 ? launch<128>(tp, q, k, v, blocks, stream) : launch<64>(tp, q, k, v, blocks, stream);
   if (rc != TOPLOC_OK) return rc;
-  // rows that see three tiles of keys at most are never cut: nothing to join
-  const long long most_keys = page > 0 ? min((long long)kv->max_pages * page, (long long)INT32_MAX) : p.max_new;
-  if (most_keys <= 3 * kKeyTile) return TOPLOC_OK;
+  if (!cut) return TOPLOC_OK;  // nothing to join
   return p.head_dim == 128 ? launch_join<128>(tp, blocks, stream) : launch_join<64>(tp, blocks, stream);
 }
 

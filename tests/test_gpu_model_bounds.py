@@ -36,3 +36,24 @@ def test_rows_outside_the_promised_ones_stay(dtype, dim, offsets, most, kept):
     assert (lse[written.to(DEV)] != 7.0).all() and not torch.isnan(out).any()
     lens = [b - a for a, b in zip(offsets, offsets[1:])]
     assert status.tolist() == [tl.TOPLOC_SEQ_BAD_LENGTH if n > most else 0 for n in lens]
+
+
+@pytest.mark.parametrize("keys,new,heads,kv_heads,dim", [(384, 1, 8, 2, 128), (384, 40, 8, 2, 64), (384, 384, 4, 2, 128),
+                                                         (300, 7, 4, 4, 64), (6000, 1, 8, 2, 64), (6000, 40, 8, 2, 128)])
+def test_nothing_behind_the_workspace_is_written(keys, new, heads, kv_heads, dim):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(keys + dim)
+    page, n = 16, 9
+    pages = -(-keys // page)
+    caches = [torch.randn((pages, page, kv_heads, dim), generator=g, device=DEV).to(torch.bfloat16) for _ in range(2)]
+    table = torch.randint(0, pages, (n, pages), generator=g, device=DEV, dtype=torch.int32)
+    q = torch.randn((n * new, heads, dim), generator=g, device=DEV).to(torch.bfloat16)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    args = (q, *caches, table, torch.arange(0, n * new + 1, new, **i32), torch.full((n,), keys, **i32), new)
+    want = tl.toploc_attention_paged(*args, want_lse=True)
+    need = tl.toploc_attention_workspace_bytes(*args[:4], new)
+    room = torch.full((need + (1 << 20),), 0x3C, dtype=torch.uint8, device=DEV)
+    got = tl.toploc_attention_paged(*args, want_lse=True, workspace=room[:need])
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert (room[need:] == 0x3C).all()

@@ -206,6 +206,17 @@ def test_wrappers_refuse_numbers_that_do_not_fit():
             lay.q_token_stride, lay.out_head_stride) == (64, 2, 2, 3, 4, 4, 0.25, 128, 64)
 
 
+def test_workspace_where_nothing_can_be_cut(lib):
+    """Keys of at most three tiles stay with one block: room for its records, not for parts."""
+    flat = kv_layout(page_size=0)
+    for lay, kv, cut in [(dict(), kv_layout(max_pages=24, table_stride=24), False),
+                         (dict(), kv_layout(max_pages=25, table_stride=25), True),
+                         (dict(max_new_tokens=384, total_tokens=1000), flat, False),
+                         (dict(max_new_tokens=385, total_tokens=1000), flat, True)]:
+        need = lib.toploc_attention_workspace_bytes(ctypes.byref(attention_layout(**lay)), ctypes.byref(kv))
+        assert need >= 148 * 2 * 256 * 129 * 4 if cut else 0 < need < 1 << 15, (lay, need)
+
+
 def test_wait_limit_refusals(lib):
     assert paged(lib, attention_layout(wait_tries=-1)) == INVALID
     assert paged(lib, attention_layout(wait_tries=5, num_seqs=0)) == 0
