@@ -60,7 +60,7 @@ const char* toploc_sequence_status_string(int sequence_status);
  * A sequence whose status is not OK takes no pages, gets kv_len 0 (attention
  * over it gives zeros) and slots -1; its rows stay in the packing.  The free
  * list runs out in order: the first sequence whose pages do not fit and all
- * later ones that need any get NO_PAGES.  A sequence whose rows would end past
+ * later ones that need any get NO_PAGES (with a negative first_free: all that need any).  A sequence whose rows would end past
  * max_tokens gets BATCH_FULL and seq_offsets stop at max_tokens.  A negative
  * t_i counts as 0.  The same inputs give the same outputs, and a repeated call
  * changes nothing.

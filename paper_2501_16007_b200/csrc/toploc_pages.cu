@@ -78,7 +78,7 @@ __device__ __forceinline__ PlannedSeq look_at(const PlanParams& p, int i, long l
 
 __device__ __forceinline__ void place(const PlanParams& p, PlannedSeq& s, long long first_page) {
   s.first_page = first_page;
-  if (s.status == TOPLOC_SEQ_OK && s.pages_needed > 0 && (first_page < 0 || first_page + s.pages_needed > p.num_free))
+  if (s.status == TOPLOC_SEQ_OK && s.pages_needed > 0 && first_page + s.pages_needed > p.num_free)
     s.status = TOPLOC_SEQ_NO_PAGES;
 }
 
@@ -121,7 +121,9 @@ __global__ void __launch_bounds__(kPlanThreads) toploc_plan_pages_kernel(const P
     pages += s.pages_needed;
     at += s.tokens;
   }
-  const long long my_page = p.first_free[0] + block_scan(pages, warp_sums, &total_pages);
+  // (no page fits behind a negative head: every sequence that needs one is in the same state)
+  const long long head = p.first_free[0] < 0 ? p.num_free : p.first_free[0];
+  const long long my_page = head + block_scan(pages, warp_sums, &total_pages);
   run_token[tid] = my_token;
   run_page[tid] = my_page;
   if (tid == 0) run_token[kPlanThreads] = total_tokens;
