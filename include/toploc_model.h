@@ -99,8 +99,9 @@ typedef struct {
  *                tokens have distinct slots)
  * d_k_cache, d_v_cache  DEVICE, as kv describes (table fields unused)
  * dtype          TOPLOC_DTYPE_* of all four
- * Pointers aligned to the element; rows of whole 16-byte vectors at 16-byte
- * aligned places move as vectors, others element by element.
+ * kv_heads * head_dim < 2^31.  Pointers aligned to the element; rows of whole
+ * 16-byte vectors at 16-byte aligned places move as vectors, others element by
+ * element.
  */
 int toploc_cache_write(const void* d_k, const void* d_v, int64_t k_token_stride, int64_t k_head_stride,
                        int64_t v_token_stride, int64_t v_head_stride, const int64_t* d_slots, int64_t num_tokens,

@@ -342,7 +342,8 @@ extern "C" int toploc_cache_write(const void* d_k, const void* d_v, int64_t k_to
   const int size = element_bytes(dtype);
   if (!kv || num_tokens < 0 || kv_heads <= 0 || head_dim <= 0 || kv->page_size <= 0 || kv->num_pages < 0)
     return TOPLOC_ERR_INVALID_ARGUMENT;
-  if (size == 0) return TOPLOC_ERR_UNSUPPORTED;
+  // (a thread's place inside a token is a 32-bit number)
+  if (size == 0 || (int64_t)kv_heads * head_dim > 0x7FFFFFFF) return TOPLOC_ERR_UNSUPPORTED;
   if (num_tokens == 0) return TOPLOC_OK;
   if (!d_k || !d_v || !d_slots || !d_k_cache || !d_v_cache || !aligned(d_slots, 8)) return TOPLOC_ERR_INVALID_ARGUMENT;
   const int64_t strides[10] = {k_token_stride, k_head_stride, kv->k_page_stride, kv->k_token_stride, kv->k_head_stride,

@@ -206,6 +206,11 @@ def test_wrappers_refuse_numbers_that_do_not_fit():
             lay.q_token_stride, lay.out_head_stride) == (64, 2, 2, 3, 4, 4, 0.25, 128, 64)
 
 
+def test_write_refuses_tokens_beyond_32_bits(lib):
+    assert write(lib, heads=1 << 20, dim=1 << 11) == UNSUPPORTED        # 2^31 elements: places in a token would wrap
+    assert write(lib, heads=(1 << 31) - 1, dim=(1 << 31) - 1) == UNSUPPORTED
+
+
 def test_workspace_where_nothing_can_be_cut(lib):
     """Keys of at most three tiles stay with one block: room for its records, not for parts."""
     flat = kv_layout(page_size=0)
