@@ -235,11 +235,19 @@ def _empty(shape, dtype, device, stream, hidden=False):
     return t
 
 
+def _bytes_of(workspace):
+    """Bytes from a workspace's beginning on that are its own: all of a contiguous tensor (an expanded one has fewer than
+    its shape says)."""
+    if not workspace.is_contiguous():
+        raise ToplocError("a workspace must be contiguous")
+    return workspace.numel() * workspace.element_size()
+
+
 def _workspace(lay, workspace, device, stream):
     need = toploc_workspace_bytes(lay)
     if workspace is None and need > 0:
         workspace = _empty((need,), torch.uint8, device, stream, hidden=True)
-    return workspace, (0 if workspace is None else workspace.numel() * workspace.element_size())
+    return workspace, (0 if workspace is None else _bytes_of(workspace))
 
 
 def toploc_build_proofs(act, lay, proofs=None, status=None, indices=None, workspace=None, stream=None,
@@ -352,7 +360,7 @@ def toploc_build_proofs_host(act, lay, proofs, status, staging, stream=None):
     with torch.cuda.device(staging.device):
         rc = load_library().toploc_build_proofs_host(
             _dev_ptr(act), ctypes.byref(lay), _dev_ptr(proofs), _dev_ptr(status), _dev_ptr(staging),
-            staging.numel() * staging.element_size(), _stream_ptr(stream))
+            _bytes_of(staging), _stream_ptr(stream))
     _check(rc, "toploc_build_proofs_host")
     return proofs, status
 
@@ -364,7 +372,7 @@ def toploc_verify_proofs_host(act, lay, proofs, thresholds, results, staging, st
     with torch.cuda.device(staging.device):
         rc = load_library().toploc_verify_proofs_host(
             _dev_ptr(act), ctypes.byref(lay), _dev_ptr(proofs), ctypes.byref(thr), _dev_ptr(results),
-            _dev_ptr(staging), staging.numel() * staging.element_size(), _stream_ptr(stream))
+            _dev_ptr(staging), _bytes_of(staging), _stream_ptr(stream))
     _check(rc, "toploc_verify_proofs_host")
     return results
 
@@ -455,7 +463,7 @@ def toploc_stream_finish(state, lay, proofs=None, status=None, indices=None, wor
     with torch.cuda.device(dev):
         rc = load_library().toploc_stream_finish(
             _dev_ptr(state), ctypes.byref(lay), _dev_ptr(proofs), _dev_ptr(status), _dev_ptr(indices),
-            _dev_ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+            _dev_ptr(workspace), _bytes_of(workspace), _stream_ptr(stream))
     _check(rc, "toploc_stream_finish")
     return proofs, status, indices
 

@@ -11,7 +11,7 @@ import struct
 import torch
 
 from . import binding
-from .binding import TOPLOC_DTYPE_BF16, TOPLOC_DTYPE_FP32, ToplocError, _empty
+from .binding import TOPLOC_DTYPE_BF16, TOPLOC_DTYPE_FP32, ToplocError, _bytes_of, _empty
 
 __all__ = [
     "TOPLOC_SEQ_OK", "TOPLOC_SEQ_BAD_LENGTH", "TOPLOC_SEQ_NO_PAGES", "TOPLOC_SEQ_TABLE_FULL", "TOPLOC_SEQ_BATCH_FULL",
@@ -209,7 +209,7 @@ def _attention_workspace(lib, lay, kv, workspace, dev, stream):
         if need == 0:
             return None, 0
         workspace = _empty((need,), torch.uint8, dev, stream, hidden=True)
-    return workspace, workspace.numel() * workspace.element_size()
+    return workspace, _bytes_of(workspace)
 
 
 def toploc_attention_workspace_bytes(q, k_cache, v_cache, block_table, max_new_tokens):
