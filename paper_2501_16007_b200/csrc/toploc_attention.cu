@@ -19,7 +19,7 @@ constexpr int kWarpRows = kRows / 4;
 __device__ __forceinline__ void split_range(int keys, int splits, int split, int* begin, int* end) {
   const int unit = ((keys + splits - 1) / splits + 128 - 1) / 128 * 128;
   *begin = (int)min((long long)unit * split, (long long)keys);
-  *end = min(*begin + unit, keys);
+  *end = (int)min((long long)*begin + unit, (long long)keys);
 }
 
 // ---- the kernel on the fp32 units: every type, layout and head size ------------------------------
