@@ -212,7 +212,9 @@ typedef struct {
  * with fp32 arithmetic on the unrounded h.  With TOPLOC_NORM_OUT_E4M3 each group
  * of channels is scaled to the type's range,
  *   scale = max(max |y| / 448, 2^-126),  stored = y / scale rounded to nearest even
- * (a zero group stores zeros), scales [rows, ceil(hidden / group)] fp32.
+ * (a zero group stores zeros), scales [rows, ceil(hidden / group)] fp32.  Both
+ * quotients are products with a reciprocal in fp32, off by a rounding or two, as
+ * y is: a value next to the middle of two e4m3 numbers may go to the other one.
  *
  * d_residual_opt     NULL: no addition, h = x
  * d_residual_out_opt NULL: not written; may be d_residual itself

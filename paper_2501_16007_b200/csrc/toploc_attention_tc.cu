@@ -25,10 +25,11 @@
 // many of the special-function units (256 * 128 exponentials, 16 a clock); it takes about 3300.  A group's softmax and
 // then its two products are one chain (2400 and 1700 clocks in a trace of an earlier, slower version), two groups in turn
 // hide half of it, and tensor memory (2 * 128 columns of scores, 2 * 128 of outputs) has no room for scores ahead.
-// Packed prompts of 16383 rows: 770 us, 1.1 PFLOP/s (0.69 of the measured bf16 rate); one sequence of 131000 keys and 17
-// tokens: 136 us.  Instruction fetch is the other bound: eleven warps run seven different pieces of code, and the kernel
-// gained more from small code (loops that are not unrolled, one code for both feeding warps, rare branches out of line: 76
-// to 57 KB, 146 to 136 us, prompts 840 to 770) than from fewer instructions.  Tried and not kept: two threads a row with
+// Packed prompts of 16383 rows: 754 us over 30 passes one behind the other (1.14 PFLOP/s, 0.70 of the measured bf16 rate),
+// 830 over 200 (the power cap), 880 to 890 on inputs that change from pass to pass (0.60); one sequence of 131000 keys and
+// 17 tokens: 136 to 141, and 163 us.  Instruction fetch is the other bound: eleven warps run seven different pieces of code,
+// and the kernel gained more from small code (loops that are not unrolled, one code for both feeding warps, rare branches
+// out of line: 76 to 57 KB, 146 to 136 us, prompts 840 to 770, all one behind the other) than from fewer instructions.  Tried and not kept: two threads a row with
 // 16 softmax warps (the same time, short prompts 52 against 46 us: the maxima have to be exchanged), a share of the
 // exponentials as a polynomial on the fp32 units (2 to 10 % slower), the row's scores kept in registers between maximum
 // and weights (the same where tiles are many, 10 % slower on short prompts: its code is unrolled).

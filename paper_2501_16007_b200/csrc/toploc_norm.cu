@@ -57,7 +57,8 @@ __device__ __forceinline__ float scale_of(float amax) {
 // Bound by memory: x and residual are read once, residual_out and y written once.  A block takes a row and keeps it in
 // registers between the two passes, 16 bytes an access where rows allow it.  What has to be in flight on an SM (50 KB and
 // more) comes from its many threads, not from many values a thread: 16 values a thread and 32 registers (2048 threads an
-// SM) take 620 us for 65536 x 8192 bf16 with e4m3 groups of 128 (6.1 TB/s), 32 values 715 us.  Rows that begin
+// SM) take 618 to 633 us for 65536 x 8192 bf16 with e4m3 groups of 128 (6.0 to 6.1 TB/s; 663 on inputs that change from
+// pass to pass), 32 values 715 us.  Rows that begin
 // anywhere (an odd hidden size) move as vectors too where all tensors share the odd place (4095 x 5001 fp32: 62 us, 5.3
 // TB/s; element by element 78 us, with 32 values a thread 135 us).  Where they do not (or 8 bits come out), single elements:
 // 4096 x 12289 in fp32 154 us, 5.2 TB/s, to e4m3 152, bf16 133 and 154 (2.3 to 3.0 TB/s).
@@ -244,7 +245,8 @@ __global__ void __launch_bounds__(kVec > 1 ? 512 : 1024,
         s = scale_of(amax[i]);
         if (c < p.hidden && (v & ((1 << p.group_shift) - 1)) == 0) p.scales[row * p.groups + (v >> p.group_shift)] = s;
       }
-      // y / s as y * (1 / s): off by an fp32 rounding or two, which moves an e4m3 result only next to the middle of two
+      // y / s as y * (1 / s): off by an fp32 rounding or two, which moves an e4m3 result only next to the middle of two (17 of
+      // a million, by the same arithmetic on the CPU; y's own roundings move as many, whichever way it is divided)
       const float inv = reciprocal(s);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) h[i][e] *= inv;
