@@ -226,12 +226,15 @@ def _empty(shape, dtype, device, stream, hidden=False):
     """A tensor that work on `stream` (None: torch's current one) may write at once: its memory is one of that stream's, so
     that neither what the current stream still does with a block freed there, nor the next allocation after this tensor is
     gone, can meet the call.  hidden: the caller never sees it; else it may be read, and dropped, on the current stream."""
-    if stream is None or stream == torch.cuda.current_stream(device):
+    now = None if stream is None else torch.cuda.current_stream(device)
+    if stream is None or stream.cuda_stream == now.cuda_stream:
         return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):  # anything else that names a CUDA stream
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device)
     with torch.cuda.stream(stream):
         t = torch.empty(shape, dtype=dtype, device=device)
     if not hidden:
-        t.record_stream(torch.cuda.current_stream(device))
+        t.record_stream(now)
     return t
 
 

@@ -56,3 +56,17 @@ def test_norm_on_a_side_stream_behind_frees_of_the_current_one():
         got = tl.toploc_rmsnorm_residual(x, None, w, 1e-5, stream=side)[0]
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+def test_a_stream_that_is_not_torchs():
+    """An object with the handle of a CUDA stream, as other libraries have them."""
+    class Named:
+        cuda_stream = torch.cuda.Stream().cuda_stream
+
+    x = torch.randn((64, 512), device=DEV)
+    w = torch.ones(512, device=DEV)
+    want = tl.toploc_rmsnorm_residual(x, None, w, 1e-5)[0]
+    torch.cuda.synchronize()
+    got = tl.toploc_rmsnorm_residual(x, None, w, 1e-5, stream=Named())[0]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)

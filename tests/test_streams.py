@@ -10,7 +10,15 @@ import torch
 import paper_2501_16007_b200 as tl
 from paper_2501_16007_b200 import binding, model_ops
 
-CURRENT, SIDE = "current", "side"
+
+class Named:
+    """Something that names a CUDA stream and is none of torch's."""
+
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+CURRENT, SIDE = Named(0), Named(77)
 
 
 @pytest.fixture
@@ -37,6 +45,7 @@ def allocations(monkeypatch):
     monkeypatch.setattr(torch, "empty", recorded_empty)
     monkeypatch.setattr(torch, "empty_like", lambda t, **kw: recorded_empty(t.shape, dtype=t.dtype))
     monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: {77: SIDE}[handle])
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: now[-1])
     monkeypatch.setattr(torch.Tensor, "record_stream", record)
     return made
@@ -46,7 +55,7 @@ def check(made, shapes, stream):
     """All allocations were made on `stream`; what the caller gets is also kept for the current one."""
     assert sorted(tuple(t.shape) for t, _, _ in made) == sorted(shapes)
     for t, where, recorded in made:
-        assert where == stream, "%s allocated on the %s stream" % (tuple(t.shape), where)
+        assert where == stream, "%s allocated on stream %d" % (tuple(t.shape), where.cuda_stream)
         if stream != CURRENT:
             assert recorded == ([] if t.shape == (640,) else [CURRENT]), tuple(t.shape)   # 640: the workspace
 
