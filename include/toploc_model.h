@@ -32,6 +32,9 @@ extern "C" {
 #define TOPLOC_SEQ_BATCH_FULL 4 /* the sequence's tokens end beyond the token buffers */
 #define TOPLOC_SEQ_BAD_PAGE 5   /* a block table entry outside the cache */
 #define TOPLOC_SEQ_WAIT_EXPIRED 6 /* a wait inside the kernel ran out of its limit; rows that were not finished are NaN */
+#define TOPLOC_SEQ_BAD_PARENT 7   /* a fork of a sequence that does not exist, or that is forked from another itself */
+#define TOPLOC_SEQ_IN_USE 8       /* a fork into a sequence that holds tokens */
+#define TOPLOC_SEQ_NO_ROOM 9      /* the free list has no room for all pages that came back */
 
 const char* toploc_sequence_status_string(int sequence_status);
 
@@ -107,6 +110,188 @@ int toploc_cache_write(const void* d_k, const void* d_v, int64_t k_token_stride,
                        int64_t v_token_stride, int64_t v_head_stride, const int64_t* d_slots, int64_t num_tokens,
                        int32_t dtype, int32_t kv_heads, int32_t head_dim, void* d_k_cache, void* d_v_cache,
                        const toploc_kv_layout* kv, void* cuda_stream);
+
+/* ---- pages that sequences share, give back or move ---------------------- */
+
+/*
+ * Sequences that begin with the same tokens (samples of one prompt) can hold the
+ * same pages.  d_shares [num_pages] says how many sequences hold a page beyond
+ * the first: zeros for a pool whose pages have one holder each, as
+ * toploc_plan_pages hands them out (it needs no shares).  Only whole pages are
+ * shared, and new tokens go behind them, so a shared page is never written.
+ *
+ * The three planners below run as one cluster of thread blocks each.  Outputs
+ * are apart from inputs (shares and lengths: two buffers used in turn), so that
+ * a repeated call gives the same; refused where they overlap.  The same inputs
+ * give the same outputs.  All arrays DEVICE; int32 4-byte aligned.  num_seqs <=
+ * 2^24, num_pages <= 2^30, max_pages >= 0, table_stride >= max_pages.
+ */
+
+/*
+ * Forks sequences: sequence i with d_parents[i] >= 0 begins as a copy of that
+ * one, length l = d_kv_lens[d_parents[i]].  It shares the parent's
+ * floor(l / page_size) whole pages; where tokens are left over it gets a page of
+ * its own off the free list (entry first_free + pages taken by earlier children
+ * on), and the pair goes to the list of copies that toploc_copy_pages works off.
+ *
+ *   d_parents     [num_seqs]   -1: the sequence stays as it is
+ *   d_kv_lens     [num_seqs]   tokens held; a child's must be 0
+ *   d_block_table [num_seqs, max_pages]  children's rows are written, entries
+ *                              0 .. ceil(l / page_size) - 1; parents' are read
+ *   d_kv_lens_out [num_seqs]   l for children that were forked, else d_kv_lens
+ *   d_shares_out  [num_pages]  shares with the children counted
+ *   d_copy_from, d_copy_to [num_seqs]  the pages to copy, in order of children,
+ *                              -1 behind the last
+ *   d_num_copies  [1]          how many
+ *   d_next_free   [1]          first_free + pages taken
+ *   d_status      [num_seqs]   TOPLOC_SEQ_*
+ *
+ * A child whose status is not OK stays as it was (its row's contents do not
+ * count): BAD_PARENT, IN_USE, BAD_LENGTH (the parent's is negative or beyond
+ * its row), BAD_PAGE (an entry of the parent's row, or of the free list, is
+ * outside the pool; a page off the list is used up all the same and its pair is
+ * -1), NO_PAGES (in order, as in toploc_plan_pages).
+ */
+int toploc_fork_pages(const int32_t* d_parents, const int32_t* d_kv_lens, int32_t num_seqs, const int32_t* d_shares,
+                      int32_t num_pages, const int32_t* d_free_pages, int32_t num_free, const int32_t* d_first_free,
+                      int32_t page_size, int32_t* d_block_table, int32_t max_pages, int64_t table_stride,
+                      int32_t* d_kv_lens_out, int32_t* d_shares_out, int32_t* d_copy_from, int32_t* d_copy_to,
+                      int32_t* d_num_copies, int32_t* d_next_free, uint8_t* d_status, void* cuda_stream);
+
+/*
+ * Releases sequences: those with d_release[i] != 0 let go of their
+ * ceil(d_kv_lens[i] / page_size) pages.  A page that nobody holds any longer
+ * goes back to the free list, in front of its head: the pages, in ascending
+ * order, become entries next_free .. first_free - 1.
+ *
+ *   d_release     [num_seqs]   bytes
+ *   d_free_pages  [num_free]   in/out, entries in front of first_free (which
+ *                              earlier steps have taken) are written
+ *   d_kv_lens_out [num_seqs]   0 for released sequences, else d_kv_lens
+ *   d_shares_out  [num_pages]  shares without the released holders
+ *   d_next_free   [1]          first_free - pages that came back
+ *   d_status      [num_seqs]   TOPLOC_SEQ_*: of released sequences, BAD_LENGTH (a
+ *                              negative one counts as 0, one beyond the row as
+ *                              the row), BAD_PAGE (an entry outside the pool,
+ *                              passed over), NO_ROOM (first_free is smaller than
+ *                              the pages that came back, so the pages were never
+ *                              all taken off this list: the highest ones that do
+ *                              not fit are left out)
+ *
+ * A first_free outside 0 .. num_free counts as the nearest of the two for the
+ * room that there is.  A page released more often than it is held comes back
+ * once.
+ */
+int toploc_release_pages(const uint8_t* d_release, const int32_t* d_kv_lens, int32_t num_seqs,
+                         const int32_t* d_block_table, int32_t max_pages, int64_t table_stride, const int32_t* d_shares,
+                         int32_t num_pages, int32_t page_size, int32_t* d_free_pages, int32_t num_free,
+                         const int32_t* d_first_free, int32_t* d_kv_lens_out, int32_t* d_shares_out,
+                         int32_t* d_next_free, uint8_t* d_status, void* cuda_stream);
+
+/*
+ * Compacts a pool: its n pages in use (those that a sequence holds) become pages
+ * 0 .. n - 1, so that the memory behind them can be given up or the pool's
+ * tail cut off.  Pages below n stay where they are; the others go to the unused
+ * places below n, both in ascending order.
+ *
+ *   d_block_table_out [num_seqs, max_pages]  entries of held pages are written,
+ *                              others left as they are; may be d_block_table
+ *                              itself (with the same stride)
+ *   d_shares_out  [num_pages]  at the pages' new places, 0 behind them
+ *   d_free_pages_out [num_free]  the unused pages n .. num_pages - 1 in its last
+ *                              num_pages - n entries, next_free and on; entries
+ *                              in front are left as they are.  num_free >=
+ *                              num_pages
+ *   d_copy_from, d_copy_to [num_pages]  the pages to copy, -1 behind the last; no
+ *                              page is in both
+ *   d_num_copies  [1]
+ *   d_next_free   [1]          num_free - (num_pages - n)
+ *   d_status      [num_seqs]   TOPLOC_SEQ_*: BAD_LENGTH and BAD_PAGE as in
+ *                              toploc_release_pages (the entry stays as it is)
+ *
+ * Lengths do not change.  Pages that no sequence holds and that were lost to the
+ * free list are found again.
+ */
+int toploc_compact_pages(const int32_t* d_kv_lens, int32_t num_seqs, const int32_t* d_block_table, int32_t max_pages,
+                         int64_t table_stride, const int32_t* d_shares, int32_t num_pages, int32_t page_size,
+                         int32_t* d_block_table_out, int64_t table_out_stride, int32_t* d_shares_out,
+                         int32_t* d_free_pages_out, int32_t num_free, int32_t* d_copy_from, int32_t* d_copy_to,
+                         int32_t* d_num_copies, int32_t* d_next_free, uint8_t* d_status, void* cuda_stream);
+
+/* Caches that share a block table (keys and values of all layers): one layout for all of them. */
+typedef struct {
+  int32_t dtype;      /* TOPLOC_DTYPE_* */
+  int32_t num_pages, page_size, kv_heads, head_dim;
+  int32_t num_caches; /* >= 0 */
+  int64_t page_stride, token_stride, head_stride; /* elements */
+} toploc_pool_layout;
+
+/*
+ * Copies pages inside every one of the caches: page d_copy_from[c] to page
+ * d_copy_to[c], c < d_num_copies[0] (at most max_copies).  Pairs with a page
+ * outside the caches are skipped.  No page may be written twice, or written and
+ * read.
+ *
+ * h_caches       HOST array of num_caches DEVICE pointers (read before the call
+ *                returns), aligned to the element
+ */
+int toploc_copy_pages(void* const* h_caches, const toploc_pool_layout* lay, const int32_t* d_copy_from,
+                      const int32_t* d_copy_to, const int32_t* d_num_copies, int32_t max_copies, void* cuda_stream);
+
+/* ---- queries and keys between projection and attention ------------------ */
+
+#define TOPLOC_ROTARY_HALVES 0     /* channel c turns with channel c + rotary_dim / 2 */
+#define TOPLOC_ROTARY_NEIGHBOURS 1 /* channel 2c turns with channel 2c + 1 */
+
+typedef struct {
+  int32_t dtype;      /* TOPLOC_DTYPE_* of all tensors and weights */
+  int32_t head_dim;   /* 1 .. 256 */
+  int32_t q_heads;    /* > 0 */
+  int32_t kv_heads;   /* > 0 */
+  int32_t rotary_dim; /* even, 0 .. head_dim: the first channels of a head turn, the rest stay */
+  int32_t pairing;    /* TOPLOC_ROTARY_* */
+  int64_t num_tokens; /* >= 0 */
+  float eps;          /* >= 0 */
+  int32_t reserved;   /* 0 */
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride; /* elements */
+  int64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+} toploc_rotary_layout;
+
+/*
+ * The RMS norm of every head of the queries and keys, and the rotation by
+ * position behind it, in one pass:
+ *   y = x * rsqrt(mean over the head's channels(x^2) + eps) * weight
+ *   (a, b) <- (a cos t - b sin t, a sin t + b cos t),  t = position * inv_freq[c]
+ * for the pairs (a, b) = channels (c, c + rotary_dim / 2) or (2c, 2c + 1) of y,
+ * c < rotary_dim / 2.  fp32 arithmetic with one rounding at the end; t is formed
+ * and reduced in 64 bits, so far positions are as exact as near ones.
+ *
+ * d_q, d_k       DEVICE [num_tokens, heads, head_dim], the last dimension
+ *                contiguous (views of one projection are fine)
+ * d_positions    DEVICE [num_tokens] int32 (as toploc_plan_pages writes them)
+ * d_inv_freq     DEVICE [rotary_dim / 2] fp32
+ * d_q_weight_opt, d_k_weight_opt  DEVICE [head_dim], NULL: no norm of that one
+ * d_q_out, d_k_out  DEVICE; each may be its input (with the same strides), else
+ *                they share no memory with the inputs
+ * Pointers aligned to the element; heads at places of 16 (8) bytes whose
+ * channels and turned channels are whole vectors of that size move as vectors,
+ * others element by element.  Asynchronous.
+ */
+int toploc_norm_rotary_prompt(const void* d_q, const void* d_k, const int32_t* d_positions, const float* d_inv_freq,
+                              const void* d_q_weight_opt, const void* d_k_weight_opt, const toploc_rotary_layout* lay,
+                              void* d_q_out, void* d_k_out, void* cuda_stream);
+
+/*
+ * The same, with keys and values [num_tokens, kv_heads, head_dim] written
+ * straight to their slots of the paged cache (as toploc_cache_write does it:
+ * negative slots and slots past the cache are skipped, distinct tokens have
+ * distinct slots; values are copied as they are).  The k_out strides are not
+ * used.
+ */
+int toploc_norm_rotary_paged(const void* d_q, const void* d_k, const void* d_v, const int32_t* d_positions,
+                             const int64_t* d_slots, const float* d_inv_freq, const void* d_q_weight_opt,
+                             const void* d_k_weight_opt, const toploc_rotary_layout* lay, void* d_q_out,
+                             void* d_k_cache, void* d_v_cache, const toploc_kv_layout* kv, void* cuda_stream);
 
 /* ---- attention -------------------------------------------------------- */
 
@@ -225,6 +410,45 @@ typedef struct {
 int toploc_rmsnorm_residual(const void* d_x, const void* d_residual_opt, const void* d_weight, float eps,
                             const toploc_norm_layout* lay, void* d_residual_out_opt, void* d_y, float* d_scales_opt,
                             void* cuda_stream);
+
+/* ---- log probabilities -------------------------------------------------- */
+
+#define TOPLOC_MAX_ALTERNATIVES 32
+
+typedef struct {
+  int32_t dtype;      /* TOPLOC_DTYPE_* of the logits */
+  int32_t vocab;      /* 1 .. 2^20 */
+  int32_t top;        /* alternatives a row, 0 .. TOPLOC_MAX_ALTERNATIVES */
+  int32_t reserved;   /* 0 */
+  int64_t rows;       /* >= 0 */
+  int64_t row_stride; /* elements, >= vocab (columns past the vocabulary are not read) */
+} toploc_logprob_layout;
+
+/*
+ * What a sampler or a validator reads off rows of logits x, in one pass over
+ * them:
+ *   logprob  = x[token] - lse,             lse = log sum_j exp(x_j)
+ *   entropy  = -sum_j p_j log p_j,         p_j = exp(x_j - lse)
+ *   top      = the `top` likeliest tokens, ordered by logit, equal ones by
+ *              index (the first is the greedy token), and their log
+ *              probabilities
+ * in fp32.  A logit of -inf is an impossible token: it has no part in entropy,
+ * its log probability is -inf, and it is no alternative; places that no token is
+ * left for get id -1 and -inf.  A row with nothing above -inf gets logprob -inf
+ * and entropy 0.  A row with a NaN or +inf gets NaN for all but the ids (which
+ * pass over NaN).
+ *
+ * d_logits           DEVICE [rows, vocab], row_stride
+ * d_tokens_opt       DEVICE [rows] int64, or NULL: no logprob; one outside the
+ *                    vocabulary gets NaN
+ * d_logprobs_opt     DEVICE [rows] fp32, NULL exactly where d_tokens is
+ * d_entropy_opt      DEVICE [rows] fp32 or NULL
+ * d_top_ids, d_top_logprobs  DEVICE [rows, top] int64 / fp32, NULL with top 0
+ * Pointers aligned to their elements.  Asynchronous, deterministic.
+ */
+int toploc_token_logprobs(const void* d_logits, const toploc_logprob_layout* lay, const int64_t* d_tokens_opt,
+                          float* d_logprobs_opt, float* d_entropy_opt, int64_t* d_top_ids, float* d_top_logprobs,
+                          void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -14,7 +14,8 @@ PROOF_SOURCES = [os.path.join(_HERE, "toploc.cu"), os.path.join(_HERE, "toploc_d
                  os.path.join(_HERE, "toploc_producer.cu")]
 MODEL_SOURCES = [os.path.join(_HERE, "toploc_pages.cu"), os.path.join(_HERE, "toploc_norm.cu"),
                  os.path.join(_HERE, "toploc_attention.cu"), os.path.join(_HERE, "toploc_attention_tc.cu"),
-                 os.path.join(_HERE, "toploc_attention_few.cu")]
+                 os.path.join(_HERE, "toploc_attention_few.cu"), os.path.join(_HERE, "toploc_pool.cu"),
+                 os.path.join(_HERE, "toploc_rotary.cu"), os.path.join(_HERE, "toploc_logits.cu")]
 SOURCES = PROOF_SOURCES + MODEL_SOURCES
 PROOF_HEADERS = [os.path.join(_INCLUDE, "toploc.h"), os.path.join(_INCLUDE, "toploc_device.cuh"),
                  os.path.join(_HERE, "nearest_ratio.cuh")]

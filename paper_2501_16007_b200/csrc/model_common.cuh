@@ -43,6 +43,23 @@ inline int allow_shared(const void* kernel, int bytes, std::atomic<uint64_t>& do
   return TOPLOC_OK;
 }
 
+// Memory of an argument: rows of `bytes`, a step apart (a vector is one row).
+struct Rows {
+  const void* at;
+  long long bytes, rows, step;
+  Rows(const void* at, long long bytes, long long rows = 1, long long step = 0)
+      : at(at), bytes(bytes), rows(rows), step(rows > 1 ? step : bytes) {}
+};
+
+// Whether a vector and rows share memory.
+inline bool overlap(const Rows& vector, const Rows& r) {
+  if (vector.bytes <= 0 || r.bytes <= 0 || r.rows <= 0) return false;
+  const long long from = (long long)(reinterpret_cast<uintptr_t>(vector.at) - reinterpret_cast<uintptr_t>(r.at));
+  // the first row that ends behind the vector's beginning has to begin in front of its end
+  const long long row = from < r.bytes ? 0 : (from - r.bytes) / r.step + 1;
+  return row < r.rows && row * r.step < from + vector.bytes;
+}
+
 inline int launched() { return cudaGetLastError() == cudaSuccess ? TOPLOC_OK : TOPLOC_ERR_CUDA; }
 
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }

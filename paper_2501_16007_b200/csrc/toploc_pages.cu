@@ -234,23 +234,6 @@ __global__ void __launch_bounds__(kPlanThreads) toploc_plan_pages_kernel(const P
   }
 }
 
-// Memory of an argument: rows of `bytes`, a step apart (a vector is one row).
-struct Rows {
-  const void* at;
-  long long bytes, rows, step;
-  Rows(const void* at, long long bytes, long long rows = 1, long long step = 0)
-      : at(at), bytes(bytes), rows(rows), step(rows > 1 ? step : bytes) {}
-};
-
-// Whether a vector and rows share memory.
-bool overlap(const Rows& vector, const Rows& r) {
-  if (vector.bytes <= 0 || r.bytes <= 0 || r.rows <= 0) return false;
-  const long long from = (long long)(reinterpret_cast<uintptr_t>(vector.at) - reinterpret_cast<uintptr_t>(r.at));
-  // the first row that ends behind the vector's beginning has to begin in front of its end
-  const long long row = from < r.bytes ? 0 : (from - r.bytes) / r.step + 1;
-  return row < r.rows && row * r.step < from + vector.bytes;
-}
-
 struct WriteParams {
   const unsigned char* src[2];
   unsigned char* cache[2];
@@ -291,6 +274,9 @@ extern "C" const char* toploc_sequence_status_string(int s) {
     case TOPLOC_SEQ_BATCH_FULL: return "tokens end beyond the token buffers";
     case TOPLOC_SEQ_BAD_PAGE: return "block table entry outside the cache";
     case TOPLOC_SEQ_WAIT_EXPIRED: return "a wait inside the kernel ran out";
+    case TOPLOC_SEQ_BAD_PARENT: return "forked from no sequence, or from one that is forked itself";
+    case TOPLOC_SEQ_IN_USE: return "forked into a sequence that holds tokens";
+    case TOPLOC_SEQ_NO_ROOM: return "free list without room for all pages that came back";
   }
   return "unknown sequence status";
 }

@@ -1,0 +1,666 @@
+// Pages that sequences share, give back or move: forks, releases, the compaction of a pool, and the copies of pages that
+// follow from them.
+//
+// The planners move little (a table's entries and an integer or two a page) and have to agree on counts between their steps.
+// Each is one launch of one cluster of eight blocks: the cluster's barrier is the hardware's, so no block spins on another,
+// and a step's counts go through the blocks' shared memory.  A row of the table belongs to the same warp of all blocks, its
+// columns to the blocks in turn; a page belongs to one warp, in ascending order, so that what is numbered comes out in order
+// whatever the atomics' order was.
+#include "model_common.cuh"
+
+#include <cooperative_groups.h>
+
+namespace {
+
+using namespace toploc_model;
+namespace cg = cooperative_groups;
+
+constexpr int kCluster = 8;
+constexpr int kThreads = 1024;
+constexpr int kWarps = kThreads / 32;          // of a block
+constexpr int kAllWarps = kCluster * kWarps;
+constexpr int kRows = 8;                       // rows of the table a warp reads at once
+
+struct PoolParams {
+  const int32_t* parents;    // fork
+  const uint8_t* release;    // release
+  const int32_t* kv_lens;
+  const int32_t* shares;
+  const int32_t* free_in;    // fork
+  const int32_t* first_free; // fork, release
+  const int32_t* table_in;   // compact
+  int32_t* table;            // fork: in and out; release: in; compact: out
+  int32_t* kv_lens_out;
+  int32_t* shares_out;
+  int32_t* free_out;         // release, compact
+  int32_t* copy_from;
+  int32_t* copy_to;
+  int32_t* num_copies;
+  int32_t* next_free;
+  uint8_t* status;
+  long long table_stride, table_in_stride;
+  int num_seqs, num_pages, num_free, page_size, max_pages;
+};
+
+__device__ __forceinline__ int pages_for(int tokens, int page_size) {
+  return (int)(((unsigned)tokens + (unsigned)page_size - 1u) / (unsigned)page_size);
+}
+
+// What another block of the cluster may have written since: from L2.
+__device__ __forceinline__ int32_t fresh(const int32_t* p) { return __ldcg(p); }
+
+__device__ __forceinline__ int warp_total(int v) { return __reduce_add_sync(0xFFFFFFFFu, v); }
+
+// Pages of a sequence that a release or a compaction goes by, and what is wrong with its length.
+__device__ __forceinline__ int held_pages(const PoolParams& p, int len, int* status) {
+  *status = TOPLOC_SEQ_OK;
+  if (len < 0) {
+    *status = TOPLOC_SEQ_BAD_LENGTH;
+    return 0;
+  }
+  const int pages = pages_for(len, p.page_size);
+  if (pages > p.max_pages) *status = TOPLOC_SEQ_BAD_LENGTH;
+  return min(pages, p.max_pages);
+}
+
+// Calls visit(entry's address, page, row) for entries of the rows' held pages: all lanes of a warp together, lanes without an
+// entry with row -1.  held(row): pages of a row (its length is read by one lane a row).
+template <typename Held, typename Visit>
+__device__ __forceinline__ void for_entries(const PoolParams& p, const int32_t* table, long long stride, int block, Held held,
+                                            Visit visit) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int base = warp; base < p.num_seqs; base += kWarps * 32) {
+    const int row = base + lane * kWarps;
+    const int mine = row < p.num_seqs ? held(row) : 0;
+    const int count = min(32, (p.num_seqs - base + kWarps - 1) / kWarps);
+    for (int first = 0; first < count; first += kRows) {
+      int pages[kRows], most = 0;
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        pages[i] = __shfl_sync(0xFFFFFFFFu, mine, (first + i) & 31);
+        if (first + i >= count) pages[i] = 0;
+        most = max(most, pages[i]);
+      }
+      for (int c0 = block * 32; c0 < most; c0 += kCluster * 32) {
+        int32_t page[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+          page[i] = 0;
+          if (c0 + lane < pages[i]) page[i] = table[(base + (first + i) * kWarps) * stride + c0 + lane];
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+          if (c0 >= pages[i]) continue;
+          const int row = base + (first + i) * kWarps;
+          visit(row, c0 + lane, page[i], c0 + lane < pages[i]);
+        }
+      }
+    }
+  }
+}
+
+// The range of pages of one warp of the cluster, whole groups of 32.
+__device__ __forceinline__ void pages_of_warp(const PoolParams& p, int warp_of_all, int* begin, int* end) {
+  const int groups = (p.num_pages + 31) / 32, each = (groups + kAllWarps - 1) / kAllWarps;
+  *begin = (int)min((long long)warp_of_all * each * 32, (long long)p.num_pages);
+  *end = (int)min((long long)*begin + each * 32, (long long)p.num_pages);
+}
+
+// Every warp's count to all blocks: counts[w] of every warp of the cluster in shared memory, after a barrier of the cluster.
+__device__ __forceinline__ void tell_count(cg::cluster_group& cluster, int* counts, int count) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (lane < kCluster) cluster.map_shared_rank(counts, lane)[(int)cluster.block_rank() * kWarps + warp] = count;
+}
+
+// Sum of the counts in front of a warp and of all, for all lanes.
+__device__ __forceinline__ int counted_before(const int* counts, int warp_of_all, int* all) {
+  const int lane = threadIdx.x & 31;
+  int before = 0, total = 0;
+#pragma unroll
+  for (int i = 0; i < kAllWarps / 32; ++i) {
+    const int c = counts[i * 32 + lane];
+    total += c;
+    if (i * 32 + lane < warp_of_all) before += c;
+  }
+  *all = warp_total(total);
+  return warp_total(before);
+}
+
+// Exclusive prefix sum over the block's threads; *total gets the sum.
+__device__ __forceinline__ int block_scan(int v, int* warp_sums, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int incl = v;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int up = __shfl_up_sync(0xFFFFFFFFu, incl, off);
+    if (lane >= off) incl += up;
+  }
+  if (lane == 31) warp_sums[warp] = incl;
+  __syncthreads();
+  int before = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const int s = warp_sums[w];
+    if (w < warp) before += s;
+    sum += s;
+  }
+  __syncthreads();
+  *total = sum;
+  return before + incl - v;
+}
+
+// ---- forks ---------------------------------------------------------------------------------------
+
+constexpr int kNeedsPage = 0x80;  // of a status byte until the end: the child asks for a page
+
+__device__ __forceinline__ int status_of(const PoolParams& p, int i) { return __ldcg(p.status + i); }
+
+// Pages that the children in front of i ask for.
+__device__ __forceinline__ int asked_before(const PoolParams& p, const int* run_before, int per, int i) {
+  int place = run_before[i / per];
+  for (int j = i / per * per; j < i; ++j) place += status_of(p, j) >> 7;
+  return place;
+}
+
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
+    toploc_fork_pages_kernel(const __grid_constant__ PoolParams p) {
+  __shared__ int warp_sums[kWarps], run_before[kThreads];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int block = (int)cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int all_tid = block * kThreads + tid, warp_of_all = block * kWarps + warp;
+
+  // who can be forked
+  for (int i = all_tid; i < p.num_pages; i += kCluster * kThreads) p.shares_out[i] = p.shares[i];
+  for (int i = warp_of_all; i < p.num_seqs; i += kAllWarps) {
+    const int parent = p.parents[i], own = p.kv_lens[i];
+    int status = TOPLOC_SEQ_OK, len = own;
+    if (parent >= 0) {
+      if (parent >= p.num_seqs || p.parents[parent] >= 0) {
+        status = TOPLOC_SEQ_BAD_PARENT;
+      } else if (own != 0) {
+        status = TOPLOC_SEQ_IN_USE;
+      } else {
+        len = p.kv_lens[parent];
+        const int pages = len < 0 ? 0 : pages_for(len, p.page_size);
+        if (len < 0 || pages > p.max_pages) {
+          status = TOPLOC_SEQ_BAD_LENGTH;
+        } else {
+          const int32_t* row = p.table + parent * p.table_stride;
+          bool bad = false;
+          for (int j = lane; j < pages; j += 32) bad = bad || (unsigned)row[j] >= (unsigned)p.num_pages;
+          if (__any_sync(0xFFFFFFFFu, bad))
+            status = TOPLOC_SEQ_BAD_PAGE;
+          else if (len % p.page_size > 0)
+            status = kNeedsPage;
+        }
+      }
+    }
+    if (lane == 0) {
+      p.kv_lens_out[i] = status == TOPLOC_SEQ_OK || status == kNeedsPage ? len : own;
+      p.status[i] = (uint8_t)status;
+    }
+  }
+  cluster.sync();
+
+  // pages asked for in front of every thread's run of sequences (every block for itself)
+  const int per = max(1, (p.num_seqs + kThreads - 1) / kThreads);
+  const int begin = min(tid * per, p.num_seqs), end = min(begin + per, p.num_seqs);
+  int asked = 0, total;
+  for (int i = begin; i < end; ++i) asked += status_of(p, i) >> 7;
+  run_before[tid] = block_scan(asked, warp_sums, &total);
+  __syncthreads();
+  const int head = p.first_free[0];
+  const int room = head < 0 ? 0 : max(0, p.num_free - head), taken = min(total, room);
+  if (all_tid == 0) {
+    p.num_copies[0] = taken;
+    p.next_free[0] = head + taken;
+  }
+  for (int i = taken + all_tid; i < p.num_seqs; i += kCluster * kThreads) p.copy_from[i] = p.copy_to[i] = -1;
+
+  // the children's rows (a status keeps its mark for those that still count)
+  for (int i = warp_of_all; i < p.num_seqs; i += kAllWarps) {
+    const int parent = p.parents[i], was = status_of(p, i);
+    if (parent < 0 || (was & ~kNeedsPage) != TOPLOC_SEQ_OK) continue;
+    const int whole = fresh(p.kv_lens_out + i) / p.page_size;
+    const int32_t* theirs = p.table + parent * p.table_stride;
+    int32_t* row = p.table + i * p.table_stride;
+    int status = TOPLOC_SEQ_OK;
+    if (was == kNeedsPage) {
+      const int place = asked_before(p, run_before, per, i);
+      if (place >= room) {
+        status = TOPLOC_SEQ_NO_PAGES;
+      } else {
+        const int32_t page = p.free_in[head + place];
+        if ((unsigned)page >= (unsigned)p.num_pages) status = TOPLOC_SEQ_BAD_PAGE;
+        if (lane == 0) {
+          if (status == TOPLOC_SEQ_OK) row[whole] = page;
+          p.copy_from[place] = status == TOPLOC_SEQ_OK ? theirs[whole] : -1;
+          p.copy_to[place] = status == TOPLOC_SEQ_OK ? page : -1;
+        }
+      }
+      if (status != TOPLOC_SEQ_OK && lane == 0) p.status[i] = (uint8_t)(status | kNeedsPage);
+    }
+    if (status != TOPLOC_SEQ_OK) continue;
+    for (int j0 = lane; j0 < whole; j0 += 32 * kRows) {
+      int32_t page[kRows];
+#pragma unroll
+      for (int e = 0; e < kRows; ++e) page[e] = j0 + e * 32 < whole ? theirs[j0 + e * 32] : 0;
+#pragma unroll
+      for (int e = 0; e < kRows; ++e) {
+        if (j0 + e * 32 >= whole) break;
+        row[j0 + e * 32] = page[e];
+        atomicAdd(p.shares_out + page[e], 1);
+      }
+    }
+  }
+  cluster.sync();
+  for (int i = all_tid; i < p.num_seqs; i += kCluster * kThreads) {
+    const int was = status_of(p, i);
+    if (was & kNeedsPage) {
+      p.status[i] = (uint8_t)(was & ~kNeedsPage);
+      if (was != kNeedsPage) p.kv_lens_out[i] = p.kv_lens[i];
+    }
+  }
+}
+
+// ---- releases ------------------------------------------------------------------------------------
+
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
+    toploc_release_pages_kernel(const __grid_constant__ PoolParams p) {
+  __shared__ int counts[kAllWarps];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int block = (int)cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int all_tid = block * kThreads + tid, warp_of_all = block * kWarps + warp;
+
+  for (int i = all_tid; i < p.num_pages; i += kCluster * kThreads) p.shares_out[i] = p.shares[i];
+  for (int i = all_tid; i < p.num_seqs; i += kCluster * kThreads) {
+    const int len = p.kv_lens[i];
+    int status = TOPLOC_SEQ_OK;
+    const bool gone = p.release[i] != 0;
+    if (gone) held_pages(p, len, &status);
+    p.kv_lens_out[i] = gone ? 0 : len;
+    p.status[i] = (uint8_t)status;
+  }
+  cluster.sync();
+
+  // a holder less for every entry; below zero: nobody is left
+  for_entries(
+      p, p.table, p.table_stride, block,
+      [&](int row) {
+        int status;
+        return p.release[row] != 0 ? held_pages(p, p.kv_lens[row], &status) : 0;
+      },
+      [&](int row, int, int32_t page, bool valid) {
+        if (!valid) return;
+        if ((unsigned)page < (unsigned)p.num_pages)
+          atomicSub(p.shares_out + page, 1);
+        else
+          p.status[row] = TOPLOC_SEQ_BAD_PAGE;
+      });
+  cluster.sync();
+
+  int begin, end, count = 0, total;
+  pages_of_warp(p, warp_of_all, &begin, &end);
+  for (int i = begin + lane; i < end; i += 32) count += fresh(p.shares_out + i) < 0;
+  tell_count(cluster, counts, warp_total(count));
+  cluster.sync();
+
+  int place = counted_before(counts, warp_of_all, &total);
+  const int room = min(max(p.first_free[0], 0), p.num_free), fit = min(total, room);
+  for (int base = begin; base < end; base += 32) {
+    const int i = base + lane;
+    const int left = i < end ? fresh(p.shares_out + i) : 0;
+    const unsigned freed = __ballot_sync(0xFFFFFFFFu, left < 0);
+    if (left < 0) {
+      const int at = place + __popc(freed & ((1u << lane) - 1));
+      if (at < fit) p.free_out[room - fit + at] = i;
+      p.shares_out[i] = 0;
+    }
+    place += __popc(freed);
+  }
+  if (all_tid == 0) p.next_free[0] = room - fit;
+  if (total > room) {
+    for (int i = all_tid; i < p.num_seqs; i += kCluster * kThreads) {
+      int status;
+      if (p.release[i] != 0 && held_pages(p, p.kv_lens[i], &status) > 0 && status_of(p, i) == TOPLOC_SEQ_OK)
+        p.status[i] = TOPLOC_SEQ_NO_ROOM;
+    }
+  }
+}
+
+// ---- compaction ----------------------------------------------------------------------------------
+
+// While it runs, shares_out holds marks: 0 for unused pages, 1 for used ones, 1 + number of the copy for those that move.
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
+    toploc_compact_pages_kernel(const __grid_constant__ PoolParams p) {
+  __shared__ int counts[kAllWarps];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int block = (int)cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int all_tid = block * kThreads + tid, warp_of_all = block * kWarps + warp;
+  int32_t* marks = p.shares_out;
+
+  for (int i = all_tid; i < p.num_pages; i += kCluster * kThreads) {
+    marks[i] = 0;
+    p.copy_from[i] = p.copy_to[i] = -1;
+  }
+  for (int i = all_tid; i < p.num_seqs; i += kCluster * kThreads) {
+    int status;
+    held_pages(p, p.kv_lens[i], &status);
+    p.status[i] = (uint8_t)status;
+  }
+  cluster.sync();
+
+  const auto held = [&](int row) {
+    int status;
+    return held_pages(p, p.kv_lens[row], &status);
+  };
+  for_entries(p, p.table_in, p.table_in_stride, block, held, [&](int row, int, int32_t page, bool valid) {
+    if (!valid) return;
+    if ((unsigned)page < (unsigned)p.num_pages)
+      marks[page] = 1;
+    else
+      p.status[row] = TOPLOC_SEQ_BAD_PAGE;
+  });
+  cluster.sync();
+
+  int begin, end, count = 0, live;
+  pages_of_warp(p, warp_of_all, &begin, &end);
+  for (int i = begin + lane; i < end; i += 32) count += fresh(marks + i) != 0;
+  tell_count(cluster, counts, warp_total(count));
+  cluster.sync();
+
+  // used pages in front of the warp's, of all, and in front of the page that they will end at
+  const int before = counted_before(counts, warp_of_all, &live);
+  int below;
+  {
+    const int groups = (p.num_pages + 31) / 32, each = (groups + kAllWarps - 1) / kAllWarps;
+    const int there = each > 0 ? min(live / (each * 32), kAllWarps - 1) : 0;
+    int from, to, all, more = 0;
+    pages_of_warp(p, there, &from, &to);
+    below = counted_before(counts, there, &all);
+    for (int i = from + lane; i < min(to, live); i += 32) more += fresh(marks + i) != 0;
+    below += warp_total(more);
+  }
+  int passed = before;
+  for (int base = begin; base < end; base += 32) {
+    const int i = base + lane;
+    const bool used = i < end && fresh(marks + i) != 0;
+    const unsigned all = __ballot_sync(0xFFFFFFFFu, used);
+    const int in_front = passed + __popc(all & ((1u << lane) - 1));
+    if (i < end) {
+      if (i < live && !used) p.copy_to[i - in_front] = i;
+      if (i >= live && used) {
+        p.copy_from[in_front - below] = i;
+        marks[i] = 1 + in_front - below;
+      }
+      if (i >= live) p.free_out[p.num_free - p.num_pages + i] = i;
+    }
+    passed += __popc(all);
+  }
+  if (all_tid == 0) {
+    p.num_copies[0] = live - below;
+    p.next_free[0] = p.num_free - (p.num_pages - live);
+  }
+  cluster.sync();
+
+  for_entries(p, p.table_in, p.table_in_stride, block, held, [&](int row, int col, int32_t page, bool valid) {
+    if (!valid) return;
+    if ((unsigned)page < (unsigned)p.num_pages && page >= live) page = fresh(p.copy_to + (fresh(marks + page) - 1));
+    p.table[row * p.table_stride + col] = page;
+  });
+  passed = before;
+  for (int base = begin; base < min(end, live); base += 32) {
+    const int i = base + lane;
+    const bool mine = i < min(end, live), used = mine && fresh(marks + i) != 0;
+    const unsigned all = __ballot_sync(0xFFFFFFFFu, used);
+    const int in_front = passed + __popc(all & ((1u << lane) - 1));
+    if (mine) p.shares_out[i] = p.shares[used ? i : fresh(p.copy_from + (i - in_front))];
+    passed += __popc(all);
+  }
+  cluster.sync();  // (the marks have been read)
+  for (int i = max(begin, live) + lane; i < end; i += 32) p.shares_out[i] = 0;
+}
+
+// ---- copies --------------------------------------------------------------------------------------
+
+constexpr int kMostCaches = 128;  // of a launch
+constexpr int kCopyThreads = 256;
+constexpr int kUnits = 4;         // a thread's, of a chunk
+
+struct CopyParams {
+  void* caches[kMostCaches];
+  const int32_t* from;
+  const int32_t* to;
+  const int32_t* count;
+  long long page, token, head;  // strides in units
+  long long units;              // of a page
+  int most, num_caches, num_pages, chunks;
+  int heads, units_per_head;    // heads 0: a page is one run of units
+};
+
+// Bound by memory: a page is read once and written once.  The number of copies is known on the device alone, so the blocks
+// share out what there is: (copy, cache, chunk of a page), four 16-byte loads in flight a thread.
+template <typename Unit>
+__global__ void __launch_bounds__(kCopyThreads) toploc_copy_pages_kernel(const __grid_constant__ CopyParams p) {
+  const long long copies = min(max(p.count[0], 0), p.most);
+  const long long per_copy = (long long)p.num_caches * p.chunks, tasks = copies * per_copy;
+  for (long long t = blockIdx.x; t < tasks; t += gridDim.x) {
+    const int copy = (int)(t / per_copy), rest = (int)(t - copy * per_copy);
+    const int cache = rest / p.chunks, chunk = rest - cache * p.chunks;
+    const int from = p.from[copy], to = p.to[copy];
+    if ((unsigned)from >= (unsigned)p.num_pages || (unsigned)to >= (unsigned)p.num_pages || from == to) continue;
+    const Unit* src = static_cast<const Unit*>(p.caches[cache]) + from * p.page;
+    Unit* dst = static_cast<Unit*>(p.caches[cache]) + to * p.page;
+    const long long first = (long long)chunk * kCopyThreads * kUnits + threadIdx.x;
+    Unit v[kUnits];
+    long long at[kUnits];
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const long long u = first + i * kCopyThreads;
+      at[i] = u;
+      if (u < p.units) {
+        if (p.heads > 0) {
+          const long long row = u / p.units_per_head;
+          at[i] = row / p.heads * p.token + row % p.heads * p.head + (u - row * p.units_per_head);
+        }
+        v[i] = src[at[i]];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i)
+      if (first + i * kCopyThreads < p.units) dst[at[i]] = v[i];
+  }
+}
+
+template <typename Unit>
+int launch_copy(const CopyParams& p, int blocks, cudaStream_t stream) {
+  toploc_copy_pages_kernel<Unit><<<blocks, kCopyThreads, 0, stream>>>(p);
+  return launched();
+}
+
+// What the three planners ask of their sizes.
+int check_pool(int num_seqs, int num_pages, int num_free, int page_size, int max_pages, int64_t table_stride) {
+  if (num_seqs < 0 || num_pages < 0 || num_free < 0 || page_size <= 0 || max_pages < 0 || table_stride < max_pages)
+    return TOPLOC_ERR_INVALID_ARGUMENT;
+  if (num_seqs > (1 << 24) || num_pages > (1 << 30)) return TOPLOC_ERR_UNSUPPORTED;
+  return TOPLOC_OK;
+}
+
+// An array of a call: where it has to be (if it has any bytes), and its memory.
+struct Argument {
+  Rows memory;
+  int align;
+  Argument(const void* at, long long bytes, int align = 4) : memory(at, bytes), align(align) {}
+  Argument(const void* at, int columns, int rows, int64_t stride)
+      : memory(at, columns * 4ll, rows, min((long long)stride, 1ll << 56) * 4), align(4) {}
+  bool usable() const { return memory.bytes <= 0 || memory.rows <= 0 || (memory.at != nullptr && aligned(memory.at, align)); }
+};
+
+// Whether two tables share memory.  With one step, rows between each other's rows do not.
+bool tables_overlap(const Rows& a, const Rows& b) {
+  if (a.bytes <= 0 || b.bytes <= 0 || a.rows <= 0 || b.rows <= 0) return false;
+  const auto extent = [](const Rows& r) {  // (rows <= 2^24)
+    return Rows(r.at, r.step > (1ll << 36) ? 1ll << 60 : (r.rows - 1) * r.step + r.bytes);
+  };
+  if (!overlap(extent(a), extent(b))) return false;
+  if (a.step != b.step) return true;
+  const uintptr_t from = reinterpret_cast<uintptr_t>(a.at), to = reinterpret_cast<uintptr_t>(b.at);
+  const long long away = (long long)(from < to ? (to - from) % (uintptr_t)a.step
+                                               : (a.step - (long long)((from - to) % (uintptr_t)a.step)) % a.step);
+  return away < a.bytes || a.step - away < b.bytes;
+}
+
+// Every output apart from every input and from the other outputs.
+template <int kIn, int kOut>
+int check_memory(const Argument (&in)[kIn], const Argument (&out)[kOut]) {
+  for (const Argument& a : in)
+    if (!a.usable()) return TOPLOC_ERR_INVALID_ARGUMENT;
+  for (const Argument& a : out)
+    if (!a.usable()) return TOPLOC_ERR_INVALID_ARGUMENT;
+  const auto meet = [](const Argument& a, const Argument& b) {
+    if (a.memory.rows <= 1) return overlap(a.memory, b.memory);
+    if (b.memory.rows <= 1) return overlap(b.memory, a.memory);
+    return tables_overlap(a.memory, b.memory);
+  };
+  for (int i = 0; i < kOut; ++i) {
+    for (int j = 0; j < kIn; ++j)
+      if (meet(out[i], in[j])) return TOPLOC_ERR_INVALID_ARGUMENT;
+    for (int j = 0; j < i; ++j)
+      if (meet(out[i], out[j])) return TOPLOC_ERR_INVALID_ARGUMENT;
+  }
+  return TOPLOC_OK;
+}
+
+template <typename Kernel>
+int launch_planner(Kernel kernel, const PoolParams& p, void* cuda_stream) {
+  kernel<<<kCluster, kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
+  return launched();
+}
+
+}  // namespace
+
+extern "C" int toploc_fork_pages(const int32_t* d_parents, const int32_t* d_kv_lens, int32_t num_seqs,
+                                 const int32_t* d_shares, int32_t num_pages, const int32_t* d_free_pages, int32_t num_free,
+                                 const int32_t* d_first_free, int32_t page_size, int32_t* d_block_table, int32_t max_pages,
+                                 int64_t table_stride, int32_t* d_kv_lens_out, int32_t* d_shares_out, int32_t* d_copy_from,
+                                 int32_t* d_copy_to, int32_t* d_num_copies, int32_t* d_next_free, uint8_t* d_status,
+                                 void* cuda_stream) {
+  if (const int rc = check_pool(num_seqs, num_pages, num_free, page_size, max_pages, table_stride)) return rc;
+  const long long seqs = num_seqs * 4ll, pages = num_pages * 4ll;
+  const Argument in[] = {{d_parents, seqs}, {d_kv_lens, seqs}, {d_shares, pages}, {d_free_pages, num_free * 4ll},
+                         {d_first_free, 4}};
+  const Argument out[] = {{d_block_table, max_pages, num_seqs, table_stride}, {d_kv_lens_out, seqs}, {d_shares_out, pages},
+                          {d_copy_from, seqs}, {d_copy_to, seqs}, {d_num_copies, 4}, {d_next_free, 4},
+                          {d_status, num_seqs, 1}};
+  if (const int rc = check_memory(in, out)) return rc;
+  if (const int rc = check_device()) return rc;
+  PoolParams p = {};
+  p.parents = d_parents, p.kv_lens = d_kv_lens, p.shares = d_shares, p.free_in = d_free_pages, p.first_free = d_first_free;
+  p.table = d_block_table, p.table_stride = table_stride;
+  p.kv_lens_out = d_kv_lens_out, p.shares_out = d_shares_out, p.copy_from = d_copy_from, p.copy_to = d_copy_to;
+  p.num_copies = d_num_copies, p.next_free = d_next_free, p.status = d_status;
+  p.num_seqs = num_seqs, p.num_pages = num_pages, p.num_free = num_free, p.page_size = page_size, p.max_pages = max_pages;
+  return launch_planner(toploc_fork_pages_kernel, p, cuda_stream);
+}
+
+extern "C" int toploc_release_pages(const uint8_t* d_release, const int32_t* d_kv_lens, int32_t num_seqs,
+                                    const int32_t* d_block_table, int32_t max_pages, int64_t table_stride,
+                                    const int32_t* d_shares, int32_t num_pages, int32_t page_size, int32_t* d_free_pages,
+                                    int32_t num_free, const int32_t* d_first_free, int32_t* d_kv_lens_out,
+                                    int32_t* d_shares_out, int32_t* d_next_free, uint8_t* d_status, void* cuda_stream) {
+  if (const int rc = check_pool(num_seqs, num_pages, num_free, page_size, max_pages, table_stride)) return rc;
+  const long long seqs = num_seqs * 4ll, pages = num_pages * 4ll;
+  const Argument in[] = {{d_release, num_seqs, 1}, {d_kv_lens, seqs}, {d_block_table, max_pages, num_seqs, table_stride},
+                         {d_shares, pages}, {d_first_free, 4}};
+  const Argument out[] = {{d_free_pages, num_free * 4ll}, {d_kv_lens_out, seqs}, {d_shares_out, pages}, {d_next_free, 4},
+                          {d_status, num_seqs, 1}};
+  if (const int rc = check_memory(in, out)) return rc;
+  if (const int rc = check_device()) return rc;
+  PoolParams p = {};
+  p.release = d_release, p.kv_lens = d_kv_lens, p.shares = d_shares, p.first_free = d_first_free;
+  p.table = const_cast<int32_t*>(d_block_table), p.table_stride = table_stride;
+  p.free_out = d_free_pages, p.kv_lens_out = d_kv_lens_out, p.shares_out = d_shares_out, p.next_free = d_next_free;
+  p.status = d_status;
+  p.num_seqs = num_seqs, p.num_pages = num_pages, p.num_free = num_free, p.page_size = page_size, p.max_pages = max_pages;
+  return launch_planner(toploc_release_pages_kernel, p, cuda_stream);
+}
+
+extern "C" int toploc_compact_pages(const int32_t* d_kv_lens, int32_t num_seqs, const int32_t* d_block_table,
+                                    int32_t max_pages, int64_t table_stride, const int32_t* d_shares, int32_t num_pages,
+                                    int32_t page_size, int32_t* d_block_table_out, int64_t table_out_stride,
+                                    int32_t* d_shares_out, int32_t* d_free_pages_out, int32_t num_free,
+                                    int32_t* d_copy_from, int32_t* d_copy_to, int32_t* d_num_copies, int32_t* d_next_free,
+                                    uint8_t* d_status, void* cuda_stream) {
+  if (const int rc = check_pool(num_seqs, num_pages, num_free, page_size, max_pages, table_stride)) return rc;
+  if (table_out_stride < max_pages || num_free < num_pages) return TOPLOC_ERR_INVALID_ARGUMENT;
+  const long long seqs = num_seqs * 4ll, pages = num_pages * 4ll;
+  const bool in_place = d_block_table_out == d_block_table && (table_out_stride == table_stride || num_seqs <= 1);
+  const Argument table(d_block_table, max_pages, num_seqs, table_stride);
+  const Argument in[] = {{d_kv_lens, seqs}, in_place ? Argument(nullptr, 0) : table, {d_shares, pages}};
+  const Argument out[] = {{d_block_table_out, max_pages, num_seqs, table_out_stride}, {d_shares_out, pages},
+                          {d_free_pages_out, num_free * 4ll}, {d_copy_from, pages}, {d_copy_to, pages}, {d_num_copies, 4},
+                          {d_next_free, 4}, {d_status, num_seqs, 1}};
+  if (const int rc = check_memory(in, out)) return rc;
+  if (const int rc = check_device()) return rc;
+  PoolParams p = {};
+  p.kv_lens = d_kv_lens, p.shares = d_shares, p.table_in = d_block_table, p.table_in_stride = table_stride;
+  p.table = d_block_table_out, p.table_stride = table_out_stride, p.shares_out = d_shares_out, p.free_out = d_free_pages_out;
+  p.copy_from = d_copy_from, p.copy_to = d_copy_to, p.num_copies = d_num_copies, p.next_free = d_next_free;
+  p.status = d_status;
+  p.num_seqs = num_seqs, p.num_pages = num_pages, p.num_free = num_free, p.page_size = page_size, p.max_pages = max_pages;
+  return launch_planner(toploc_compact_pages_kernel, p, cuda_stream);
+}
+
+extern "C" int toploc_copy_pages(void* const* h_caches, const toploc_pool_layout* lay, const int32_t* d_copy_from,
+                                 const int32_t* d_copy_to, const int32_t* d_num_copies, int32_t max_copies,
+                                 void* cuda_stream) {
+  if (!lay || lay->num_pages < 0 || lay->page_size <= 0 || lay->kv_heads <= 0 || lay->head_dim <= 0 || lay->num_caches < 0 ||
+      lay->page_stride < 0 || lay->token_stride < 0 || lay->head_stride < 0 || max_copies < 0)
+    return TOPLOC_ERR_INVALID_ARGUMENT;
+  const int size = element_bytes(lay->dtype);
+  const int64_t row = lay->head_dim;
+  if (size == 0 || row * lay->kv_heads > 0x7FFFFFFF || row * lay->kv_heads * lay->page_size > 0x7FFFFFFF)
+    return TOPLOC_ERR_UNSUPPORTED;
+  if (lay->num_caches == 0 || max_copies == 0 || lay->num_pages == 0) return TOPLOC_OK;
+  if (!h_caches || !d_copy_from || !d_copy_to || !d_num_copies || !aligned(d_copy_from, 4) || !aligned(d_copy_to, 4) ||
+      !aligned(d_num_copies, 4))
+    return TOPLOC_ERR_INVALID_ARGUMENT;
+  const int64_t heads = lay->kv_heads, tokens = lay->page_size;
+  // a page whose tokens and heads lie side by side, in either order, is one run
+  const bool run = (lay->head_stride == row || heads == 1) && (lay->token_stride == heads * row || tokens == 1);
+  const bool run_by_head = (lay->token_stride == row || tokens == 1) && (lay->head_stride == tokens * row || heads == 1);
+  const bool dense = run || run_by_head;
+  int unit = 16;
+  while (unit > size) {  // the widest that everything is a multiple of
+    bool fits = (dense ? tokens * heads * row : row) * size % unit == 0 && lay->page_stride * size % unit == 0 &&
+                (dense || (lay->token_stride * size % unit == 0 && lay->head_stride * size % unit == 0));
+    for (int i = 0; i < lay->num_caches && fits; ++i) fits = aligned(h_caches[i], unit);
+    if (fits) break;
+    unit = unit == 16 && size <= 4 ? 4 : size;
+  }
+  for (int i = 0; i < lay->num_caches; ++i)
+    if (!h_caches[i] || !aligned(h_caches[i], size)) return TOPLOC_ERR_INVALID_ARGUMENT;
+  int sms = 0;
+  if (const int rc = check_device(&sms)) return rc;
+  const int per = unit / size;
+  CopyParams p;
+  p.from = d_copy_from, p.to = d_copy_to, p.count = d_num_copies, p.most = max_copies, p.num_pages = lay->num_pages;
+  p.page = lay->page_stride / per, p.token = lay->token_stride / per, p.head = lay->head_stride / per;
+  p.units = tokens * heads * row / per;
+  p.heads = dense ? 0 : (int)heads;
+  p.units_per_head = (int)(row / per);
+  p.chunks = (int)((p.units + kCopyThreads * kUnits - 1) / (kCopyThreads * kUnits));
+  for (int first = 0; first < lay->num_caches; first += kMostCaches) {
+    p.num_caches = min(lay->num_caches - first, kMostCaches);
+    for (int i = 0; i < p.num_caches; ++i) p.caches[i] = h_caches[first + i];
+    // what the list has room for, at most eight blocks an SM
+    const long long most = (long long)max_copies * p.num_caches * p.chunks;
+    const int blocks = (int)min(most, 8ll * sms);
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const int rc = unit == 16  ? launch_copy<uint4>(p, blocks, stream)
+                   : unit == 4 ? launch_copy<uint32_t>(p, blocks, stream)
+                               : launch_copy<uint16_t>(p, blocks, stream);
+    if (rc) return rc;
+  }
+  return TOPLOC_OK;
+}

@@ -15,10 +15,14 @@ from .binding import TOPLOC_DTYPE_BF16, TOPLOC_DTYPE_FP32, ToplocError, _bytes_o
 
 __all__ = [
     "TOPLOC_SEQ_OK", "TOPLOC_SEQ_BAD_LENGTH", "TOPLOC_SEQ_NO_PAGES", "TOPLOC_SEQ_TABLE_FULL", "TOPLOC_SEQ_BATCH_FULL",
-    "TOPLOC_SEQ_BAD_PAGE", "TOPLOC_SEQ_WAIT_EXPIRED", "TOPLOC_NORM_OUT_SAME", "TOPLOC_NORM_OUT_E4M3",
-    "ToplocKvLayout", "ToplocAttentionLayout", "ToplocNormLayout", "toploc_sequence_status_string",
+    "TOPLOC_SEQ_BAD_PAGE", "TOPLOC_SEQ_WAIT_EXPIRED", "TOPLOC_SEQ_BAD_PARENT", "TOPLOC_SEQ_IN_USE", "TOPLOC_SEQ_NO_ROOM",
+    "TOPLOC_NORM_OUT_SAME", "TOPLOC_NORM_OUT_E4M3", "TOPLOC_ROTARY_HALVES", "TOPLOC_ROTARY_NEIGHBOURS",
+    "TOPLOC_MAX_ALTERNATIVES", "ToplocKvLayout", "ToplocAttentionLayout", "ToplocNormLayout", "ToplocPoolLayout",
+    "ToplocRotaryLayout", "ToplocLogprobLayout", "toploc_sequence_status_string",
     "toploc_plan_pages", "toploc_cache_write", "toploc_attention_workspace_bytes",
     "toploc_attention_paged", "toploc_attention_prompt", "toploc_rmsnorm_residual",
+    "toploc_fork_pages", "toploc_release_pages", "toploc_compact_pages", "toploc_copy_pages",
+    "toploc_norm_rotary_prompt", "toploc_norm_rotary_paged", "toploc_token_logprobs",
 ]
 
 TOPLOC_SEQ_OK = 0
@@ -28,8 +32,14 @@ TOPLOC_SEQ_TABLE_FULL = 3
 TOPLOC_SEQ_BATCH_FULL = 4
 TOPLOC_SEQ_BAD_PAGE = 5
 TOPLOC_SEQ_WAIT_EXPIRED = 6
+TOPLOC_SEQ_BAD_PARENT = 7
+TOPLOC_SEQ_IN_USE = 8
+TOPLOC_SEQ_NO_ROOM = 9
 TOPLOC_NORM_OUT_SAME = 0
 TOPLOC_NORM_OUT_E4M3 = 1
+TOPLOC_ROTARY_HALVES = 0
+TOPLOC_ROTARY_NEIGHBOURS = 1
+TOPLOC_MAX_ALTERNATIVES = 32
 
 _DTYPES = {torch.bfloat16: TOPLOC_DTYPE_BF16, torch.float32: TOPLOC_DTYPE_FP32}
 _i32, _i64, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
@@ -53,9 +63,28 @@ class ToplocNormLayout(ctypes.Structure):
                 ("x_stride", _i64), ("residual_stride", _i64), ("residual_out_stride", _i64), ("y_stride", _i64)]
 
 
-# The three structures as the wrappers pass them: their bytes (packing is several times as fast as ctypes fields, and a
+class ToplocPoolLayout(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("num_pages", _i32), ("page_size", _i32), ("kv_heads", _i32), ("head_dim", _i32),
+                ("num_caches", _i32), ("page_stride", _i64), ("token_stride", _i64), ("head_stride", _i64)]
+
+
+class ToplocRotaryLayout(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("head_dim", _i32), ("q_heads", _i32), ("kv_heads", _i32), ("rotary_dim", _i32),
+                ("pairing", _i32), ("num_tokens", _i64), ("eps", ctypes.c_float), ("reserved", _i32),
+                ("q_token_stride", _i64), ("q_head_stride", _i64), ("k_token_stride", _i64), ("k_head_stride", _i64),
+                ("v_token_stride", _i64), ("v_head_stride", _i64), ("q_out_token_stride", _i64),
+                ("q_out_head_stride", _i64), ("k_out_token_stride", _i64), ("k_out_head_stride", _i64)]
+
+
+class ToplocLogprobLayout(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("vocab", _i32), ("top", _i32), ("reserved", _i32), ("rows", _i64),
+                ("row_stride", _i64)]
+
+
+# The structures as the wrappers pass them: their bytes (packing is several times as fast as ctypes fields, and a
 # decode step's call is short)
 _KV, _ATTENTION, _NORM = struct.Struct("=4i7q"), struct.Struct("=6iqfi4q"), struct.Struct("=4i5q")
+_POOL, _ROTARY, _LOGPROB = struct.Struct("=6i3q"), struct.Struct("=6iqfi10q"), struct.Struct("=4i2q")
 
 _LIB = None
 
@@ -85,6 +114,23 @@ def _library():
         lib.toploc_rmsnorm_residual.restype = ctypes.c_int
         lib.toploc_rmsnorm_residual.argtypes = [_vp, _vp, _vp, ctypes.c_float, norm_p, _vp,
                                                 _vp, _vp, _vp]
+        lib.toploc_fork_pages.restype = ctypes.c_int
+        lib.toploc_fork_pages.argtypes = [_vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _i32, _i64, _vp, _vp,
+                                          _vp, _vp, _vp, _vp, _vp, _vp]
+        lib.toploc_release_pages.restype = ctypes.c_int
+        lib.toploc_release_pages.argtypes = [_vp, _vp, _i32, _vp, _i32, _i64, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _vp,
+                                             _vp, _vp, _vp]
+        lib.toploc_compact_pages.restype = ctypes.c_int
+        lib.toploc_compact_pages.argtypes = [_vp, _i32, _vp, _i32, _i64, _vp, _i32, _i32, _vp, _i64, _vp, _vp, _i32,
+                                             _vp, _vp, _vp, _vp, _vp, _vp]
+        lib.toploc_copy_pages.restype = ctypes.c_int
+        lib.toploc_copy_pages.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _vp]
+        lib.toploc_norm_rotary_prompt.restype = ctypes.c_int
+        lib.toploc_norm_rotary_prompt.argtypes = [_vp] * 10
+        lib.toploc_norm_rotary_paged.restype = ctypes.c_int
+        lib.toploc_norm_rotary_paged.argtypes = [_vp] * 14
+        lib.toploc_token_logprobs.restype = ctypes.c_int
+        lib.toploc_token_logprobs.argtypes = [_vp] * 8
         _LIB = lib
     return _LIB
 
@@ -313,3 +359,204 @@ def toploc_rmsnorm_residual(x, residual, weight, eps, residual_out=None, y=None,
     _call(_library().toploc_rmsnorm_residual, "toploc_rmsnorm_residual", dev, stream, _ptr(x), _ptr(residual),
           _ptr(weight), eps, lay, _ptr(residual_out), _ptr(y), _ptr(scales) if quant else None)
     return y, residual_out, scales if quant else None
+
+
+_PAIRINGS = {"halves": TOPLOC_ROTARY_HALVES, "neighbours": TOPLOC_ROTARY_NEIGHBOURS}
+
+
+def _rotary_layout(q, k, v, positions, inv_freq, q_weight, k_weight, eps, pairing, q_out, k_out):
+    for t, what in ((q, "q"), (k, "k")):
+        _need(t.dim() == 3 and t.stride(2) == 1 and t.dtype is q.dtype,
+              "%s must be [tokens, heads, head_dim] of one type, the last dimension contiguous" % what)
+    _need(q.dtype in _DTYPES, "queries and keys must be bfloat16 or float32")
+    tokens, heads, dim = q.shape
+    _need(k.shape[0] == tokens and k.shape[2] == dim, "k must have q's tokens and head_dim")
+    _need(v is None or (v.shape == k.shape and v.dtype is q.dtype and v.stride(2) == 1),
+          "v must have k's shape and type, the last dimension contiguous")
+    _need(q_out.shape == q.shape and q_out.dtype is q.dtype and q_out.stride(2) == 1, "q_out must have q's shape and type")
+    _need(k_out is None or (k_out.shape == k.shape and k_out.dtype is q.dtype and k_out.stride(2) == 1),
+          "k_out must have k's shape and type")
+    _vector(positions, torch.int32, tokens, "positions")
+    _need(inv_freq.dtype is torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and
+          2 * inv_freq.shape[0] <= dim, "inv_freq must be a contiguous float32 vector of at most head_dim / 2 entries")
+    for weight in (q_weight, k_weight):
+        _need(weight is None or (weight.dtype is q.dtype and weight.shape == (dim,) and weight.is_contiguous()),
+              "a norm's weight must be [head_dim] of q's type")
+    _need(pairing in _PAIRINGS, "pairing must be 'halves' or 'neighbours'")
+    (qt, qh, _), (kt, kh, _), (ot, oh, _) = q.stride(), k.stride(), q_out.stride()
+    vt, vh, _ = (0, 0, 0) if v is None else v.stride()
+    pt, ph, _ = (0, 0, 0) if k_out is None else k_out.stride()
+    return _pack(_ROTARY, _DTYPES[q.dtype], dim, heads, k.shape[1], 2 * inv_freq.shape[0], _PAIRINGS[pairing], tokens,
+                 eps, 0, qt, qh, kt, kh, vt, vh, ot, oh, pt, ph)
+
+
+def toploc_norm_rotary_prompt(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6, pairing="halves",
+                              q_out=None, k_out=None, stream=None):
+    """RMS norm of every head of q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim] (a weight that is None:
+    no norm of that one) and the rotation by position: positions int32 [tokens], inv_freq float32 [pairs]; the first
+    2 * pairs channels of a head turn, channel c with c + pairs ("halves") or 2c with 2c + 1 ("neighbours").  q_out may be
+    q, k_out may be k.  Returns (q_out, k_out)."""
+    if q_out is None:
+        q_out = _empty(q.shape, q.dtype, q.device, stream)
+    if k_out is None:
+        k_out = _empty(k.shape, k.dtype, k.device, stream)
+    dev = _device("toploc_norm_rotary_prompt", q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out)
+    lay = _rotary_layout(q, k, None, positions, inv_freq, q_weight, k_weight, eps, pairing, q_out, k_out)
+    _call(_library().toploc_norm_rotary_prompt, "toploc_norm_rotary_prompt", dev, stream, _ptr(q), _ptr(k),
+          _ptr(positions), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), lay, _ptr(q_out), _ptr(k_out))
+    return q_out, k_out
+
+
+def toploc_norm_rotary_paged(q, k, v, positions, slots, inv_freq, k_cache, v_cache, q_weight=None, k_weight=None,
+                             eps=1e-6, pairing="halves", q_out=None, stream=None):
+    """toploc_norm_rotary_prompt with the keys' result and the values v [tokens, kv_heads, head_dim] written straight to
+    their slots (int64 [tokens], negative: skipped) of the caches [num_pages, page_size, kv_heads, head_dim].  Returns
+    q_out."""
+    if q_out is None:
+        q_out = _empty(q.shape, q.dtype, q.device, stream)
+    dev = _device("toploc_norm_rotary_paged", q, k, v, positions, slots, inv_freq, k_cache, v_cache, q_weight, k_weight,
+                  q_out)
+    lay = _rotary_layout(q, k, v, positions, inv_freq, q_weight, k_weight, eps, pairing, q_out, None)
+    kv = _cache_layout(k_cache, v_cache)
+    _need(k_cache.dtype is q.dtype and k_cache.shape[2:] == k.shape[1:], "the caches must have k's type, heads and head_dim")
+    _vector(slots, torch.int64, q.shape[0], "slots")
+    _call(_library().toploc_norm_rotary_paged, "toploc_norm_rotary_paged", dev, stream, _ptr(q), _ptr(k), _ptr(v),
+          _ptr(positions), _ptr(slots), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), lay, _ptr(q_out), _ptr(k_cache),
+          _ptr(v_cache), kv)
+    return q_out
+
+
+def toploc_token_logprobs(logits, tokens=None, top=0, want_entropy=False, logprobs=None, entropy=None, top_ids=None,
+                          top_logprobs=None, stream=None):
+    """Of every row of logits [rows, vocab] (bfloat16 or float32): the log probability of its token (int64 [rows]; None:
+    none), the entropy (where wanted, or a tensor is given), and the `top` likeliest tokens with their log probabilities,
+    in order (equal logits by index).  Returns (logprobs [rows] or None, entropy [rows] or None, top_ids int64 [rows, top]
+    or None, top_logprobs [rows, top] or None)."""
+    _need(logits.dtype in _DTYPES and logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1),
+          "logits must be bfloat16 or float32 [rows, vocab]")
+    _need(top >= 0, "top must not be negative")
+    (rows, vocab), dev, fp32 = logits.shape, logits.device, torch.float32
+    if tokens is None:
+        _need(logprobs is None, "logprobs need tokens")
+    elif logprobs is None:
+        logprobs = _empty((rows,), fp32, dev, stream)
+    if entropy is None and want_entropy:
+        entropy = _empty((rows,), fp32, dev, stream)
+    if top == 0:
+        _need(top_ids is None and top_logprobs is None, "alternatives with top 0")
+    else:
+        if top_ids is None:
+            top_ids = _empty((rows, top), torch.int64, dev, stream)
+        if top_logprobs is None:
+            top_logprobs = _empty((rows, top), fp32, dev, stream)
+        _need(top_ids.dtype is torch.int64 and top_logprobs.dtype is fp32 and
+              top_ids.shape == top_logprobs.shape == (rows, top) and top_ids.is_contiguous() and
+              top_logprobs.is_contiguous(), "top_ids and top_logprobs must be contiguous int64 and float32 [rows, top]")
+    dev = _device("toploc_token_logprobs", logits, tokens, logprobs, entropy, top_ids, top_logprobs)
+    if tokens is not None:
+        _vector(tokens, torch.int64, rows, "tokens")
+        _vector(logprobs, fp32, rows, "logprobs")
+    if entropy is not None:
+        _vector(entropy, fp32, rows, "entropy")
+    lay = _pack(_LOGPROB, _DTYPES[logits.dtype], vocab, top, 0, rows, logits.stride(0) if rows > 1 else vocab)
+    _call(_library().toploc_token_logprobs, "toploc_token_logprobs", dev, stream, _ptr(logits), lay, _ptr(tokens),
+          _ptr(logprobs), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs))
+    return logprobs, entropy, top_ids, top_logprobs
+
+
+def _int32s(name, **vectors):
+    """Contiguous int32 vectors of the lengths given beside them."""
+    for what, (t, length) in vectors.items():
+        if t.dtype is not torch.int32 or not t.is_contiguous() or t.dim() != 1 or t.shape[0] != length:
+            raise ToplocError("%s: %s must be a contiguous int32 tensor of %d entries" % (name, what, length))
+
+
+def _table(t, n, what):
+    """(columns, elements between rows) of a block table [n, max_pages]."""
+    _need(t.dtype is torch.int32 and t.dim() == 2 and t.shape[0] == n and
+          (t.stride(1) == 1 or t.shape[1] <= 1 or n == 0), "%s must be int32 [n, max_pages]" % what)
+    return t.shape[1], t.stride(0) if n > 1 else t.shape[1]
+
+
+def toploc_fork_pages(parents, kv_lens, shares, free_pages, first_free, block_table, page_size, kv_lens_out, shares_out,
+                      copy_from, copy_to, num_copies, next_free, status, stream=None):
+    """Sequences with parents[i] >= 0 begin as copies of their parents (see the header): whole pages are shared, a page
+    that is not full is copied, by toploc_copy_pages from the list that this leaves.  int32 CUDA tensors parents, kv_lens,
+    kv_lens_out, copy_from, copy_to [n], shares, shares_out [num_pages], free_pages [any], first_free, num_copies,
+    next_free [1], block_table [n, max_pages]; status uint8 [n].  The last seven are written, and the children's rows of
+    the block table."""
+    name, n = "toploc_fork_pages", parents.numel()
+    dev = _device(name, parents, kv_lens, shares, free_pages, first_free, block_table, kv_lens_out, shares_out, copy_from,
+                  copy_to, num_copies, next_free, status)
+    pages, free = shares.numel(), free_pages.numel()
+    _int32s(name, parents=(parents, n), kv_lens=(kv_lens, n), shares=(shares, pages), free_pages=(free_pages, free),
+            first_free=(first_free, 1), kv_lens_out=(kv_lens_out, n), shares_out=(shares_out, pages),
+            copy_from=(copy_from, n), copy_to=(copy_to, n), num_copies=(num_copies, 1), next_free=(next_free, 1))
+    _vector(status, torch.uint8, n, "status")
+    width, stride = _table(block_table, n, "block_table")
+    _call(_library().toploc_fork_pages, name, dev, stream, _ptr(parents), _ptr(kv_lens), n, _ptr(shares), pages,
+          _ptr(free_pages), free, _ptr(first_free), page_size, _ptr(block_table), width, stride, _ptr(kv_lens_out),
+          _ptr(shares_out), _ptr(copy_from), _ptr(copy_to), _ptr(num_copies), _ptr(next_free), _ptr(status))
+
+
+def toploc_release_pages(release, kv_lens, block_table, shares, page_size, free_pages, first_free, kv_lens_out,
+                         shares_out, next_free, status, stream=None):
+    """Sequences with release[i] != 0 (uint8 [n]) let go of their pages; those that nobody holds any longer go back to the
+    free list, in front of its head (see the header).  int32 CUDA tensors kv_lens, kv_lens_out [n], shares, shares_out
+    [num_pages], free_pages [any], first_free, next_free [1], block_table [n, max_pages]; status uint8 [n].  The last four
+    are written, and the entries of free_pages in front of first_free."""
+    name, n = "toploc_release_pages", kv_lens.numel()
+    dev = _device(name, release, kv_lens, block_table, shares, free_pages, first_free, kv_lens_out, shares_out, next_free,
+                  status)
+    pages, free = shares.numel(), free_pages.numel()
+    _vector(release, torch.uint8, n, "release")
+    _int32s(name, kv_lens=(kv_lens, n), shares=(shares, pages), free_pages=(free_pages, free), first_free=(first_free, 1),
+            kv_lens_out=(kv_lens_out, n), shares_out=(shares_out, pages), next_free=(next_free, 1))
+    _vector(status, torch.uint8, n, "status")
+    width, stride = _table(block_table, n, "block_table")
+    _call(_library().toploc_release_pages, name, dev, stream, _ptr(release), _ptr(kv_lens), n, _ptr(block_table), width,
+          stride, _ptr(shares), pages, page_size, _ptr(free_pages), free, _ptr(first_free), _ptr(kv_lens_out),
+          _ptr(shares_out), _ptr(next_free), _ptr(status))
+
+
+def toploc_compact_pages(kv_lens, block_table, shares, page_size, block_table_out, shares_out, free_pages_out, copy_from,
+                         copy_to, num_copies, next_free, status, stream=None):
+    """The pool's pages in use become its first ones (see the header); toploc_copy_pages moves their contents by the list
+    that this leaves.  int32 CUDA tensors kv_lens [n], block_table, block_table_out [n, max_pages] (may be one tensor),
+    shares, shares_out, copy_from, copy_to [num_pages], free_pages_out [num_pages or more], num_copies, next_free [1];
+    status uint8 [n].  The last eight are written."""
+    name, n = "toploc_compact_pages", kv_lens.numel()
+    dev = _device(name, kv_lens, block_table, shares, block_table_out, shares_out, free_pages_out, copy_from, copy_to,
+                  num_copies, next_free, status)
+    pages, free = shares.numel(), free_pages_out.numel()
+    _int32s(name, kv_lens=(kv_lens, n), shares=(shares, pages), shares_out=(shares_out, pages),
+            free_pages_out=(free_pages_out, free), copy_from=(copy_from, pages), copy_to=(copy_to, pages),
+            num_copies=(num_copies, 1), next_free=(next_free, 1))
+    _vector(status, torch.uint8, n, "status")
+    width, stride = _table(block_table, n, "block_table")
+    out_width, out_stride = _table(block_table_out, n, "block_table_out")
+    _need(width == out_width, "block_table_out must have block_table's shape")
+    _call(_library().toploc_compact_pages, name, dev, stream, _ptr(kv_lens), n, _ptr(block_table), width, stride,
+          _ptr(shares), pages, page_size, _ptr(block_table_out), out_stride, _ptr(shares_out), _ptr(free_pages_out), free,
+          _ptr(copy_from), _ptr(copy_to), _ptr(num_copies), _ptr(next_free), _ptr(status))
+
+
+def toploc_copy_pages(caches, copy_from, copy_to, num_copies, stream=None):
+    """Copies page copy_from[c] to page copy_to[c], c < num_copies[0], inside every one of the caches, a list of CUDA
+    tensors [num_pages, page_size, kv_heads, head_dim] of one type and layout (keys and values of all layers); copy_from,
+    copy_to int32 [any], num_copies int32 [1]."""
+    name = "toploc_copy_pages"
+    if not caches:
+        return
+    dev, one, strides = _device(name, copy_from, copy_to, num_copies, *caches), caches[0], caches[0].stride()
+    _need(one.dim() == 4 and one.dtype in _DTYPES and strides[3] == 1,
+          "caches must be bfloat16 or float32 [pages, page_size, kv_heads, head_dim], the last dimension contiguous")
+    for c in caches:
+        _need(c.shape == one.shape and c.dtype is one.dtype and c.stride() == strides, "caches must have one type and layout")
+    most = copy_from.numel()
+    _int32s(name, copy_from=(copy_from, most), copy_to=(copy_to, most), num_copies=(num_copies, 1))
+    pages, tokens, heads, dim = one.shape
+    lay = _pack(_POOL, _DTYPES[one.dtype], pages, tokens, heads, dim, len(caches), strides[0], strides[1], strides[2])
+    pointers = (ctypes.c_void_p * len(caches))(*[c.data_ptr() for c in caches])
+    _call(_library().toploc_copy_pages, name, dev, stream, pointers, lay, _ptr(copy_from), _ptr(copy_to),
+          _ptr(num_copies), most)
