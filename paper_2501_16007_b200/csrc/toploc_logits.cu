@@ -5,12 +5,18 @@
 // c is renewed only when a value passes it by 2^8, so a few times a thread and not with every new maximum (it costs precision
 // too: y_j is off by half a step, 2^-22 just below 2^3).
 //
-// Alternatives: while it streams, a block leaves the largest of every 8 logits in shared memory (2 bytes of 16).  The
-// threads' own maxima give a bound that at least `top` logits reach; behind the pass only the groups that reach it are read
+// Bound by memory (one pass), with the powers, 16 a cycle and SM, not far behind: 4097 x 128000 bf16 takes 160 us without
+// alternatives (6.6 TB/s; the powers alone 130) and 172 with five.  What counts is many warps with many independent operations each: 40 warps an
+// SM (48 registers) and four vectors a thread at a time.  Copies ahead through shared memory or registers, which cost warps,
+// took 180 to 220 us.
+//
+// Alternatives: while it streams, a block leaves the largest of every two vectors (16 or 8 logits) in shared memory.  The
+// threads' own maxima give a bound that at least `top` logits reach; behind the row only the vectors that reach it are read
 // again, a few dozen, and their logits ranked by (value, index).
 #include "model_common.cuh"
 
 #include <cooperative_groups.h>
+#include <cfloat>
 
 namespace {
 
@@ -19,11 +25,15 @@ namespace cg = cooperative_groups;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kGroup = 8;             // logits whose largest is kept
+// Of an SM: with fp32 there is half as much to compute a byte, and 64 registers a thread do more for it than a fifth block
+// (1000 x 50257: 35.6 us against 37.9; bf16, 4097 x 128000: 188 against 172).
+template <typename T>
+constexpr int kBlocksPerSm = sizeof(T) == 2 ? 5 : 4;
 constexpr int kMostVocab = 1 << 20;
 constexpr int kMostTop = TOPLOC_MAX_ALTERNATIVES;
 constexpr int kMostCluster = 8;       // blocks that share a row
-constexpr int kMostGroups = 512;      // groups, and logits in them, that reach the bound; more take the ordered way
+constexpr int kMaximaBytes = 32768;   // of shared memory that the maxima of a block take, as a rule (five blocks fit an SM)
+constexpr int kMostPairs = 256;       // pairs of vectors, and logits in them, that reach the bound; more take the ordered way
 constexpr int kMostKeys = 256;
 static_assert(kMostKeys >= kThreads && kMostCluster * kMostTop <= kThreads, "a thread for each of a row's candidates");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -44,19 +54,25 @@ struct LogitParams {
   int vocab, top;
 };
 
-// What the blocks of a row tell each other.
+// Some of a row: its largest logit, and the sums against it.
 struct Part {
-  float top, s, w;  // largest logit; sums against it (top * log2 e; kFar: top)
+  float top, s, w;
+};
+
+// A whole row: what log probabilities are made of.
+struct Whole {
+  float top, s, w, log2_s;
 };
 
 struct Shared {
-  Part part;
-  float warp_top[kWarps], warp_s[kWarps], warp_w[kWarps];
+  Part of_warp[kWarps];
   unsigned warp_best[kWarps * 4];        // each warp's four largest thread maxima
+  Part part;
+  Whole whole;
   float bound;
-  int num_groups, num_keys;
+  int num_pairs, num_keys;
   unsigned long long best[kMostTop];     // the block's alternatives
-  unsigned groups[kMostGroups];
+  unsigned pairs[kMostPairs];
   unsigned long long keys[kMostKeys];
 };
 
@@ -118,59 +134,51 @@ __device__ __forceinline__ unsigned long long key_of(float v, int index) {
   return (unsigned long long)ordered(v) << 32 | (0xFFFFFFFFu - (unsigned)index);
 }
 
-// Eight logits in registers.
+// 16 bytes of logits.
 template <typename T>
-struct Eight;
+struct Vector;
 template <>
-struct Eight<__nv_bfloat16> {
-  using Kept = __nv_bfloat16;  // a group's maximum in shared memory
-  uint4 q;
-  __device__ void load(const __nv_bfloat16* p) { q = __ldcs(reinterpret_cast<const uint4*>(p)); }
-  __device__ float largest() const {  // passes over NaN
-    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&q);
-    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-    return __bfloat162float(__hmax(__low2bfloat16(m), __high2bfloat16(m)));
+struct Vector<__nv_bfloat16> {
+  static constexpr int kSize = 8;
+  using Kept = uint16_t;  // a maximum in shared memory
+  static constexpr uint32_t kNothing = 0xFF80FF80u;  // -inf twice
+  static __device__ uint32_t larger(uint32_t a, uint32_t b) {  // of two at once; passes over NaN
+    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
   }
-  __device__ void values(float* v) const {
+  static __device__ float largest(const uint4& a, const uint4& b) {
+    const uint32_t m = larger(larger(larger(a.x, a.y), larger(a.z, a.w)), larger(larger(b.x, b.y), larger(b.z, b.w)));
+    return fmaxf(bf16_low(m), bf16_high(m));
+  }
+  static __device__ void floored(const uint4& q, Pair* v) {  // no smaller than kTiny; NaN stays
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = bf16_low(w[i]), v[2 * i + 1] = bf16_high(w[i]);
-  }
-  __device__ void floored(float* v) const {  // no smaller than kTiny; NaN stays
-    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&q);
     const __nv_bfloat162 tiny = __float2bfloat162_rn(kTiny);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 f = __hmax2_nan(h[i], tiny);
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(&f);
-      v[2 * i] = bf16_low(w), v[2 * i + 1] = bf16_high(w);
+      const __nv_bfloat162 f = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), tiny);
+      const uint32_t u = *reinterpret_cast<const uint32_t*>(&f);
+      v[i] = pair_of(bf16_low(u), bf16_high(u));
     }
   }
+  static __device__ Kept kept(float m) { return (Kept)(__float_as_uint(m) >> 16); }  // (exact: it was one)
+  static __device__ float value(Kept m) { return __uint_as_float((uint32_t)m << 16); }
 };
 template <>
-struct Eight<float> {
+struct Vector<float> {
+  static constexpr int kSize = 4;
   using Kept = float;
-  float4 q[2];
-  __device__ void load(const float* p) {
-    q[0] = __ldcs(reinterpret_cast<const float4*>(p));
-    q[1] = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+  static constexpr uint32_t kNothing = 0xFF800000u;
+  static __device__ float of(uint32_t w) { return __uint_as_float(w); }
+  static __device__ float largest(const uint4& a, const uint4& b) {
+    return fmaxf(fmaxf(fmaxf(of(a.x), of(a.y)), fmaxf(of(a.z), of(a.w))), fmaxf(fmaxf(of(b.x), of(b.y)), fmaxf(of(b.z), of(b.w))));
   }
-  __device__ float largest() const {
-    return fmaxf(fmaxf(fmaxf(q[0].x, q[0].y), fmaxf(q[0].z, q[0].w)), fmaxf(fmaxf(q[1].x, q[1].y), fmaxf(q[1].z, q[1].w)));
+  static __device__ void floored(const uint4& q, Pair* v) {
+    v[0] = pair_of(max_nan(of(q.x), kTiny), max_nan(of(q.y), kTiny));
+    v[1] = pair_of(max_nan(of(q.z), kTiny), max_nan(of(q.w), kTiny));
   }
-  __device__ void values(float* v) const {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) v[4 * i] = q[i].x, v[4 * i + 1] = q[i].y, v[4 * i + 2] = q[i].z, v[4 * i + 3] = q[i].w;
-  }
-  __device__ void floored(float* v) const {
-    values(v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = max_nan(v[i], kTiny);
-  }
+  static __device__ Kept kept(float m) { return m; }
+  static __device__ float value(Kept m) { return m; }
 };
-
-__device__ __forceinline__ void keep(__nv_bfloat16* at, float v) { *at = __float2bfloat16_rn(v); }  // (exact: it was one)
-__device__ __forceinline__ void keep(float* at, float v) { *at = v; }
 
 // A thread's sums, even and odd values apart.
 struct Sums {
@@ -186,40 +194,83 @@ struct Sums {
     s2 = pair_of(f * s.x, f * s.y);
     c = reference;
   }
-  // v: floored, largest: of the eight.  The eight are added up among themselves first: a thread's sums then have an eighth of
-  // the roundings in a row.
-  __device__ __forceinline__ void add(const float* v, float largest) {
+  // In front of values up to `largest`.
+  __device__ __forceinline__ void meet(float largest) {
     top = fmaxf(top, largest);
     if (powers_of(largest) > c + kSlack) renew(powers_of(largest));
+  }
+  // Floored values, kPairs times two.  They are added up among themselves first: a thread's sums then have so many fewer
+  // roundings in a row.
+  template <int kPairs>
+  __device__ __forceinline__ void add(const Pair* v) {
     const Pair scale = pair_of(kLog2e, kLog2e), minus = pair_of(-c, -c);
-    Pair y[kGroup / 2], e[kGroup / 2];
+    Pair y[kPairs], e[kPairs];
 #pragma unroll
-    for (int i = 0; i < kGroup / 2; ++i) {
-      y[i] = fma2(pair_of(v[2 * i], v[2 * i + 1]), scale, minus);
+    for (int i = 0; i < kPairs; ++i) {
+      y[i] = fma2(v[i], scale, minus);
       const float2 q = both(y[i]);
       e[i] = pair_of(exp2_fast(q.x), exp2_fast(q.y));
     }
-    s2 = add2(s2, add2(add2(e[0], e[1]), add2(e[2], e[3])));
-    w2 = add2(w2, fma2(e[3], y[3], fma2(e[2], y[2], fma2(e[1], y[1], mul2(e[0], y[0])))));
-  }
-};
-
-// One row, or one block's share of it.
-template <typename T>
-struct Row {
-  const T* at;   // the row
-  int shift;     // groups are laid from a 16-byte place on, `shift` logits in front of the row
-  int vocab, begin, end;  // groups of this block
-
-  __device__ int first(int g) const { return g * kGroup - shift; }
-  __device__ bool whole(int g) const { return first(g) >= 0 && first(g) + kGroup <= vocab; }
-  // logits of a group, -inf outside the row
-  __device__ void load(int g, float* v) const {
-    const int c = first(g);
+    Pair w = mul2(e[0], y[0]);
 #pragma unroll
-    for (int e = 0; e < kGroup; ++e) v[e] = c + e >= 0 && c + e < vocab ? to_float(at[c + e]) : -INFINITY;
+    for (int i = 1; i < kPairs; ++i) w = fma2(e[i], y[i], w);
+    w2 = add2(w2, w);
+#pragma unroll
+    for (int n = kPairs / 2; n > 0; n /= 2)
+#pragma unroll
+      for (int i = 0; i < n; ++i) e[i] = add2(e[i], e[i + n]);
+    s2 = add2(s2, e[0]);
   }
 };
+
+// A block's share of a row: vectors at 16-byte places, the first `shift` logits of which lie in front of the row.
+template <typename T>
+struct Share {
+  static constexpr int kSize = Vector<T>::kSize;
+  const T* at;  // the row
+  int shift, vocab, begin, end;
+  int inner, inner_end;  // vectors that lie in the row as a whole
+
+  __device__ __forceinline__ Share(const LogitParams& p, long long r, int rank, int blocks) {
+    at = static_cast<const T*>(p.logits) + r * p.stride;
+    vocab = p.vocab;
+    shift = (int)(reinterpret_cast<uintptr_t>(at) % 16 / sizeof(T));
+    const int all = (vocab + shift + kSize - 1) / kSize, each = (all + blocks - 1) / blocks;
+    begin = min(rank * each, all);
+    end = min(begin + each, all);
+    inner = begin == 0 && shift > 0 ? 1 : begin;
+    inner_end = end == all && (vocab + shift) % kSize != 0 ? end - 1 : end;
+  }
+  // (an empty share has one batch, of nothing)
+  __device__ __forceinline__ int batches() const { return max(1, (end - begin + 2 * kThreads - 1) / (2 * kThreads)); }
+  // the two vectors of a batch and thread: `half` 0 and 1
+  __device__ __forceinline__ int vector(int batch, int thread, int half) const {
+    return begin + (2 * batch + half) * kThreads + thread;
+  }
+  __device__ __forceinline__ int first(int v) const { return v * kSize - shift; }
+  __device__ __forceinline__ bool in_row(int v, int e) const { return v < end && first(v) + e >= 0 && first(v) + e < vocab; }
+  __device__ __forceinline__ float value(int v, int e) const { return in_row(v, e) ? to_float(at[first(v) + e]) : -INFINITY; }
+};
+
+// A vector: what lies outside the row is -inf, so that nothing behind has to look.
+template <typename T>
+__device__ __forceinline__ uint4 fetch(const Share<T>& row, int v) {
+  if (v >= row.inner && v < row.inner_end) return __ldcs(reinterpret_cast<const uint4*>(row.at + row.first(v)));
+  constexpr uint32_t kNothing = Vector<T>::kNothing;
+  uint4 q = make_uint4(kNothing, kNothing, kNothing, kNothing);
+  if (v < row.end) {  // the row begins or ends inside it
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 2)
+        w[i] = pack_bf16(row.value(v, 2 * i), row.value(v, 2 * i + 1));
+      else
+        w[i] = __float_as_uint(row.value(v, i));
+    }
+    q = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return q;
+}
 
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -232,44 +283,73 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Sums of the block into sh.part, against the block's maximum.
-__device__ void block_sums(Shared& sh, float top, float s, float w) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  s = warp_sum(s);
-  w = warp_sum(w);
-  if (lane == 0) sh.warp_s[warp] = s, sh.warp_w[warp] = w;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    s = w = 0.f;
-    for (int i = 0; i < kWarps; ++i) s += sh.warp_s[i], w += sh.warp_w[i];
-    sh.part = {top, s, w};
+// Numbers of the lanes that go up and down once (or down and up) in descending order; ascending with flip 31 (the lanes'
+// numbers read backwards).  The first exchange is with the lane `from` away.
+__device__ __forceinline__ void warp_merge(unsigned& v, int from, int flip) {
+  const int lane = (threadIdx.x & 31) ^ flip;
+#pragma unroll
+  for (int j = 16; j > 0; j >>= 1) {
+    if (j > from) continue;
+    const unsigned other = __shfl_xor_sync(0xFFFFFFFFu, v, j);
+    v = (lane & j) == 0 ? max(v, other) : min(v, other);
   }
 }
+__device__ __forceinline__ void warp_sort(unsigned& v, int flip) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int k = 1; k <= 16; k <<= 1)  // runs of 2 k, every other one the other way round
+    warp_merge(v, k, flip ^ (k < 16 && (((lane ^ flip) & (2 * k)) != 0) ? 31 : 0));
+}
 
-// The block's alternatives one after the other, for rows with more candidates than fit (many equal logits, as a rule): a warp
-// goes through the groups' maxima in order and keeps the best in its lanes.
+// A row, or a block's share, from its parts in lanes 0 .. count - 1, for all lanes of the warp.
+__device__ __forceinline__ Part join_parts(Part q, int count) {
+  const int lane = threadIdx.x & 31;
+  if (lane >= count) q = {-INFINITY, 0.f, 0.f};
+  const float top = warp_max(q.top);
+  // (a part with nothing above -inf has sums of 0, or of NaN)
+  const float d = !(q.top > -INFINITY)                           ? 0.f
+                  : !(fabsf(top) < kFar) || !(fabsf(q.top) < kFar) ? fmaxf((q.top - top) * kLog2e, kTiny)
+                                                                   : powers_of(q.top) - powers_of(top);
+  const float f = exp2_fast(d);
+  return {top, warp_sum(f * q.s), warp_sum(f > 0.f ? f * fmaf(d, q.s, q.w) : f * q.s)};
+}
+
+__device__ __forceinline__ float logprob_of(const Whole& row, float x) {
+  if (row.s != row.s) return row.s;
+  if (x == -INFINITY || row.top == -INFINITY) return -INFINITY;
+  const float y = fabsf(row.top) < kFar ? fmaf(x, kLog2e, -powers_of(row.top)) : (x - row.top) * kLog2e;
+  return (y - row.log2_s) * kLn2;
+}
+
+__device__ __forceinline__ void write_row(const LogitParams& p, long long r, const Whole& row, bool known, float given) {
+  if (p.tokens) p.logprobs[r] = known ? logprob_of(row, given) : __uint_as_float(0x7FFFFFFFu);
+  if (p.entropy) p.entropy[r] = row.top == -INFINITY && row.s == row.s ? 0.f : (row.log2_s - row.w / row.s) * kLn2;
+}
+
+// The block's alternatives one after the other, where more candidates reach the bound than there is room for (many equal
+// logits, as a rule): through the vectors in order, the best so far in a warp's lanes.  What only equals the least of a full
+// list is passed over, so long runs of equal logits cost a look at their maxima.
 template <typename T>
-__device__ void best_in_order(const Row<T>& row, const typename Eight<T>::Kept* maxima, float bound, int top,
-                              unsigned long long* best) {
+__device__ __noinline__ unsigned long long best_in_order(const Share<T> row, const typename Vector<T>::Kept* maxima, float bound,
+                                                         int top) {
   const int lane = threadIdx.x & 31;
   unsigned long long mine = 0;  // lane i: the i-th best
-  float least = bound;          // a group has to reach it, and pass it once the list is full (equal ones later lose)
+  float least = bound;          // to be reached, and passed once the list is full (equal ones later lose)
   bool full = false;
-  for (int g0 = row.begin; g0 < row.end; g0 += 32) {
-    const int g = g0 + lane;
-    const float m = g < row.end ? to_float(maxima[g - row.begin]) : -INFINITY;
+  for (int n = 0; n < row.batches() * 2 * kWarps; ++n) {  // 32 vectors
+    const int batch = n / (2 * kWarps), half = n / kWarps & 1, thread = n % kWarps * 32;
+    const float m = Vector<T>::value(maxima[batch * kThreads + thread + lane]);
     unsigned hits = __ballot_sync(0xFFFFFFFFu, m > -INFINITY && (full ? m > least : m >= least));
     while (hits) {
-      const int from = __ffs(hits) - 1;
+      const int v = row.vector(batch, thread + __ffs(hits) - 1, half);
       hits &= hits - 1;
-      const int c = row.first(g0 + from) + lane;
       unsigned long long key = 0;
-      if (lane < kGroup && c >= 0 && c < row.vocab) {
-        const float v = to_float(row.at[c]);
-        if (v > -INFINITY) key = key_of(v, c);
+      if (lane < Vector<T>::kSize) {
+        const float x = row.value(v, lane);
+        if (x > -INFINITY) key = key_of(x, row.first(v) + lane);
       }
 #pragma unroll 1
-      for (int e = 0; e < kGroup; ++e) {
+      for (int e = 0; e < Vector<T>::kSize; ++e) {
         const unsigned long long k = __shfl_sync(0xFFFFFFFFu, key, e);
         const int place = __popc(__ballot_sync(0xFFFFFFFFu, lane < top && mine > k));
         if (k == 0 || place >= top) continue;
@@ -282,231 +362,238 @@ __device__ void best_in_order(const Row<T>& row, const typename Eight<T>::Kept* 
       if (last != 0) full = true, least = value_of((unsigned)(last >> 32));
     }
   }
-  if (lane < top) best[lane] = mine;
+  return mine;
 }
 
-// The block's `top` best into sh.best, from the groups' maxima.
+// Logits of the block's share that reach sh.bound to sh.keys; false where there is no room (sh.best has them then).
 template <typename T>
-__device__ void block_best(Shared& sh, const Row<T>& row, const typename Eight<T>::Kept* maxima, float thread_top, int top) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // a bound: the top-th largest of the warps' four largest thread maxima, each of them another logit
-  unsigned o = thread_top > -INFINITY ? ordered(thread_top) : 0;
+__device__ __forceinline__ bool gather_keys(Shared& sh, const Share<T>& row, const typename Vector<T>::Kept* maxima, int top) {
+  using Kept = typename Vector<T>::Kept;
+  const int tid = threadIdx.x;
+  const float bound = sh.bound;  // (above -inf)
+  constexpr int kAtOnce = 16 / sizeof(Kept), kSize = Vector<T>::kSize;
+  for (int i0 = tid * kAtOnce; i0 < row.batches() * kThreads; i0 += kThreads * kAtOnce) {
+    const uint4 q = *reinterpret_cast<const uint4*>(maxima + i0);
+    const Kept* m = reinterpret_cast<const Kept*>(&q);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const unsigned m = __reduce_max_sync(0xFFFFFFFFu, o);
-    const unsigned who = __ballot_sync(0xFFFFFFFFu, o == m);
-    if (lane == __ffs(who) - 1) o = 0;
-    if (lane == 0) sh.warp_best[warp * 4 + i] = m;
-  }
-  if (tid < kMostTop) sh.best[tid] = 0;
-  if (tid == 0) sh.num_groups = sh.num_keys = 0;
-  __syncthreads();
-  static_assert(kWarps * 4 == 32 && kMostTop == 32, "one of the warps' maxima a lane");
-  if (warp == 0) {
-    const unsigned mine = sh.warp_best[lane];
-    int above = 0;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const unsigned other = __shfl_sync(0xFFFFFFFFu, mine, i);
-      above += other > mine || (other == mine && i < lane);
-    }
-    if (above == top - 1) sh.bound = mine == 0 ? -INFINITY : value_of(mine);
-  }
-  __syncthreads();
-  const float bound = sh.bound;
-  for (int g = row.begin + tid; g < row.end; g += kThreads) {
-    const float m = to_float(maxima[g - row.begin]);
-    if (m > -INFINITY && m >= bound) {
-      const int at = atomicAdd(&sh.num_groups, 1);
-      if (at < kMostGroups) sh.groups[at] = g;
-    }
-  }
-  __syncthreads();
-  const int groups = sh.num_groups;
-  if (groups <= kMostGroups) {
-    for (int i = tid; i < groups * kGroup; i += kThreads) {
-      const int c = row.first(sh.groups[i / kGroup]) + i % kGroup;
-      if (c < 0 || c >= row.vocab) continue;
-      const float v = to_float(row.at[c]);
-      if (v > -INFINITY && v >= bound) {
-        const int at = atomicAdd(&sh.num_keys, 1);
-        if (at < kMostKeys) sh.keys[at] = key_of(v, c);
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float v = Vector<T>::value(m[i]);
+      if (v >= bound) {
+        const int at = atomicAdd(&sh.num_pairs, 1);
+        if (at < kMostPairs) sh.pairs[at] = i0 + i;
       }
     }
   }
   __syncthreads();
-  const int keys = sh.num_keys;
-  if (groups > kMostGroups || keys > kMostKeys) {
-    if (warp == 0) best_in_order<T>(row, maxima, bound, top, sh.best);
-  } else if (tid < keys) {  // the place of a key is the number of larger ones
-    const unsigned long long mine = sh.keys[tid];
-    int place = 0;
-    for (int i = 0; i < keys; ++i) place += sh.keys[i] > mine;
-    if (place < top) sh.best[place] = mine;
+  const int pairs = sh.num_pairs;
+  if (pairs <= kMostPairs) {
+    for (int i = tid; i < pairs * 2 * kSize; i += kThreads) {
+      const int pair = sh.pairs[i / (2 * kSize)], half = i / kSize & 1, e = i % kSize;
+      const int v = row.vector(pair / kThreads, pair % kThreads, half);
+      const float x = row.value(v, e);
+      if (x >= bound) {
+        const int at = atomicAdd(&sh.num_keys, 1);
+        if (at < kMostKeys) sh.keys[at] = key_of(x, row.first(v) + e);
+      }
+    }
   }
+  __syncthreads();
+  if (pairs <= kMostPairs && sh.num_keys <= kMostKeys) return true;
+  if (tid < 32) {
+    const unsigned long long k = best_in_order<T>(row, maxima, bound, top);
+    if (tid < top) sh.best[tid] = k;
+  }
+  __syncthreads();
+  return false;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 5) toploc_token_logprobs_kernel(const __grid_constant__ LogitParams p) {
+template <typename T, bool kTops>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm<T>)
+    toploc_token_logprobs_kernel(const __grid_constant__ LogitParams p) {
   extern __shared__ __align__(16) unsigned char raw[];
   __shared__ Shared sh;
-  using Kept = typename Eight<T>::Kept;
+  using V = Vector<T>;
+  using Kept = typename V::Kept;
   Kept* maxima = reinterpret_cast<Kept*>(raw);
   cg::cluster_group cluster = cg::this_cluster();
   const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  const long long r = blockIdx.x / (unsigned)blocks;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-
-  Row<T> row;
-  row.at = static_cast<const T*>(p.logits) + r * p.stride;
-  row.vocab = p.vocab;
-  row.shift = (int)(reinterpret_cast<uintptr_t>(row.at) % 16 / sizeof(T));
-  const int all = (p.vocab + row.shift + kGroup - 1) / kGroup, share = (all + blocks - 1) / blocks;
-  row.begin = min(rank * share, all);
-  row.end = min(row.begin + share, all);
-
-  float given = 0.f;
-  bool known = false;
-  if (rank == 0 && tid == 0 && p.tokens) {
-    const int64_t t = p.tokens[r];
-    known = t >= 0 && t < p.vocab;
-    if (known) given = to_float(row.at[t]);
-  }
+  const long long r = blockIdx.x / (unsigned)blocks;
+  const Share<T> row(p, r, rank, blocks);
+  const bool gives = rank == 0 && tid == 0 && p.tokens;
+  if (gives) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.tokens + r));
 
   Sums sums;
-  const int inner_begin = row.begin + (row.begin < row.end && !row.whole(row.begin) ? 1 : 0);
-  const int inner_end = max(inner_begin, row.end - (row.begin < row.end && !row.whole(row.end - 1) ? 1 : 0));
-  constexpr int kUnroll = sizeof(T) == 2 ? 4 : 2;
-  for (int g0 = inner_begin + tid; g0 < inner_end; g0 += kUnroll * kThreads) {
-    Eight<T> x[kUnroll];
+  const int batches = row.batches();
+  const auto take = [&](const uint4* x, int b, int pairs) {  // two batches, or one
+    float m[2], most = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      if (g0 + u * kThreads < inner_end) x[u].load(row.at + row.first(g0 + u * kThreads));
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int g = g0 + u * kThreads;
-      if (g >= inner_end) break;
-      const float m = x[u].largest();
-      if (p.top) keep(maxima + (g - row.begin), m);
-      float v[kGroup];
-      x[u].floored(v);
-      sums.add(v, m);
+    for (int i = 0; i < 2; ++i) {
+      if (i == pairs) break;
+      m[i] = V::largest(x[2 * i], x[2 * i + 1]);
+      most = fmaxf(most, m[i]);
+      if (kTops) maxima[(b + i) * kThreads + tid] = V::kept(m[i]);
     }
-  }
-  // the first and the last group, where the row begins or ends inside them
-  for (int i = 0; i < 2; ++i) {
-    const int g = i == 0 ? row.begin : row.end - 1;
-    const bool due = i == 0 ? inner_begin > row.begin : inner_end < row.end && row.end - 1 >= inner_begin;
-    if (due && tid == i * 32) {
-      float v[kGroup], m = -INFINITY;
-      row.load(g, v);
+    sums.meet(most);
 #pragma unroll
-      for (int e = 0; e < kGroup; ++e) m = fmaxf(m, v[e]), v[e] = max_nan(v[e], kTiny);
-      if (p.top) keep(maxima + (g - row.begin), m);
-      sums.add(v, m);
+    for (int i = 0; i < 2; ++i) {
+      if (i == pairs) break;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        Pair v[V::kSize / 2];
+        V::floored(x[2 * i + j], v);
+        sums.add<V::kSize / 2>(v);
+      }
     }
-  }
-
-  // the block's maximum, and its sums against it
-  float top = warp_max(sums.top);
-  if (lane == 0) sh.warp_top[warp] = top;
-  __syncthreads();
-  top = sh.warp_top[0];
+  };
+  const auto take_any = [&](int b) {
+    const uint4 x[2] = {fetch(row, row.vector(b, tid, 0)), fetch(row, row.vector(b, tid, 1))};
+    take(x, b, 1);
+  };
+  // two batches at a time where they lie in the row as a whole
+  const int inside = (row.inner_end - row.begin) / (2 * kThreads);  // batches up to the row's last part of a vector
+  int b = 0;
+  if (row.inner > row.begin) take_any(b++);  // the row begins inside a vector
+  const uint4* at = reinterpret_cast<const uint4*>(row.at - row.shift) + row.vector(b, tid, 0);
+  for (; b + 2 <= inside; b += 2, at += 4 * kThreads) {
+    uint4 x[4];
 #pragma unroll
-  for (int i = 1; i < kWarps; ++i) top = fmaxf(top, sh.warp_top[i]);
-  if (fabsf(top) < kFar) sums.renew(powers_of(top));
-  block_sums(sh, top, sums.s(), sums.w());
-  if (p.top) block_best<T>(sh, row, maxima, sums.top, p.top);
+    for (int i = 0; i < 4; ++i) x[i] = __ldcs(at + i * kThreads);
+    take(x, b, 2);
+  }
+#pragma unroll 1
+  for (; b < batches; ++b) take_any(b);
+  const int64_t token = gives ? p.tokens[r] : -1;
+  const bool known = token >= 0 && token < p.vocab;
+  const float given = known ? to_float(row.at[token]) : 0.f;
 
-  // the row's
-  cluster.sync();
-  float row_top = -INFINITY;
-  for (int i = 0; i < blocks; ++i) row_top = fmaxf(row_top, cluster.map_shared_rank(&sh, i)->part.top);
-  const bool far = !(fabsf(row_top) < kFar) && row_top > -INFINITY;
-  if (far) {  // summed again against the maximum itself: differences from it do not overflow upwards
-    cluster.sync();  // (all have read what is written again)
+  // the warp's part
+  Part part;
+  part.top = warp_max(sums.top);
+  if (part.top > -INFINITY && !(fabsf(part.top) < kFar)) {  // once more, by differences that do not overflow upwards
     float s = 0.f, w = 0.f;
-    for (int g = row.begin + tid; g < row.end; g += kThreads) {
-      float v[kGroup];
-      row.load(g, v);
-#pragma unroll
-      for (int e = 0; e < kGroup; ++e) {
-        const float y = max_nan((v[e] - row_top) * kLog2e, kTiny), x = exp2_fast(y);
+    for (int i = 0; i < 2 * batches; ++i) {
+      const int v = row.vector(i / 2, tid, i % 2);
+      for (int e = 0; e < V::kSize; ++e) {
+        const float y = max_nan((row.value(v, e) - part.top) * kLog2e, kTiny), x = exp2_fast(y);
         s += x;
         w = fmaf(x, y, w);
       }
     }
-    block_sums(sh, row_top, s, w);
-    cluster.sync();
+    part.s = warp_sum(s), part.w = warp_sum(w);
+  } else {
+    if (fabsf(part.top) < kFar) sums.renew(powers_of(part.top));
+    part.s = warp_sum(sums.s()), part.w = warp_sum(sums.w());
   }
-  if (rank == 0) {
-    float s = 0.f, w = 0.f;
-    for (int i = 0; i < blocks; ++i) {
-      const Part q = cluster.map_shared_rank(&sh, i)->part;
-      if (far) {
-        s += q.s, w += q.w;
-      } else {
-        // (a row with nothing above -inf has sums of 0, or of NaN)
-        const float d = row_top > -INFINITY ? fmaxf(powers_of(q.top), kTiny) - powers_of(row_top) : 0.f, f = exp2_fast(d);
-        s += f * q.s;
-        w += f > 0.f ? f * fmaf(d, q.s, q.w) : f * q.s;
+  if (lane == 0) sh.of_warp[warp] = part;
+  if (kTops) {
+    unsigned o = sums.top > -INFINITY ? ordered(sums.top) : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned m = __reduce_max_sync(0xFFFFFFFFu, o);
+      if (lane == __ffs(__ballot_sync(0xFFFFFFFFu, o == m)) - 1) o = 0;
+      if (lane == i) sh.warp_best[warp * 4 + i] = m;
+    }
+  }
+  __syncthreads();
+
+  if (warp == 0) {
+    const Part all = join_parts(sh.of_warp[lane % kWarps], kWarps);
+    if (blocks == 1) {
+      const Whole whole = {all.top, all.s, all.w, log2f(all.s)};
+      if (lane == 0) {
+        sh.whole = whole;
+        write_row(p, r, whole, known, given);
+      }
+    } else if (lane == 0) {
+      sh.part = all;
+    }
+    if (kTops) {  // the bound: the top-th largest of the warps' four largest thread maxima, each of them another logit
+      unsigned mine = sh.warp_best[lane];
+      warp_sort(mine, 0);
+      mine = __shfl_sync(0xFFFFFFFFu, mine, p.top - 1);
+      if (lane == 0) {
+        sh.bound = mine == 0 ? -FLT_MAX : value_of(mine);  // (every logit above -inf)
+        sh.num_pairs = sh.num_keys = 0;
       }
     }
-    const float log2_s = log2f(s);
-    const bool none = row_top == -INFINITY && !(s != s);
-    const auto logprob = [&](float x) {
-      if (none || x == -INFINITY) return s != s ? s : -INFINITY;
-      return ((far ? (x - row_top) * kLog2e : fmaf(x, kLog2e, -powers_of(row_top))) - log2_s) * kLn2;
-    };
-    if (tid == 0) {
-      if (p.tokens) p.logprobs[r] = known ? logprob(given) : __uint_as_float(0x7FFFFFFFu);
-      if (p.entropy) p.entropy[r] = none ? 0.f : (log2_s - w / s) * kLn2;
+  }
+  if constexpr (kTops) {
+    __syncthreads();
+    const bool in_keys = gather_keys<T>(sh, row, maxima, p.top);
+    const int keys = in_keys ? sh.num_keys : p.top;
+    const unsigned long long mine = tid < keys ? in_keys ? sh.keys[tid] : sh.best[tid] : 0;
+    int place_of_mine = kMostTop;
+    if (mine != 0) {  // its place: the number of larger ones
+      place_of_mine = 0;
+      const unsigned long long* list = in_keys ? sh.keys : sh.best;
+      for (int i = 0; i < keys; ++i) place_of_mine += list[i] > mine;
     }
-    if (p.top) {  // of all blocks' alternatives: the place of each is the number of larger ones
-      const bool has = tid < blocks * p.top;
-      const unsigned long long mine = has ? cluster.map_shared_rank(&sh, tid / p.top)->best[tid % p.top] : 0;
-      sh.keys[tid] = mine;
+    if (blocks == 1) {
       const int held = __syncthreads_count(mine != 0);
-      if (mine != 0) {
-        int place = 0;
-        for (int i = 0; i < blocks; ++i) {  // (each block's are in order)
-          int lo = 0, hi = p.top;
-          while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (sh.keys[i * p.top + mid] > mine) lo = mid + 1; else hi = mid;
-          }
-          place += lo;
-        }
-        if (place < p.top) {
-          p.top_ids[r * p.top + place] = (int64_t)(0xFFFFFFFFu - (unsigned)mine);
-          p.top_logprobs[r * p.top + place] = logprob(value_of((unsigned)(mine >> 32)));
-        }
+      if (place_of_mine < p.top) {
+        p.top_ids[r * p.top + place_of_mine] = (int64_t)(0xFFFFFFFFu - (unsigned)mine);
+        p.top_logprobs[r * p.top + place_of_mine] = logprob_of(sh.whole, value_of((unsigned)(mine >> 32)));
       }
       if (tid < p.top && tid >= held) {
         p.top_ids[r * p.top + tid] = -1;
-        p.top_logprobs[r * p.top + tid] = s != s ? s : -INFINITY;
+        p.top_logprobs[r * p.top + tid] = logprob_of(sh.whole, -INFINITY);
       }
+    } else if (in_keys) {
+      if (tid < p.top && tid >= keys) sh.best[tid] = 0;
+      if (place_of_mine < p.top) sh.best[place_of_mine] = mine;
     }
   }
-  cluster.sync();  // nobody leaves while its shared memory is read
+  if (blocks > 1) {  // the row, from the cluster's shares
+    cluster.sync();
+    if (rank == 0) {
+      if (warp == 0) {
+        const Part all = join_parts(cluster.map_shared_rank(&sh, lane % blocks)->part, blocks);
+        const Whole whole = {all.top, all.s, all.w, log2f(all.s)};
+        if (lane == 0) {
+          sh.whole = whole;
+          write_row(p, r, whole, known, given);
+        }
+      }
+      if constexpr (kTops) {
+        const bool has = tid < blocks * p.top;
+        const unsigned long long mine = has ? cluster.map_shared_rank(&sh, tid / p.top)->best[tid % p.top] : 0;
+        sh.keys[tid] = mine;
+        const int held = __syncthreads_count(mine != 0);
+        if (mine != 0) {
+          int above = 0;
+          for (int i = 0; i < blocks; ++i) {  // (each block's are in order)
+            int lo = 0, hi = p.top;
+            while (lo < hi) {
+              const int mid = (lo + hi) >> 1;
+              if (sh.keys[i * p.top + mid] > mine) lo = mid + 1; else hi = mid;
+            }
+            above += lo;
+          }
+          if (above < p.top) {
+            p.top_ids[r * p.top + above] = (int64_t)(0xFFFFFFFFu - (unsigned)mine);
+            p.top_logprobs[r * p.top + above] = logprob_of(sh.whole, value_of((unsigned)(mine >> 32)));
+          }
+        }
+        if (tid < p.top && tid >= held) {
+          p.top_ids[r * p.top + tid] = -1;
+          p.top_logprobs[r * p.top + tid] = logprob_of(sh.whole, -INFINITY);
+        }
+      }
+    }
+    cluster.sync();  // nobody leaves while its shared memory is read
+  }
 }
 
-template <typename T>
-int launch(const LogitParams& p, long long rows, int sms, cudaStream_t stream) {
-  using Kept = typename Eight<T>::Kept;
-  const int groups = (p.vocab + 16 / (int)sizeof(T) - 1 + kGroup - 1) / kGroup;  // at most
-  // A row's blocks: enough for six a processor, but none with less than two rounds of loads, and none whose maxima take more
-  // than 32.5 KB (so that six fit).
-  int blocks = 1;
-  while (blocks < kMostCluster && ((rows * blocks < 6ll * sms && groups / (2 * blocks) >= 4 * kThreads) ||
-                                   (p.top && groups / blocks * sizeof(Kept) > 32 * 1024 + 512)))
-    blocks *= 2;
-  if (rows * blocks > 0x7FFFFFFF) return TOPLOC_ERR_UNSUPPORTED;
-  const size_t bytes = p.top ? (size_t)((groups + blocks - 1) / blocks) * sizeof(Kept) : 0;
-  constexpr int kMostBytes = (kMostVocab / kGroup + 2) / kMostCluster * (int)sizeof(Kept) + 64;
+template <typename T, bool kTops>
+int launch_rows(const LogitParams& p, long long rows, int blocks, size_t bytes, cudaStream_t stream) {
+  const auto kernel = toploc_token_logprobs_kernel<T, kTops>;
   static std::atomic<uint64_t> allowed{0};
-  const void* kernel = reinterpret_cast<const void*>(toploc_token_logprobs_kernel<T>);
-  if (const int rc = allow_shared(kernel, kMostBytes > 65536 ? kMostBytes : 65536, allowed)) return rc;
+  // (the most: the maxima of an eighth of the largest vocabulary)
+  constexpr int kMostMaxima = (kMostVocab / Vector<T>::kSize / kMostCluster / 2 + 2 * kThreads) *
+                              (int)sizeof(typename Vector<T>::Kept);
+  constexpr int kMostBytes = (kMostMaxima > kMaximaBytes ? kMostMaxima : kMaximaBytes);
+  if (const int rc = allow_shared(reinterpret_cast<const void*>(kernel), kMostBytes, allowed)) return rc;
   cudaLaunchConfig_t config = {};
   config.gridDim = dim3((unsigned)(rows * blocks));
   config.blockDim = dim3(kThreads);
@@ -518,11 +605,33 @@ int launch(const LogitParams& p, long long rows, int sms, cudaStream_t stream) {
   cluster[0].val.clusterDim.y = cluster[0].val.clusterDim.z = 1;
   config.attrs = cluster;
   config.numAttrs = 1;
-  if (cudaLaunchKernelEx(&config, toploc_token_logprobs_kernel<T>, p) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&config, kernel, p) != cudaSuccess) {
     cudaGetLastError();
     return TOPLOC_ERR_CUDA;
   }
   return launched();
+}
+
+template <typename T>
+int launch(const LogitParams& p, long long rows, int sms, cudaStream_t stream) {
+  constexpr int kSize = Vector<T>::kSize;
+  const int vectors = (p.vocab + 2 * (kSize - 1)) / kSize;  // at most
+  const auto batches = [&](int blocks) { return ((vectors + blocks - 1) / blocks + 2 * kThreads - 1) / (2 * kThreads); };
+  const auto bytes = [&](int blocks) { return (size_t)batches(blocks) * kThreads * sizeof(typename Vector<T>::Kept); };
+  // A row's blocks: what gets through the rows soonest, as many blocks at a time as fit, where a block's time is its batches
+  // and as much as 7 + blocks of them for its beginning and end (measured with 128000 bf16, one row: 14.4, 10.7, 8.9 and 9.3 us
+  // for 1, 2, 4 and 8 blocks; 64 rows: 20.8, 15.1, 12.5 and 13.8; 4097 rows: 172, 208, 297 and 510).
+  int blocks = 0;
+  long long least = 0;
+  for (int n = 1; n <= kMostCluster; n *= 2) {
+    if (p.top && n < kMostCluster && bytes(n) > kMaximaBytes) continue;
+    const long long at_once = (long long)kBlocksPerSm<T> * sms, rounds = (rows * n + at_once - 1) / at_once;
+    const long long cost = rounds * (batches(n) + 7 + n);
+    if (blocks == 0 || cost < least) blocks = n, least = cost;
+  }
+  if (rows * blocks > 0x7FFFFFFF) return TOPLOC_ERR_UNSUPPORTED;
+  return p.top ? launch_rows<T, true>(p, rows, blocks, bytes(blocks), stream)
+               : launch_rows<T, false>(p, rows, blocks, 0, stream);
 }
 
 }  // namespace
