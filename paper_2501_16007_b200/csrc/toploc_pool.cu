@@ -2,10 +2,13 @@
 // follow from them.
 //
 // The planners move little (a table's entries and an integer or two a page) and have to agree on counts between their steps.
-// Each is one launch of one cluster of eight blocks: the cluster's barrier is the hardware's, so no block spins on another,
-// and a step's counts go through the blocks' shared memory.  A row of the table belongs to the same warp of all blocks, its
-// columns to the blocks in turn; a page belongs to one warp, in ascending order, so that what is numbered comes out in order
-// whatever the atomics' order was.
+// Each is one launch of one block, or of one cluster of eight where there is more to do: the barriers are the hardware's, so no
+// block spins on another, and a step's counts go through the blocks' shared memory.  A row of the table belongs to the same
+// warp of all blocks, its columns to the blocks in turn; a page belongs to one warp, in ascending order, so that what is
+// numbered comes out in order whatever the atomics' order was.
+//
+// Small plans are bound by latency: steps of dependent loads from L2, and code that is fetched for the first time (so little is
+// unrolled).  One block's barriers take a tenth of a cluster's (1000 to 3000 clocks each).
 #include "model_common.cuh"
 
 #include <cooperative_groups.h>
@@ -15,11 +18,11 @@ namespace {
 using namespace toploc_model;
 namespace cg = cooperative_groups;
 
-constexpr int kCluster = 8;
+constexpr int kMostBlocks = 8;                 // of a planner's cluster
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;          // of a block
-constexpr int kAllWarps = kCluster * kWarps;
-constexpr int kRows = 8;                       // rows of the table a warp reads at once
+constexpr long long kOneBlock = 16384;         // entries and pages that one block plans for
+constexpr int kAtOnce = 4;                     // loads of a thread on their way at once
 
 struct PoolParams {
   const int32_t* parents;    // fork
@@ -63,64 +66,119 @@ __device__ __forceinline__ int held_pages(const PoolParams& p, int len, int* sta
   return min(pages, p.max_pages);
 }
 
-// Calls visit(entry's address, page, row) for entries of the rows' held pages: all lanes of a warp together, lanes without an
-// entry with row -1.  held(row): pages of a row (its length is read by one lane a row).
+// The planner's threads: one block, or the blocks of one cluster.
+struct Team {
+  int blocks, block, all_warps, all_threads, warp_of_all, all_tid;
+
+  __device__ __forceinline__ Team() {
+    const cg::cluster_group cluster = cg::this_cluster();
+    blocks = (int)cluster.num_blocks();
+    block = (int)cluster.block_rank();
+    all_warps = blocks * kWarps;
+    all_threads = blocks * kThreads;
+    all_tid = block * kThreads + (int)threadIdx.x;
+    warp_of_all = all_tid >> 5;
+  }
+  __device__ __forceinline__ void sync() const {
+    if (blocks == 1)
+      __syncthreads();
+    else
+      cg::this_cluster().sync();
+  }
+};
+
+// Entries of the rows' held pages, kAtOnce rows of a warp together: visit(rows, column, pages, valid), arrays of kAtOnce; all
+// lanes of a warp together.  held(row): pages of a row (its length is read by one lane a row).
 template <typename Held, typename Visit>
-__device__ __forceinline__ void for_entries(const PoolParams& p, const int32_t* table, long long stride, int block, Held held,
-                                            Visit visit) {
+__device__ __forceinline__ void for_entries(const PoolParams& p, const Team& team, const int32_t* table, long long stride,
+                                            Held held, Visit visit) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll 1
   for (int base = warp; base < p.num_seqs; base += kWarps * 32) {
     const int row = base + lane * kWarps;
     const int mine = row < p.num_seqs ? held(row) : 0;
     const int count = min(32, (p.num_seqs - base + kWarps - 1) / kWarps);
-    for (int first = 0; first < count; first += kRows) {
-      int pages[kRows], most = 0;
+#pragma unroll 1
+    for (int first = 0; first < count; first += kAtOnce) {
+      int rows[kAtOnce], held_pages[kAtOnce], most = 0;
 #pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        pages[i] = __shfl_sync(0xFFFFFFFFu, mine, (first + i) & 31);
-        if (first + i >= count) pages[i] = 0;
-        most = max(most, pages[i]);
+      for (int i = 0; i < kAtOnce; ++i) {
+        rows[i] = base + (first + i) * kWarps;
+        held_pages[i] = __shfl_sync(0xFFFFFFFFu, mine, (first + i) & 31);
+        if (first + i >= count) held_pages[i] = 0;
+        most = max(most, held_pages[i]);
       }
-      for (int c0 = block * 32; c0 < most; c0 += kCluster * 32) {
-        int32_t page[kRows];
+#pragma unroll 1
+      for (int c0 = team.block * 32; c0 < most; c0 += team.blocks * 32) {
+        int32_t page[kAtOnce];
+        bool valid[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-          page[i] = 0;
-          if (c0 + lane < pages[i]) page[i] = table[(base + (first + i) * kWarps) * stride + c0 + lane];
+        for (int i = 0; i < kAtOnce; ++i) {
+          valid[i] = c0 + lane < held_pages[i];
+          page[i] = valid[i] ? table[rows[i] * stride + c0 + lane] : 0;
         }
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-          if (c0 >= pages[i]) continue;
-          const int row = base + (first + i) * kWarps;
-          visit(row, c0 + lane, page[i], c0 + lane < pages[i]);
-        }
+        visit(rows, c0 + lane, page, valid);
       }
     }
   }
 }
 
-// The range of pages of one warp of the cluster, whole groups of 32.
-__device__ __forceinline__ void pages_of_warp(const PoolParams& p, int warp_of_all, int* begin, int* end) {
-  const int groups = (p.num_pages + 31) / 32, each = (groups + kAllWarps - 1) / kAllWarps;
+// The range of pages of one warp of the team, whole groups of 32.
+__device__ __forceinline__ int groups_each(const PoolParams& p, const Team& team) {
+  return ((p.num_pages + 31) / 32 + team.all_warps - 1) / team.all_warps;
+}
+__device__ __forceinline__ void pages_of_warp(const PoolParams& p, int each, int warp_of_all, int* begin, int* end) {
   *begin = (int)min((long long)warp_of_all * each * 32, (long long)p.num_pages);
   *end = (int)min((long long)*begin + each * 32, (long long)p.num_pages);
 }
 
-// Every warp's count to all blocks: counts[w] of every warp of the cluster in shared memory, after a barrier of the cluster.
-__device__ __forceinline__ void tell_count(cg::cluster_group& cluster, int* counts, int count) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (lane < kCluster) cluster.map_shared_rank(counts, lane)[(int)cluster.block_rank() * kWarps + warp] = count;
+// Calls visit(page, value) for the pages of a warp's range in groups of 32, in order, all lanes together (value 0 past the
+// end).
+template <typename Visit>
+__device__ __forceinline__ void for_pages(const int32_t* values, int begin, int end, Visit visit) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int base = begin; base < end; base += 32 * kAtOnce) {
+    int32_t v[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = base + k * 32 + lane;
+      v[k] = i < end ? fresh(values + i) : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (base + k * 32 < end) visit(base + k * 32 + lane, v[k]);
+  }
+}
+
+// Copies a vector, the team's threads side by side.
+__device__ __forceinline__ void copy_vector(int32_t* to, const int32_t* from, int count, const Team& team) {
+#pragma unroll 1
+  for (long long i = team.all_tid; i < count; i += (long long)team.all_threads * kAtOnce) {
+    int32_t v[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (i + k * team.all_threads < count) v[k] = from[i + k * team.all_threads];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (i + k * team.all_threads < count) to[i + k * team.all_threads] = v[k];
+  }
+}
+
+// Every warp's count to all blocks: counts[w] of every warp of the team in shared memory, behind a barrier of the team.
+__device__ __forceinline__ void tell_count(const Team& team, int* counts, int count) {
+  const int lane = threadIdx.x & 31;
+  if (lane < team.blocks) cg::this_cluster().map_shared_rank(counts, lane)[team.warp_of_all] = count;
 }
 
 // Sum of the counts in front of a warp and of all, for all lanes.
-__device__ __forceinline__ int counted_before(const int* counts, int warp_of_all, int* all) {
+__device__ __forceinline__ int counted_before(const Team& team, const int* counts, int warp_of_all, int* all) {
   const int lane = threadIdx.x & 31;
   int before = 0, total = 0;
-#pragma unroll
-  for (int i = 0; i < kAllWarps / 32; ++i) {
-    const int c = counts[i * 32 + lane];
+  for (int i = lane; i < team.all_warps; i += 32) {
+    const int c = counts[i];
     total += c;
-    if (i * 32 + lane < warp_of_all) before += c;
+    if (i < warp_of_all) before += c;
   }
   *all = warp_total(total);
   return warp_total(before);
@@ -162,16 +220,14 @@ __device__ __forceinline__ int asked_before(const PoolParams& p, const int* run_
   return place;
 }
 
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
-    toploc_fork_pages_kernel(const __grid_constant__ PoolParams p) {
+__global__ void __launch_bounds__(kThreads, 1) toploc_fork_pages_kernel(const __grid_constant__ PoolParams p) {
   __shared__ int warp_sums[kWarps], run_before[kThreads];
-  cg::cluster_group cluster = cg::this_cluster();
-  const int block = (int)cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int all_tid = block * kThreads + tid, warp_of_all = block * kWarps + warp;
+  const Team team;
+  const int tid = threadIdx.x, lane = tid & 31, all_tid = team.all_tid;
 
   // who can be forked
-  for (int i = all_tid; i < p.num_pages; i += kCluster * kThreads) p.shares_out[i] = p.shares[i];
-  for (int i = warp_of_all; i < p.num_seqs; i += kAllWarps) {
+  copy_vector(p.shares_out, p.shares, p.num_pages, team);
+  for (int i = team.warp_of_all; i < p.num_seqs; i += team.all_warps) {
     const int parent = p.parents[i], own = p.kv_lens[i];
     int status = TOPLOC_SEQ_OK, len = own;
     if (parent >= 0) {
@@ -200,7 +256,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
       p.status[i] = (uint8_t)status;
     }
   }
-  cluster.sync();
+  team.sync();
 
   // pages asked for in front of every thread's run of sequences (every block for itself)
   const int per = max(1, (p.num_seqs + kThreads - 1) / kThreads);
@@ -215,10 +271,10 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     p.num_copies[0] = taken;
     p.next_free[0] = head + taken;
   }
-  for (int i = taken + all_tid; i < p.num_seqs; i += kCluster * kThreads) p.copy_from[i] = p.copy_to[i] = -1;
+  for (int i = taken + all_tid; i < p.num_seqs; i += team.all_threads) p.copy_from[i] = p.copy_to[i] = -1;
 
   // the children's rows (a status keeps its mark for those that still count)
-  for (int i = warp_of_all; i < p.num_seqs; i += kAllWarps) {
+  for (int i = team.warp_of_all; i < p.num_seqs; i += team.all_warps) {
     const int parent = p.parents[i], was = status_of(p, i);
     if (parent < 0 || (was & ~kNeedsPage) != TOPLOC_SEQ_OK) continue;
     const int whole = fresh(p.kv_lens_out + i) / p.page_size;
@@ -241,20 +297,20 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
       if (status != TOPLOC_SEQ_OK && lane == 0) p.status[i] = (uint8_t)(status | kNeedsPage);
     }
     if (status != TOPLOC_SEQ_OK) continue;
-    for (int j0 = lane; j0 < whole; j0 += 32 * kRows) {
-      int32_t page[kRows];
+    for (int j0 = lane; j0 < whole; j0 += 32 * kAtOnce) {
+      int32_t page[kAtOnce];
 #pragma unroll
-      for (int e = 0; e < kRows; ++e) page[e] = j0 + e * 32 < whole ? theirs[j0 + e * 32] : 0;
+      for (int e = 0; e < kAtOnce; ++e) page[e] = j0 + e * 32 < whole ? theirs[j0 + e * 32] : 0;
 #pragma unroll
-      for (int e = 0; e < kRows; ++e) {
+      for (int e = 0; e < kAtOnce; ++e) {
         if (j0 + e * 32 >= whole) break;
         row[j0 + e * 32] = page[e];
         atomicAdd(p.shares_out + page[e], 1);
       }
     }
   }
-  cluster.sync();
-  for (int i = all_tid; i < p.num_seqs; i += kCluster * kThreads) {
+  team.sync();
+  for (int i = all_tid; i < p.num_seqs; i += team.all_threads) {
     const int was = status_of(p, i);
     if (was & kNeedsPage) {
       p.status[i] = (uint8_t)(was & ~kNeedsPage);
@@ -265,15 +321,13 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
 
 // ---- releases ------------------------------------------------------------------------------------
 
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
-    toploc_release_pages_kernel(const __grid_constant__ PoolParams p) {
-  __shared__ int counts[kAllWarps];
-  cg::cluster_group cluster = cg::this_cluster();
-  const int block = (int)cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int all_tid = block * kThreads + tid, warp_of_all = block * kWarps + warp;
+__global__ void __launch_bounds__(kThreads, 1) toploc_release_pages_kernel(const __grid_constant__ PoolParams p) {
+  __shared__ int counts[kMostBlocks * kWarps];
+  const Team team;
+  const int lane = threadIdx.x & 31, all_tid = team.all_tid;
 
-  for (int i = all_tid; i < p.num_pages; i += kCluster * kThreads) p.shares_out[i] = p.shares[i];
-  for (int i = all_tid; i < p.num_seqs; i += kCluster * kThreads) {
+  copy_vector(p.shares_out, p.shares, p.num_pages, team);
+  for (int i = all_tid; i < p.num_seqs; i += team.all_threads) {
     const int len = p.kv_lens[i];
     int status = TOPLOC_SEQ_OK;
     const bool gone = p.release[i] != 0;
@@ -281,35 +335,37 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
     p.kv_lens_out[i] = gone ? 0 : len;
     p.status[i] = (uint8_t)status;
   }
-  cluster.sync();
+  team.sync();
 
   // a holder less for every entry; below zero: nobody is left
   for_entries(
-      p, p.table, p.table_stride, block,
+      p, team, p.table, p.table_stride,
       [&](int row) {
         int status;
         return p.release[row] != 0 ? held_pages(p, p.kv_lens[row], &status) : 0;
       },
-      [&](int row, int, int32_t page, bool valid) {
-        if (!valid) return;
-        if ((unsigned)page < (unsigned)p.num_pages)
-          atomicSub(p.shares_out + page, 1);
-        else
-          p.status[row] = TOPLOC_SEQ_BAD_PAGE;
+      [&](const int* rows, int, const int32_t* page, const bool* valid) {
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          if (!valid[i]) continue;
+          if ((unsigned)page[i] < (unsigned)p.num_pages)
+            atomicSub(p.shares_out + page[i], 1);
+          else
+            p.status[rows[i]] = TOPLOC_SEQ_BAD_PAGE;
+        }
       });
-  cluster.sync();
+  team.sync();
 
   int begin, end, count = 0, total;
-  pages_of_warp(p, warp_of_all, &begin, &end);
-  for (int i = begin + lane; i < end; i += 32) count += fresh(p.shares_out + i) < 0;
-  tell_count(cluster, counts, warp_total(count));
-  cluster.sync();
+  const int each = groups_each(p, team);
+  pages_of_warp(p, each, team.warp_of_all, &begin, &end);
+  for_pages(p.shares_out, begin, end, [&](int, int left) { count += left < 0; });
+  tell_count(team, counts, warp_total(count));
+  team.sync();
 
-  int place = counted_before(counts, warp_of_all, &total);
+  int place = counted_before(team, counts, team.warp_of_all, &total);
   const int room = min(max(p.first_free[0], 0), p.num_free), fit = min(total, room);
-  for (int base = begin; base < end; base += 32) {
-    const int i = base + lane;
-    const int left = i < end ? fresh(p.shares_out + i) : 0;
+  for_pages(p.shares_out, begin, end, [&](int i, int left) {
     const unsigned freed = __ballot_sync(0xFFFFFFFFu, left < 0);
     if (left < 0) {
       const int at = place + __popc(freed & ((1u << lane) - 1));
@@ -317,10 +373,10 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
       p.shares_out[i] = 0;
     }
     place += __popc(freed);
-  }
+  });
   if (all_tid == 0) p.next_free[0] = room - fit;
   if (total > room) {
-    for (int i = all_tid; i < p.num_seqs; i += kCluster * kThreads) {
+    for (int i = all_tid; i < p.num_seqs; i += team.all_threads) {
       int status;
       if (p.release[i] != 0 && held_pages(p, p.kv_lens[i], &status) > 0 && status_of(p, i) == TOPLOC_SEQ_OK)
         p.status[i] = TOPLOC_SEQ_NO_ROOM;
@@ -331,60 +387,61 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
 // ---- compaction ----------------------------------------------------------------------------------
 
 // While it runs, shares_out holds marks: 0 for unused pages, 1 for used ones, 1 + number of the copy for those that move.
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
-    toploc_compact_pages_kernel(const __grid_constant__ PoolParams p) {
-  __shared__ int counts[kAllWarps];
-  cg::cluster_group cluster = cg::this_cluster();
-  const int block = (int)cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int all_tid = block * kThreads + tid, warp_of_all = block * kWarps + warp;
+__global__ void __launch_bounds__(kThreads, 1) toploc_compact_pages_kernel(const __grid_constant__ PoolParams p) {
+  __shared__ int counts[kMostBlocks * kWarps];
+  const Team team;
+  const int lane = threadIdx.x & 31, all_tid = team.all_tid;
   int32_t* marks = p.shares_out;
 
-  for (int i = all_tid; i < p.num_pages; i += kCluster * kThreads) {
+  for (int i = all_tid; i < p.num_pages; i += team.all_threads) {
     marks[i] = 0;
     p.copy_from[i] = p.copy_to[i] = -1;
   }
-  for (int i = all_tid; i < p.num_seqs; i += kCluster * kThreads) {
+  for (int i = all_tid; i < p.num_seqs; i += team.all_threads) {
     int status;
     held_pages(p, p.kv_lens[i], &status);
     p.status[i] = (uint8_t)status;
   }
-  cluster.sync();
+  team.sync();
 
   const auto held = [&](int row) {
     int status;
     return held_pages(p, p.kv_lens[row], &status);
   };
-  for_entries(p, p.table_in, p.table_in_stride, block, held, [&](int row, int, int32_t page, bool valid) {
-    if (!valid) return;
-    if ((unsigned)page < (unsigned)p.num_pages)
-      marks[page] = 1;
-    else
-      p.status[row] = TOPLOC_SEQ_BAD_PAGE;
-  });
-  cluster.sync();
+  for_entries(p, team, p.table_in, p.table_in_stride, held,
+              [&](const int* rows, int, const int32_t* page, const bool* valid) {
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) {
+                  if (!valid[i]) continue;
+                  if ((unsigned)page[i] < (unsigned)p.num_pages)
+                    marks[page[i]] = 1;
+                  else
+                    p.status[rows[i]] = TOPLOC_SEQ_BAD_PAGE;
+                }
+              });
+  team.sync();
 
   int begin, end, count = 0, live;
-  pages_of_warp(p, warp_of_all, &begin, &end);
-  for (int i = begin + lane; i < end; i += 32) count += fresh(marks + i) != 0;
-  tell_count(cluster, counts, warp_total(count));
-  cluster.sync();
+  const int each = groups_each(p, team);
+  pages_of_warp(p, each, team.warp_of_all, &begin, &end);
+  for_pages(marks, begin, end, [&](int, int mark) { count += mark != 0; });
+  tell_count(team, counts, warp_total(count));
+  team.sync();
 
   // used pages in front of the warp's, of all, and in front of the page that they will end at
-  const int before = counted_before(counts, warp_of_all, &live);
+  const int before = counted_before(team, counts, team.warp_of_all, &live);
   int below;
   {
-    const int groups = (p.num_pages + 31) / 32, each = (groups + kAllWarps - 1) / kAllWarps;
-    const int there = each > 0 ? min(live / (each * 32), kAllWarps - 1) : 0;
+    const int there = each > 0 ? min(live / (each * 32), team.all_warps - 1) : 0;
     int from, to, all, more = 0;
-    pages_of_warp(p, there, &from, &to);
-    below = counted_before(counts, there, &all);
-    for (int i = from + lane; i < min(to, live); i += 32) more += fresh(marks + i) != 0;
+    pages_of_warp(p, each, there, &from, &to);
+    below = counted_before(team, counts, there, &all);
+    for_pages(marks, from, min(to, live), [&](int, int mark) { more += mark != 0; });
     below += warp_total(more);
   }
   int passed = before;
-  for (int base = begin; base < end; base += 32) {
-    const int i = base + lane;
-    const bool used = i < end && fresh(marks + i) != 0;
+  for_pages(marks, begin, end, [&](int i, int mark) {
+    const bool used = mark != 0;
     const unsigned all = __ballot_sync(0xFFFFFFFFu, used);
     const int in_front = passed + __popc(all & ((1u << lane) - 1));
     if (i < end) {
@@ -396,28 +453,35 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
       if (i >= live) p.free_out[p.num_free - p.num_pages + i] = i;
     }
     passed += __popc(all);
-  }
+  });
   if (all_tid == 0) {
     p.num_copies[0] = live - below;
     p.next_free[0] = p.num_free - (p.num_pages - live);
   }
-  cluster.sync();
+  team.sync();
 
-  for_entries(p, p.table_in, p.table_in_stride, block, held, [&](int row, int col, int32_t page, bool valid) {
-    if (!valid) return;
-    if ((unsigned)page < (unsigned)p.num_pages && page >= live) page = fresh(p.copy_to + (fresh(marks + page) - 1));
-    p.table[row * p.table_stride + col] = page;
-  });
+  for_entries(p, team, p.table_in, p.table_in_stride, held,
+              [&](const int* rows, int col, const int32_t* page, const bool* valid) {
+                int32_t to[kAtOnce];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) {
+                  to[i] = 0;
+                  if (valid[i] && page[i] >= live && page[i] < p.num_pages) to[i] = fresh(marks + page[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) to[i] = to[i] > 0 ? fresh(p.copy_to + (to[i] - 1)) : page[i];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i)
+                  if (valid[i]) p.table[rows[i] * p.table_stride + col] = to[i];
+              });
   passed = before;
-  for (int base = begin; base < min(end, live); base += 32) {
-    const int i = base + lane;
-    const bool mine = i < min(end, live), used = mine && fresh(marks + i) != 0;
-    const unsigned all = __ballot_sync(0xFFFFFFFFu, used);
+  for_pages(marks, begin, min(end, live), [&](int i, int mark) {
+    const unsigned all = __ballot_sync(0xFFFFFFFFu, mark != 0);
     const int in_front = passed + __popc(all & ((1u << lane) - 1));
-    if (mine) p.shares_out[i] = p.shares[used ? i : fresh(p.copy_from + (i - in_front))];
+    if (i < min(end, live)) p.shares_out[i] = p.shares[mark != 0 ? i : fresh(p.copy_from + (i - in_front))];
     passed += __popc(all);
-  }
-  cluster.sync();  // (the marks have been read)
+  });
+  team.sync();  // (the marks have been read)
   for (int i = max(begin, live) + lane; i < end; i += 32) p.shares_out[i] = 0;
 }
 
@@ -439,16 +503,28 @@ struct CopyParams {
 };
 
 // Bound by memory: a page is read once and written once.  The number of copies is known on the device alone, so the blocks
-// share out what there is: (copy, cache, chunk of a page), four 16-byte loads in flight a thread.
+// share out what there is: (cache, copy, chunk of a page), four 16-byte loads in flight a thread.  A cache's copies are done
+// together, so that a page which is copied several times (the last one of a prompt with many samples) comes from L2 from the
+// second time on.
 template <typename Unit>
 __global__ void __launch_bounds__(kCopyThreads) toploc_copy_pages_kernel(const __grid_constant__ CopyParams p) {
-  const long long copies = min(max(p.count[0], 0), p.most);
-  const long long per_copy = (long long)p.num_caches * p.chunks, tasks = copies * per_copy;
-  for (long long t = blockIdx.x; t < tasks; t += gridDim.x) {
-    const int copy = (int)(t / per_copy), rest = (int)(t - copy * per_copy);
-    const int cache = rest / p.chunks, chunk = rest - cache * p.chunks;
-    const int from = p.from[copy], to = p.to[copy];
-    if ((unsigned)from >= (unsigned)p.num_pages || (unsigned)to >= (unsigned)p.num_pages || from == to) continue;
+  const int copies = min(max(p.count[0], 0), p.most);
+  const long long per_cache = (long long)copies * p.chunks, tasks = per_cache * p.num_caches;
+  // (the task's pages are looked up while the one in front is copied)
+  long long t = blockIdx.x;
+  int cache = 0, copy = 0, chunk = 0, from = -1, to = -1;
+  const auto look_up = [&]() {
+    if (t >= tasks) return;
+    cache = (int)(t / per_cache);
+    const long long rest = t - cache * per_cache;
+    copy = (int)((unsigned long long)rest <= 0xFFFFFFFFull ? (unsigned)rest / (unsigned)p.chunks : rest / p.chunks);
+    chunk = (int)(rest - (long long)copy * p.chunks);
+    from = p.from[copy];
+    to = p.to[copy];
+  };
+  look_up();
+  while (t < tasks) {
+    const bool good = (unsigned)from < (unsigned)p.num_pages && (unsigned)to < (unsigned)p.num_pages && from != to;
     const Unit* src = static_cast<const Unit*>(p.caches[cache]) + from * p.page;
     Unit* dst = static_cast<Unit*>(p.caches[cache]) + to * p.page;
     const long long first = (long long)chunk * kCopyThreads * kUnits + threadIdx.x;
@@ -458,7 +534,7 @@ __global__ void __launch_bounds__(kCopyThreads) toploc_copy_pages_kernel(const _
     for (int i = 0; i < kUnits; ++i) {
       const long long u = first + i * kCopyThreads;
       at[i] = u;
-      if (u < p.units) {
+      if (good && u < p.units) {
         if (p.heads > 0) {
           const long long row = u / p.units_per_head;
           at[i] = row / p.heads * p.token + row % p.heads * p.head + (u - row * p.units_per_head);
@@ -466,9 +542,11 @@ __global__ void __launch_bounds__(kCopyThreads) toploc_copy_pages_kernel(const _
         v[i] = src[at[i]];
       }
     }
+    t += gridDim.x;
+    look_up();
 #pragma unroll
     for (int i = 0; i < kUnits; ++i)
-      if (first + i * kCopyThreads < p.units) dst[at[i]] = v[i];
+      if (good && first + i * kCopyThreads < p.units) __stcs(dst + at[i], v[i]);
   }
 }
 
@@ -531,9 +609,25 @@ int check_memory(const Argument (&in)[kIn], const Argument (&out)[kOut]) {
   return TOPLOC_OK;
 }
 
+// One block, or a cluster of eight where the entries (at most) and pages make many rounds for one.
 template <typename Kernel>
 int launch_planner(Kernel kernel, const PoolParams& p, void* cuda_stream) {
-  kernel<<<kCluster, kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
+  const long long work = (long long)p.num_seqs * p.max_pages + p.num_pages;
+  cudaLaunchConfig_t config = {};
+  cudaLaunchAttribute cluster[1];
+  const unsigned blocks = work <= kOneBlock ? 1 : kMostBlocks;
+  config.gridDim = dim3(blocks);
+  config.blockDim = dim3(kThreads);
+  config.stream = static_cast<cudaStream_t>(cuda_stream);
+  cluster[0].id = cudaLaunchAttributeClusterDimension;
+  cluster[0].val.clusterDim.x = blocks;
+  cluster[0].val.clusterDim.y = cluster[0].val.clusterDim.z = 1;
+  config.attrs = cluster;
+  config.numAttrs = 1;
+  if (cudaLaunchKernelEx(&config, kernel, p) != cudaSuccess) {
+    cudaGetLastError();
+    return TOPLOC_ERR_CUDA;
+  }
   return launched();
 }
 

@@ -365,29 +365,30 @@ _PAIRINGS = {"halves": TOPLOC_ROTARY_HALVES, "neighbours": TOPLOC_ROTARY_NEIGHBO
 
 
 def _rotary_layout(q, k, v, positions, inv_freq, q_weight, k_weight, eps, pairing, q_out, k_out):
-    for t, what in ((q, "q"), (k, "k")):
-        _need(t.dim() == 3 and t.stride(2) == 1 and t.dtype is q.dtype,
-              "%s must be [tokens, heads, head_dim] of one type, the last dimension contiguous" % what)
-    _need(q.dtype in _DTYPES, "queries and keys must be bfloat16 or float32")
-    tokens, heads, dim = q.shape
-    _need(k.shape[0] == tokens and k.shape[2] == dim, "k must have q's tokens and head_dim")
-    _need(v is None or (v.shape == k.shape and v.dtype is q.dtype and v.stride(2) == 1),
-          "v must have k's shape and type, the last dimension contiguous")
-    _need(q_out.shape == q.shape and q_out.dtype is q.dtype and q_out.stride(2) == 1, "q_out must have q's shape and type")
-    _need(k_out is None or (k_out.shape == k.shape and k_out.dtype is q.dtype and k_out.stride(2) == 1),
-          "k_out must have k's shape and type")
-    _vector(positions, torch.int32, tokens, "positions")
-    _need(inv_freq.dtype is torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and
-          2 * inv_freq.shape[0] <= dim, "inv_freq must be a contiguous float32 vector of at most head_dim / 2 entries")
+    dtype, shape = q.dtype, k.shape
+    (tokens, heads, dim), (k_tokens, kv_heads, k_dim), (pairs,) = q.shape, shape, inv_freq.shape
+    (qt, qh, q1), (kt, kh, k1), (ot, oh, o1) = q.stride(), k.stride(), q_out.stride()
+    (vt, vh, v1), (pt, ph, p1) = (0, 0, 1) if v is None else v.stride(), (0, 0, 1) if k_out is None else k_out.stride()
+    if not (dtype in _DTYPES and dtype is k.dtype is q_out.dtype and k_tokens == tokens and k_dim == dim and
+            q_out.shape == (tokens, heads, dim) and q1 == k1 == o1 == v1 == p1 == 1 and
+            (v is None or (v.shape == shape and v.dtype is dtype)) and
+            (k_out is None or (k_out.shape == shape and k_out.dtype is dtype))):
+        raise ToplocError("queries and their output must be [tokens, q_heads, head_dim], keys, values and the keys' output "
+                          "[tokens, kv_heads, head_dim], all bfloat16 or all float32, the last dimension contiguous")
+    if not (positions.dtype is torch.int32 and positions.shape == (tokens,) and positions.is_contiguous() and
+            inv_freq.dtype is torch.float32 and inv_freq.is_contiguous() and 2 * pairs <= dim):
+        raise ToplocError("positions must be a contiguous int32 vector of %d entries, inv_freq a contiguous float32 vector of "
+                          "at most head_dim / 2" % tokens)
     for weight in (q_weight, k_weight):
-        _need(weight is None or (weight.dtype is q.dtype and weight.shape == (dim,) and weight.is_contiguous()),
-              "a norm's weight must be [head_dim] of q's type")
-    _need(pairing in _PAIRINGS, "pairing must be 'halves' or 'neighbours'")
-    (qt, qh, _), (kt, kh, _), (ot, oh, _) = q.stride(), k.stride(), q_out.stride()
-    vt, vh, _ = (0, 0, 0) if v is None else v.stride()
-    pt, ph, _ = (0, 0, 0) if k_out is None else k_out.stride()
-    return _pack(_ROTARY, _DTYPES[q.dtype], dim, heads, k.shape[1], 2 * inv_freq.shape[0], _PAIRINGS[pairing], tokens,
-                 eps, 0, qt, qh, kt, kh, vt, vh, ot, oh, pt, ph)
+        if not (weight is None or (weight.dtype is dtype and weight.shape == (dim,) and weight.is_contiguous())):
+            raise ToplocError("a norm's weight must be [head_dim] of q's type")
+    if pairing not in _PAIRINGS:
+        raise ToplocError("pairing must be 'halves' or 'neighbours'")
+    return _pack(_ROTARY, _DTYPES[dtype], dim, heads, kv_heads, 2 * pairs, _PAIRINGS[pairing], tokens, eps, 0, qt, qh, kt,
+                 kh, vt, vh, ot, oh, pt, ph)
+
+
+_DIMENSIONS = "%s takes queries, keys and values of three dimensions and inv_freq of one"
 
 
 def toploc_norm_rotary_prompt(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6, pairing="halves",
@@ -396,13 +397,16 @@ def toploc_norm_rotary_prompt(q, k, positions, inv_freq, q_weight=None, k_weight
     no norm of that one) and the rotation by position: positions int32 [tokens], inv_freq float32 [pairs]; the first
     2 * pairs channels of a head turn, channel c with c + pairs ("halves") or 2c with 2c + 1 ("neighbours").  q_out may be
     q, k_out may be k.  Returns (q_out, k_out)."""
+    name = "toploc_norm_rotary_prompt"
     if q_out is None:
         q_out = _empty(q.shape, q.dtype, q.device, stream)
     if k_out is None:
         k_out = _empty(k.shape, k.dtype, k.device, stream)
-    dev = _device("toploc_norm_rotary_prompt", q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out)
+    dev = _device(name, q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out)
+    if not q.dim() == k.dim() == q_out.dim() == k_out.dim() == 3 or inv_freq.dim() != 1:
+        raise ToplocError(_DIMENSIONS % name)
     lay = _rotary_layout(q, k, None, positions, inv_freq, q_weight, k_weight, eps, pairing, q_out, k_out)
-    _call(_library().toploc_norm_rotary_prompt, "toploc_norm_rotary_prompt", dev, stream, _ptr(q), _ptr(k),
+    _call(_library().toploc_norm_rotary_prompt, name, dev, stream, _ptr(q), _ptr(k),
           _ptr(positions), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), lay, _ptr(q_out), _ptr(k_out))
     return q_out, k_out
 
@@ -412,15 +416,19 @@ def toploc_norm_rotary_paged(q, k, v, positions, slots, inv_freq, k_cache, v_cac
     """toploc_norm_rotary_prompt with the keys' result and the values v [tokens, kv_heads, head_dim] written straight to
     their slots (int64 [tokens], negative: skipped) of the caches [num_pages, page_size, kv_heads, head_dim].  Returns
     q_out."""
+    name = "toploc_norm_rotary_paged"
     if q_out is None:
         q_out = _empty(q.shape, q.dtype, q.device, stream)
-    dev = _device("toploc_norm_rotary_paged", q, k, v, positions, slots, inv_freq, k_cache, v_cache, q_weight, k_weight,
-                  q_out)
+    dev = _device(name, q, k, v, positions, slots, inv_freq, k_cache, v_cache, q_weight, k_weight, q_out)
+    if not q.dim() == k.dim() == v.dim() == q_out.dim() == 3 or inv_freq.dim() != 1:
+        raise ToplocError(_DIMENSIONS % name)
     lay = _rotary_layout(q, k, v, positions, inv_freq, q_weight, k_weight, eps, pairing, q_out, None)
     kv = _cache_layout(k_cache, v_cache)
-    _need(k_cache.dtype is q.dtype and k_cache.shape[2:] == k.shape[1:], "the caches must have k's type, heads and head_dim")
-    _vector(slots, torch.int64, q.shape[0], "slots")
-    _call(_library().toploc_norm_rotary_paged, "toploc_norm_rotary_paged", dev, stream, _ptr(q), _ptr(k), _ptr(v),
+    if not (k_cache.dtype is q.dtype and k_cache.shape[2:] == k.shape[1:] and slots.dtype is torch.int64 and
+            slots.shape == positions.shape and slots.is_contiguous()):
+        raise ToplocError("the caches must have k's type, heads and head_dim, slots must be a contiguous int64 vector of "
+                          "as many entries as there are tokens")
+    _call(_library().toploc_norm_rotary_paged, name, dev, stream, _ptr(q), _ptr(k), _ptr(v),
           _ptr(positions), _ptr(slots), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), lay, _ptr(q_out), _ptr(k_cache),
           _ptr(v_cache), kv)
     return q_out
@@ -464,18 +472,28 @@ def toploc_token_logprobs(logits, tokens=None, top=0, want_entropy=False, logpro
     return logprobs, entropy, top_ids, top_logprobs
 
 
-def _int32s(name, **vectors):
-    """Contiguous int32 vectors of the lengths given beside them."""
-    for what, (t, length) in vectors.items():
-        if t.dtype is not torch.int32 or not t.is_contiguous() or t.dim() != 1 or t.shape[0] != length:
-            raise ToplocError("%s: %s must be a contiguous int32 tensor of %d entries" % (name, what, length))
+def _vectors(name, n, per_seq, pages, per_page, single, free_pages, flags):
+    """int32 vectors of n, of as many entries as there are pages and of one, the free list, and uint8 vectors of n."""
+    i32 = torch.int32
+    for group, entries in ((per_seq, n), (per_page, pages), (single, 1)):
+        for t in group:
+            if t.dtype is not i32 or t.numel() != entries or not t.is_contiguous():
+                raise ToplocError("%s: contiguous int32 vectors of %d entries for the sequences, of %d for the pages, and of "
+                                  "one (see its documentation)" % (name, n, pages))
+    if free_pages.dtype is not i32 or not free_pages.is_contiguous():
+        raise ToplocError("%s: the free list must be a contiguous int32 vector" % name)
+    for t in flags:
+        if t.dtype is not torch.uint8 or t.numel() != n or not t.is_contiguous():
+            raise ToplocError("%s: status and release must be contiguous uint8 vectors of %d entries" % (name, n))
 
 
 def _table(t, n, what):
     """(columns, elements between rows) of a block table [n, max_pages]."""
-    _need(t.dtype is torch.int32 and t.dim() == 2 and t.shape[0] == n and
-          (t.stride(1) == 1 or t.shape[1] <= 1 or n == 0), "%s must be int32 [n, max_pages]" % what)
-    return t.shape[1], t.stride(0) if n > 1 else t.shape[1]
+    if t.dtype is torch.int32 and t.dim() == 2:
+        (rows, width), (stride, one) = t.shape, t.stride()
+        if rows == n and (one == 1 or width <= 1 or n == 0):
+            return width, stride if n > 1 else width
+    raise ToplocError("%s must be int32 [n, max_pages]" % what)
 
 
 def toploc_fork_pages(parents, kv_lens, shares, free_pages, first_free, block_table, page_size, kv_lens_out, shares_out,
@@ -489,10 +507,8 @@ def toploc_fork_pages(parents, kv_lens, shares, free_pages, first_free, block_ta
     dev = _device(name, parents, kv_lens, shares, free_pages, first_free, block_table, kv_lens_out, shares_out, copy_from,
                   copy_to, num_copies, next_free, status)
     pages, free = shares.numel(), free_pages.numel()
-    _int32s(name, parents=(parents, n), kv_lens=(kv_lens, n), shares=(shares, pages), free_pages=(free_pages, free),
-            first_free=(first_free, 1), kv_lens_out=(kv_lens_out, n), shares_out=(shares_out, pages),
-            copy_from=(copy_from, n), copy_to=(copy_to, n), num_copies=(num_copies, 1), next_free=(next_free, 1))
-    _vector(status, torch.uint8, n, "status")
+    _vectors(name, n, (parents, kv_lens, kv_lens_out, copy_from, copy_to), pages, (shares, shares_out),
+             (first_free, num_copies, next_free), free_pages, (status,))
     width, stride = _table(block_table, n, "block_table")
     _call(_library().toploc_fork_pages, name, dev, stream, _ptr(parents), _ptr(kv_lens), n, _ptr(shares), pages,
           _ptr(free_pages), free, _ptr(first_free), page_size, _ptr(block_table), width, stride, _ptr(kv_lens_out),
@@ -509,10 +525,8 @@ def toploc_release_pages(release, kv_lens, block_table, shares, page_size, free_
     dev = _device(name, release, kv_lens, block_table, shares, free_pages, first_free, kv_lens_out, shares_out, next_free,
                   status)
     pages, free = shares.numel(), free_pages.numel()
-    _vector(release, torch.uint8, n, "release")
-    _int32s(name, kv_lens=(kv_lens, n), shares=(shares, pages), free_pages=(free_pages, free), first_free=(first_free, 1),
-            kv_lens_out=(kv_lens_out, n), shares_out=(shares_out, pages), next_free=(next_free, 1))
-    _vector(status, torch.uint8, n, "status")
+    _vectors(name, n, (kv_lens, kv_lens_out), pages, (shares, shares_out), (first_free, next_free), free_pages,
+             (status, release))
     width, stride = _table(block_table, n, "block_table")
     _call(_library().toploc_release_pages, name, dev, stream, _ptr(release), _ptr(kv_lens), n, _ptr(block_table), width,
           stride, _ptr(shares), pages, page_size, _ptr(free_pages), free, _ptr(first_free), _ptr(kv_lens_out),
@@ -529,10 +543,8 @@ def toploc_compact_pages(kv_lens, block_table, shares, page_size, block_table_ou
     dev = _device(name, kv_lens, block_table, shares, block_table_out, shares_out, free_pages_out, copy_from, copy_to,
                   num_copies, next_free, status)
     pages, free = shares.numel(), free_pages_out.numel()
-    _int32s(name, kv_lens=(kv_lens, n), shares=(shares, pages), shares_out=(shares_out, pages),
-            free_pages_out=(free_pages_out, free), copy_from=(copy_from, pages), copy_to=(copy_to, pages),
-            num_copies=(num_copies, 1), next_free=(next_free, 1))
-    _vector(status, torch.uint8, n, "status")
+    _vectors(name, n, (kv_lens,), pages, (shares, shares_out, copy_from, copy_to), (num_copies, next_free), free_pages_out,
+             (status,))
     width, stride = _table(block_table, n, "block_table")
     out_width, out_stride = _table(block_table_out, n, "block_table_out")
     _need(width == out_width, "block_table_out must have block_table's shape")
@@ -548,15 +560,22 @@ def toploc_copy_pages(caches, copy_from, copy_to, num_copies, stream=None):
     name = "toploc_copy_pages"
     if not caches:
         return
-    dev, one, strides = _device(name, copy_from, copy_to, num_copies, *caches), caches[0], caches[0].stride()
-    _need(one.dim() == 4 and one.dtype in _DTYPES and strides[3] == 1,
-          "caches must be bfloat16 or float32 [pages, page_size, kv_heads, head_dim], the last dimension contiguous")
+    one = caches[0]
+    dev, shape, strides, dtype, most = _device(name, copy_from, copy_to, num_copies, one), one.shape, one.stride(), one.dtype, \
+        copy_from.numel()
+    index, pointers = dev.index, []
+    if len(shape) != 4 or dtype not in _DTYPES or strides[3] != 1:
+        raise ToplocError("caches must be bfloat16 or float32 [pages, page_size, kv_heads, head_dim], the last dimension "
+                          "contiguous")
     for c in caches:
-        _need(c.shape == one.shape and c.dtype is one.dtype and c.stride() == strides, "caches must have one type and layout")
-    most = copy_from.numel()
-    _int32s(name, copy_from=(copy_from, most), copy_to=(copy_to, most), num_copies=(num_copies, 1))
-    pages, tokens, heads, dim = one.shape
-    lay = _pack(_POOL, _DTYPES[one.dtype], pages, tokens, heads, dim, len(caches), strides[0], strides[1], strides[2])
-    pointers = (ctypes.c_void_p * len(caches))(*[c.data_ptr() for c in caches])
-    _call(_library().toploc_copy_pages, name, dev, stream, pointers, lay, _ptr(copy_from), _ptr(copy_to),
-          _ptr(num_copies), most)
+        if c.shape != shape or c.stride() != strides or c.dtype is not dtype or c.get_device() != index:
+            raise ToplocError("caches must have one type and layout, and be on one device")
+        pointers.append(c.data_ptr())
+    i32 = torch.int32
+    if not (copy_from.dtype is copy_to.dtype is num_copies.dtype is i32 and copy_from.shape == copy_to.shape == (most,) and
+            num_copies.shape == (1,) and copy_from.is_contiguous() and copy_to.is_contiguous()):
+        raise ToplocError("copy_from and copy_to must be contiguous int32 vectors of one length, num_copies int32 [1]")
+    pages, tokens, heads, dim = shape
+    lay = _pack(_POOL, _DTYPES[dtype], pages, tokens, heads, dim, len(pointers), strides[0], strides[1], strides[2])
+    _call(_library().toploc_copy_pages, name, dev, stream, struct.pack("=%dQ" % len(pointers), *pointers), lay,
+          _ptr(copy_from), _ptr(copy_to), _ptr(num_copies), most)
