@@ -82,34 +82,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
-// Two fp32 numbers in one register pair, and the instructions that take both at once.
-using Pair = unsigned long long;
-__device__ __forceinline__ Pair pair_of(float a, float b) {
-  Pair r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 both(Pair v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ Pair add2(Pair a, Pair b) {
-  Pair r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
-  Pair r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
-  Pair r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-
 // A logit in powers of 2 as a reference has it: rounded by itself, never as part of a sum (all that is taken off a reference
 // has to take off the same number).
 __device__ __forceinline__ float powers_of(float x) { return __fmul_rn(x, kLog2e); }

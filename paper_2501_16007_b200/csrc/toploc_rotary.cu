@@ -7,6 +7,7 @@ namespace {
 using namespace toploc_model;
 
 constexpr int kWarps = 4;             // of a block
+constexpr int kBlocksPerSm = 7;
 constexpr int kMostHeadDim = 256;
 constexpr int kMostHalf = kMostHeadDim / 2;
 
@@ -26,10 +27,11 @@ struct RotaryParams {
   long long num_tokens, num_slots;
   float eps, per_channel;  // 1 / head_dim
   int head_dim, half;      // channels, turned pairs
-  int q_heads, qk_heads, heads;  // ends of queries, of keys, of all
+  int q_heads, kv_heads;
   int page_size;
   int lane_shift, lanes;   // a head is 2^lane_shift lanes, the first `lanes` of which have channels
-  int steps, steps_per_warp;
+  int q_steps, qk_steps, steps;  // ends of the queries' steps, the keys', of all
+  int steps_per_warp;
 };
 
 // cos and sin of position * freq.  The angle is taken in turns and brought into one turn in 64 bits (position and frequency
@@ -72,43 +74,53 @@ template <typename T, int kVec>
 using Packed = typename Word<sizeof(T) * kVec>::type;
 
 template <typename T, int kVec>
-__device__ __forceinline__ void unpack(const Packed<T, kVec>& q, float* v) {
-  constexpr int kWords = sizeof(T) * kVec / 4;
+__device__ __forceinline__ void unpack(const Packed<T, kVec>& q, Pair* v) {
   const uint32_t* w = reinterpret_cast<const uint32_t*>(&q);
 #pragma unroll
-  for (int i = 0; i < kWords; ++i) {
+  for (int i = 0; i < kVec / 2; ++i) {
     if constexpr (sizeof(T) == 2)
-      v[2 * i] = bf16_low(w[i]), v[2 * i + 1] = bf16_high(w[i]);
+      v[i] = pair_of(bf16_low(w[i]), bf16_high(w[i]));
     else
-      v[i] = __uint_as_float(w[i]);
+      v[i] = pair_of(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
   }
 }
 
 template <typename T, int kVec>
-__device__ __forceinline__ Packed<T, kVec> pack(const float* v) {
-  constexpr int kWords = sizeof(T) * kVec / 4;
+__device__ __forceinline__ Packed<T, kVec> pack(const Pair* v) {
   Packed<T, kVec> q;
   uint32_t* w = reinterpret_cast<uint32_t*>(&q);
 #pragma unroll
-  for (int i = 0; i < kWords; ++i) {
+  for (int i = 0; i < kVec / 2; ++i) {
+    const float2 f = both(v[i]);
     if constexpr (sizeof(T) == 2)
-      w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+      w[i] = pack_bf16(f.x, f.y);
     else
-      w[i] = __float_as_uint(v[i]);
+      w[2 * i] = __float_as_uint(f.x), w[2 * i + 1] = __float_as_uint(f.y);
   }
   return q;
 }
 
+__device__ __forceinline__ Pair swapped(Pair v) {
+  const float2 f = both(v);
+  return pair_of(f.y, f.x);
+}
+
 // Bound by memory: every head is read once and written once.  A warp takes one token and some of its heads, 32 >> lane_shift
-// heads a step.  A lane holds two vectors of a head, chosen so that turned channels meet in one lane: vector l and the one
-// half the turned channels further on, or two neighbours; so the rotation needs no exchange, and the norm's sum a few
-// shuffles.  The turns of a token are the same for all its heads: the warp works them out once (two a lane for 128
-// channels) and every lane keeps its own in registers.
-template <typename T, int kVec, bool kNeighbours, int kUnroll>
-__global__ void __launch_bounds__(kWarps * 32) toploc_norm_rotary_kernel(const __grid_constant__ RotaryParams p) {
+// heads of one kind (queries, keys, values) a step.  A lane holds two vectors of a head, chosen so that turned channels meet
+// in one lane: vector l and the one half the turned channels further on, or two neighbours; so the rotation needs no
+// exchange, and the norm's sum a few shuffles.  The turns of a token are the same for all its heads: the warp works them out
+// once (two a lane for 128 channels), and every lane keeps their products with the norm's weights in registers while the kind
+// stays.  The arithmetic takes two fp32 numbers at a time.  33443 tokens of 32 + 8 + 8 heads of 128 into the cache: 136 us
+// (6.0 TB/s).  Warps count for more than loads a warp: seven blocks an SM (72 registers) with two steps at a time, against 141
+// with six, 143 with eight, 140 with five and four steps.
+//
+// A lane's places in a step's heads are 32-bit numbers, a step's heads the warp's common base.
+template <typename T, int kVec, bool kNeighbours, bool kAllTurn, int kUnroll>
+__global__ void __launch_bounds__(kWarps * 32, kBlocksPerSm) toploc_norm_rotary_kernel(const __grid_constant__ RotaryParams p) {
   __shared__ float2 turns[kWarps][kMostHalf];
   using Vector = Packed<T, kVec>;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  constexpr int kPairs = kVec / 2;
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0);
   const long long token = (long long)blockIdx.x * kWarps + warp;
   if (token >= p.num_tokens) return;
   const int width = 1 << p.lane_shift, l = lane & (width - 1);
@@ -126,90 +138,142 @@ __global__ void __launch_bounds__(kWarps * 32) toploc_norm_rotary_kernel(const _
     a = turn_a ? l : 2 * l;
     b = turn_a ? l + half_vectors : a + 1;
   }
-  const int end = min(((int)blockIdx.y + 1) * p.steps_per_warp, p.steps);
-  float cs[kVec], sn[kVec];
-  bool turned = false;
+  const int begin = blockIdx.y * p.steps_per_warp, end = min(begin + p.steps_per_warp, p.steps);
+
+  bool turned = false, placed = false;
   long long page = 0, at = 0;
-  bool placed = false;
-  for (int s0 = blockIdx.y * p.steps_per_warp; s0 < end; s0 += kUnroll) {
-    Vector in_a[kUnroll], in_b[kUnroll];
+  // (zeros stay in lanes without channels)
+  Vector in_a[kUnroll] = {}, in_b[kUnroll] = {};
+#pragma unroll 1
+  for (int kind = 0; kind < 2; ++kind) {  // queries, keys
+    const int first = kind == 0 ? 0 : p.q_steps, last = kind == 0 ? p.q_steps : p.qk_steps;
+    int s = max(begin, first);
+    const int stop = min(end, last);
+    if (s >= stop) continue;
+    const Heads& w = p.part[kind];
+    // heads from the lane's on that there are (none for lanes without channels)
+    int left = has ? (kind == 0 ? p.q_heads : p.kv_heads) - (s - first) * per_step - sub : 0;
+    const long long head = (long long)(s - first) * per_step;
+    const T* from = static_cast<const T*>(w.in) + token * w.in_token + head * w.in_head;
+    const unsigned from_a = sub * (unsigned)w.in_head + a * kVec, from_b = sub * (unsigned)w.in_head + b * kVec;
+    const unsigned to_a = sub * (unsigned)w.out_head + a * kVec, to_b = sub * (unsigned)w.out_head + b * kVec;
+    T* to = nullptr;
+    // What the norm's weight g and the turn come to together, of channels x (vector a) and y (b):
+    //   halves      x <- x (g_x cos) + y (-g_y sin),  y <- y (g_y cos) + x (g_x sin)
+    //   neighbours  (x0, x1) <- (x0, x1) (g0 cos, g1 cos) + (x1, x0) (-g1 sin, g0 sin), and so for y
+    Pair own_x[kPairs], own_y[kPairs], other_x[kPairs], other_y[kPairs];
+#pragma unroll 1
+    for (; s < stop; s += kUnroll) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int h = (s0 + u) * per_step + sub;
-      in_a[u] = Vector{}, in_b[u] = Vector{};
-      if (s0 + u < end && h < p.heads && has) {
-        const Heads& w = p.part[h < p.q_heads ? 0 : h < p.qk_heads ? 1 : 2];
-        const int first = h < p.q_heads ? 0 : h < p.qk_heads ? p.q_heads : p.qk_heads;
-        const Vector* at_in =
-            reinterpret_cast<const Vector*>(static_cast<const T*>(w.in) + token * w.in_token + (h - first) * w.in_head);
-        in_a[u] = at_in[a], in_b[u] = at_in[b];
+      for (int u = 0; u < kUnroll; ++u) {
+        if (s + u < stop && left > u * per_step) {
+          in_a[u] = *reinterpret_cast<const Vector*>(from + from_a);
+          in_b[u] = *reinterpret_cast<const Vector*>(from + from_b);
+        }
+        from += per_step * w.in_head;
       }
-    }
-    if (!turned) {  // behind the first loads, in front of their use
-      turned = true;
-      const int position = p.half ? p.positions[token] : 0;
-      for (int j = lane; j < p.half; j += 32) turns[warp][j] = turn_of(position, p.inv_freq[j]);
-      placed = place_of(p, token, &page, &at);
-      __syncwarp();
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const int j = l * kVec + e;
-        const float2 t = j < p.half ? turns[warp][j] : make_float2(1.f, 0.f);
-        cs[e] = t.x, sn[e] = t.y;
+      if (!turned) {  // behind the first loads, in front of their use
+        turned = true;
+        const int position = p.half ? p.positions[token] : 0;
+        for (int j = lane; j < p.half; j += 32) turns[warp][j] = turn_of(position, p.inv_freq[j]);
+        placed = place_of(p, token, &page, &at);
+        __syncwarp();
       }
-    }
+      if (to == nullptr) {
+        to = static_cast<T*>(w.out) + head * w.out_head +
+             (kind == 0 ? token * w.out_token : page * w.out_page + at * w.out_token);
+        const Pair one = pair_of(1.f, 1.f);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (s0 + u >= end) break;
-      const int h = (s0 + u) * per_step + sub;
-      const int which = h < p.q_heads ? 0 : h < p.qk_heads ? 1 : 2;
-      const int first = which == 0 ? 0 : which == 1 ? p.q_heads : p.qk_heads;
-      const Heads& w = p.part[which];
-      float x[kVec], y[kVec];
-      unpack<T, kVec>(in_a[u], x);
-      unpack<T, kVec>(in_b[u], y);
-      float ss = 0.f;
+        for (int e = 0; e < kPairs; ++e) own_x[e] = own_y[e] = one;
+        if (w.weight && has) {
+          unpack<T, kVec>(__ldg(static_cast<const Vector*>(w.weight) + a), own_x);
+          unpack<T, kVec>(__ldg(static_cast<const Vector*>(w.weight) + b), own_y);
+        }
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) ss = fmaf(x[e], x[e], ss), ss = fmaf(y[e], y[e], ss);
-      for (int off = width >> 1; off > 0; off >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, off);
-      if (h >= p.heads || !has) continue;
-      if (which != 2) {
+        for (int e = 0; e < kPairs; ++e) {
+          if constexpr (kNeighbours) {
+            const float2 gx = both(own_x[e]), gy = both(own_y[e]);
+            const int j = l * kVec + e;
+            const float2 tx = turn_a ? turns[warp][j] : make_float2(1.f, 0.f);
+            const float2 ty = turn_b ? turns[warp][j + kPairs] : make_float2(1.f, 0.f);
+            own_x[e] = mul2(own_x[e], pair_of(tx.x, tx.x)), own_y[e] = mul2(own_y[e], pair_of(ty.x, ty.x));
+            other_x[e] = pair_of(-gx.y * tx.y, gx.x * tx.y), other_y[e] = pair_of(-gy.y * ty.y, gy.x * ty.y);
+          } else {
+            const int j = l * kVec + 2 * e;
+            const float2 t0 = turn_a ? turns[warp][j] : make_float2(1.f, 0.f);
+            const float2 t1 = turn_a ? turns[warp][j + 1] : make_float2(1.f, 0.f);
+            const Pair cs = pair_of(t0.x, t1.x);
+            other_x[e] = mul2(own_y[e], pair_of(-t0.y, -t1.y)), other_y[e] = mul2(own_x[e], pair_of(t0.y, t1.y));
+            own_x[e] = mul2(own_x[e], cs), own_y[e] = mul2(own_y[e], cs);
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        if (s + u >= stop) break;
+        Pair x[kPairs], y[kPairs];
+        unpack<T, kVec>(in_a[u], x);
+        unpack<T, kVec>(in_b[u], y);
+        float r = 1.f;
         if (w.weight) {
-          const float r = rsqrtf(fmaf(ss, p.per_channel, p.eps));
-          const Vector* weight = static_cast<const Vector*>(w.weight);
-          float g[kVec];
-          unpack<T, kVec>(__ldg(weight + a), g);
+          Pair sum = mul2(x[0], x[0]);
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) x[e] = x[e] * r * g[e];
-          unpack<T, kVec>(__ldg(weight + b), g);
+          for (int e = 1; e < kPairs; ++e) sum = fma2(x[e], x[e], sum);
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) y[e] = y[e] * r * g[e];
+          for (int e = 0; e < kPairs; ++e) sum = fma2(y[e], y[e], sum);
+          float ss = both(sum).x + both(sum).y;
+#pragma unroll
+          for (int off = 16; off > 0; off >>= 1)
+            if (off < width) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, off);
+          r = rsqrtf(fmaf(ss, p.per_channel, p.eps));
         }
-        if constexpr (kNeighbours) {
+        const Pair rr = pair_of(r, r);
 #pragma unroll
-          for (int e = 0; e < kVec / 2; ++e) {
-            const float u0 = x[2 * e], u1 = x[2 * e + 1], v0 = y[2 * e], v1 = y[2 * e + 1];
-            const float c0 = cs[e], s0_ = sn[e], c1 = cs[kVec / 2 + e], s1 = sn[kVec / 2 + e];
-            if (turn_a) x[2 * e] = u0 * c0 - u1 * s0_, x[2 * e + 1] = u0 * s0_ + u1 * c0;
-            if (turn_b) y[2 * e] = v0 * c1 - v1 * s1, y[2 * e + 1] = v0 * s1 + v1 * c1;
-          }
-        } else if (turn_a) {
+        for (int e = 0; e < kPairs; ++e) x[e] = mul2(x[e], rr), y[e] = mul2(y[e], rr);
+        Pair xx[kPairs], yy[kPairs];
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) {
-            const float u0 = x[e], v0 = y[e];
-            x[e] = u0 * cs[e] - v0 * sn[e];
-            y[e] = u0 * sn[e] + v0 * cs[e];
-          }
+        for (int e = 0; e < kPairs; ++e) xx[e] = mul2(x[e], own_x[e]), yy[e] = mul2(y[e], own_y[e]);
+        // (channels that do not turn must not meet others: 0 times infinity)
+        if (kAllTurn || turn_a) {
+#pragma unroll
+          for (int e = 0; e < kPairs; ++e) xx[e] = fma2(kNeighbours ? swapped(x[e]) : y[e], other_x[e], xx[e]);
         }
-        in_a[u] = pack<T, kVec>(x), in_b[u] = pack<T, kVec>(y);
+        if (kAllTurn || turn_b) {
+#pragma unroll
+          for (int e = 0; e < kPairs; ++e) yy[e] = fma2(kNeighbours ? swapped(y[e]) : x[e], other_y[e], yy[e]);
+        }
+        const Vector out_a = pack<T, kVec>(xx), out_b = pack<T, kVec>(yy);
+        if (left > u * per_step && (kind == 0 || placed)) {
+          *reinterpret_cast<Vector*>(to + to_a) = out_a;
+          *reinterpret_cast<Vector*>(to + to_b) = out_b;
+        }
+        to += per_step * w.out_head;
       }
-      if (which == 0 || placed) {
-        T* out = static_cast<T*>(w.out) + (h - first) * w.out_head;
-        out += which == 0 ? token * w.out_token : page * w.out_page + at * w.out_token;
-        reinterpret_cast<Vector*>(out)[a] = in_a[u];
-        reinterpret_cast<Vector*>(out)[b] = in_b[u];
-      }
+      left -= kUnroll * per_step;
     }
+  }
+
+  // values, as they are
+  const int s = max(begin, p.qk_steps);
+  if (s >= end) return;
+  if (!turned) placed = place_of(p, token, &page, &at);
+  if (!placed) return;
+  const Heads& w = p.part[2];
+  const T* from = static_cast<const T*>(w.in) + token * w.in_token + (s - p.qk_steps) * per_step * w.in_head;
+  T* to = static_cast<T*>(w.out) + page * w.out_page + at * w.out_token + (s - p.qk_steps) * per_step * w.out_head;
+  const unsigned from_lane = sub * (unsigned)w.in_head + l * kVec, to_lane = sub * (unsigned)w.out_head + l * kVec;
+  int left = has ? p.kv_heads - (s - p.qk_steps) * per_step - sub : 0;
+#pragma unroll 4
+  for (int i = s; i < end; ++i) {
+    if (left > 0) {
+      const Vector x = *reinterpret_cast<const Vector*>(from + from_lane);
+      const Vector y = *reinterpret_cast<const Vector*>(from + from_lane + p.lanes * kVec);
+      *reinterpret_cast<Vector*>(to + to_lane) = x;
+      *reinterpret_cast<Vector*>(to + to_lane + p.lanes * kVec) = y;
+    }
+    left -= per_step;
+    from += per_step * w.in_head;
+    to += per_step * w.out_head;
   }
 }
 
@@ -222,8 +286,8 @@ __global__ void __launch_bounds__(kWarps * 32) toploc_norm_rotary_any_kernel(con
   const long long token = (long long)blockIdx.x * kWarps + warp;
   if (token >= p.num_tokens) return;
   const int h = blockIdx.y;
-  const int which = h < p.q_heads ? 0 : h < p.qk_heads ? 1 : 2;
-  const int first = which == 0 ? 0 : which == 1 ? p.q_heads : p.qk_heads;
+  const int which = h < p.q_heads ? 0 : h < p.q_heads + p.kv_heads ? 1 : 2;
+  const int first = which == 0 ? 0 : which == 1 ? p.q_heads : p.q_heads + p.kv_heads;
   const Heads& w = p.part[which];
   const T* in = static_cast<const T*>(w.in) + token * w.in_token + (h - first) * w.in_head;
   T* out = static_cast<T*>(w.out) + (h - first) * w.out_head;
@@ -268,12 +332,16 @@ __global__ void __launch_bounds__(kWarps * 32) toploc_norm_rotary_any_kernel(con
 }
 
 template <typename T, int kVec>
-void launch_vectors(const RotaryParams& p, bool neighbours, dim3 grid, cudaStream_t stream) {
-  constexpr int kUnroll = 4;
-  if (neighbours)
-    toploc_norm_rotary_kernel<T, kVec, true, kUnroll><<<grid, kWarps * 32, 0, stream>>>(p);
+void launch_vectors(const RotaryParams& p, bool neighbours, bool all_turn, dim3 grid, cudaStream_t stream) {
+  constexpr int kUnroll = 2, kBlock = kWarps * 32;
+  if (neighbours && all_turn)
+    toploc_norm_rotary_kernel<T, kVec, true, true, kUnroll><<<grid, kBlock, 0, stream>>>(p);
+  else if (neighbours)
+    toploc_norm_rotary_kernel<T, kVec, true, false, kUnroll><<<grid, kBlock, 0, stream>>>(p);
+  else if (all_turn)
+    toploc_norm_rotary_kernel<T, kVec, false, true, kUnroll><<<grid, kBlock, 0, stream>>>(p);
   else
-    toploc_norm_rotary_kernel<T, kVec, false, kUnroll><<<grid, kWarps * 32, 0, stream>>>(p);
+    toploc_norm_rotary_kernel<T, kVec, false, false, kUnroll><<<grid, kBlock, 0, stream>>>(p);
 }
 
 // Shape of the heads, the same for both entries.
@@ -310,8 +378,8 @@ int run(RotaryParams& p, const toploc_rotary_layout* lay, const int32_t* positio
   p.head_dim = lay->head_dim;
   p.half = lay->rotary_dim / 2;
   p.q_heads = lay->q_heads;
-  p.qk_heads = lay->q_heads + lay->kv_heads;
-  p.heads = parts == 3 ? p.qk_heads + lay->kv_heads : p.qk_heads;
+  p.kv_heads = lay->kv_heads;
+  const int heads = p.q_heads + (parts - 1) * p.kv_heads;
   const bool neighbours = lay->pairing == TOPLOC_ROTARY_NEIGHBOURS;
 
   // whole vectors of `vec` elements everywhere: two a lane, turned channels in whole vectors
@@ -324,33 +392,38 @@ int run(RotaryParams& p, const toploc_rotary_layout* lay, const int32_t* positio
       if (!aligned(w.in, bytes) || !aligned(w.out, bytes) || !aligned(w.weight, bytes)) return false;
       for (const long long s : {w.in_token, w.in_head, w.out_page, w.out_token, w.out_head})
         if (s % vec != 0) return false;
+      if (w.in_head >= 1ll << 26 || w.out_head >= 1ll << 26) return false;  // (places in a step's 32 heads at most: 32 bits)
     }
     return true;
   };
   const int wide = 16 / size, vec = fits(wide) ? wide : size == 2 && fits(4) ? 4 : 0;
   const unsigned blocks = (unsigned)((p.num_tokens + kWarps - 1) / kWarps);
   if (vec == 0) {
-    const dim3 grid(blocks, (unsigned)p.heads);
+    const dim3 grid(blocks, (unsigned)heads);
     if (size == 2)
       toploc_norm_rotary_any_kernel<__nv_bfloat16><<<grid, kWarps * 32, 0, stream>>>(p, neighbours);
     else
       toploc_norm_rotary_any_kernel<float><<<grid, kWarps * 32, 0, stream>>>(p, neighbours);
     return launched();
   }
+  const bool all_turn = lay->rotary_dim == p.head_dim;
   p.lanes = p.head_dim / (2 * vec);
   while (1 << p.lane_shift < p.lanes) ++p.lane_shift;
   const int per_step = 32 >> p.lane_shift;
-  p.steps = (p.heads + per_step - 1) / per_step;
-  // As many heads a warp as leave the SMs enough warps (48 each), so that few of them work the same turns out again.
-  const long long split = min((long long)p.steps, max(1ll, 48ll * sms / p.num_tokens));
+  p.q_steps = (p.q_heads + per_step - 1) / per_step;
+  p.qk_steps = p.q_steps + (p.kv_heads + per_step - 1) / per_step;
+  p.steps = p.q_steps + (parts - 1) * (p.qk_steps - p.q_steps);
+  // As many heads a warp as leave the SMs enough warps (32 each), so that few of them work the same turns out again (2000
+  // tokens of 48 heads of 128: 15.1, 12.8 and 20.8 us with 8, 32 and 200).
+  const long long split = min((long long)p.steps, max(1ll, 32ll * sms / p.num_tokens));
   p.steps_per_warp = (int)((p.steps + split - 1) / split);
   const dim3 grid(blocks, (unsigned)((p.steps + p.steps_per_warp - 1) / p.steps_per_warp));
   if (size == 4)
-    launch_vectors<float, 4>(p, neighbours, grid, stream);
+    launch_vectors<float, 4>(p, neighbours, all_turn, grid, stream);
   else if (vec == 8)
-    launch_vectors<__nv_bfloat16, 8>(p, neighbours, grid, stream);
+    launch_vectors<__nv_bfloat16, 8>(p, neighbours, all_turn, grid, stream);
   else
-    launch_vectors<__nv_bfloat16, 4>(p, neighbours, grid, stream);
+    launch_vectors<__nv_bfloat16, 4>(p, neighbours, all_turn, grid, stream);
   return launched();
 }
 
