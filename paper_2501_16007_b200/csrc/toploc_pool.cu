@@ -22,6 +22,7 @@ constexpr int kMostBlocks = 8;                 // of a planner's cluster
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;          // of a block
 constexpr long long kOneBlock = 16384;         // entries and pages that one block plans for
+constexpr long long kOneCluster = 65536;      // of a release that one cluster does
 constexpr int kAtOnce = 4;                     // loads of a thread on their way at once
 
 struct PoolParams {
@@ -321,66 +322,114 @@ __global__ void __launch_bounds__(kThreads, 1) toploc_fork_pages_kernel(const __
 
 // ---- releases ------------------------------------------------------------------------------------
 
+// What a sequence's length and status become; pages of those that are released.
+__device__ __forceinline__ void release_sequence(const PoolParams& p, int i) {
+  const int len = p.kv_lens[i];
+  int status = TOPLOC_SEQ_OK;
+  const bool gone = p.release[i] != 0;
+  if (gone) held_pages(p, len, &status);
+  p.kv_lens_out[i] = gone ? 0 : len;
+  p.status[i] = (uint8_t)status;
+}
+__device__ __forceinline__ int released_pages(const PoolParams& p, int i) {
+  int status;
+  return p.release[i] != 0 ? held_pages(p, p.kv_lens[i], &status) : 0;
+}
+// A holder less; below zero: nobody is left.
+__device__ __forceinline__ void release_entry(const PoolParams& p, int seq, int32_t page) {
+  if ((unsigned)page < (unsigned)p.num_pages)
+    atomicSub(p.shares_out + page, 1);
+  else
+    p.status[seq] = TOPLOC_SEQ_BAD_PAGE;
+}
+
+// Large releases take three launches: eight SMs send an atomic every other clock each, so the sequences' pages (65 thousand:
+// 10 of 22 us) are spread over all SMs, and so is the copy of the shares; the numbering behind them stays with the cluster.
+constexpr int kWideThreads = 256;
+constexpr int kEntriesAtOnce = 32 * kAtOnce;  // of a row, a warp's
+
+__global__ void __launch_bounds__(kWideThreads) toploc_release_begin_kernel(const __grid_constant__ PoolParams p) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  const int all = gridDim.x * kWideThreads, tid = blockIdx.x * kWideThreads + threadIdx.x;
+  for (long long i = tid; i < p.num_pages; i += all) p.shares_out[i] = p.shares[i];
+  for (int i = tid; i < p.num_seqs; i += all) release_sequence(p, i);
+}
+
+__global__ void __launch_bounds__(kWideThreads) toploc_release_entries_kernel(const __grid_constant__ PoolParams p) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int lane = threadIdx.x & 31, parts = (p.max_pages + kEntriesAtOnce - 1) / kEntriesAtOnce;
+  const long long warps = gridDim.x * (kWideThreads / 32), items = (long long)p.num_seqs * parts;
+  for (long long item = blockIdx.x * (kWideThreads / 32) + threadIdx.x / 32; item < items; item += warps) {
+    const int seq = (int)(item / parts), first = (int)(item - (long long)seq * parts) * kEntriesAtOnce + lane;
+    const int pages = released_pages(p, seq);
+    int32_t page[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (first + k * 32 < pages) page[k] = p.table[seq * p.table_stride + first + k * 32];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (first + k * 32 < pages) release_entry(p, seq, page[k]);
+  }
+}
+
+// kAll: the whole release, else what is left to do behind the two kernels above.
+template <bool kAll>
 __global__ void __launch_bounds__(kThreads, 1) toploc_release_pages_kernel(const __grid_constant__ PoolParams p) {
   __shared__ int counts[kMostBlocks * kWarps];
   const Team team;
   const int lane = threadIdx.x & 31, all_tid = team.all_tid;
 
-  copy_vector(p.shares_out, p.shares, p.num_pages, team);
-  for (int i = all_tid; i < p.num_seqs; i += team.all_threads) {
-    const int len = p.kv_lens[i];
-    int status = TOPLOC_SEQ_OK;
-    const bool gone = p.release[i] != 0;
-    if (gone) held_pages(p, len, &status);
-    p.kv_lens_out[i] = gone ? 0 : len;
-    p.status[i] = (uint8_t)status;
+  if constexpr (kAll) {
+    copy_vector(p.shares_out, p.shares, p.num_pages, team);
+    for (int i = all_tid; i < p.num_seqs; i += team.all_threads) release_sequence(p, i);
+    team.sync();
+    for_entries(
+        p, team, p.table, p.table_stride, [&](int row) { return released_pages(p, row); },
+        [&](const int* rows, int, const int32_t* page, const bool* valid) {
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i)
+            if (valid[i]) release_entry(p, rows[i], page[i]);
+        });
+  } else {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
   }
   team.sync();
 
-  // a holder less for every entry; below zero: nobody is left
-  for_entries(
-      p, team, p.table, p.table_stride,
-      [&](int row) {
-        int status;
-        return p.release[row] != 0 ? held_pages(p, p.kv_lens[row], &status) : 0;
-      },
-      [&](const int* rows, int, const int32_t* page, const bool* valid) {
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-          if (!valid[i]) continue;
-          if ((unsigned)page[i] < (unsigned)p.num_pages)
-            atomicSub(p.shares_out + page[i], 1);
-          else
-            p.status[rows[i]] = TOPLOC_SEQ_BAD_PAGE;
-        }
-      });
-  team.sync();
-
+  // the pages that came back: counted, then numbered in order
   int begin, end, count = 0, total;
   const int each = groups_each(p, team);
   pages_of_warp(p, each, team.warp_of_all, &begin, &end);
-  for_pages(p.shares_out, begin, end, [&](int, int left) { count += left < 0; });
-  tell_count(team, counts, warp_total(count));
+  unsigned mine = 0;  // lane k: those of the range's k-th group of 32
+  int group = 0;
+  for_pages(p.shares_out, begin, end, [&](int, int left) {
+    const unsigned freed = __ballot_sync(0xFFFFFFFFu, left < 0);
+    if (lane == group) mine = freed;
+    count += __popc(freed);
+    ++group;
+  });
+  tell_count(team, counts, count);
   team.sync();
 
   int place = counted_before(team, counts, team.warp_of_all, &total);
   const int room = min(max(p.first_free[0], 0), p.num_free), fit = min(total, room);
-  for_pages(p.shares_out, begin, end, [&](int i, int left) {
-    const unsigned freed = __ballot_sync(0xFFFFFFFFu, left < 0);
-    if (left < 0) {
+  const auto give_back = [&](int i, unsigned freed) {
+    if (freed >> lane & 1) {
       const int at = place + __popc(freed & ((1u << lane) - 1));
       if (at < fit) p.free_out[room - fit + at] = i;
       p.shares_out[i] = 0;
     }
     place += __popc(freed);
-  });
+  };
+  if (each <= 32) {
+    for (int k = 0; k < group; ++k) give_back(begin + k * 32 + lane, __shfl_sync(0xFFFFFFFFu, mine, k));
+  } else {
+    for_pages(p.shares_out, begin, end, [&](int i, int left) { give_back(i, __ballot_sync(0xFFFFFFFFu, left < 0)); });
+  }
   if (all_tid == 0) p.next_free[0] = room - fit;
   if (total > room) {
-    for (int i = all_tid; i < p.num_seqs; i += team.all_threads) {
-      int status;
-      if (p.release[i] != 0 && held_pages(p, p.kv_lens[i], &status) > 0 && status_of(p, i) == TOPLOC_SEQ_OK)
-        p.status[i] = TOPLOC_SEQ_NO_ROOM;
-    }
+    for (int i = all_tid; i < p.num_seqs; i += team.all_threads)
+      if (released_pages(p, i) > 0 && status_of(p, i) == TOPLOC_SEQ_OK) p.status[i] = TOPLOC_SEQ_NO_ROOM;
   }
 }
 
@@ -609,26 +658,38 @@ int check_memory(const Argument (&in)[kIn], const Argument (&out)[kOut]) {
   return TOPLOC_OK;
 }
 
-// One block, or a cluster of eight where the entries (at most) and pages make many rounds for one.
+// A launch of `blocks` blocks, in clusters of `cluster`; early: it may begin before the one in front of it has ended (and waits
+// for that end itself).
 template <typename Kernel>
-int launch_planner(Kernel kernel, const PoolParams& p, void* cuda_stream) {
-  const long long work = (long long)p.num_seqs * p.max_pages + p.num_pages;
+int launch(Kernel kernel, const PoolParams& p, unsigned blocks, unsigned threads, unsigned cluster, bool early,
+           void* cuda_stream) {
   cudaLaunchConfig_t config = {};
-  cudaLaunchAttribute cluster[1];
-  const unsigned blocks = work <= kOneBlock ? 1 : kMostBlocks;
+  cudaLaunchAttribute attributes[2];
   config.gridDim = dim3(blocks);
-  config.blockDim = dim3(kThreads);
+  config.blockDim = dim3(threads);
   config.stream = static_cast<cudaStream_t>(cuda_stream);
-  cluster[0].id = cudaLaunchAttributeClusterDimension;
-  cluster[0].val.clusterDim.x = blocks;
-  cluster[0].val.clusterDim.y = cluster[0].val.clusterDim.z = 1;
-  config.attrs = cluster;
-  config.numAttrs = 1;
+  attributes[0].id = cudaLaunchAttributeClusterDimension;
+  attributes[0].val.clusterDim.x = cluster;
+  attributes[0].val.clusterDim.y = attributes[0].val.clusterDim.z = 1;
+  attributes[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attributes[1].val.programmaticStreamSerializationAllowed = 1;
+  config.attrs = attributes;
+  config.numAttrs = early ? 2 : 1;
   if (cudaLaunchKernelEx(&config, kernel, p) != cudaSuccess) {
     cudaGetLastError();
     return TOPLOC_ERR_CUDA;
   }
   return launched();
+}
+
+// Entries (at most) and pages of a plan.
+long long work_of(const PoolParams& p) { return (long long)p.num_seqs * p.max_pages + p.num_pages; }
+
+// One block, or a cluster of eight where the work makes many rounds for one.
+template <typename Kernel>
+int launch_planner(Kernel kernel, const PoolParams& p, void* cuda_stream) {
+  const unsigned blocks = work_of(p) <= kOneBlock ? 1 : kMostBlocks;
+  return launch(kernel, p, blocks, kThreads, blocks, false, cuda_stream);
 }
 
 }  // namespace
@@ -669,14 +730,19 @@ extern "C" int toploc_release_pages(const uint8_t* d_release, const int32_t* d_k
   const Argument out[] = {{d_free_pages, num_free * 4ll}, {d_kv_lens_out, seqs}, {d_shares_out, pages}, {d_next_free, 4},
                           {d_status, num_seqs, 1}};
   if (const int rc = check_memory(in, out)) return rc;
-  if (const int rc = check_device()) return rc;
+  int sms = 0;
+  if (const int rc = check_device(&sms)) return rc;
   PoolParams p = {};
   p.release = d_release, p.kv_lens = d_kv_lens, p.shares = d_shares, p.first_free = d_first_free;
   p.table = const_cast<int32_t*>(d_block_table), p.table_stride = table_stride;
   p.free_out = d_free_pages, p.kv_lens_out = d_kv_lens_out, p.shares_out = d_shares_out, p.next_free = d_next_free;
   p.status = d_status;
   p.num_seqs = num_seqs, p.num_pages = num_pages, p.num_free = num_free, p.page_size = page_size, p.max_pages = max_pages;
-  return launch_planner(toploc_release_pages_kernel, p, cuda_stream);
+  if (work_of(p) <= kOneCluster) return launch_planner(toploc_release_pages_kernel<true>, p, cuda_stream);
+  const unsigned blocks = (unsigned)(2 * sms);
+  if (const int rc = launch(toploc_release_begin_kernel, p, blocks, kWideThreads, 1, false, cuda_stream)) return rc;
+  if (const int rc = launch(toploc_release_entries_kernel, p, 4 * blocks, kWideThreads, 1, true, cuda_stream)) return rc;
+  return launch(toploc_release_pages_kernel<false>, p, kMostBlocks, kThreads, kMostBlocks, true, cuda_stream);
 }
 
 extern "C" int toploc_compact_pages(const int32_t* d_kv_lens, int32_t num_seqs, const int32_t* d_block_table,
