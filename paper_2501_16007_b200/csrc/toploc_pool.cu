@@ -226,34 +226,60 @@ __global__ void __launch_bounds__(kThreads, 1) toploc_fork_pages_kernel(const __
   const Team team;
   const int tid = threadIdx.x, lane = tid & 31, all_tid = team.all_tid;
 
-  // who can be forked
+  asm volatile("griddepcontrol.launch_dependents;");  // the copies may get ready
+
+  // who can be forked: a lane a sequence, then the warp a parent's row
   copy_vector(p.shares_out, p.shares, p.num_pages, team);
-  for (int i = team.warp_of_all; i < p.num_seqs; i += team.all_warps) {
-    const int parent = p.parents[i], own = p.kv_lens[i];
-    int status = TOPLOC_SEQ_OK, len = own;
+#pragma unroll 1
+  for (int base = team.warp_of_all; base < p.num_seqs; base += team.all_warps * 32) {
+    const int i = base + lane * team.all_warps;
+    int parent = -1, status = TOPLOC_SEQ_OK, own = 0, len = 0, pages = 0;
+    if (i < p.num_seqs) {
+      parent = p.parents[i];
+      own = len = p.kv_lens[i];
+    }
     if (parent >= 0) {
-      if (parent >= p.num_seqs || p.parents[parent] >= 0) {
+      const bool there = parent < p.num_seqs;
+      const int theirs = there ? p.kv_lens[parent] : 0;
+      if (!there || p.parents[parent] >= 0) {
         status = TOPLOC_SEQ_BAD_PARENT;
       } else if (own != 0) {
         status = TOPLOC_SEQ_IN_USE;
       } else {
-        len = p.kv_lens[parent];
-        const int pages = len < 0 ? 0 : pages_for(len, p.page_size);
-        if (len < 0 || pages > p.max_pages) {
-          status = TOPLOC_SEQ_BAD_LENGTH;
-        } else {
-          const int32_t* row = p.table + parent * p.table_stride;
-          bool bad = false;
-          for (int j = lane; j < pages; j += 32) bad = bad || (unsigned)row[j] >= (unsigned)p.num_pages;
-          if (__any_sync(0xFFFFFFFFu, bad))
-            status = TOPLOC_SEQ_BAD_PAGE;
-          else if (len % p.page_size > 0)
-            status = kNeedsPage;
-        }
+        pages = held_pages(p, theirs, &status);
+        len = theirs;
+        if (status == TOPLOC_SEQ_OK && len % p.page_size > 0) status = kNeedsPage;
       }
     }
-    if (lane == 0) {
-      p.kv_lens_out[i] = status == TOPLOC_SEQ_OK || status == kNeedsPage ? len : own;
+    if ((status & ~kNeedsPage) != TOPLOC_SEQ_OK) len = own, pages = 0;
+    const int most = __reduce_max_sync(0xFFFFFFFFu, pages);
+    if (most > 0) {  // entries outside the pool, of all the lanes' parents
+      const int count = min(32, (p.num_seqs - base + team.all_warps - 1) / team.all_warps);
+#pragma unroll 1
+      for (int first = 0; first < count; first += kAtOnce) {
+        bool bad[kAtOnce] = {};
+        int held[kAtOnce], from[kAtOnce], longest = 0;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          held[k] = first + k < 32 ? __shfl_sync(0xFFFFFFFFu, pages, (first + k) & 31) : 0;
+          from[k] = __shfl_sync(0xFFFFFFFFu, parent, (first + k) & 31);
+          longest = max(longest, held[k]);
+        }
+#pragma unroll 1
+        for (int j = lane; j < longest; j += 32) {
+          int32_t page[kAtOnce];
+#pragma unroll
+          for (int k = 0; k < kAtOnce; ++k) page[k] = j < held[k] ? p.table[from[k] * p.table_stride + j] : 0;
+#pragma unroll
+          for (int k = 0; k < kAtOnce; ++k) bad[k] = bad[k] || (j < held[k] && (unsigned)page[k] >= (unsigned)p.num_pages);
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+          if (__any_sync(0xFFFFFFFFu, bad[k]) && lane == first + k) status = TOPLOC_SEQ_BAD_PAGE, len = own;
+      }
+    }
+    if (i < p.num_seqs) {
+      p.kv_lens_out[i] = len;
       p.status[i] = (uint8_t)status;
     }
   }
@@ -441,6 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1) toploc_compact_pages_kernel(const
   const Team team;
   const int lane = threadIdx.x & 31, all_tid = team.all_tid;
   int32_t* marks = p.shares_out;
+  asm volatile("griddepcontrol.launch_dependents;");  // the copies may get ready
 
   for (int i = all_tid; i < p.num_pages; i += team.all_threads) {
     marks[i] = 0;
@@ -538,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) toploc_compact_pages_kernel(const
 
 constexpr int kMostCaches = 128;  // of a launch
 constexpr int kCopyThreads = 256;
-constexpr int kUnits = 4;         // a thread's, of a chunk
+constexpr int kUnits = 8;         // a thread's, of a chunk
 
 struct CopyParams {
   void* caches[kMostCaches];
@@ -552,11 +579,12 @@ struct CopyParams {
 };
 
 // Bound by memory: a page is read once and written once.  The number of copies is known on the device alone, so the blocks
-// share out what there is: (cache, copy, chunk of a page), four 16-byte loads in flight a thread.  A cache's copies are done
+// share out what there is: (cache, copy, chunk of a page), eight 16-byte loads in flight a thread.  A cache's copies are done
 // together, so that a page which is copied several times (the last one of a prompt with many samples) comes from L2 from the
 // second time on.
 template <typename Unit>
 __global__ void __launch_bounds__(kCopyThreads) toploc_copy_pages_kernel(const __grid_constant__ CopyParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int copies = min(max(p.count[0], 0), p.most);
   const long long per_cache = (long long)copies * p.chunks, tasks = per_cache * p.num_caches;
   // (the task's pages are looked up while the one in front is copied)
@@ -599,9 +627,22 @@ __global__ void __launch_bounds__(kCopyThreads) toploc_copy_pages_kernel(const _
   }
 }
 
+// (It may begin before the plan in front of it has ended, and waits for that end itself.)
 template <typename Unit>
 int launch_copy(const CopyParams& p, int blocks, cudaStream_t stream) {
-  toploc_copy_pages_kernel<Unit><<<blocks, kCopyThreads, 0, stream>>>(p);
+  cudaLaunchConfig_t config = {};
+  cudaLaunchAttribute early[1];
+  config.gridDim = dim3((unsigned)blocks);
+  config.blockDim = dim3(kCopyThreads);
+  config.stream = stream;
+  early[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early[0].val.programmaticStreamSerializationAllowed = 1;
+  config.attrs = early;
+  config.numAttrs = 1;
+  if (cudaLaunchKernelEx(&config, toploc_copy_pages_kernel<Unit>, p) != cudaSuccess) {
+    cudaGetLastError();
+    return TOPLOC_ERR_CUDA;
+  }
   return launched();
 }
 
