@@ -480,14 +480,14 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<T>)
     } else if (lane == 0) {
       sh.part = all;
     }
-    if (kTops) {  // the bound: the top-th largest of the warps' four largest thread maxima, each of them another logit
-      unsigned mine = sh.warp_best[lane];
-      warp_sort(mine, 0);
-      mine = __shfl_sync(0xFFFFFFFFu, mine, p.top - 1);
-      if (lane == 0) {
-        sh.bound = mine == 0 ? -FLT_MAX : value_of(mine);  // (every logit above -inf)
-        sh.num_pairs = sh.num_keys = 0;
-      }
+  }
+  if (kTops && warp == 1) {  // the bound: the top-th largest of the warps' four largest thread maxima, each of them another logit
+    unsigned mine = sh.warp_best[lane];
+    warp_sort(mine, 0);
+    mine = __shfl_sync(0xFFFFFFFFu, mine, p.top - 1);
+    if (lane == 0) {
+      sh.bound = mine == 0 ? -FLT_MAX : value_of(mine);  // (every logit above -inf)
+      sh.num_pairs = sh.num_keys = 0;
     }
   }
   if constexpr (kTops) {
@@ -518,30 +518,25 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<T>)
   }
   if (blocks > 1) {  // the row, from the cluster's shares
     cluster.sync();
+    unsigned long long mine = 0;
     if (rank == 0) {
       if (warp == 0) {
         const Part all = join_parts(cluster.map_shared_rank(&sh, lane % blocks)->part, blocks);
-        const Whole whole = {all.top, all.s, all.w, log2f(all.s)};
-        if (lane == 0) {
-          sh.whole = whole;
-          write_row(p, r, whole, known, given);
-        }
+        if (lane == 0) sh.whole = {all.top, all.s, all.w, log2f(all.s)};
       }
+      if (kTops && tid < blocks * p.top) mine = cluster.map_shared_rank(&sh, tid / p.top)->best[tid % p.top];
+      sh.keys[tid] = mine;
+    }
+    const int held = __syncthreads_count(mine != 0);
+    // (the other blocks may leave now: their shared memory has been read)
+    auto token_of_barrier = cluster.barrier_arrive();
+    if (rank == 0) {
+      if (tid == 0) write_row(p, r, sh.whole, known, given);
       if constexpr (kTops) {
-        const bool has = tid < blocks * p.top;
-        const unsigned long long mine = has ? cluster.map_shared_rank(&sh, tid / p.top)->best[tid % p.top] : 0;
-        sh.keys[tid] = mine;
-        const int held = __syncthreads_count(mine != 0);
         if (mine != 0) {
           int above = 0;
-          for (int i = 0; i < blocks; ++i) {  // (each block's are in order)
-            int lo = 0, hi = p.top;
-            while (lo < hi) {
-              const int mid = (lo + hi) >> 1;
-              if (sh.keys[i * p.top + mid] > mine) lo = mid + 1; else hi = mid;
-            }
-            above += lo;
-          }
+#pragma unroll 8
+          for (int i = 0; i < blocks * p.top; ++i) above += sh.keys[i] > mine;
           if (above < p.top) {
             p.top_ids[r * p.top + above] = (int64_t)(0xFFFFFFFFu - (unsigned)mine);
             p.top_logprobs[r * p.top + above] = logprob_of(sh.whole, value_of((unsigned)(mine >> 32)));
@@ -553,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<T>)
         }
       }
     }
-    cluster.sync();  // nobody leaves while its shared memory is read
+    cluster.barrier_wait(std::move(token_of_barrier));
   }
 }
 
