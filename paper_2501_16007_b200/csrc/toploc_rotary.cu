@@ -367,6 +367,11 @@ int run(RotaryParams& p, const toploc_rotary_layout* lay, const int32_t* positio
     if (!w.in || !w.out || !aligned(w.in, size) || !aligned(w.out, size) || !aligned(w.weight, size) || w.in_token < 0 ||
         w.in_head < 0 || w.out_page < 0 || w.out_token < 0 || w.out_head < 0)
       return TOPLOC_ERR_INVALID_ARGUMENT;
+    // in place, but not each head at its own place
+    const int heads = i == 0 ? lay->q_heads : lay->kv_heads;
+    if (w.in == w.out && (i == 0 || parts == 2) &&
+        ((lay->num_tokens > 1 && w.in_token != w.out_token) || (heads > 1 && w.in_head != w.out_head)))
+      return TOPLOC_ERR_INVALID_ARGUMENT;
   }
   int sms = 0;
   if (const int rc = check_device(&sms)) return rc;

@@ -96,6 +96,10 @@ def test_rotary_argument_refusals(lib):
     assert paged(lib, kv=kv_layout(page_size=0)) == INVALID and paged(lib, kv=kv_layout(num_pages=-1)) == INVALID
     assert paged(lib, kv=kv_layout(v_page_stride=-1)) == INVALID
     assert prompt(lib, rotary_layout(num_tokens=0), q=None) == 0
+    assert passes(prompt, lib, qo=at(0), ko=at(1))                                     # in place
+    assert prompt(lib, rotary_layout(q_out_token_stride=2048), qo=at(0)) == INVALID    # but every head at its own place
+    assert prompt(lib, rotary_layout(k_out_head_stride=256), ko=at(1)) == INVALID
+    assert paged(lib, rotary_layout(q_out_head_stride=256), qo=at(0)) == INVALID
     assert passes(prompt, lib, rotary_layout(rotary_dim=0), pos=None, freq=None)       # nothing turns
     assert lib.toploc_norm_rotary_prompt(at(0), at(1), at(2), at(3), None, None, None, at(6), at(7), None) == INVALID
 
