@@ -10,7 +10,7 @@
 // SM (48 registers) and four vectors a thread at a time.  Copies ahead through shared memory or registers, which cost warps,
 // took 180 to 220 us.
 //
-// Alternatives: while it streams, a block leaves the largest of every two vectors (16 or 8 logits) in shared memory.  The
+// Alternatives: while it streams, a block leaves the largest of every four vectors (32 or 16 logits) in shared memory.  The
 // threads' own maxima give a bound that at least `top` logits reach; behind the row only the vectors that reach it are read
 // again, a few dozen, and their logits ranked by (value, index).
 #include "model_common.cuh"
@@ -33,11 +33,13 @@ constexpr int kMostVocab = 1 << 20;
 constexpr int kMostTop = TOPLOC_MAX_ALTERNATIVES;
 constexpr int kMostCluster = 8;       // blocks that share a row
 constexpr int kMaximaBytes = 32768;   // of shared memory that the maxima of a block take, as a rule (five blocks fit an SM)
-constexpr int kMostPairs = 256;       // pairs of vectors, and logits in them, that reach the bound; more take the ordered way
+constexpr int kBatch = 4;             // vectors of a thread that are loaded together, and whose largest logit is kept
+constexpr int kMostBatches = 256;     // threads' batches, and logits in them, that reach the bound; more take the ordered way
 constexpr int kMostKeys = 256;
 static_assert(kMostKeys >= kThreads && kMostCluster * kMostTop <= kThreads, "a thread for each of a row's candidates");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;         // powers of 2 that a value may pass the reference by
+constexpr float kNothing = 60.f;      // powers of 2 below the reference: 2^20 such logits are nothing in a sum of 24 bits
 // Beyond these a product with log2 e could leave fp32: smaller logits count as kTiny (their weight is 0 next to anything
 // larger), and rows whose maximum is out of +-kFar are summed again against the maximum itself.
 constexpr float kTiny = -1e30f, kFar = 1e29f;
@@ -70,9 +72,9 @@ struct Shared {
   Part part;
   Whole whole;
   float bound;
-  int num_pairs, num_keys;
+  int num_batches, num_keys;
   unsigned long long best[kMostTop];     // the block's alternatives
-  unsigned pairs[kMostPairs];
+  unsigned batches[kMostBatches];
   unsigned long long keys[kMostKeys];
 };
 
@@ -114,13 +116,20 @@ struct Vector<__nv_bfloat16> {
   static constexpr int kSize = 8;
   using Kept = uint16_t;  // a maximum in shared memory
   static constexpr uint32_t kNothing = 0xFF80FF80u;  // -inf twice
-  static __device__ uint32_t larger(uint32_t a, uint32_t b) {  // of two at once; passes over NaN
-    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+  // The larger two of two; a NaN wins, or is passed over.
+  template <bool kNaN>
+  static __device__ uint32_t larger(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 x = *reinterpret_cast<__nv_bfloat162*>(&a), y = *reinterpret_cast<__nv_bfloat162*>(&b);
+    const __nv_bfloat162 m = kNaN ? __hmax2_nan(x, y) : __hmax2(x, y);
     return *reinterpret_cast<const uint32_t*>(&m);
   }
-  static __device__ float largest(const uint4& a, const uint4& b) {
-    const uint32_t m = larger(larger(larger(a.x, a.y), larger(a.z, a.w)), larger(larger(b.x, b.y), larger(b.z, b.w)));
-    return fmaxf(bf16_low(m), bf16_high(m));
+  template <bool kNaN>
+  static __device__ float largest(const uint4* q) {
+    uint32_t m = 0xFF80FF80u;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      m = larger<kNaN>(m, larger<kNaN>(larger<kNaN>(q[i].x, q[i].y), larger<kNaN>(q[i].z, q[i].w)));
+    return kNaN ? max_nan(bf16_low(m), bf16_high(m)) : fmaxf(bf16_low(m), bf16_high(m));
   }
   static __device__ void floored(const uint4& q, Pair* v) {  // no smaller than kTiny; NaN stays
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
@@ -141,8 +150,15 @@ struct Vector<float> {
   using Kept = float;
   static constexpr uint32_t kNothing = 0xFF800000u;
   static __device__ float of(uint32_t w) { return __uint_as_float(w); }
-  static __device__ float largest(const uint4& a, const uint4& b) {
-    return fmaxf(fmaxf(fmaxf(of(a.x), of(a.y)), fmaxf(of(a.z), of(a.w))), fmaxf(fmaxf(of(b.x), of(b.y)), fmaxf(of(b.z), of(b.w))));
+  template <bool kNaN>
+  static __device__ float larger(float a, float b) { return kNaN ? max_nan(a, b) : fmaxf(a, b); }
+  template <bool kNaN>
+  static __device__ float largest(const uint4* q) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      m = larger<kNaN>(m, larger<kNaN>(larger<kNaN>(of(q[i].x), of(q[i].y)), larger<kNaN>(of(q[i].z), of(q[i].w))));
+    return m;
   }
   static __device__ void floored(const uint4& q, Pair* v) {
     v[0] = pair_of(max_nan(of(q.x), kTiny), max_nan(of(q.y), kTiny));
@@ -214,10 +230,10 @@ struct Share {
     inner_end = end == all && (vocab + shift) % kSize != 0 ? end - 1 : end;
   }
   // (an empty share has one batch, of nothing)
-  __device__ __forceinline__ int batches() const { return max(1, (end - begin + 2 * kThreads - 1) / (2 * kThreads)); }
-  // the two vectors of a batch and thread: `half` 0 and 1
-  __device__ __forceinline__ int vector(int batch, int thread, int half) const {
-    return begin + (2 * batch + half) * kThreads + thread;
+  __device__ __forceinline__ int batches() const { return max(1, (end - begin + kBatch * kThreads - 1) / (kBatch * kThreads)); }
+  // vector i of a thread's batch
+  __device__ __forceinline__ int vector(int batch, int thread, int i) const {
+    return begin + (kBatch * batch + i) * kThreads + thread;
   }
   __device__ __forceinline__ int first(int v) const { return v * kSize - shift; }
   __device__ __forceinline__ bool in_row(int v, int e) const { return v < end && first(v) + e >= 0 && first(v) + e < vocab; }
@@ -308,12 +324,12 @@ __device__ __noinline__ unsigned long long best_in_order(const Share<T> row, con
   unsigned long long mine = 0;  // lane i: the i-th best
   float least = bound;          // to be reached, and passed once the list is full (equal ones later lose)
   bool full = false;
-  for (int n = 0; n < row.batches() * 2 * kWarps; ++n) {  // 32 vectors
-    const int batch = n / (2 * kWarps), half = n / kWarps & 1, thread = n % kWarps * 32;
+  for (int n = 0; n < row.batches() * kBatch * kWarps; ++n) {  // 32 vectors
+    const int batch = n / (kBatch * kWarps), i = n / kWarps % kBatch, thread = n % kWarps * 32;
     const float m = Vector<T>::value(maxima[batch * kThreads + thread + lane]);
     unsigned hits = __ballot_sync(0xFFFFFFFFu, m > -INFINITY && (full ? m > least : m >= least));
     while (hits) {
-      const int v = row.vector(batch, thread + __ffs(hits) - 1, half);
+      const int v = row.vector(batch, thread + __ffs(hits) - 1, i);
       hits &= hits - 1;
       unsigned long long key = 0;
       if (lane < Vector<T>::kSize) {
@@ -351,17 +367,17 @@ __device__ __forceinline__ bool gather_keys(Shared& sh, const Share<T>& row, con
     for (int i = 0; i < kAtOnce; ++i) {
       const float v = Vector<T>::value(m[i]);
       if (v >= bound) {
-        const int at = atomicAdd(&sh.num_pairs, 1);
-        if (at < kMostPairs) sh.pairs[at] = i0 + i;
+        const int at = atomicAdd(&sh.num_batches, 1);
+        if (at < kMostBatches) sh.batches[at] = i0 + i;
       }
     }
   }
   __syncthreads();
-  const int pairs = sh.num_pairs;
-  if (pairs <= kMostPairs) {
-    for (int i = tid; i < pairs * 2 * kSize; i += kThreads) {
-      const int pair = sh.pairs[i / (2 * kSize)], half = i / kSize & 1, e = i % kSize;
-      const int v = row.vector(pair / kThreads, pair % kThreads, half);
+  const int batches = sh.num_batches;
+  if (batches <= kMostBatches) {
+    for (int n = tid; n < batches * kBatch * kSize; n += kThreads) {
+      const int batch = sh.batches[n / (kBatch * kSize)], e = n % kSize;
+      const int v = row.vector(batch / kThreads, batch % kThreads, n / kSize % kBatch);
       const float x = row.value(v, e);
       if (x >= bound) {
         const int at = atomicAdd(&sh.num_keys, 1);
@@ -370,7 +386,7 @@ __device__ __forceinline__ bool gather_keys(Shared& sh, const Share<T>& row, con
     }
   }
   __syncthreads();
-  if (pairs <= kMostPairs && sh.num_keys <= kMostKeys) return true;
+  if (batches <= kMostBatches && sh.num_keys <= kMostKeys) return true;
   if (tid < 32) {
     const unsigned long long k = best_in_order<T>(row, maxima, bound, top);
     if (tid < top) sh.best[tid] = k;
@@ -397,41 +413,36 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<T>)
 
   Sums sums;
   const int batches = row.batches();
-  const auto take = [&](const uint4* x, int b, int pairs) {  // two batches, or one
-    float m[2], most = -INFINITY;
+  const auto take = [&](const uint4* x, int b) {
+    const float m = V::template largest<true>(x);  // NaN where there is one
+    if (kTops) maxima[b * kThreads + tid] = V::kept(m == m ? m : V::template largest<false>(x));
+    sums.meet(m);
+    // (where nothing comes near the reference, as where a mask leaves no token, the powers are below 2^-60 of the sums')
+    if (powers_of(m) < sums.c - kNothing) return;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (i == pairs) break;
-      m[i] = V::largest(x[2 * i], x[2 * i + 1]);
-      most = fmaxf(most, m[i]);
-      if (kTops) maxima[(b + i) * kThreads + tid] = V::kept(m[i]);
-    }
-    sums.meet(most);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (i == pairs) break;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        Pair v[V::kSize / 2];
-        V::floored(x[2 * i + j], v);
-        sums.add<V::kSize / 2>(v);
-      }
+    for (int i = 0; i < kBatch; ++i) {
+      Pair v[V::kSize / 2];
+      V::floored(x[i], v);
+      sums.add<V::kSize / 2>(v);
     }
   };
   const auto take_any = [&](int b) {
-    const uint4 x[2] = {fetch(row, row.vector(b, tid, 0)), fetch(row, row.vector(b, tid, 1))};
-    take(x, b, 1);
+    uint4 x[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) x[i] = fetch(row, row.vector(b, tid, i));
+    take(x, b);
   };
-  // two batches at a time where they lie in the row as a whole
-  const int inside = (row.inner_end - row.begin) / (2 * kThreads);  // batches up to the row's last part of a vector
+  // without a look at every vector's place where the batch lies in the row as a whole
+  const int inside = (row.inner_end - row.begin) / (kBatch * kThreads);  // batches up to the row's last part of a vector
   int b = 0;
   if (row.inner > row.begin) take_any(b++);  // the row begins inside a vector
   const uint4* at = reinterpret_cast<const uint4*>(row.at - row.shift) + row.vector(b, tid, 0);
-  for (; b + 2 <= inside; b += 2, at += 4 * kThreads) {
-    uint4 x[4];
+#pragma unroll 1
+  for (; b < inside; ++b, at += kBatch * kThreads) {
+    uint4 x[kBatch];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = __ldcs(at + i * kThreads);
-    take(x, b, 2);
+    for (int i = 0; i < kBatch; ++i) x[i] = __ldcs(at + i * kThreads);
+    take(x, b);
   }
 #pragma unroll 1
   for (; b < batches; ++b) take_any(b);
@@ -444,8 +455,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<T>)
   part.top = warp_max(sums.top);
   if (part.top > -INFINITY && !(fabsf(part.top) < kFar)) {  // once more, by differences that do not overflow upwards
     float s = 0.f, w = 0.f;
-    for (int i = 0; i < 2 * batches; ++i) {
-      const int v = row.vector(i / 2, tid, i % 2);
+    for (int i = 0; i < kBatch * batches; ++i) {
+      const int v = row.vector(i / kBatch, tid, i % kBatch);
       for (int e = 0; e < V::kSize; ++e) {
         const float y = max_nan((row.value(v, e) - part.top) * kLog2e, kTiny), x = exp2_fast(y);
         s += x;
@@ -487,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<T>)
     mine = __shfl_sync(0xFFFFFFFFu, mine, p.top - 1);
     if (lane == 0) {
       sh.bound = mine == 0 ? -FLT_MAX : value_of(mine);  // (every logit above -inf)
-      sh.num_pairs = sh.num_keys = 0;
+      sh.num_batches = sh.num_keys = 0;
     }
   }
   if constexpr (kTops) {
@@ -557,7 +568,7 @@ int launch_rows(const LogitParams& p, long long rows, int blocks, size_t bytes, 
   const auto kernel = toploc_token_logprobs_kernel<T, kTops>;
   static std::atomic<uint64_t> allowed{0};
   // (the most: the maxima of an eighth of the largest vocabulary)
-  constexpr int kMostMaxima = (kMostVocab / Vector<T>::kSize / kMostCluster / 2 + 2 * kThreads) *
+  constexpr int kMostMaxima = (kMostVocab / Vector<T>::kSize / kMostCluster / kBatch + 2 * kThreads) *
                               (int)sizeof(typename Vector<T>::Kept);
   constexpr int kMostBytes = (kMostMaxima > kMaximaBytes ? kMostMaxima : kMaximaBytes);
   if (const int rc = allow_shared(reinterpret_cast<const void*>(kernel), kMostBytes, allowed)) return rc;
@@ -583,17 +594,17 @@ template <typename T>
 int launch(const LogitParams& p, long long rows, int sms, cudaStream_t stream) {
   constexpr int kSize = Vector<T>::kSize;
   const int vectors = (p.vocab + 2 * (kSize - 1)) / kSize;  // at most
-  const auto batches = [&](int blocks) { return ((vectors + blocks - 1) / blocks + 2 * kThreads - 1) / (2 * kThreads); };
+  const auto batches = [&](int blocks) { return ((vectors + blocks - 1) / blocks + kBatch * kThreads - 1) / (kBatch * kThreads); };
   const auto bytes = [&](int blocks) { return (size_t)batches(blocks) * kThreads * sizeof(typename Vector<T>::Kept); };
-  // A row's blocks: what gets through the rows soonest, as many blocks at a time as fit, where a block's time is its batches
-  // and as much as 7 + blocks of them for its beginning and end (measured with 128000 bf16, one row: 14.4, 10.7, 8.9 and 9.3 us
+  // A row's blocks: what gets through the rows soonest, as many blocks at a time as fit, where a block's time is twice its
+  // batches and 7 + blocks for its beginning and end (measured with 128000 bf16, one row: 14.4, 10.7, 8.9 and 9.3 us
   // for 1, 2, 4 and 8 blocks; 64 rows: 20.8, 15.1, 12.5 and 13.8; 4097 rows: 172, 208, 297 and 510).
   int blocks = 0;
   long long least = 0;
   for (int n = 1; n <= kMostCluster; n *= 2) {
     if (p.top && n < kMostCluster && bytes(n) > kMaximaBytes) continue;
     const long long at_once = (long long)kBlocksPerSm<T> * sms, rounds = (rows * n + at_once - 1) / at_once;
-    const long long cost = rounds * (batches(n) + 7 + n);
+    const long long cost = rounds * (2 * batches(n) + 7 + n);
     if (blocks == 0 || cost < least) blocks = n, least = cost;
   }
   if (rows * blocks > 0x7FFFFFFF) return TOPLOC_ERR_UNSUPPORTED;
