@@ -493,3 +493,33 @@ def test_captured_and_replayed_on_another_stream():
     assert_fork([host(t) for t in [table] + out], want)
     k = want[5]
     assert torch.equal(cache[ints(want[4][:k], torch.int64)], begun[ints(want[3][:k], torch.int64)])
+
+
+@pytest.mark.parametrize("seqs,longest,page,family,spare", [
+    (900, 1500, 16, 3, 10),        # a release of many pages: three launches
+    (5, 100, 16, 1, 300000),       # few pages of a large pool are held: a warp's range is longer than its lanes' marks
+    (600, 3000, 8, 2, 280000)])
+def test_large_pools(seqs, longest, page, family, spare):
+    p = Pool(seqs, seqs, longest, page, family, spare, empty=0.3)
+    gone = (p.r.random(seqs) < 0.6).astype(np.int64)
+    assert_release(run_release(p, gone), release_reference(p, gone))
+    assert_compact(run_compact(p), compact_reference(p))
+    parents = children(p)
+    assert_fork(run_fork(p, parents), fork_reference(p, parents))
+
+
+def test_large_releases_of_what_is_not_as_promised():
+    p = Pool(13, 900, 1500, 16, 3)
+    gone = np.ones(900, np.int64)
+    able = np.nonzero(p.lens > 700)[0]
+    p.table[able[0], 1] = p.pages
+    p.table[able[1], 0] = -1
+    p.table[able[2], 1] = p.table[able[2], 0]
+    p.lens[able[3]] = -1
+    p.lens[able[4]] = 2 ** 31 - 1
+    p.table[able[4]] = np.clip(p.table[able[4]], 0, p.pages - 1)
+    assert_release(run_release(p, gone), release_reference(p, gone))
+    for head in (-5, 0, 1000, 10 ** 6):
+        want = release_reference(p, gone, head)
+        assert_release(run_release(p, gone, head), want)
+        assert head == 10 ** 6 or tl.TOPLOC_SEQ_NO_ROOM in want[4]
