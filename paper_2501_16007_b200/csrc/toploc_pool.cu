@@ -22,7 +22,7 @@ constexpr int kMostBlocks = 8;                 // of a planner's cluster
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;          // of a block
 constexpr long long kOneBlock = 16384;         // entries and pages that one block plans for
-constexpr long long kOneCluster = 65536;      // of a release that one cluster does
+constexpr long long kOneCluster = 65536;       // and of a release that one cluster does
 constexpr int kAtOnce = 4;                     // loads of a thread on their way at once
 
 struct PoolParams {
@@ -101,13 +101,13 @@ __device__ __forceinline__ void for_entries(const PoolParams& p, const Team& tea
     const int count = min(32, (p.num_seqs - base + kWarps - 1) / kWarps);
 #pragma unroll 1
     for (int first = 0; first < count; first += kAtOnce) {
-      int rows[kAtOnce], held_pages[kAtOnce], most = 0;
+      int rows[kAtOnce], held_of[kAtOnce], most = 0;
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
         rows[i] = base + (first + i) * kWarps;
-        held_pages[i] = __shfl_sync(0xFFFFFFFFu, mine, (first + i) & 31);
-        if (first + i >= count) held_pages[i] = 0;
-        most = max(most, held_pages[i]);
+        held_of[i] = __shfl_sync(0xFFFFFFFFu, mine, (first + i) & 31);
+        if (first + i >= count) held_of[i] = 0;
+        most = max(most, held_of[i]);
       }
 #pragma unroll 1
       for (int c0 = team.block * 32; c0 < most; c0 += team.blocks * 32) {
@@ -115,7 +115,7 @@ __device__ __forceinline__ void for_entries(const PoolParams& p, const Team& tea
         bool valid[kAtOnce];
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-          valid[i] = c0 + lane < held_pages[i];
+          valid[i] = c0 + lane < held_of[i];
           page[i] = valid[i] ? table[rows[i] * stride + c0 + lane] : 0;
         }
         visit(rows, c0 + lane, page, valid);
@@ -214,11 +214,11 @@ constexpr int kNeedsPage = 0x80;  // of a status byte until the end: the child a
 
 __device__ __forceinline__ int status_of(const PoolParams& p, int i) { return __ldcg(p.status + i); }
 
-// Pages that the children in front of i ask for.
+// Pages that the children in front of i ask for; all lanes of a warp together.
 __device__ __forceinline__ int asked_before(const PoolParams& p, const int* run_before, int per, int i) {
-  int place = run_before[i / per];
-  for (int j = i / per * per; j < i; ++j) place += status_of(p, j) >> 7;
-  return place;
+  int more = 0;
+  for (int j = i / per * per + (threadIdx.x & 31); j < i; j += 32) more += status_of(p, j) >> 7;
+  return run_before[i / per] + warp_total(more);
 }
 
 __global__ void __launch_bounds__(kThreads, 1) toploc_fork_pages_kernel(const __grid_constant__ PoolParams p) {

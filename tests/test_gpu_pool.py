@@ -523,3 +523,12 @@ def test_large_releases_of_what_is_not_as_promised():
         want = release_reference(p, gone, head)
         assert_release(run_release(p, gone, head), want)
         assert head == 10 ** 6 or tl.TOPLOC_SEQ_NO_ROOM in want[4]
+
+
+def test_forks_among_a_hundred_thousand_sequences():
+    """Many sequences a thread of the plan."""
+    p = Pool(14, 100000, 20, 16, empty=0.5, spare=30000)
+    parents = children(p)
+    want = fork_reference(p, parents)
+    assert tl.TOPLOC_SEQ_NO_PAGES in want[7]
+    assert_fork(run_fork(p, parents), want)
