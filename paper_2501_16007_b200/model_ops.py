@@ -365,22 +365,22 @@ _PAIRINGS = {"halves": TOPLOC_ROTARY_HALVES, "neighbours": TOPLOC_ROTARY_NEIGHBO
 
 
 def _rotary_layout(q, k, v, positions, inv_freq, q_weight, k_weight, eps, pairing, q_out, k_out):
-    dtype, shape = q.dtype, k.shape
-    (tokens, heads, dim), (k_tokens, kv_heads, k_dim), (pairs,) = q.shape, shape, inv_freq.shape
+    dtype, q_shape, k_shape = q.dtype, q.shape, k.shape
+    (tokens, heads, dim), (k_tokens, kv_heads, k_dim), pairs = q_shape, k_shape, inv_freq.numel()
     (qt, qh, q1), (kt, kh, k1), (ot, oh, o1) = q.stride(), k.stride(), q_out.stride()
     (vt, vh, v1), (pt, ph, p1) = (0, 0, 1) if v is None else v.stride(), (0, 0, 1) if k_out is None else k_out.stride()
     if not (dtype in _DTYPES and dtype is k.dtype is q_out.dtype and k_tokens == tokens and k_dim == dim and
-            q_out.shape == (tokens, heads, dim) and q1 == k1 == o1 == v1 == p1 == 1 and
-            (v is None or (v.shape == shape and v.dtype is dtype)) and
-            (k_out is None or (k_out.shape == shape and k_out.dtype is dtype))):
+            q_out.shape == q_shape and q1 == k1 == o1 == v1 == p1 == 1 and
+            (v is None or (v.shape == k_shape and v.dtype is dtype)) and
+            (k_out is None or (k_out.shape == k_shape and k_out.dtype is dtype))):
         raise ToplocError("queries and their output must be [tokens, q_heads, head_dim], keys, values and the keys' output "
                           "[tokens, kv_heads, head_dim], all bfloat16 or all float32, the last dimension contiguous")
-    if not (positions.dtype is torch.int32 and positions.shape == (tokens,) and positions.is_contiguous() and
+    if not (positions.dtype is torch.int32 and positions.numel() == tokens and positions.is_contiguous() and
             inv_freq.dtype is torch.float32 and inv_freq.is_contiguous() and 2 * pairs <= dim):
         raise ToplocError("positions must be a contiguous int32 vector of %d entries, inv_freq a contiguous float32 vector of "
                           "at most head_dim / 2" % tokens)
     for weight in (q_weight, k_weight):
-        if not (weight is None or (weight.dtype is dtype and weight.shape == (dim,) and weight.is_contiguous())):
+        if weight is not None and (weight.dtype is not dtype or weight.numel() != dim or not weight.is_contiguous()):
             raise ToplocError("a norm's weight must be [head_dim] of q's type")
     if pairing not in _PAIRINGS:
         raise ToplocError("pairing must be 'halves' or 'neighbours'")
@@ -388,7 +388,7 @@ def _rotary_layout(q, k, v, positions, inv_freq, q_weight, k_weight, eps, pairin
                  kh, vt, vh, ot, oh, pt, ph)
 
 
-_DIMENSIONS = "%s takes queries, keys and values of three dimensions and inv_freq of one"
+_DIMENSIONS = "%s takes queries, keys and values of three dimensions"
 
 
 def toploc_norm_rotary_prompt(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6, pairing="halves",
@@ -403,7 +403,7 @@ def toploc_norm_rotary_prompt(q, k, positions, inv_freq, q_weight=None, k_weight
     if k_out is None:
         k_out = _empty(k.shape, k.dtype, k.device, stream)
     dev = _device(name, q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out)
-    if not q.dim() == k.dim() == q_out.dim() == k_out.dim() == 3 or inv_freq.dim() != 1:
+    if not q.dim() == k.dim() == q_out.dim() == k_out.dim() == 3:
         raise ToplocError(_DIMENSIONS % name)
     lay = _rotary_layout(q, k, None, positions, inv_freq, q_weight, k_weight, eps, pairing, q_out, k_out)
     _call(_library().toploc_norm_rotary_prompt, name, dev, stream, _ptr(q), _ptr(k),
@@ -420,12 +420,12 @@ def toploc_norm_rotary_paged(q, k, v, positions, slots, inv_freq, k_cache, v_cac
     if q_out is None:
         q_out = _empty(q.shape, q.dtype, q.device, stream)
     dev = _device(name, q, k, v, positions, slots, inv_freq, k_cache, v_cache, q_weight, k_weight, q_out)
-    if not q.dim() == k.dim() == v.dim() == q_out.dim() == 3 or inv_freq.dim() != 1:
+    if not q.dim() == k.dim() == v.dim() == q_out.dim() == 3:
         raise ToplocError(_DIMENSIONS % name)
     lay = _rotary_layout(q, k, v, positions, inv_freq, q_weight, k_weight, eps, pairing, q_out, None)
     kv = _cache_layout(k_cache, v_cache)
     if not (k_cache.dtype is q.dtype and k_cache.shape[2:] == k.shape[1:] and slots.dtype is torch.int64 and
-            slots.shape == positions.shape and slots.is_contiguous()):
+            slots.numel() == positions.numel() and slots.is_contiguous()):
         raise ToplocError("the caches must have k's type, heads and head_dim, slots must be a contiguous int64 vector of "
                           "as many entries as there are tokens")
     _call(_library().toploc_norm_rotary_paged, name, dev, stream, _ptr(q), _ptr(k), _ptr(v),
