@@ -187,3 +187,37 @@ def test_logits_past_32_bits():
     log = float(np.log(128000))
     # 2^-24 (62 sums of partial sums in a row and 45 more) of a sum, and roundings of 12
     assert (got[0][:-2] + log).abs().max().item() < 1e-5 and (got[1][:-2] - log).abs().max().item() < 2e-5
+
+
+@pytest.mark.parametrize("before", ["nothing", "set", "copy", "kernel", "another stream", "two streams"])
+def test_copies_captured_behind_anything(before):
+    """The copies may begin before a kernel in front of them has ended; what is in front may be something else."""
+    cache = torch.randn((8, 16, 2, 64), device=DEV)
+    begun = cache.clone()
+    source, target, count = ints([0, 0, 0]), ints([4, 5, 6]), ints([3])
+    pages, other = ints([1, 2, 3]), torch.zeros(1 << 22, device=DEV)
+    side, third = torch.cuda.Stream(), torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        if before == "set":
+            other.zero_()
+            source.zero_()
+        elif before == "copy":
+            source.copy_(pages)
+        elif before == "kernel":
+            source.add_(1)
+        elif before != "nothing":
+            third.wait_stream(side)
+            with torch.cuda.stream(third):
+                other.add_(1)
+                source.copy_(pages)
+            if before == "two streams":
+                count.add_(0)
+            side.wait_stream(third)
+        tl.toploc_copy_pages([cache], source, target, count)
+    graph.replay()
+    torch.cuda.synchronize()
+    first = {"nothing": [0, 0, 0], "set": [0, 0, 0], "kernel": [1, 1, 1]}.get(before, [1, 2, 3])
+    assert torch.equal(cache[4:7], begun[first])
+    assert torch.equal(cache[:4], begun[:4]) and torch.equal(cache[7], begun[7])
