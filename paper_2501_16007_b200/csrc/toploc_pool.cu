@@ -21,8 +21,13 @@ namespace cg = cooperative_groups;
 constexpr int kMostBlocks = 8;                 // of a planner's cluster
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;          // of a block
-constexpr long long kOneBlock = 16384;         // entries and pages that one block plans for
-constexpr long long kOneCluster = 65536;       // and of a release that one cluster does
+// Entries of the table (at most) and pages that one block plans for; a cluster of eight is faster from there on (releases of
+// 4, 8, 15 and 57 thousand: 5.0, 5.6, 7.7 and 15.5 us against 6.3, 6.3, 6.6 and 8.0; forks of 1, 5 and 18: 7.5, 9.9 and 17.8
+// against 8.7, 9.7 and 10.0; compactions of 1, 6 and 12: 9.0, 12.0 and 16.2 against 11.4, 13.1 and 14.3).
+constexpr long long kOneBlock = 8192;
+// And of a release that one cluster does.  Three launches over all SMs are faster on the GPU from 50 thousand on (57, 112 and
+// 412 thousand: 7.5, 8.4 and 11.9 us against 8.0, 10.7 and 22.2), but take 4 us more of the calling thread.
+constexpr long long kOneCluster = 131072;
 constexpr int kAtOnce = 4;                     // loads of a thread on their way at once
 
 struct PoolParams {
@@ -369,8 +374,8 @@ __device__ __forceinline__ void release_entry(const PoolParams& p, int seq, int3
     p.status[seq] = TOPLOC_SEQ_BAD_PAGE;
 }
 
-// Large releases take three launches: eight SMs send an atomic every other clock each, so the sequences' pages (65 thousand:
-// 10 of 22 us) are spread over all SMs, and so is the copy of the shares; the numbering behind them stays with the cluster.
+// Large releases take three launches: an SM sends an atomic every other clock, so the sequences' pages (65 thousand take eight
+// SMs 10 us) are spread over all SMs, and so is the copy of the shares; the numbering behind them stays with the cluster.
 constexpr int kWideThreads = 256;
 constexpr int kEntriesAtOnce = 32 * kAtOnce;  // of a row, a warp's
 

@@ -496,7 +496,7 @@ def test_captured_and_replayed_on_another_stream():
 
 
 @pytest.mark.parametrize("seqs,longest,page,family,spare", [
-    (900, 1500, 16, 3, 10),        # a release of many pages: three launches
+    (2500, 1500, 16, 3, 10),       # a release of many pages: three launches
     (5, 100, 16, 1, 300000),       # few pages of a large pool are held: a warp's range is longer than its lanes' marks
     (600, 3000, 8, 2, 280000)])
 def test_large_pools(seqs, longest, page, family, spare):
@@ -509,8 +509,8 @@ def test_large_pools(seqs, longest, page, family, spare):
 
 
 def test_large_releases_of_what_is_not_as_promised():
-    p = Pool(13, 900, 1500, 16, 3)
-    gone = np.ones(900, np.int64)
+    p = Pool(13, 2500, 1500, 16, 3)
+    gone = np.ones(2500, np.int64)
     able = np.nonzero(p.lens > 700)[0]
     p.table[able[0], 1] = p.pages
     p.table[able[1], 0] = -1
