@@ -387,7 +387,9 @@ int run(RotaryParams& p, const toploc_rotary_layout* lay, const int32_t* positio
   const int heads = p.q_heads + (parts - 1) * p.kv_heads;
   const bool neighbours = lay->pairing == TOPLOC_ROTARY_NEIGHBOURS;
 
-  // whole vectors of `vec` elements everywhere: two a lane, turned channels in whole vectors
+  // Whole vectors of `vec` elements everywhere: two a lane, turned channels in whole vectors.  16 bytes where they fit (34
+  // thousand tokens of heads of 128: 136 us, with 8 bytes 172, element by element 712), else 8 (heads of 80 of which 40 turn:
+  // 165 us, element by element 586).
   const auto fits = [&](int vec) {
     const int bytes = vec * size;
     if (p.head_dim % (2 * vec) != 0 || (neighbours ? lay->rotary_dim : p.half) % vec != 0 || p.head_dim / (2 * vec) > 32)
