@@ -3,10 +3,12 @@
  *
  * A proof (toploc.h) commits to the last hidden states of a model.  These are
  * the operators of the passes that produce those states: a provider plans
- * pages, writes keys and values to a paged cache and lets a chunk of new
- * tokens attend over it (Section 5.5: a proof per 32 new tokens); a validator
- * recomputes whole prompts in one packed pass (Section 5.1); both close every
- * layer with a residual addition and an RMS norm.
+ * pages, norms and turns queries and keys, writes keys and values to a paged
+ * cache and lets a chunk of new tokens attend over it (Section 5.5: a proof per
+ * 32 new tokens); a validator recomputes whole prompts in one packed pass
+ * (Section 5.1); both close every layer with a residual addition and an RMS
+ * norm and read log probabilities off the logits; sequences are forked, end and
+ * give their pages back.
  *
  * The rules of toploc.h hold here: plain C, the caller owns every buffer,
  * nothing is allocated, work is only enqueued on the given stream, no kernel
@@ -120,11 +122,11 @@ int toploc_cache_write(const void* d_k, const void* d_v, int64_t k_token_stride,
  * toploc_plan_pages hands them out (it needs no shares).  Only whole pages are
  * shared, and new tokens go behind them, so a shared page is never written.
  *
- * The three planners below run as one cluster of thread blocks each.  Outputs
- * are apart from inputs (shares and lengths: two buffers used in turn), so that
- * a repeated call gives the same; refused where they overlap.  The same inputs
- * give the same outputs.  All arrays DEVICE; int32 4-byte aligned.  num_seqs <=
- * 2^24, num_pages <= 2^30, max_pages >= 0, table_stride >= max_pages.
+ * Outputs of the three planners below are apart from inputs (shares and
+ * lengths: two buffers used in turn), so that a repeated call gives the same;
+ * refused where they overlap.  The same inputs give the same outputs.  All
+ * arrays DEVICE; int32 4-byte aligned.  page_size > 0, num_seqs <= 2^24,
+ * num_pages <= 2^30, max_pages >= 0, table_stride >= max_pages.
  */
 
 /*
@@ -246,11 +248,11 @@ int toploc_copy_pages(void* const* h_caches, const toploc_pool_layout* lay, cons
 typedef struct {
   int32_t dtype;      /* TOPLOC_DTYPE_* of all tensors and weights */
   int32_t head_dim;   /* 1 .. 256 */
-  int32_t q_heads;    /* > 0 */
-  int32_t kv_heads;   /* > 0 */
+  int32_t q_heads;    /* 1 .. 16384 */
+  int32_t kv_heads;   /* 1 .. 16384 */
   int32_t rotary_dim; /* even, 0 .. head_dim: the first channels of a head turn, the rest stay */
   int32_t pairing;    /* TOPLOC_ROTARY_* */
-  int64_t num_tokens; /* >= 0 */
+  int64_t num_tokens; /* 0 .. 2^31 - 1 */
   float eps;          /* >= 0 */
   int32_t reserved;   /* 0 */
   int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride; /* elements */
@@ -273,9 +275,9 @@ typedef struct {
  * d_q_weight_opt, d_k_weight_opt  DEVICE [head_dim], NULL: no norm of that one
  * d_q_out, d_k_out  DEVICE; each may be its input (with the same strides), else
  *                they share no memory with the inputs
- * Pointers aligned to the element; heads at places of 16 (8) bytes whose
- * channels and turned channels are whole vectors of that size move as vectors,
- * others element by element.  Asynchronous.
+ * Pointers aligned to the element; heads at places of 16 (8) bytes, less than
+ * 2^26 elements apart, whose channels and turned channels are whole vectors of
+ * that size move as vectors, others element by element.  Asynchronous.
  */
 int toploc_norm_rotary_prompt(const void* d_q, const void* d_k, const int32_t* d_positions, const float* d_inv_freq,
                               const void* d_q_weight_opt, const void* d_k_weight_opt, const toploc_rotary_layout* lay,
@@ -420,7 +422,7 @@ typedef struct {
   int32_t vocab;      /* 1 .. 2^20 */
   int32_t top;        /* alternatives a row, 0 .. TOPLOC_MAX_ALTERNATIVES */
   int32_t reserved;   /* 0 */
-  int64_t rows;       /* >= 0 */
+  int64_t rows;       /* 0 .. 2^31 - 1 */
   int64_t row_stride; /* elements, >= vocab (columns past the vocabulary are not read) */
 } toploc_logprob_layout;
 

@@ -16,7 +16,9 @@
 #include "model_common.cuh"
 
 #include <cooperative_groups.h>
+
 #include <cfloat>
+#include <utility>
 
 namespace {
 
