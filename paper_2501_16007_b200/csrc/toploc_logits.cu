@@ -5,10 +5,10 @@
 // c is renewed only when a value passes it by 2^8, so a few times a thread and not with every new maximum (it costs precision
 // too: y_j is off by half a step, 2^-22 just below 2^3).
 //
-// Bound by memory (one pass), with the powers, 16 a cycle and SM, not far behind: 4097 x 128000 bf16 takes 160 us without
-// alternatives (6.6 TB/s; the powers alone 130) and 172 with five.  What counts is many warps with many independent operations each: 40 warps an
-// SM (48 registers) and four vectors a thread at a time.  Copies ahead through shared memory or registers, which cost warps,
-// took 180 to 220 us.
+// Bound by memory (one pass), with the powers, 16 a cycle and SM, not far behind: 4097 x 128000 bf16 takes 162 us without
+// alternatives (6.5 TB/s; the powers alone 130) and 171 with five; in long runs, where the board's power brings the clock down
+// to 1.6 GHz, 189.  What counts is many warps with many independent operations each: 40 warps an SM (48 registers) and four
+// vectors a thread at a time.  Copies ahead through shared memory or registers, which cost warps, took 205 to 255 us.
 //
 // Alternatives: while it streams, a block leaves the largest of every four vectors (32 or 16 logits) in shared memory.  The
 // threads' own maxima give a bound that at least `top` logits reach; behind the row only the vectors that reach it are read

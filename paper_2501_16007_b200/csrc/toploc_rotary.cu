@@ -391,17 +391,17 @@ int run(RotaryParams& p, const toploc_rotary_layout* lay, const int32_t* positio
   // thousand tokens of heads of 128: 136 us, with 8 bytes 172, element by element 712), else 8 (heads of 80 of which 40 turn:
   // 165 us, element by element 586).
   const auto fits = [&](int vec) {
-    const int bytes = vec * size;
-    if (p.head_dim % (2 * vec) != 0 || (neighbours ? lay->rotary_dim : p.half) % vec != 0 || p.head_dim / (2 * vec) > 32)
-      return false;
+    const uintptr_t bytes = vec * size;
+    long long off = 0;  // bits of places and steps that a vector's must not have
+    uintptr_t away = 0;
     for (int i = 0; i < parts; ++i) {
       const Heads& w = p.part[i];
-      if (!aligned(w.in, bytes) || !aligned(w.out, bytes) || !aligned(w.weight, bytes)) return false;
-      for (const long long s : {w.in_token, w.in_head, w.out_page, w.out_token, w.out_head})
-        if (s % vec != 0) return false;
+      away |= reinterpret_cast<uintptr_t>(w.in) | reinterpret_cast<uintptr_t>(w.out) | reinterpret_cast<uintptr_t>(w.weight);
+      off |= w.in_token | w.in_head | w.out_page | w.out_token | w.out_head;
       if (w.in_head >= 1ll << 26 || w.out_head >= 1ll << 26) return false;  // (places in a step's 32 heads at most: 32 bits)
     }
-    return true;
+    return p.head_dim % (2 * vec) == 0 && (neighbours ? lay->rotary_dim : p.half) % vec == 0 &&
+           p.head_dim / (2 * vec) <= 32 && (away & (bytes - 1)) == 0 && (off & (vec - 1)) == 0;
   };
   const int wide = 16 / size, vec = fits(wide) ? wide : size == 2 && fits(4) ? 4 : 0;
   const unsigned blocks = (unsigned)((p.num_tokens + kWarps - 1) / kWarps);

@@ -212,14 +212,14 @@ def toploc_plan_pages(cached_lens, new_lens, free_pages, first_free, block_table
 
 def _cache_layout(k_cache, v_cache, block_table=None):
     """Layout of a cache [num_pages, page_size, kv_heads, head_dim]; a permuted view gives any order."""
-    _need(k_cache.dim() == 4 and k_cache.shape == v_cache.shape and k_cache.dtype == v_cache.dtype and
-          k_cache.stride(3) == 1 and v_cache.stride(3) == 1,
+    shape, k_strides, v_strides = k_cache.shape, k_cache.stride(), v_cache.stride()
+    _need(len(shape) == 4 and v_cache.shape == shape and k_cache.dtype is v_cache.dtype and
+          k_strides[3] == 1 and v_strides[3] == 1,
           "the caches must be [pages, page_size, kv_heads, head_dim] of one type, the last dimension contiguous")
     width = 0 if block_table is None else block_table.shape[1]
     stride = 0 if block_table is None else block_table.stride(0) if block_table.shape[0] > 1 else width
-    kp, kt, kh, _ = k_cache.stride()
-    vp, vt, vh, _ = v_cache.stride()
-    return _pack(_KV, k_cache.shape[1], k_cache.shape[0], width, 0, stride, kp, kt, kh, vp, vt, vh)
+    (pages, page, _, _), (kp, kt, kh, _), (vp, vt, vh, _) = shape, k_strides, v_strides
+    return _pack(_KV, page, pages, width, 0, stride, kp, kt, kh, vp, vt, vh)
 
 
 def toploc_cache_write(k, v, slots, k_cache, v_cache, stream=None):
@@ -424,13 +424,14 @@ def toploc_norm_rotary_paged(q, k, v, positions, slots, inv_freq, k_cache, v_cac
         raise ToplocError(_DIMENSIONS % name)
     lay = _rotary_layout(q, k, v, positions, inv_freq, q_weight, k_weight, eps, pairing, q_out, None)
     kv = _cache_layout(k_cache, v_cache)
-    if not (k_cache.dtype is q.dtype and k_cache.shape[2:] == k.shape[1:] and slots.dtype is torch.int64 and
-            slots.numel() == positions.numel() and slots.is_contiguous()):
+    (_, _, heads, dim), (tokens, kv_heads, head_dim) = k_cache.shape, k.shape
+    if not (k_cache.dtype is q.dtype and heads == kv_heads and dim == head_dim and slots.dtype is torch.int64 and
+            slots.numel() == tokens and slots.is_contiguous()):
         raise ToplocError("the caches must have k's type, heads and head_dim, slots must be a contiguous int64 vector of "
                           "as many entries as there are tokens")
-    _call(_library().toploc_norm_rotary_paged, name, dev, stream, _ptr(q), _ptr(k), _ptr(v),
-          _ptr(positions), _ptr(slots), _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), lay, _ptr(q_out), _ptr(k_cache),
-          _ptr(v_cache), kv)
+    _call(_library().toploc_norm_rotary_paged, name, dev, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+          positions.data_ptr(), slots.data_ptr(), inv_freq.data_ptr(), _ptr(q_weight), _ptr(k_weight), lay,
+          q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), kv)
     return q_out
 
 
