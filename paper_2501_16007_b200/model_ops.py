@@ -473,21 +473,6 @@ def toploc_token_logprobs(logits, tokens=None, top=0, want_entropy=False, logpro
     return logprobs, entropy, top_ids, top_logprobs
 
 
-def _vectors(name, n, per_seq, pages, per_page, single, free_pages, flags):
-    """int32 vectors of n, of as many entries as there are pages and of one, the free list, and uint8 vectors of n."""
-    i32 = torch.int32
-    for group, entries in ((per_seq, n), (per_page, pages), (single, 1)):
-        for t in group:
-            if t.dtype is not i32 or t.numel() != entries or not t.is_contiguous():
-                raise ToplocError("%s: contiguous int32 vectors of %d entries for the sequences, of %d for the pages, and of "
-                                  "one (see its documentation)" % (name, n, pages))
-    if free_pages.dtype is not i32 or not free_pages.is_contiguous():
-        raise ToplocError("%s: the free list must be a contiguous int32 vector" % name)
-    for t in flags:
-        if t.dtype is not torch.uint8 or t.numel() != n or not t.is_contiguous():
-            raise ToplocError("%s: status and release must be contiguous uint8 vectors of %d entries" % (name, n))
-
-
 def _table(t, n, what):
     """(columns, elements between rows) of a block table [n, max_pages]."""
     if t.dtype is torch.int32 and t.dim() == 2:
@@ -508,12 +493,22 @@ def toploc_fork_pages(parents, kv_lens, shares, free_pages, first_free, block_ta
     dev = _device(name, parents, kv_lens, shares, free_pages, first_free, block_table, kv_lens_out, shares_out, copy_from,
                   copy_to, num_copies, next_free, status)
     pages, free = shares.numel(), free_pages.numel()
-    _vectors(name, n, (parents, kv_lens, kv_lens_out, copy_from, copy_to), pages, (shares, shares_out),
-             (first_free, num_copies, next_free), free_pages, (status,))
+    i32 = torch.int32
+    if not (parents.dtype is kv_lens.dtype is shares.dtype is free_pages.dtype is first_free.dtype is kv_lens_out.dtype is
+            shares_out.dtype is copy_from.dtype is copy_to.dtype is num_copies.dtype is next_free.dtype is i32 and
+            status.dtype is torch.uint8 and
+            kv_lens.numel() == kv_lens_out.numel() == copy_from.numel() == copy_to.numel() == status.numel() == n and
+            shares_out.numel() == pages and first_free.numel() == num_copies.numel() == next_free.numel() == 1 and
+            parents.is_contiguous() and kv_lens.is_contiguous() and shares.is_contiguous() and
+            free_pages.is_contiguous() and kv_lens_out.is_contiguous() and shares_out.is_contiguous() and
+            copy_from.is_contiguous() and copy_to.is_contiguous() and status.is_contiguous()):
+        raise ToplocError("toploc_fork_pages: contiguous int32 parents, kv_lens, kv_lens_out, copy_from, copy_to [n], shares, "
+                          "shares_out [num_pages], free_pages, first_free, num_copies, next_free [1]; uint8 status [n]")
     width, stride = _table(block_table, n, "block_table")
-    _call(_library().toploc_fork_pages, name, dev, stream, _ptr(parents), _ptr(kv_lens), n, _ptr(shares), pages,
-          _ptr(free_pages), free, _ptr(first_free), page_size, _ptr(block_table), width, stride, _ptr(kv_lens_out),
-          _ptr(shares_out), _ptr(copy_from), _ptr(copy_to), _ptr(num_copies), _ptr(next_free), _ptr(status))
+    _call(_library().toploc_fork_pages, name, dev, stream, parents.data_ptr(), kv_lens.data_ptr(), n,
+          shares.data_ptr(), pages, free_pages.data_ptr(), free, first_free.data_ptr(), page_size,
+          block_table.data_ptr(), width, stride, kv_lens_out.data_ptr(), shares_out.data_ptr(), copy_from.data_ptr(),
+          copy_to.data_ptr(), num_copies.data_ptr(), next_free.data_ptr(), status.data_ptr())
 
 
 def toploc_release_pages(release, kv_lens, block_table, shares, page_size, free_pages, first_free, kv_lens_out,
@@ -526,12 +521,20 @@ def toploc_release_pages(release, kv_lens, block_table, shares, page_size, free_
     dev = _device(name, release, kv_lens, block_table, shares, free_pages, first_free, kv_lens_out, shares_out, next_free,
                   status)
     pages, free = shares.numel(), free_pages.numel()
-    _vectors(name, n, (kv_lens, kv_lens_out), pages, (shares, shares_out), (first_free, next_free), free_pages,
-             (status, release))
+    i32, u8 = torch.int32, torch.uint8
+    if not (kv_lens.dtype is shares.dtype is free_pages.dtype is first_free.dtype is kv_lens_out.dtype is shares_out.dtype is
+            next_free.dtype is i32 and release.dtype is status.dtype is u8 and
+            release.numel() == kv_lens_out.numel() == status.numel() == n and shares_out.numel() == pages and
+            first_free.numel() == next_free.numel() == 1 and release.is_contiguous() and kv_lens.is_contiguous() and
+            shares.is_contiguous() and free_pages.is_contiguous() and kv_lens_out.is_contiguous() and
+            shares_out.is_contiguous() and status.is_contiguous()):
+        raise ToplocError("toploc_release_pages: contiguous int32 kv_lens, kv_lens_out [n], shares, shares_out [num_pages], "
+                          "free_pages, first_free, next_free [1]; uint8 release, status [n]")
     width, stride = _table(block_table, n, "block_table")
-    _call(_library().toploc_release_pages, name, dev, stream, _ptr(release), _ptr(kv_lens), n, _ptr(block_table), width,
-          stride, _ptr(shares), pages, page_size, _ptr(free_pages), free, _ptr(first_free), _ptr(kv_lens_out),
-          _ptr(shares_out), _ptr(next_free), _ptr(status))
+    _call(_library().toploc_release_pages, name, dev, stream, release.data_ptr(), kv_lens.data_ptr(), n,
+          block_table.data_ptr(), width, stride, shares.data_ptr(), pages, page_size, free_pages.data_ptr(), free,
+          first_free.data_ptr(), kv_lens_out.data_ptr(), shares_out.data_ptr(), next_free.data_ptr(),
+          status.data_ptr())
 
 
 def toploc_compact_pages(kv_lens, block_table, shares, page_size, block_table_out, shares_out, free_pages_out, copy_from,
@@ -544,14 +547,22 @@ def toploc_compact_pages(kv_lens, block_table, shares, page_size, block_table_ou
     dev = _device(name, kv_lens, block_table, shares, block_table_out, shares_out, free_pages_out, copy_from, copy_to,
                   num_copies, next_free, status)
     pages, free = shares.numel(), free_pages_out.numel()
-    _vectors(name, n, (kv_lens,), pages, (shares, shares_out, copy_from, copy_to), (num_copies, next_free), free_pages_out,
-             (status,))
+    i32 = torch.int32
+    if not (kv_lens.dtype is shares.dtype is shares_out.dtype is free_pages_out.dtype is copy_from.dtype is copy_to.dtype is
+            num_copies.dtype is next_free.dtype is i32 and status.dtype is torch.uint8 and status.numel() == n and
+            shares_out.numel() == copy_from.numel() == copy_to.numel() == pages and
+            num_copies.numel() == next_free.numel() == 1 and kv_lens.is_contiguous() and shares.is_contiguous() and
+            shares_out.is_contiguous() and free_pages_out.is_contiguous() and copy_from.is_contiguous() and
+            copy_to.is_contiguous() and status.is_contiguous()):
+        raise ToplocError("toploc_compact_pages: contiguous int32 kv_lens [n], shares, shares_out, copy_from, copy_to "
+                          "[num_pages], free_pages_out, num_copies, next_free [1]; uint8 status [n]")
     width, stride = _table(block_table, n, "block_table")
     out_width, out_stride = _table(block_table_out, n, "block_table_out")
     _need(width == out_width, "block_table_out must have block_table's shape")
-    _call(_library().toploc_compact_pages, name, dev, stream, _ptr(kv_lens), n, _ptr(block_table), width, stride,
-          _ptr(shares), pages, page_size, _ptr(block_table_out), out_stride, _ptr(shares_out), _ptr(free_pages_out), free,
-          _ptr(copy_from), _ptr(copy_to), _ptr(num_copies), _ptr(next_free), _ptr(status))
+    _call(_library().toploc_compact_pages, name, dev, stream, kv_lens.data_ptr(), n, block_table.data_ptr(), width,
+          stride, shares.data_ptr(), pages, page_size, block_table_out.data_ptr(), out_stride, shares_out.data_ptr(),
+          free_pages_out.data_ptr(), free, copy_from.data_ptr(), copy_to.data_ptr(), num_copies.data_ptr(),
+          next_free.data_ptr(), status.data_ptr())
 
 
 def toploc_copy_pages(caches, copy_from, copy_to, num_copies, stream=None):
@@ -579,4 +590,4 @@ def toploc_copy_pages(caches, copy_from, copy_to, num_copies, stream=None):
     pages, tokens, heads, dim = shape
     lay = _pack(_POOL, _DTYPES[dtype], pages, tokens, heads, dim, len(pointers), strides[0], strides[1], strides[2])
     _call(_library().toploc_copy_pages, name, dev, stream, struct.pack("=%dQ" % len(pointers), *pointers), lay,
-          _ptr(copy_from), _ptr(copy_to), _ptr(num_copies), most)
+          copy_from.data_ptr(), copy_to.data_ptr(), num_copies.data_ptr(), most)
