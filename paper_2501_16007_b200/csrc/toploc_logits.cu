@@ -307,8 +307,9 @@ __device__ __forceinline__ Part join_parts(Part q, int count) {
 __device__ __forceinline__ float logprob_of(const Whole& row, float x) {
   if (row.s != row.s) return row.s;
   if (x == -INFINITY || row.top == -INFINITY) return -INFINITY;
-  const float y = fabsf(row.top) < kFar ? fmaf(x, kLog2e, -powers_of(row.top)) : (x - row.top) * kLog2e;
-  return (y - row.log2_s) * kLn2;
+  // (in powers of 2 the sum's own reference cancels to the bit; but products with log2 e must not leave fp32)
+  if (fabsf(row.top) < kFar && fabsf(x) < kFar) return (fmaf(x, kLog2e, -powers_of(row.top)) - row.log2_s) * kLn2;
+  return x - row.top - row.log2_s * kLn2;
 }
 
 __device__ __forceinline__ void write_row(const LogitParams& p, long long r, const Whole& row, bool known, float given) {

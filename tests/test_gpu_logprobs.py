@@ -260,3 +260,17 @@ def test_captured_and_replayed_on_another_stream():
         torch.cuda.synchronize()
         want = check(x, None, 3)
         assert torch.equal(out[0], want[2]) and torch.equal(out[1], want[3])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,vocab,top", [(1, 9, 9), (3, 105047, 5), (700, 1130, 32), (5, 40, 32)])
+def test_log_probabilities_of_masked_tokens(dtype, rows, vocab, top):
+    """Of tokens at the type's lowest value: their distance from the sum, finite like it, and -inf where that does not fit."""
+    g = generator(11)
+    low = torch.finfo(dtype).min
+    x = logits_of(g, rows, vocab, dtype)
+    x[:, min(3, vocab // 3):] = low
+    check(x, torch.full((rows,), vocab - 1, device=DEV), top)
+    x[0, 0] = -low
+    got = tl.toploc_token_logprobs(x[:1], torch.full((1,), vocab - 1, device=DEV), 2)
+    assert got[0].item() == -math.inf and got[3][0, 0].item() == 0.0
