@@ -265,8 +265,9 @@ typedef struct {
  *   y = x * rsqrt(mean over the head's channels(x^2) + eps) * weight
  *   (a, b) <- (a cos t - b sin t, a sin t + b cos t),  t = position * inv_freq[c]
  * for the pairs (a, b) = channels (c, c + rotary_dim / 2) or (2c, 2c + 1) of y,
- * c < rotary_dim / 2.  fp32 arithmetic with one rounding at the end; t is formed
- * and reduced in 64 bits, so far positions are as exact as near ones.
+ * c < rotary_dim / 2.  fp32 arithmetic with one rounding at the end (a head's sum
+ * of squares has to fit fp32); t is formed and reduced in 64 bits, so far
+ * positions are as exact as near ones.
  *
  * d_q, d_k       DEVICE [num_tokens, heads, head_dim], the last dimension
  *                contiguous (views of one projection are fine)

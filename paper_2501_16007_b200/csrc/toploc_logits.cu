@@ -42,10 +42,12 @@ static_assert(kMostKeys >= kThreads && kMostCluster * kMostTop <= kThreads, "a t
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;         // powers of 2 that a value may pass the reference by
 constexpr float kNothing = 60.f;      // powers of 2 below the reference: 2^20 such logits are nothing in a sum of 24 bits
-// Beyond these a product with log2 e could leave fp32: smaller logits count as kTiny (their weight is 0 next to anything
-// larger), and rows whose maximum is out of +-kFar are summed again against the maximum itself.
-constexpr float kTiny = -1e30f, kFar = 1e29f;
-constexpr float kNoReference = -1e30f;  // above kTiny * log2 e: weight 0 for what a thread meets before its first reference
+// The reference is off its logit by half a step of its own, a power of 2 at kSums and more than fp32 has powers a little further
+// on.  So rows whose maximum is out of +-kFar are summed again by differences from it.  In other rows nothing below -kSums has
+// any weight: such parts' sums are left out, and logits below kTiny count as kTiny.
+constexpr float kFar = 1e7f, kSums = 2e7f, kTiny = -3e7f;
+constexpr float kNoReference = -4e7f;   // above kTiny log2 e: weight 0 for what a thread meets before its first reference
+constexpr float kLeast = -1e30f;        // powers of 2 that differences count as at least
 
 struct LogitParams {
   const void* logits;
@@ -291,24 +293,24 @@ __device__ __forceinline__ void warp_sort(unsigned& v, int flip) {
     warp_merge(v, k, flip ^ (k < 16 && (((lane ^ flip) & (2 * k)) != 0) ? 31 : 0));
 }
 
-// A row, or a block's share, from its parts in lanes 0 .. count - 1, for all lanes of the warp.
+__device__ __forceinline__ bool is_far(float top) { return top > -INFINITY && !(fabsf(top) < kFar); }
+
+// A row, or a block's share, from its parts in lanes 0 .. count - 1, for all lanes of the warp.  Parts whose maximum is out of
+// +-kSums have sums of 0 (or of NaN); in a far row all have been summed again against its maximum.
 __device__ __forceinline__ Part join_parts(Part q, int count) {
   const int lane = threadIdx.x & 31;
   if (lane >= count) q = {-INFINITY, 0.f, 0.f};
   const float top = warp_max(q.top);
-  // (a part with nothing above -inf has sums of 0, or of NaN)
-  const float d = !(q.top > -INFINITY)                           ? 0.f
-                  : !(fabsf(top) < kFar) || !(fabsf(q.top) < kFar) ? fmaxf((q.top - top) * kLog2e, kTiny)
-                                                                   : powers_of(q.top) - powers_of(top);
-  const float f = exp2_fast(d);
+  const float d = fabsf(top) < kSums && fabsf(q.top) < kSums ? powers_of(q.top) - powers_of(top) : 0.f, f = exp2_fast(d);
   return {top, warp_sum(f * q.s), warp_sum(f > 0.f ? f * fmaf(d, q.s, q.w) : f * q.s)};
 }
 
 __device__ __forceinline__ float logprob_of(const Whole& row, float x) {
   if (row.s != row.s) return row.s;
   if (x == -INFINITY || row.top == -INFINITY) return -INFINITY;
-  // (in powers of 2 the sum's own reference cancels to the bit; but products with log2 e must not leave fp32)
-  if (fabsf(row.top) < kFar && fabsf(x) < kFar) return (fmaf(x, kLog2e, -powers_of(row.top)) - row.log2_s) * kLn2;
+  // in powers of 2, so that the sums' own reference cancels to the bit, but for a far row, whose sums are against the maximum
+  // itself, and where the product with log2 e could leave fp32
+  if (fabsf(row.top) < kFar && x > kLeast) return (fmaf(x, kLog2e, -powers_of(row.top)) - row.log2_s) * kLn2;
   return x - row.top - row.log2_s * kLn2;
 }
 
@@ -456,21 +458,28 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<T>)
   // the warp's part
   Part part;
   part.top = warp_max(sums.top);
-  if (part.top > -INFINITY && !(fabsf(part.top) < kFar)) {  // once more, by differences that do not overflow upwards
+  if (fabsf(part.top) < kSums) {
+    sums.renew(powers_of(part.top));
+    part.s = warp_sum(sums.s()), part.w = warp_sum(sums.w());
+  } else {  // (nothing beside a row's maximum that is not far, else summed again; a NaN stays)
+    part.s = warp_sum(sums.s());
+    part.s = part.w = part.s != part.s ? part.s : 0.f;
+  }
+  // the warp's part once more, by differences from the row's maximum: they do not overflow upwards
+  const auto sum_again = [&](float top) {
     float s = 0.f, w = 0.f;
     for (int i = 0; i < kBatch * batches; ++i) {
       const int v = row.vector(i / kBatch, tid, i % kBatch);
       for (int e = 0; e < V::kSize; ++e) {
-        const float y = max_nan((row.value(v, e) - part.top) * kLog2e, kTiny), x = exp2_fast(y);
+        const float y = max_nan((row.value(v, e) - top) * kLog2e, kLeast), x = exp2_fast(y);
         s += x;
         w = fmaf(x, y, w);
       }
     }
-    part.s = warp_sum(s), part.w = warp_sum(w);
-  } else {
-    if (fabsf(part.top) < kFar) sums.renew(powers_of(part.top));
-    part.s = warp_sum(sums.s()), part.w = warp_sum(sums.w());
-  }
+    const Part again = {top, warp_sum(s), warp_sum(w)};
+    if (lane == 0) sh.of_warp[warp] = again;
+    __syncthreads();
+  };
   if (lane == 0) sh.of_warp[warp] = part;
   if (kTops) {
     unsigned o = sums.top > -INFINITY ? ordered(sums.top) : 0;
@@ -483,6 +492,15 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<T>)
   }
   __syncthreads();
 
+  if (blocks == 1) {
+    float top = sh.of_warp[0].top;
+#pragma unroll
+    for (int i = 1; i < kWarps; ++i) top = fmaxf(top, sh.of_warp[i].top);
+    if (is_far(top)) {
+      __syncthreads();  // (all have read what is written again)
+      sum_again(top);
+    }
+  }
   if (warp == 0) {
     const Part all = join_parts(sh.of_warp[lane % kWarps], kWarps);
     if (blocks == 1) {
@@ -532,6 +550,17 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<T>)
   }
   if (blocks > 1) {  // the row, from the cluster's shares
     cluster.sync();
+    float top = -INFINITY;
+    for (int i = 0; i < blocks; ++i) top = fmaxf(top, cluster.map_shared_rank(&sh, i)->part.top);
+    if (is_far(top)) {
+      cluster.sync();  // (all have read what is written again)
+      sum_again(top);
+      if (warp == 0) {
+        const Part all = join_parts(sh.of_warp[lane % kWarps], kWarps);
+        if (lane == 0) sh.part = all;
+      }
+      cluster.sync();
+    }
     unsigned long long mine = 0;
     if (rank == 0) {
       if (warp == 0) {

@@ -16,6 +16,9 @@ import paper_2501_16007_b200 as tl
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
 UNIT = 2.0 ** -24
+# In the place of infinities in what tolerances are relative to: beyond all numbers of fp32 (one of 4.5e31 is rounded by up to
+# 2^-24 4.5e31 = 2.7e24, so nothing smaller will do).
+HUGE = 1e39
 
 
 def generator(seed):
@@ -37,10 +40,10 @@ def check(x, tokens, top, entropy=True, **kw):
     p = x64 - most
     p = p - torch.log(p.exp().sum(1, keepdim=True))
     units = vocab // 2048 + 41 + 4 * math.log(vocab)
-    far = (most - x64).clamp(max=1e30)
+    far = (most - x64).clamp(max=HUGE)
     if tokens is not None:
         want = p.gather(1, tokens[:, None])[:, 0]
-        allowed = UNIT * (units + 4 * far.gather(1, tokens[:, None])[:, 0] + 2 * want.abs().clamp(max=1e30))
+        allowed = UNIT * (units + 4 * far.gather(1, tokens[:, None])[:, 0] + 2 * want.abs().clamp(max=HUGE))
         close(got[0], want, allowed)
     else:
         assert got[0] is None
@@ -56,7 +59,7 @@ def check(x, tokens, top, entropy=True, **kw):
         ids = torch.where(alive, order, -1)
         assert torch.equal(got[2][:, :n], ids)
         assert bool((got[2][:, n:] == -1).all()) and bool((got[3][:, n:] == -math.inf).all())
-        close(got[3][:, :n], want, UNIT * (units + 4 * far.gather(1, order) + 2 * want.abs().clamp(max=1e30)))
+        close(got[3][:, :n], want, UNIT * (units + 4 * far.gather(1, order) + 2 * want.abs().clamp(max=HUGE)))
     return got
 
 
@@ -274,3 +277,35 @@ def test_log_probabilities_of_masked_tokens(dtype, rows, vocab, top):
     x[0, 0] = -low
     got = tl.toploc_token_logprobs(x[:1], torch.full((1,), vocab - 1, device=DEV), 2)
     assert got[0].item() == -math.inf and got[3][0, 0].item() == 0.0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("mask", [-1e4, -65504.0, -1e6, -1e7, -2.8e7, -3e7, -1e8, -1e9, -1e10, -1e15, -1e20, -1e29, -1e30, -1e35])
+@pytest.mark.parametrize("rows,vocab", [(2, 40000), (900, 3000)])
+def test_masks_of_any_size(dtype, mask, rows, vocab):
+    """Tokens that a large number is put in the place of, or taken off: in front, behind, everywhere but one, or all."""
+    g = generator(12)
+    x = logits_of(g, rows, vocab, dtype)
+    last = torch.full((rows,), vocab - 1, device=DEV)
+    for hide in (slice(0, vocab // 2), slice(100, vocab), slice(0, vocab - 1), slice(0, vocab, 2)):
+        y = x.clone()
+        y[:, hide] = mask
+        check(y, last, 5)
+    check(x + mask, last, 5)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,vocab", [(3, 30000), (800, 500)])
+def test_logits_of_any_size(dtype, rows, vocab):
+    g = generator(13)
+    x = logits_of(g, rows, vocab, torch.float32, 1.0)
+    tokens = torch.randint(vocab, (rows,), generator=g, device=DEV)
+    for size in range(0, 38):
+        y = (x * 10.0 ** size).clamp(-1.6e38, 1.6e38).to(dtype)
+        check(y, tokens, 3)
+        y[0] = y[0].abs()
+        y[-1] = -y[-1].abs()
+        check(y, tokens, 3)
+    near = (9.9e6 + 2e5 * torch.rand((rows, vocab), generator=g, device=DEV)).round()
+    for sign in (1, -1):                # maxima on both sides of where the kernel sums another way
+        check((sign * near).to(dtype), tokens, 3)
