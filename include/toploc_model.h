@@ -435,11 +435,11 @@ typedef struct {
  *   top      = the `top` likeliest tokens, ordered by logit, equal ones by
  *              index (the first is the greedy token), and their log
  *              probabilities
- * in fp32.  A logit of -inf is an impossible token: it has no part in entropy,
- * its log probability is -inf, and it is no alternative; places that no token is
- * left for get id -1 and -inf.  A row with nothing above -inf gets logprob -inf
- * and entropy 0.  A row with a NaN or +inf gets NaN for all but the ids (which
- * pass over NaN).
+ * in fp32, log probabilities at most 0, entropies at least 0.  A logit of -inf
+ * is an impossible token: it has no part in entropy, its log probability is
+ * -inf, and it is no alternative; places that no token is left for get id -1 and
+ * -inf.  A row with nothing above -inf gets logprob -inf and entropy 0.  A row
+ * with a NaN or +inf gets NaN for all but the ids (which pass over NaN).
  *
  * d_logits           DEVICE [rows, vocab], row_stride
  * d_tokens_opt       DEVICE [rows] int64, or NULL: no logprob; one outside the

@@ -305,18 +305,21 @@ __device__ __forceinline__ Part join_parts(Part q, int count) {
   return {top, warp_sum(f * q.s), warp_sum(f > 0.f ? f * fmaf(d, q.s, q.w) : f * q.s)};
 }
 
+// (The sums' roundings leave up to 8e-8 of the wrong sign where one token has nearly all the weight: the largest term is 2 to
+// the reference's own rounding, and log2 s gives that back only to a rounding.  A caller's log1p(-exp(logprob)) and sqrt(entropy)
+// would be NaN, so both are held to their range.)
 __device__ __forceinline__ float logprob_of(const Whole& row, float x) {
   if (row.s != row.s) return row.s;
   if (x == -INFINITY || row.top == -INFINITY) return -INFINITY;
   // in powers of 2, so that the sums' own reference cancels to the bit, but for a far row, whose sums are against the maximum
   // itself, and where the product with log2 e could leave fp32
-  if (fabsf(row.top) < kFar && x > kLeast) return (fmaf(x, kLog2e, -powers_of(row.top)) - row.log2_s) * kLn2;
-  return x - row.top - row.log2_s * kLn2;
+  if (fabsf(row.top) < kFar && x > kLeast) return fminf((fmaf(x, kLog2e, -powers_of(row.top)) - row.log2_s) * kLn2, 0.f);
+  return fminf(x - row.top - row.log2_s * kLn2, 0.f);
 }
 
 __device__ __forceinline__ void write_row(const LogitParams& p, long long r, const Whole& row, bool known, float given) {
   if (p.tokens) p.logprobs[r] = known ? logprob_of(row, given) : __uint_as_float(0x7FFFFFFFu);
-  if (p.entropy) p.entropy[r] = row.top == -INFINITY && row.s == row.s ? 0.f : (row.log2_s - row.w / row.s) * kLn2;
+  if (p.entropy) p.entropy[r] = row.top == -INFINITY && row.s == row.s ? 0.f : max_nan((row.log2_s - row.w / row.s) * kLn2, 0.f);
 }
 
 // The block's alternatives one after the other, where more candidates reach the bound than there is room for (many equal
