@@ -115,12 +115,12 @@ __device__ __forceinline__ void for_entries(const PoolParams& p, const Team& tea
         most = max(most, held_of[i]);
       }
 #pragma unroll 1
-      for (int c0 = team.block * 32; c0 < most; c0 += team.blocks * 32) {
+      for (unsigned c0 = team.block * 32; c0 < (unsigned)most; c0 += team.blocks * 32) {  // (rows of up to 2^31 - 1)
         int32_t page[kAtOnce];
         bool valid[kAtOnce];
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-          valid[i] = c0 + lane < held_of[i];
+          valid[i] = c0 + lane < (unsigned)held_of[i];
           page[i] = valid[i] ? table[rows[i] * stride + c0 + lane] : 0;
         }
         visit(rows, c0 + lane, page, valid);
@@ -263,7 +263,8 @@ __global__ void __launch_bounds__(kThreads, 1) toploc_fork_pages_kernel(const __
 #pragma unroll 1
       for (int first = 0; first < count; first += kAtOnce) {
         bool bad[kAtOnce] = {};
-        int held[kAtOnce], from[kAtOnce], longest = 0;
+        int from[kAtOnce];
+        unsigned held[kAtOnce], longest = 0;
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
           held[k] = first + k < 32 ? __shfl_sync(0xFFFFFFFFu, pages, (first + k) & 31) : 0;
@@ -271,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 1) toploc_fork_pages_kernel(const __
           longest = max(longest, held[k]);
         }
 #pragma unroll 1
-        for (int j = lane; j < longest; j += 32) {
+        for (unsigned j = lane; j < longest; j += 32) {
           int32_t page[kAtOnce];
 #pragma unroll
           for (int k = 0; k < kAtOnce; ++k) page[k] = j < held[k] ? p.table[from[k] * p.table_stride + j] : 0;
@@ -309,7 +310,7 @@ __global__ void __launch_bounds__(kThreads, 1) toploc_fork_pages_kernel(const __
   for (int i = team.warp_of_all; i < p.num_seqs; i += team.all_warps) {
     const int parent = p.parents[i], was = status_of(p, i);
     if (parent < 0 || (was & ~kNeedsPage) != TOPLOC_SEQ_OK) continue;
-    const int whole = fresh(p.kv_lens_out + i) / p.page_size;
+    const unsigned whole = (unsigned)fresh(p.kv_lens_out + i) / (unsigned)p.page_size;
     const int32_t* theirs = p.table + parent * p.table_stride;
     int32_t* row = p.table + i * p.table_stride;
     int status = TOPLOC_SEQ_OK;
@@ -329,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1) toploc_fork_pages_kernel(const __
       if (status != TOPLOC_SEQ_OK && lane == 0) p.status[i] = (uint8_t)(status | kNeedsPage);
     }
     if (status != TOPLOC_SEQ_OK) continue;
-    for (int j0 = lane; j0 < whole; j0 += 32 * kAtOnce) {
+    for (unsigned j0 = lane; j0 < whole; j0 += 32 * kAtOnce) {
       int32_t page[kAtOnce];
 #pragma unroll
       for (int e = 0; e < kAtOnce; ++e) page[e] = j0 + e * 32 < whole ? theirs[j0 + e * 32] : 0;
@@ -389,11 +390,12 @@ __global__ void __launch_bounds__(kWideThreads) toploc_release_begin_kernel(cons
 __global__ void __launch_bounds__(kWideThreads) toploc_release_entries_kernel(const __grid_constant__ PoolParams p) {
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int lane = threadIdx.x & 31, parts = (p.max_pages + kEntriesAtOnce - 1) / kEntriesAtOnce;
+  const int lane = threadIdx.x & 31, parts = ((unsigned)p.max_pages + kEntriesAtOnce - 1) / kEntriesAtOnce;
   const long long warps = gridDim.x * (kWideThreads / 32), items = (long long)p.num_seqs * parts;
   for (long long item = blockIdx.x * (kWideThreads / 32) + threadIdx.x / 32; item < items; item += warps) {
-    const int seq = (int)(item / parts), first = (int)(item - (long long)seq * parts) * kEntriesAtOnce + lane;
-    const int pages = released_pages(p, seq);
+    const int seq = (int)(item / parts);
+    const unsigned first = (unsigned)(item - (long long)seq * parts) * kEntriesAtOnce + lane;
+    const unsigned pages = released_pages(p, seq);
     int32_t page[kAtOnce];
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k)
@@ -417,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1) toploc_release_pages_kernel(const
     team.sync();
     for_entries(
         p, team, p.table, p.table_stride, [&](int row) { return released_pages(p, row); },
-        [&](const int* rows, int, const int32_t* page, const bool* valid) {
+        [&](const int* rows, unsigned, const int32_t* page, const bool* valid) {
 #pragma unroll
           for (int i = 0; i < kAtOnce; ++i)
             if (valid[i]) release_entry(p, rows[i], page[i]);
@@ -490,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) toploc_compact_pages_kernel(const
     return held_pages(p, p.kv_lens[row], &status);
   };
   for_entries(p, team, p.table_in, p.table_in_stride, held,
-              [&](const int* rows, int, const int32_t* page, const bool* valid) {
+              [&](const int* rows, unsigned, const int32_t* page, const bool* valid) {
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) {
                   if (!valid[i]) continue;
@@ -542,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, 1) toploc_compact_pages_kernel(const
   team.sync();
 
   for_entries(p, team, p.table_in, p.table_in_stride, held,
-              [&](const int* rows, int col, const int32_t* page, const bool* valid) {
+              [&](const int* rows, unsigned col, const int32_t* page, const bool* valid) {
                 int32_t to[kAtOnce];
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) {
