@@ -266,8 +266,9 @@ typedef struct {
  *   (a, b) <- (a cos t - b sin t, a sin t + b cos t),  t = position * inv_freq[c]
  * for the pairs (a, b) = channels (c, c + rotary_dim / 2) or (2c, 2c + 1) of y,
  * c < rotary_dim / 2.  fp32 arithmetic with one rounding at the end (a head's sum
- * of squares has to fit fp32); t is formed and reduced in 64 bits, so far
- * positions are as exact as near ones.
+ * of squares has to fit fp32); t is formed and brought into one turn in 64 bits
+ * with remainders, so that far positions are as exact as near ones, up to
+ * |position * inv_freq| = 2^64.
  *
  * d_q, d_k       DEVICE [num_tokens, heads, head_dim], the last dimension
  *                contiguous (views of one projection are fine)

@@ -34,14 +34,20 @@ struct RotaryParams {
   int steps_per_warp;
 };
 
-// cos and sin of position * freq.  The angle is taken in turns and brought into one turn in 64 bits (position and frequency
-// have 31 and 24 bits: nothing is lost before the product), so what remains in 32 is below 2^-25 turns off wherever the
-// position is.
+// cos and sin of position * freq.  The angle is taken in turns and brought into one turn in 64 bits before it is rounded to 32
+// (half a step of half a turn: 2^-26 turns).  A product of 31 and 24 bits has more than a double holds, and a position far away
+// has many turns whose whole part is nothing: so the products with the position and with 1 / (2 pi) keep their remainders, and
+// 1 / (2 pi) has a second number (without them the angle at position 2^31 and frequency 1 was 2^-24 turns off).  What is lost is
+// about 2^-104 of the turns: below 2^-40 turns up to |position * freq| = 2^64.
 __device__ __forceinline__ float2 turn_of(int position, float freq) {
-  double t = (double)position * (double)freq * 0.15915494309189533577;  // 1 / 2 pi
-  t -= rint(t);
+  constexpr double kTurns = 0.15915494309189535, kTurnsRest = -9.839338337591243e-18;  // their sum is 1 / (2 pi)
+  const double p = position, f = freq, x = __dmul_rn(p, f), x_rest = fma(p, f, -x);
+  // (rounded by itself: as part of the difference from rint its remainder would count twice)
+  const double t = __dmul_rn(x, kTurns), t_rest = fma(x, kTurns, -t) + fma(x, kTurnsRest, x_rest * kTurns);
+  double one = (t - rint(t)) + t_rest;
+  one -= rint(one);
   float2 r;
-  sincospif(2.f * (float)t, &r.y, &r.x);
+  sincospif(2.f * (float)one, &r.y, &r.x);
   return r;
 }
 
