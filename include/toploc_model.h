@@ -123,10 +123,11 @@ int toploc_cache_write(const void* d_k, const void* d_v, int64_t k_token_stride,
  * shared, and new tokens go behind them, so a shared page is never written.
  *
  * Outputs of the three planners below are apart from inputs (shares and
- * lengths: two buffers used in turn), so that a repeated call gives the same;
- * refused where they overlap.  The same inputs give the same outputs.  All
- * arrays DEVICE; int32 4-byte aligned.  page_size > 0, num_seqs <= 2^24,
- * num_pages <= 2^30, max_pages >= 0, table_stride >= max_pages.
+ * lengths: two buffers used in turn), so that a repeated call gives the same,
+ * but for a compaction of the table in place; refused where they overlap.  The
+ * same inputs give the same outputs.  All arrays DEVICE; int32 4-byte aligned.
+ * page_size > 0, num_seqs <= 2^24, num_pages <= 2^30, max_pages >= 0,
+ * table_stride >= max_pages.
  */
 
 /*
@@ -198,7 +199,11 @@ int toploc_release_pages(const uint8_t* d_release, const int32_t* d_kv_lens, int
  *
  *   d_block_table_out [num_seqs, max_pages]  entries of held pages are written,
  *                              others left as they are; may be d_block_table
- *                              itself (with the same stride)
+ *                              itself (with the same stride).  A call in
+ *                              place leaves new page numbers, which d_shares
+ *                              does not go by: it is not to be repeated or
+ *                              replayed before d_shares holds what
+ *                              d_shares_out got
  *   d_shares_out  [num_pages]  at the pages' new places, 0 behind them
  *   d_free_pages_out [num_free]  the unused pages n .. num_pages - 1 in its last
  *                              num_pages - n entries, next_free and on; entries

@@ -542,7 +542,8 @@ def toploc_compact_pages(kv_lens, block_table, shares, page_size, block_table_ou
     """The pool's pages in use become its first ones (see the header); toploc_copy_pages moves their contents by the list
     that this leaves.  int32 CUDA tensors kv_lens [n], block_table, block_table_out [n, max_pages] (may be one tensor),
     shares, shares_out, copy_from, copy_to [num_pages], free_pages_out [num_pages or more], num_copies, next_free [1];
-    status uint8 [n].  The last eight are written."""
+    status uint8 [n].  The last eight are written.  A call with one tensor for both tables is not to be repeated, or replayed,
+    before shares holds what shares_out got."""
     name, n = "toploc_compact_pages", kv_lens.numel()
     dev = _device(name, kv_lens, block_table, shares, block_table_out, shares_out, free_pages_out, copy_from, copy_to,
                   num_copies, next_free, status)
