@@ -281,7 +281,8 @@ typedef struct {
  * d_inv_freq     DEVICE [rotary_dim / 2] fp32
  * d_q_weight_opt, d_k_weight_opt  DEVICE [head_dim], NULL: no norm of that one
  * d_q_out, d_k_out  DEVICE; each may be its input (with the same strides), else
- *                they share no memory with the inputs
+ *                they share no memory with the inputs or each other (refused,
+ *                but not looked for where both have gaps of different lengths)
  * Pointers aligned to the element; heads at places of 16 (8) bytes, less than
  * 2^26 elements apart, whose channels and turned channels are whole vectors of
  * that size move as vectors, others element by element.  Asynchronous.

@@ -350,6 +350,47 @@ void launch_vectors(const RotaryParams& p, bool neighbours, bool all_turn, dim3 
     toploc_norm_rotary_kernel<T, kVec, false, false, kUnroll><<<grid, kBlock, 0, stream>>>(p);
 }
 
+// Memory of an argument: runs of `bytes`, `count` of them `step` bytes apart in two directions (heads, tokens).
+struct Area {
+  uintptr_t at;
+  long long bytes, count[2], step[2];
+  __int128 extent;
+
+  Area(const void* p, long long bytes) : Area(p, bytes, 1, 0, 1, 0) {}
+  Area(const void* p, long long run, long long heads, long long head_step, long long tokens, long long token_step)
+      : at(reinterpret_cast<uintptr_t>(p)), bytes(p ? run : 0), count{heads, tokens}, step{head_step, token_step} {
+    for (int n = 0; n < 2; ++n)
+      for (int d = 0; d < 2; ++d)  // runs side by side are one
+        if (count[d] == 1 || step[d] <= bytes) bytes += (count[d] - 1) * step[d], count[d] = 1, step[d] = 0;
+    extent = bytes;
+    for (int d = 0; d < 2; ++d) extent += (__int128)(count[d] - 1) * step[d];
+  }
+};
+
+// Whether two areas share memory.  Known where their steps are the same, or one has none, in either direction; others count as
+// apart.
+bool meet(const Area& a, const Area& b) {
+  if (a.bytes <= 0 || b.bytes <= 0 || a.extent > 1ll << 60 || b.extent > 1ll << 60) return false;
+  const long long away = (long long)(a.at - b.at);
+  if (away >= (long long)b.extent || away <= -(long long)a.extent) return false;
+  long long step[2], low[2], high[2];  // of the places of a run of a, less those of one of b
+  for (int d = 0; d < 2; ++d) {
+    if (a.count[d] > 1 && b.count[d] > 1 && a.step[d] != b.step[d]) return false;
+    step[d] = max(a.step[d], b.step[d]), low[d] = 1 - b.count[d], high[d] = a.count[d] - 1;
+  }
+  const int outer = high[0] - low[0] <= high[1] - low[1] ? 0 : 1, inner = 1 - outer;
+  for (long long e = low[outer]; e <= high[outer]; ++e) {
+    // the first place in the other direction that is not in front of b's run
+    const long long from = away + e * step[outer], least = -a.bytes - from;
+    long long i = low[inner];
+    if (step[inner] > 0)
+      i = max(i, least >= 0 ? least / step[inner] + 1 : -((-least - 1) / step[inner]));
+    const long long gap = from + i * step[inner];
+    if (i <= high[inner] && gap > -a.bytes && gap < b.bytes) return true;
+  }
+  return false;
+}
+
 // Shape of the heads, the same for both entries.
 int check_layout(const toploc_rotary_layout* lay) {
   if (!lay || lay->head_dim <= 0 || lay->q_heads <= 0 || lay->kv_heads <= 0 || lay->rotary_dim < 0 ||
@@ -378,6 +419,24 @@ int run(RotaryParams& p, const toploc_rotary_layout* lay, const int32_t* positio
     if (w.in == w.out && (i == 0 || parts == 2) &&
         ((lay->num_tokens > 1 && w.in_token != w.out_token) || (heads > 1 && w.in_head != w.out_head)))
       return TOPLOC_ERR_INVALID_ARGUMENT;
+  }
+  const long long head = (long long)lay->head_dim * size;
+  // outputs (not the caches) apart from inputs and each other: other warps read and write them
+  const auto area = [&](int i, bool out) {
+    const Heads& w = p.part[i];
+    const auto bytes = [&](long long step) { return min(step, 1ll << 57) * size; };
+    return Area(out ? w.out : w.in, head, i == 0 ? lay->q_heads : lay->kv_heads,
+                bytes(out ? w.out_head : w.in_head), lay->num_tokens, bytes(out ? w.out_token : w.in_token));
+  };
+  const Area vectors[] = {{lay->rotary_dim > 0 ? positions : nullptr, lay->num_tokens * 4}, {inv_freq, lay->rotary_dim * 2ll},
+                          {p.part[0].weight, head}, {p.part[1].weight, head}, {p.slots, lay->num_tokens * 8}};
+  for (int o = 0; o < (parts == 2 ? 2 : 1); ++o) {
+    const Area out = area(o, true);
+    for (int i = 0; i < parts; ++i)
+      if ((i != o || p.part[i].in != p.part[o].out) && meet(out, area(i, false))) return TOPLOC_ERR_INVALID_ARGUMENT;
+    for (const Area& v : vectors)
+      if (meet(out, v)) return TOPLOC_ERR_INVALID_ARGUMENT;
+    if (o == 1 && meet(out, area(0, true))) return TOPLOC_ERR_INVALID_ARGUMENT;
   }
   int sms = 0;
   if (const int rc = check_device(&sms)) return rc;
