@@ -454,7 +454,11 @@ typedef struct {
  * d_logprobs_opt     DEVICE [rows] fp32, NULL exactly where d_tokens is
  * d_entropy_opt      DEVICE [rows] fp32 or NULL
  * d_top_ids, d_top_logprobs  DEVICE [rows, top] int64 / fp32, NULL with top 0
- * Pointers aligned to their elements.  Asynchronous, deterministic.
+ * Pointers aligned to their elements.  Asynchronous.  The same call gives the same
+ * bits.  How a row is summed goes by the number of rows too, so the same row in a
+ * call of another size can differ in the last bits of its log probabilities and
+ * its entropy (not in its ids): a provider's and a validator's numbers are
+ * compared with a tolerance.
  */
 int toploc_token_logprobs(const void* d_logits, const toploc_logprob_layout* lay, const int64_t* d_tokens_opt,
                           float* d_logprobs_opt, float* d_entropy_opt, int64_t* d_top_ids, float* d_top_logprobs,
