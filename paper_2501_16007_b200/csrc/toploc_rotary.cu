@@ -35,19 +35,17 @@ struct RotaryParams {
 };
 
 // cos and sin of position * freq.  The angle is taken in turns and brought into one turn in 64 bits before it is rounded to 32
-// (half a step of half a turn: 2^-26 turns).  A product of 31 and 24 bits has more than a double holds, and a position far away
-// has many turns whose whole part is nothing: so the products with the position and with 1 / (2 pi) keep their remainders, and
-// 1 / (2 pi) has a second number (without them the angle at position 2^31 and frequency 1 was 2^-24 turns off).  What is lost is
-// about 2^-104 of the turns: below 2^-40 turns up to |position * freq| = 2^64.
+// (half a step of half a turn: 2^-26 turns).  The turns of one position, freq / (2 pi), need two numbers of 53 bits: the angle of
+// position 2^31 has 2^28 whole turns, which are nothing, and with one number the rest was 2^-24 turns off.  The product with the
+// position is rounded once the whole turns are off it.  What is lost is about 2^-104 of the turns: below 2^-40 turns up to
+// |position * freq| = 2^64.
 __device__ __forceinline__ float2 turn_of(int position, float freq) {
   constexpr double kTurns = 0.15915494309189535, kTurnsRest = -9.839338337591243e-18;  // their sum is 1 / (2 pi)
-  const double p = position, f = freq, x = __dmul_rn(p, f), x_rest = fma(p, f, -x);
-  // (rounded by itself: as part of the difference from rint its remainder would count twice)
-  const double t = __dmul_rn(x, kTurns), t_rest = fma(x, kTurns, -t) + fma(x, kTurnsRest, x_rest * kTurns);
-  double one = (t - rint(t)) + t_rest;
-  one -= rint(one);
+  const double p = position, f = freq, each = __dmul_rn(f, kTurns), each_rest = fma(f, kTurnsRest, fma(f, kTurns, -each));
+  double t = fma(p, each_rest, fma(p, each, -rint(p * each)));
+  t -= rint(t);  // (far beyond 2^53 turns the first whole ones are not all)
   float2 r;
-  sincospif(2.f * (float)one, &r.y, &r.x);
+  sincospif(2.f * (float)t, &r.y, &r.x);
   return r;
 }
 
@@ -324,17 +322,16 @@ __global__ void __launch_bounds__(kWarps * 32) toploc_norm_rotary_any_kernel(con
     __syncwarp();
   }
   const int position = p.half ? p.positions[token] : 0;
-  for (int c = lane; c < p.head_dim; c += 32) {
-    float y = head[warp][c];
-    if (c < 2 * p.half) {
-      const bool second = neighbours ? c & 1 : c >= p.half;
-      const int pair = neighbours ? c >> 1 : second ? c - p.half : c;
-      const float other = head[warp][neighbours ? c ^ 1 : second ? c - p.half : c + p.half];
-      const float2 t = turn_of(position, p.inv_freq[pair]);
-      y = second ? other * t.y + y * t.x : y * t.x - other * t.y;
-    }
-    store_as(out + c, y);
+  for (int j = lane; j < p.half; j += 32) {  // (a pair's turn once: it takes longer than the rest of its channels)
+    float& a = head[warp][neighbours ? 2 * j : j];
+    float& b = head[warp][neighbours ? 2 * j + 1 : j + p.half];
+    const float x = a, y = b;
+    const float2 t = turn_of(position, p.inv_freq[j]);
+    a = x * t.x - y * t.y;
+    b = x * t.y + y * t.x;
   }
+  __syncwarp();
+  for (int c = lane; c < p.head_dim; c += 32) store_as(out + c, head[warp][c]);
 }
 
 template <typename T, int kVec>
@@ -453,8 +450,8 @@ int run(RotaryParams& p, const toploc_rotary_layout* lay, const int32_t* positio
   const bool neighbours = lay->pairing == TOPLOC_ROTARY_NEIGHBOURS;
 
   // Whole vectors of `vec` elements everywhere: two a lane, turned channels in whole vectors.  16 bytes where they fit (34
-  // thousand tokens of heads of 128: 136 us, with 8 bytes 172, element by element 712), else 8 (heads of 80 of which 40 turn:
-  // 165 us, element by element 586).
+  // thousand tokens of heads of 128: 136 us, with 8 bytes 172, element by element 609), else 8 (heads of 80 of which 40 turn:
+  // 164 us, element by element 567).
   const auto fits = [&](int vec) {
     const uintptr_t bytes = vec * size;
     long long off = 0;  // bits of places and steps that a vector's must not have
