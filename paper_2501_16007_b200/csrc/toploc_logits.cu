@@ -11,8 +11,9 @@
 // vectors a thread at a time.  Copies ahead through shared memory or registers, which cost warps, took 205 to 255 us.
 //
 // Alternatives: while it streams, a block leaves the largest of every four vectors (32 or 16 logits) in shared memory.  The
-// threads' own maxima give a bound that at least `top` logits reach; behind the row only the vectors that reach it are read
-// again, a few dozen, and their logits ranked by (value, index).
+// four largest of each warp's threads' maxima give a bound that at least `top` logits reach; behind the row only the vectors
+// that reach it are read again, a few dozen, and their logits ranked by (value, index).  Where fewer than top / 4 warps have any
+// candidates there is no bound, and with more than 256 of them one warp takes them in order (best_in_order).
 #include "model_common.cuh"
 
 #include <cooperative_groups.h>
@@ -28,7 +29,7 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 // Of an SM: with fp32 there is half as much to compute a byte, and 64 registers a thread do more for it than a fifth block
-// (1000 x 50257: 35.6 us against 37.9; bf16, 4097 x 128000: 188 against 172).
+// (1000 x 50257, on one board: 35.6 us against 37.9; bf16, 4097 x 128000: 188 against 172).
 template <typename T>
 constexpr int kBlocksPerSm = sizeof(T) == 2 ? 5 : 4;
 constexpr int kMostVocab = 1 << 20;
@@ -322,9 +323,11 @@ __device__ __forceinline__ void write_row(const LogitParams& p, long long r, con
   if (p.entropy) p.entropy[r] = row.top == -INFINITY && row.s == row.s ? 0.f : max_nan((row.log2_s - row.w / row.s) * kLn2, 0.f);
 }
 
-// The block's alternatives one after the other, where more candidates reach the bound than there is room for (many equal
-// logits, as a rule): through the vectors in order, the best so far in a warp's lanes.  What only equals the least of a full
-// list is passed over, so long runs of equal logits cost a look at their maxima.
+// The block's alternatives one after the other, where more candidates reach the bound than there is room for: many equal logits,
+// or no bound, because the candidates lie in fewer than top / 4 warps (rows of 257 to 1816 logits by number of alternatives and
+// type, a mask that leaves some hundred neighbours, or anything but the type's lowest value).  Through the vectors in order, the
+// best so far in a warp's lanes; what only equals the least of a full list is passed over, so long runs of equal logits cost a
+// look at their maxima.  64 x 1000 bf16, 20 alternatives: 94 us (with 5, by the bound, 4.6); 64 x 128000 all equal: 40.
 template <typename T>
 __device__ __noinline__ unsigned long long best_in_order(const Share<T> row, const typename Vector<T>::Kept* maxima, float bound,
                                                          int top) {
